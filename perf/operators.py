@@ -1,0 +1,411 @@
+"""The paged cache of codes as it is measured: what a serving program asks of it, token after token and prompt after prompt.
+
+Two operators, each in its plain form (elementary torch operations in 32 or 64 bits) and as the library offers it:
+
+  append   the keys and values of new tokens go into pages: the keys are rotated to their positions, then both are
+           quantized, per head, to 2, 3 or 4 bits a value.  The outputs are the rows as the pages hold them, as the
+           values that the codes and scales stand for (bf16).
+  attend   soft-max attention of the last tokens of every sequence over all of its tokens, read from the pages.
+
+Shapes are those of this repository: 8 kv heads x 128, 24 to 64 query heads, grids of 16 / 64 / 256 points or the uniform
+backbone, contexts from a few tokens to 131072.
+"""
+import functools
+import math
+
+import torch
+
+own = False
+
+H, G = 8, 128
+D = H * G
+SCALE = G ** -0.5
+CODE_BITS = {("grid", 2): 4, ("grid", 3): 6, ("grid", 4): 8, ("rtn", 2): 4, ("rtn", 4): 8}     # bits per pair of values
+
+
+# ---------------------------------------------------------------------------------------------------- the cases
+def listed():
+    def append(name, tokens, bits=4, backbone="grid", q_heads=32, rope=True, padded=False):
+        return dict(name=name, kind="append", tokens=tokens, bits=bits, backbone=backbone, q_heads=q_heads, rope=rope,
+                    padded=padded, page=64)
+
+    def attend(name, batch, context, queries=1, q_heads=32, bits=4, backbone="grid", page=64, dtype="bf16"):
+        return dict(name=name, kind="attend", batch=batch, context=context, queries=queries, q_heads=q_heads, bits=bits,
+                    backbone=backbone, page=page, dtype=dtype)
+
+    return [
+        # the newest token of one sequence, once per layer and generated token: latency
+        append("append-1", 1),
+        # one token each of a batch that is padded to the size its graph was captured with, uniform backbone
+        append("append-61-padded-rtn", 61, backbone="rtn", q_heads=64, padded=True),
+        # a short prompt at 2 bits, keys held from before the rotary embedding
+        append("append-777-2bit", 777, bits=2, rope=False),
+        # a long prompt
+        append("append-8192", 8192),
+        # one sequence of a chat: latency
+        attend("attend-1x700", 1, 700),
+        # an ordinary batch of sequences of different lengths
+        attend("attend-24x3000", 24, 3000, page=24),
+        # one sequence of the longest context
+        attend("attend-1x131072", 1, 131072, q_heads=64, page=128),
+        # the largest batch
+        attend("attend-32x16384", 32, 16384),
+        # uniform backbone
+        attend("attend-16x6000-rtn", 16, 6000, backbone="rtn", q_heads=24, page=16),
+        # drafts of 5 tokens checked at once, 3 bits
+        attend("attend-8x5x9999-3bit", 8, 9999, queries=5, bits=3),
+        # a chunk of a prompt behind what is cached already
+        attend("attend-2048x12288", 1, 12288, queries=2048),
+        # everything in fp32
+        attend("attend-3x1500-fp32", 3, 1500, dtype="fp32", page=32),
+    ]
+
+
+def draw(rng):
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    backbone, bits = rng.choice([("grid", 4)] * 4 + [("rtn", 4)] * 2 + [("grid", 3), ("grid", 2), ("rtn", 2)])
+    q_heads, page = rng.choice([24, 32, 32, 40, 64]), rng.choice([8, 16, 24, 32, 64, 128, 256])
+    if rng.random() < 0.35:
+        return dict(kind="append", tokens=log_int(1, 8192), bits=bits, backbone=backbone, q_heads=q_heads,
+                    rope=rng.random() < 0.7, padded=rng.random() < 0.4, page=page)
+    if rng.random() < 0.2:                                     # a chunk of a prompt
+        context = log_int(64, 12288)
+        return dict(kind="attend", batch=1, context=context, queries=log_int(16, min(context, 2048)), q_heads=min(q_heads, 32),
+                    bits=bits, backbone=backbone, page=page, dtype="bf16")
+    if rng.random() < 0.15:
+        return dict(kind="attend", batch=log_int(1, 8), context=log_int(8, 4096), queries=rng.choice([1, 1, 3]), q_heads=q_heads,
+                    bits=bits, backbone=backbone, page=page, dtype="fp32")
+    batch, queries = log_int(1, 32), rng.choice([1, 1, 1, 2, 4, 7])
+    return dict(kind="attend", batch=batch, context=log_int(8, min(131072, 262144 // batch)), queries=queries, q_heads=q_heads,
+                bits=bits, backbone=backbone, page=page, dtype="bf16")
+
+
+def lengths(case):
+    """From the longest context down to less than half of it."""
+    n, b = case["context"], case["batch"]
+    return [max(case["queries"], n - (37 * i * n) // (64 * b)) for i in range(b)]
+
+
+# ---------------------------------------------------------------------------------------------------- inputs
+@functools.lru_cache(maxsize=None)
+def grid(bits):
+    """A Gaussian-optimal grid of 4**bits points in the plane (Lloyd iterations; sums in integers, so the same on every
+    run), and the points nearest to 65536 Gaussian samples: codes as they are distributed in a cache."""
+    n = 4 ** bits
+    gen = torch.Generator(device="cuda").manual_seed(20250131)
+    x = torch.randn(1 << 16, 2, generator=gen, device="cuda", dtype=torch.float64)
+    fixed = (x * 2.0 ** 32).round().to(torch.int64)
+
+    def nearest(c):
+        return torch.cat([((p[:, None, :] - c[None]) ** 2).sum(-1).argmin(1) for p in x.split(1 << 14)])
+
+    c = x[:n].clone()
+    for _ in range(50):
+        near = nearest(c)
+        count = torch.bincount(near, minlength=n)
+        total = torch.zeros(n, 2, dtype=torch.int64, device="cuda").index_add_(0, near, fixed)
+        c = torch.where(count[:, None] > 0, total.double() / 2.0 ** 32 / count.clamp(min=1)[:, None], c)
+    pts = torch.tensor(sorted(map(tuple, c.cpu().tolist())), dtype=torch.float32, device="cuda")
+    return pts, nearest(pts.double()).to(torch.uint8)
+
+
+def randn(gen, *shape):
+    return torch.randn(*shape, generator=gen, device="cuda")
+
+
+def signs(gen):
+    return (torch.randint(0, 2, (D,), generator=gen, device="cuda") * 2 - 1).to(torch.int8)
+
+
+def rope_tables(positions):
+    angle = torch.arange(positions, device="cuda", dtype=torch.float64)[:, None] * 10000.0 ** (
+        -torch.arange(0, G, 2, device="cuda", dtype=torch.float64) / G)[None]
+    return angle.cos().float().contiguous(), angle.sin().float().contiguous()
+
+
+def make_format(case, gen, dtype):
+    """The quantizer: a grid behind rotations by `signs`, or none of both (uniform)."""
+    s = dict(case=case, grid=None, signs=(None, None), handle=None)
+    if case["backbone"] == "grid":
+        s.update(grid=grid(case["bits"])[0], signs=(signs(gen), signs(gen)))
+    if own:
+        from paper_2501_19392_amd import binding as B
+        if case["backbone"] == "grid":
+            s["handle"] = B.Layer(H, G, s["grid"], *s["signs"], dtype, search_table=B.build_search_table(s["grid"]))
+        else:
+            s["handle"] = B.Layer(H, G, None, None, None, dtype, rtn_bits=case["bits"])
+    return s
+
+
+def make_pool(s, case, pages, fill):
+    """Room for `pages` pages; fill: (codes, scales) of the keys and of the values, or None (all zero)."""
+    rows, row = pages * case["page"], D * CODE_BITS[case["backbone"], case["bits"]] // 16
+    shape = (rows, H) if case["backbone"] == "grid" else (rows, H * G // 64, 2)
+    for t in "kv":
+        s[t + "_codes"], s[t + "_scales"] = fill[t] if fill else (
+            torch.zeros(rows, H, row // H, dtype=torch.uint8, device="cuda"), torch.zeros(shape, dtype=torch.int16, device="cuda"))
+    if own:
+        from paper_2501_19392_amd import binding as B
+        s["pages"] = B.Pages(s["handle"], pages, case["page"], k_codes=s["k_codes"], k_scales=s["k_scales"],
+                             v_codes=s["v_codes"], v_scales=s["v_scales"])
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return globals()["prepare_" + case["kind"]](case, gen)
+
+
+def prepare_append(case, gen):
+    T, page = case["tokens"], case["page"]
+    s = make_format(case, gen, torch.bfloat16)
+    # keys and values as slices of the layer's joint product, log-normal channels with two outliers
+    size = randn(gen, 2 * D).exp()
+    size[torch.randint(0, 2 * D, (2,), generator=gen, device="cuda")] *= 10.0
+    qkv = torch.empty(T, case["q_heads"] * G + 2 * D, dtype=torch.bfloat16, device="cuda")
+    qkv[:, case["q_heads"] * G:] = (randn(gen, T, 2 * D) * size).bfloat16()
+    kv = qkv[:, case["q_heads"] * G:]
+    s["K"], s["V"] = kv[:, :D].view(T, H, G), kv[:, D:].view(T, H, G)
+    pages = -(-T // page) + 3
+    make_pool(s, case, pages, None)
+    # pages in any order; a prompt's tokens one after the other, generated tokens of a batch anywhere
+    order = torch.randperm(pages, generator=gen, device="cuda")
+    t = torch.arange(T, device="cuda")
+    if T <= 64:
+        s["slots"] = torch.randperm(pages * page, generator=gen, device="cuda")[:T]
+        s["positions"] = torch.randint(0, 16384, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    else:
+        s["slots"] = order[t // page] * page + t % page
+        s["positions"] = (t + 1234).to(torch.int32)
+    if case["padded"]:
+        s["slots"][T - T // 4:] = -1
+    s["slots"] = s["slots"].contiguous()
+    s["rope"] = rope_tables(16384) if case["rope"] else None
+    s["Khat"], s["Vhat"] = (torch.zeros(T, H, G, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    return s
+
+
+def random_codes(case, gen, rows):
+    """Codes and scales of `rows` tokens as they are distributed in a cache."""
+    bits = case["bits"]
+    if case["backbone"] == "grid":
+        codes = grid(bits)[1][torch.randint(0, 1 << 16, (rows, H, G // 2), generator=gen, device="cuda")]
+        scales = (0.3 * randn(gen, rows, H)).exp().half().view(torch.int16)
+        if bits == 3:                                          # 4 codes in 3 bytes
+            c = codes.view(rows, H, G // 8, 4).to(torch.int32)
+            word = c[..., 0] | c[..., 1] << 6 | c[..., 2] << 12 | c[..., 3] << 18
+            codes = torch.stack([word & 255, word >> 8 & 255, word >> 16], -1).to(torch.uint8).view(rows, H, -1)
+        elif bits == 2:
+            codes = codes[..., 0::2] | codes[..., 1::2] << 4
+        return codes.contiguous(), scales
+    top = 2 ** bits - 1
+    c = (top / 2 + top / 6 * randn(gen, rows, H, G)).round().clamp(0, top).to(torch.uint8)
+    c = c[..., 0::2] | c[..., 1::2] << bits
+    if bits == 2:
+        c = c[..., 0::2] | c[..., 1::2] << 4
+    zero = torch.randint(top // 2, top // 2 + 2, (rows, 2 * H), generator=gen, device="cuda").to(torch.int16)
+    step = ((0.3 * randn(gen, rows, 2 * H)).exp() * (6 / top)).half().view(torch.int16)
+    return c.contiguous(), torch.stack([step, zero], -1)
+
+
+def prepare_attend(case, gen):
+    n, page = lengths(case), case["page"]
+    dtype = torch.float32 if case["dtype"] == "fp32" else torch.bfloat16
+    s = make_format(case, gen, dtype)
+    used = [-(-m // page) for m in n]
+    pages = sum(used) + 5
+    fill = {t: random_codes(case, gen, pages * page) for t in "kv"}
+    order = torch.randperm(pages, generator=gen, device="cuda").to(torch.int32)
+    table = torch.full((case["batch"], max(used)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, m in enumerate(used):
+        table[b, :m] = order[at:at + m]
+        at += m
+        if n[b] % page:                                        # behind the last token a page holds anything
+            for t in "kv":
+                fill[t][1][order[at - 1].long() * page + torch.arange(n[b] % page, page, device="cuda")] = 0x7e01
+    make_pool(s, case, pages, fill)
+    s["table"], s["lens"] = table, torch.tensor(n, dtype=torch.int32, device="cuda")
+    rows = case["batch"] * case["queries"]
+    s["q"] = (1.5 * randn(gen, rows, case["q_heads"], G)).to(dtype)
+    s["out"] = torch.empty(rows, case["q_heads"], G, dtype=dtype, device="cuda")
+    if own:
+        from paper_2501_19392_amd import binding as B
+        size = B.aquakv_paged_workspace_bytes(s["handle"], s["pages"], case["batch"], case["q_heads"], max(used), rows, case["queries"])
+        s["ws"] = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+    return s
+
+
+# ---------------------------------------------------------------------------------------------------- run
+def run(state):
+    return globals()["run_" + state["case"]["kind"]](state)
+
+
+def run_append(s):
+    if own:
+        from paper_2501_19392_amd import binding as B
+        cos, sin = s["rope"] or (None, None)
+        B.aquakv_paged_append(s["handle"], s["pages"], s["case"]["tokens"], s["K"], s["V"], s["slots"],
+                              s["positions"] if s["rope"] else None, cos, sin, s["Khat"], s["Vhat"])
+        return dict(Khat=s["Khat"], Vhat=s["Vhat"])
+    # in 64 bits: scales and codes are decisions between neighbours
+    K, V = s["K"].double(), s["V"].double()
+    if s["rope"]:
+        cos, sin = (t[s["positions"].long()].double()[:, None] for t in s["rope"])
+        lo, hi = K[..., :64], K[..., 64:]
+        K = torch.cat([lo * cos - hi * sin, hi * cos + lo * sin], -1)
+    kept = (s["slots"] >= 0)[:, None, None]
+    values = functools.partial(held_values, s)
+    return dict(Khat=torch.where(kept, values(K, s["signs"][0]), 0).bfloat16(), Vhat=torch.where(kept, values(V, s["signs"][1]), 0).bfloat16())
+
+
+def hadamard(dtype):
+    h = torch.ones(1, 1, dtype=dtype, device="cuda")
+    while h.shape[0] < G:
+        h = torch.cat([torch.cat([h, h], 1), torch.cat([h, -h], 1)], 0)
+    return h / G ** 0.5
+
+
+def held_values(s, x, sign):
+    """x [T, H, 128] as codes and scales hold it."""
+    if s["grid"] is None:
+        top = 2 ** s["case"]["bits"] - 1
+        r = x.reshape(x.shape[0], D // 64, 64)
+        lo, hi = r.amin(-1, keepdim=True).clamp(max=0), r.amax(-1, keepdim=True).clamp(min=0)
+        step = ((hi - lo) / top).clamp(max=65504).half().double()
+        safe = torch.where(step > 0, step, 1)
+        zero = torch.where(step > 0, (-lo / safe).round().clamp(0, top), 0)
+        code = ((r / safe).round() + zero).clamp(0, top)
+        return ((code - zero) * step).view_as(x)
+    h, sign, c = hadamard(x.dtype), sign.view(H, G).to(x.dtype), s["grid"].to(x.dtype)
+    z = (x * sign) @ h
+    sigma = z.square().mean(-1, keepdim=True).sqrt().clamp(max=65504).half().to(x.dtype)
+    y = (z / torch.where(sigma > 0, sigma, 1)).view(-1, 2)
+    near = torch.addmm(-0.5 * c.square().sum(-1), y, c.T).argmax(-1)
+    return (c[near].view_as(z) * sigma) @ h * sign
+
+
+def unpacked(s, t, dtype):
+    """All rows of the pool's keys or values, [rows, H, 128], as the values they stand for."""
+    codes, bits = s[t + "_codes"], s["case"]["bits"]
+    if s["grid"] is None:
+        each = 8 // bits
+        c = torch.stack([codes >> bits * i & 2 ** bits - 1 for i in range(each)], -1).view(-1, D // 64, 64)
+        step = s[t + "_scales"][..., 0].contiguous().view(torch.float16).to(dtype)
+        zero = s[t + "_scales"][..., 1].to(dtype)
+        return ((c.to(dtype) - zero[..., None]) * step[..., None]).view(-1, H, G)
+    if bits == 4:
+        c = codes.long()
+    elif bits == 2:
+        c = torch.stack([codes & 15, codes >> 4], -1).long()
+    else:
+        b = codes.view(*codes.shape[:2], -1, 3).long()
+        word = b[..., 0] | b[..., 1] << 8 | b[..., 2] << 16
+        c = torch.stack([word >> 6 * i & 63 for i in range(4)], -1)
+    sign = s["signs"]["kv".index(t)].view(H, G).to(dtype)
+    z = s["grid"].to(dtype)[c.view(codes.shape[0], H, G // 2)].view(-1, H, G) * s[t + "_scales"].view(torch.float16).to(dtype)[..., None]
+    return z @ hadamard(dtype) * sign
+
+
+def run_attend(s):
+    c = s["case"]
+    if own:
+        from paper_2501_19392_amd import binding as B
+        B.aquakv_paged_attend(s["handle"], s["pages"], c["batch"], c["q_heads"], s["table"], s["lens"], s["q"], c["queries"], None, SCALE,
+                              s["out"], s["ws"])
+        return s["out"]
+    b, n, qh, page = c["batch"], c["queries"], c["q_heads"], c["page"]
+    T, rep = s["table"].shape[1] * page, qh // H
+    at = torch.arange(T, device="cuda")
+    rows = s["table"].clamp(min=0).long()[:, at // page] * page + at % page                       # [b, T]
+    there = at[None] < s["lens"][:, None]
+    K, V = (torch.where(there[:, :, None, None], unpacked(s, t, torch.float32)[rows], 0).transpose(1, 2).contiguous() for t in "kv")
+    q = s["q"].float().view(b, n, H, rep, G).permute(0, 2, 3, 1, 4).reshape(b, H, rep * n, G)
+    last = s["lens"][:, None] - n + torch.arange(n, device="cuda")[None]                          # [b, n]
+    seen = at[None, None] <= last[:, :, None]                                                     # [b, n, T]
+    x = (q @ K.transpose(2, 3) * SCALE).view(b, H, rep, n, T).masked_fill(~seen[:, None, None], -math.inf)
+    p = (x - x.amax(-1, keepdim=True)).exp_()
+    p = p / p.sum(-1, keepdim=True)
+    out = p.view(b, H, rep * n, T) @ V
+    return out.view(b, H, rep, n, G).permute(0, 3, 1, 2, 4).reshape(b * n, qh, G).to(s["q"].dtype)
+
+
+# ---------------------------------------------------------------------------------------------------- work, exact
+def work(case):
+    stored = D * CODE_BITS[case["backbone"], case["bits"]] // 16 + (2 * H if case["backbone"] == "grid" else 8 * H)     # a token's keys or values
+    if case["kind"] == "append":
+        T = case["tokens"] - (case["tokens"] // 4 if case["padded"] else 0)
+        rotation, search = (8 * D if case["backbone"] == "grid" else 0), (5 * D if case["backbone"] == "grid" else 4 * D)
+        return dict(bytes=T * (2 * 2 * D + 2 * stored + 2 * 2 * D + 8 + (4 + 4 * G if case["rope"] else 0)), flops=T * 2 * (2 * rotation + search))
+    n, qh = lengths(case), case["q_heads"]
+    pairs = sum(case["queries"] * m - case["queries"] * (case["queries"] - 1) // 2 for m in n)
+    size = 4 if case["dtype"] == "fp32" else 2
+    return dict(bytes=2 * stored * sum(n) + 2 * size * case["batch"] * case["queries"] * qh * G + 4 * sum(-(-m // case["page"]) for m in n),
+                flops=4 * G * qh * pairs)
+
+
+def exact(case, seed):
+    """By the definition, in 64 bits, one head (and sequence) after the other."""
+    s = prepare(case, seed)
+    index = torch.arange(G, device="cuda")
+    both = index[:, None] & index[None]
+    odd = sum(both >> i & 1 for i in range(7)) % 2
+    rot = (1.0 - 2.0 * odd.double()) / math.sqrt(G)                                               # Walsh functions
+    top = 2 ** case["bits"] - 1
+    if case["kind"] == "append":
+        out = {}
+        for t, sign in zip("KV", s["signs"]):
+            x = s[t].double()
+            if t == "K" and s["rope"]:
+                turn = torch.complex(*(a.double()[s["positions"].long()] for a in s["rope"]))[:, None]
+                x = torch.view_as_real(torch.complex(x[..., :64], x[..., 64:]) * turn)
+                x = torch.cat([x[..., 0], x[..., 1]], -1)
+            y = torch.zeros_like(x)
+            for h in range(H):
+                if s["grid"] is None:
+                    for half in (0, 64):
+                        v = x[:, h, half:half + 64]
+                        low = torch.minimum(v.min(1).values, torch.zeros(1, dtype=v.dtype, device="cuda"))
+                        high = torch.maximum(v.max(1).values, torch.zeros(1, dtype=v.dtype, device="cuda"))
+                        step = ((high - low) / top).clamp(max=65504.0).half().double()[:, None]
+                        unit = torch.where(step == 0, 1.0, step)
+                        zero = torch.round(-low[:, None] / unit).clamp(0, top) * (step != 0)
+                        y[:, h, half:half + 64] = step * ((torch.round(v / unit) + zero).clamp(0, top) - zero)
+                    continue
+                sg, c = sign.view(H, G)[h].double(), s["grid"].double()
+                for part, z in zip(y[:, h].split(2048), ((x[:, h] * sg) @ rot).split(2048)):
+                    size = (z.norm(dim=1) / math.sqrt(G)).clamp(max=65504.0).half().double()[:, None]
+                    u = torch.where(size == 0, 0.0, z / size).view(-1, G // 2, 1, 2)
+                    w = c[(u - c).square().sum(-1).argmin(-1)].view(-1, G)
+                    part.copy_((w * size) @ rot * sg)
+            y[s["slots"] < 0] = 0
+            out[t + "hat"] = y
+        return out
+    n, qh, page, pairs = case["queries"], case["q_heads"], case["page"], CODE_BITS[case["backbone"], case["bits"]]
+    rep, result = qh // H, torch.zeros(case["batch"] * case["queries"], qh, G, dtype=torch.float64, device="cuda")
+    shift = torch.arange(8, device="cuda", dtype=torch.uint8)
+    weight = 2 ** torch.arange(pairs if s["grid"] is not None else case["bits"], device="cuda")
+    for b, m in enumerate(lengths(case)):
+        rows = torch.cat([torch.arange(page, device="cuda") + p * page for p in s["table"][b].tolist() if p >= 0])[:m]
+        for h in range(H):
+            side = []
+            for t, sign in zip("kv", s["signs"]):
+                string = (s[t + "_codes"][rows, h][:, :, None] >> shift & 1).view(m, -1, len(weight)).long()      # little-endian bits
+                number = (string * weight).sum(-1)
+                scale = s[t + "_scales"][rows]
+                if s["grid"] is None:
+                    f = scale[:, 2 * h:2 * h + 2, 0].contiguous().view(torch.float16).double()
+                    side.append(((number.view(m, 2, 64) - scale[:, 2 * h:2 * h + 2, 1:].long()) * f[..., None]).view(m, G))
+                else:
+                    f = scale[:, h].contiguous().view(torch.float16).double()
+                    side.append((s["grid"].double()[number].view(m, G) * f[:, None]) @ rot * sign.view(H, G)[h].double())
+            k, v = side
+            for i in range(0, n, 512):
+                j = min(n, i + 512)
+                q = s["q"][b * n + i:b * n + j, h * rep:(h + 1) * rep].double()
+                score = torch.einsum("jrd,td->rjt", q, k) * SCALE
+                hidden = torch.arange(m, device="cuda")[None, :] > torch.arange(m - n + i, m - n + j, device="cuda")[:, None]
+                p = torch.softmax(score.masked_fill(hidden, -math.inf), -1)
+                result[b * n + i:b * n + j, h * rep:(h + 1) * rep] = (p @ v).transpose(0, 1)
+    return result
