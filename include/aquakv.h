@@ -495,6 +495,59 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
                         const float* rope_cos, const float* rope_sin, float score_scale, void* const* hat,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * A cache of one layer in pages, held as codes (4 bits a value and the other widths): for layers without predictors (d_in_k =
+ * d_in_v = 0, the backbone quantizer of Sect. 2 by itself), so that a page needs no other one, and with groups within a head
+ * (rht_group 0, or 128 / 64); AQUAKV_EUNSUPPORTED otherwise.  The pool is n_pages * page_tokens rows of codes and scales in the
+ * layouts of aquakv_quantize (which may fill rows as well); row page * page_tokens + i is token i of a page.
+ * page_tokens: a multiple of 8.  All four arrays are 16-byte aligned.  What unused rows hold does not matter.
+ *
+ * aquakv_paged_append -- `tokens` new tokens go to rows of the pool: token t with its keys K + t * k_stride, values V + t *
+ *   v_stride (elements; [kv_heads, 128] contiguous, rows 16-byte aligned, so that slices of a joint product need no copy) to row
+ *   slots[t].  rope_cos / rope_sin (both NULL, or device fp32 [rope_rows, 64]): the keys are rotated by row positions[t] of the
+ *   tables on the way, in the convention of aquakv_decode_attn_scores_rope; the pool then holds rotated keys.  Then both are quantized as
+ *   aquakv_quantize does (codes and scales of unrotated rows: the same bits).  Khat, Vhat (nullable, dtype, [tokens, kv_heads, 128]):
+ *   the rows as the pool holds them.  A token whose slot is outside the pool (-1, say: a padded batch) or whose position is outside
+ *   the tables is left out: nothing is written for it, Khat and Vhat neither.  Slots of the others must differ from each other: a
+ *   row that two tokens name holds anything afterwards, the other rows are not affected.  slots: device int64, positions: device
+ *   int32, each aligned to its type (positions unused without tables).
+ *
+ * aquakv_paged_attend -- soft-max attention over pages, one or more queries per sequence:
+ *   out[r, qh, :] = sum_t p_t vhat_t,  p = softmax over t of score_scale * q[r, qh, :] . khat_t, of kv head qh / (q_heads / kv_heads),
+ *   khat, vhat what codes and scales stand for, unrounded.  Sequence b has seq_lens[b] tokens in the cache, token t in page
+ *   page_table[b, t / page_tokens]; its queries are its last tokens: query i of n sees the tokens t <= seq_lens[b] - n + i, which
+ *   must have been appended already.  A query that sees no token gives 0.  Queries are taken as already rotated.
+ *   q [q_rows, q_heads, 128], row r at q + r * q_stride elements (16-byte aligned rows); out [q_rows, q_heads, 128]; both dtype.
+ *   q_start NULL: max_queries queries of every sequence, q_rows = batch * max_queries.  Else device int32 [batch + 1], ascending:
+ *   sequence b has the rows q_start[b] ... q_start[b + 1] - 1, at most max_queries (rows beyond that, and rows of no sequence, are
+ *   left as they were).  Counts are read on the device, so a captured call follows them: lengths are cut to 0 ... table_pages *
+ *   page_tokens, row numbers to 0 ... q_rows, and tokens of a page that is not in the pool (page_table outside 0 ... n_pages - 1)
+ *   are not seen.  page_table, seq_lens, q_start: aligned to 4 bytes.
+ *   bf16: products in fp16 with fp32 sums (queries and grid points rounded to fp16 behind a power of two, weights likewise), results within a
+ *   rounding of bf16; fp32: fp32 throughout.
+ *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments), for the same arguments or any that are at least as
+ *   large; the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same time, captured ones included,
+ *   need workspaces of their own.
+ *
+ * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.
+ */
+typedef struct aquakv_pages {
+  int32_t n_pages, page_tokens;
+  uint8_t* k_codes;
+  uint16_t* k_scales;
+  uint8_t* v_codes;
+  uint16_t* v_scales;
+} aquakv_pages;
+int aquakv_paged_append(const aquakv_layer* layer, const aquakv_pages* pages, int64_t tokens, const void* K, int64_t k_stride,
+                        const void* V, int64_t v_stride, const int64_t* slots, const int32_t* positions, const float* rope_cos,
+                        const float* rope_sin, int32_t rope_rows, void* Khat, void* Vhat, void* stream);
+size_t aquakv_paged_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads,
+                                    int32_t table_pages, int64_t q_rows, int32_t max_queries);
+int aquakv_paged_attend(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                        int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
+                        const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -42,6 +42,7 @@ EXPORTS = [
     "aquakv_fit_workspace_bytes", "aquakv_fit_predictor",
     "aquakv_softmax", "aquakv_weighted_workspace_bytes", "aquakv_decode_values_weighted", "aquakv_decode_values_attend",
     "aquakv_attend_raw", "aquakv_copy_ranges", "aquakv_encode_layers", "aquakv_attend_cache_workspace_bytes", "aquakv_attend_cache",
+    "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend",
 ]
 
 
@@ -65,6 +66,11 @@ class aquakv_cache_layer(ctypes.Structure):
 class aquakv_cache_shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "kv_heads", "q_heads", "batch", "sink_rows", "recent_rows")] + [
         ("capacity", ctypes.c_int64)]
+
+
+class aquakv_pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in (
+        "k_codes", "k_scales", "v_codes", "v_scales")]
 
 
 _P = ctypes.c_void_p
@@ -115,7 +121,12 @@ _CLP, _CSP = ctypes.POINTER(aquakv_cache_layer), ctypes.POINTER(aquakv_cache_sha
 _lib.aquakv_attend_cache_workspace_bytes.restype = ctypes.c_size_t
 _lib.aquakv_attend_cache_workspace_bytes.argtypes = [_CLP, ctypes.c_int32, _CSP]
 _lib.aquakv_attend_cache.argtypes = [_CLP, ctypes.c_int32, _CSP] + [_P] * 5 + [ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
-for _n in ("aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
+_PP, _I32, _I64 = ctypes.POINTER(aquakv_pages), ctypes.c_int32, ctypes.c_int64
+_lib.aquakv_paged_append.argtypes = [_LP, _PP, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _I32, _P, _P, _P]
+_lib.aquakv_paged_workspace_bytes.restype = ctypes.c_size_t
+_lib.aquakv_paged_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, _I32]
+_lib.aquakv_paged_attend.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
+for _n in ("aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
            "aquakv_decode_attn_scores", "aquakv_decode_attn_scores_rope", "aquakv_decode_attn_scores_folded",
            "aquakv_decode_attn_scores_folded_static", "aquakv_encode_keys", "aquakv_encode_values",
            "aquakv_decode_values", "aquakv_fit_predictor"):
@@ -254,6 +265,28 @@ class Layer:
         """Workspace of aquakv_decode_values_weighted / aquakv_decode_values_attend."""
         return torch.empty(max(aquakv_weighted_workspace_bytes(self, batch, seq_len, q_heads), 16), dtype=torch.uint8,
                            device=device)
+
+
+class Pages:
+    """A layer's cache in pages: owns the code and scale tensors of n_pages * page_tokens rows (given ones, or new ones) and the
+    C struct that points at them."""
+
+    def __init__(self, layer: Layer, n_pages: int, page_tokens: int, device="cuda", k_codes=None, k_scales=None, v_codes=None, v_scales=None):
+        self.n_pages, self.page_tokens = n_pages, page_tokens
+        given = (k_codes, k_scales, v_codes, v_scales)
+        if all(t is None for t in given):
+            given = (*layer.alloc_codes(n_pages * page_tokens, device), *layer.alloc_codes(n_pages * page_tokens, device))
+        rows = n_pages * page_tokens
+        code_bytes, scale_words = rows * layer.kv_heads * layer.code_bytes_per_group, rows * layer.d // layer.rht_group * layer.scale_words_per_group
+        for t, size in zip(given, (code_bytes, 2 * scale_words) * 2):
+            if t is None or not t.is_contiguous() or t.nbytes != size:
+                raise ValueError(f"codes and scales of {rows} rows, all four of them, contiguous")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = given
+        self.c = aquakv_pages(n_pages, page_tokens, *(t.data_ptr() for t in given))
+
+
+def _pages_ref(pages):
+    return ctypes.byref(pages.c if isinstance(pages, Pages) else pages)
 
 
 def _layer_ref(layer):
@@ -432,6 +465,53 @@ def aquakv_attend_cache(layers, shape, n_sink, n_compressed, n_recent, score_sca
     w, wb = _ws(workspace)
     _check(_lib.aquakv_attend_cache(layers, len(layers), ctypes.byref(shape), at, at + 4 * n, at + 8 * n, _ptr(rope_cos),
                                     _ptr(rope_sin), score_scale, hats.buffer_info()[0], w, wb, _stream(stream)))
+
+
+def _rows(x, row: int):
+    """Rows of heads x 128 that may lie apart -> (address, elements from row to row); an address: one behind the other."""
+    if not isinstance(x, torch.Tensor):
+        return _ptr(x), row
+    if x.dim() != 3 or x.shape[1] * x.shape[2] != row or x.stride(2) != 1 or x.stride(1) != x.shape[2]:
+        raise ValueError(f"rows of {row} elements, each contiguous")
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else row
+
+
+def _typed(x, dtype, name: str, shape=None):
+    if isinstance(x, torch.Tensor) and (x.dtype != dtype or (shape is not None and x.shape != shape)):
+        raise ValueError(f"{name} must be {dtype}{'' if shape is None else list(shape)}")
+    return _ptr(x)
+
+
+def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_cos, rope_sin, Khat, Vhat, stream=None) -> None:
+    """K, V: [tokens, kv_heads, 128], rows may lie apart; rope_cos, rope_sin: [rope_rows, 64] tensors (None: no rotation, positions unused)."""
+    row = layer.kv_heads * layer.head_dim
+    k, ks = _rows(K, row)
+    v, vs = _rows(V, row)
+    if any(isinstance(x, torch.Tensor) and (x.shape[0] != tokens or x.dtype != layer.dtype) for x in (K, V, Khat, Vhat)):
+        raise ValueError(f"{tokens} rows of {layer.dtype}")
+    rows = 0 if rope_cos is None else min(rope_cos.shape[0], rope_sin.shape[0])
+    _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, "slots", (tokens,)),
+                                    _typed(positions, torch.int32, "positions", (tokens,)), _typed(rope_cos, torch.float32, "rope_cos"),
+                                    _typed(rope_sin, torch.float32, "rope_sin"), rows, _ptr(Khat), _ptr(Vhat), _stream(stream)))
+
+
+def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_pages: int, q_rows: int, max_queries: int) -> int:
+    return _lib.aquakv_paged_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table_pages, q_rows, max_queries)
+
+
+def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
+                        workspace, stream=None) -> None:
+    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence]."""
+    at, stride = _rows(q, q_heads * layer.head_dim)
+    if page_table.dim() != 2 or page_table.shape[0] != batch:
+        raise ValueError("page_table must be [batch, pages]")
+    if q.dtype != layer.dtype or out.dtype != layer.dtype or out.numel() != q.numel():
+        raise ValueError(f"q and out must be of one size, {layer.dtype}")
+    ws, nbytes = _ws(workspace)
+    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads, _typed(page_table, torch.int32, "page_table"),
+                                    page_table.shape[1], _typed(seq_lens, torch.int32, "seq_lens", (batch,)), q.shape[0], max_queries,
+                                    _typed(q_start, torch.int32, "q_start", (batch + 1,)), at, stride, score_scale, _ptr(out), ws, nbytes,
+                                    _stream(stream)))
 
 
 def aquakv_fit_workspace_bytes(d_in: int, d_out: int) -> int:

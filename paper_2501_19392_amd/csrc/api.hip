@@ -1628,4 +1628,141 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
   return AQUAKV_OK;
 }
 
+// ---- a cache in pages of codes ----------------------------------------------------------------------------------
+namespace {
+inline bool misaligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) != 0; }
+int check_array(const void* p, const char* name, unsigned align) {
+  if (p == nullptr) return fail(AQUAKV_ENULL, "%s is NULL", name);
+  if (misaligned_to(p, align)) return fail(AQUAKV_EALIGN, "%s is not %u-byte aligned", name, align);
+  return AQUAKV_OK;
+}
+
+int check_pages(const aquakv_layer* L, const aquakv_pages* pg) {
+  CHECK(check_layer(L));
+  if (L->d_in_k != 0 || L->d_in_v != 0) return fail(AQUAKV_EUNSUPPORTED, "pages hold layers without predictors");
+  if (is_wide(L)) return fail(AQUAKV_EUNSUPPORTED, "rht_group=%d: pages hold groups within a head", L->rht_group);
+  if (pg == nullptr) return fail(AQUAKV_ENULL, "pages is NULL");
+  if (pg->n_pages < 1) return fail(AQUAKV_EINVAL, "n_pages=%d", pg->n_pages);
+  if (pg->page_tokens < 8 || pg->page_tokens % 8) return fail(AQUAKV_EINVAL, "page_tokens=%d must be a positive multiple of 8", pg->page_tokens);
+  if ((int64_t)pg->n_pages * pg->page_tokens > 0x7fffffffLL)
+    return fail(AQUAKV_EUNSUPPORTED, "%d pages of %d tokens: at most 2^31 - 1 tokens", pg->n_pages, pg->page_tokens);
+  CHECK(check_ptr(pg->k_codes, "k_codes", true));
+  CHECK(check_ptr(pg->k_scales, "k_scales", true));
+  CHECK(check_ptr(pg->v_codes, "v_codes", true));
+  return check_ptr(pg->v_scales, "v_scales", true);
+}
+aquakv::PagedPool pool_of(const aquakv_pages* pg) {
+  return {pg->k_codes, pg->k_scales, pg->v_codes, pg->v_scales, (int64_t)pg->n_pages * pg->page_tokens, pg->n_pages, pg->page_tokens};
+}
+struct PoolRanges { Range r[4]; };
+PoolRanges pool_ranges(const aquakv_layer* L, const aquakv_pages* pg) {
+  const size_t rows = (size_t)pg->n_pages * pg->page_tokens, codes = rows * make_plan(L, 1).code_row, scales = rows * scale_row_bytes(L);
+  return {{{pg->k_codes, codes, "k_codes"}, {pg->k_scales, scales, "k_scales"}, {pg->v_codes, codes, "v_codes"}, {pg->v_scales, scales, "v_scales"}}};
+}
+// rows of `row` elements, `stride` elements apart
+int check_rows(const void* p, const char* name, int64_t stride, int64_t row, size_t eb) {
+  CHECK(check_ptr(p, name, true));
+  if (stride < row || stride > ((int64_t)1 << 40)) return fail(AQUAKV_EINVAL, "%s: rows of %lld elements, %lld apart", name, (long long)row, (long long)stride);
+  if (stride * (int64_t)eb % 16) return fail(AQUAKV_EALIGN, "%s: rows %lld elements apart are not 16-byte aligned", name, (long long)stride);
+  return AQUAKV_OK;
+}
+inline size_t rows_bytes(int64_t n, int64_t stride, int64_t row, size_t eb) { return n == 0 ? 0 : ((size_t)(n - 1) * stride + row) * eb; }
+
+int check_paged_shape(const aquakv_layer* L, const aquakv_pages* pg, int32_t batch, int32_t q_heads, int32_t table_pages, int64_t q_rows,
+                      int32_t max_queries) {
+  CHECK(check_pages(L, pg));
+  if (batch < 0 || table_pages < 1 || q_rows < 0 || max_queries < 0)
+    return fail(AQUAKV_EINVAL, "batch=%d table_pages=%d q_rows=%lld max_queries=%d", batch, table_pages, (long long)q_rows, max_queries);
+  if (q_heads < 1 || q_heads % L->kv_heads) return fail(AQUAKV_EINVAL, "q_heads=%d must be a multiple of kv_heads=%d", q_heads, L->kv_heads);
+  if (batch > 65535) return fail(AQUAKV_EUNSUPPORTED, "batch=%d: at most 65535 sequences", batch);
+  if ((int64_t)max_queries * q_heads > 0x7fffffffLL || q_rows > 0x7fffffffLL)
+    return fail(AQUAKV_EUNSUPPORTED, "%lld rows, %d queries of %d heads", (long long)q_rows, max_queries, q_heads);
+  if ((int64_t)table_pages * pg->page_tokens > 0x7fffffffLL - 4096)
+    return fail(AQUAKV_EUNSUPPORTED, "%d pages of %d tokens in a sequence", table_pages, pg->page_tokens);
+  return AQUAKV_OK;
+}
+}  // namespace
+
+int aquakv_paged_append(const aquakv_layer* L, const aquakv_pages* pages, int64_t tokens, const void* K, int64_t k_stride, const void* V,
+                        int64_t v_stride, const int64_t* slots, const int32_t* positions, const float* rope_cos, const float* rope_sin,
+                        int32_t rope_rows, void* Khat, void* Vhat, void* stream) {
+  CHECK(check_pages(L, pages));
+  if (tokens < 0) return fail(AQUAKV_EINVAL, "tokens=%lld", (long long)tokens);
+  if (tokens > 0x7fffffffLL / L->kv_heads) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, L->kv_heads);
+  const int64_t D = (int64_t)L->kv_heads * 128;
+  const size_t eb = elem_bytes(L->dtype);
+  CHECK(check_rows(K, "K", k_stride, D, eb));
+  CHECK(check_rows(V, "V", v_stride, D, eb));
+  CHECK(check_array(slots, "slots", 8));
+  if ((rope_cos == nullptr) != (rope_sin == nullptr)) return fail(AQUAKV_ENULL, "rope_cos and rope_sin go together");
+  if (rope_cos != nullptr) {
+    if (rope_rows < 1) return fail(AQUAKV_EINVAL, "rope_rows=%d", rope_rows);
+    CHECK(check_ptr(rope_cos, "rope_cos", true));
+    CHECK(check_ptr(rope_sin, "rope_sin", true));
+    CHECK(check_array(positions, "positions", 4));
+  }
+  CHECK(check_ptr(Khat, "Khat", false));
+  CHECK(check_ptr(Vhat, "Vhat", false));
+  if (tokens == 0) return AQUAKV_OK;
+  const PoolRanges pool = pool_ranges(L, pages);
+  const Params params = params_of(L);
+  const size_t hat = (size_t)tokens * D * eb, angles = rope_cos == nullptr ? 0 : (size_t)rope_rows * 64 * sizeof(float);
+  const Range outs[] = {pool.r[0], pool.r[1], pool.r[2], pool.r[3], {Khat, hat, "Khat"}, {Vhat, hat, "Vhat"}};
+  const Range ins[] = {{K, rows_bytes(tokens, k_stride, D, eb), "K"}, {V, rows_bytes(tokens, v_stride, D, eb), "V"},
+                       {slots, (size_t)tokens * sizeof(int64_t), "slots"},
+                       {positions, rope_cos == nullptr ? 0 : (size_t)tokens * sizeof(int32_t), "positions"},
+                       {rope_cos, angles, "rope_cos"}, {rope_sin, angles, "rope_sin"}, params.r[4], params.r[5], params.r[6], params.r[7]};
+  CHECK(check_no_alias(outs, 6, ins, 10));
+  aquakv::PagedAppendArgs a = {};
+  a.pool = pool_of(pages);
+  a.K = K; a.V = V; a.k_stride = k_stride; a.v_stride = v_stride; a.tokens = tokens;
+  a.slots = slots; a.positions = positions; a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.rope_rows = rope_rows;
+  a.H = L->kv_heads; a.signs_k = L->signs_k; a.signs_v = L->signs_v; a.codebook = L->codebook;
+  a.table = static_cast<const uint32_t*>(L->search_table);
+  a.Khat = Khat; a.Vhat = Vhat;
+  HIP_TRY(aquakv::launch_paged_append(L->dtype, quantizer_id(L), a, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
+}
+
+size_t aquakv_paged_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, int32_t table_pages,
+                                    int64_t q_rows, int32_t max_queries) {
+  if (check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries) != AQUAKV_OK) return 0;
+  return 16;
+}
+
+int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                        int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
+                        const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  CHECK(check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries));
+  if (q_start == nullptr && q_rows != (int64_t)batch * max_queries)
+    return fail(AQUAKV_EINVAL, "q_rows=%lld: without q_start every one of %d sequences has %d", (long long)q_rows, batch, max_queries);
+  const int64_t row = (int64_t)q_heads * 128;
+  const size_t eb = elem_bytes(L->dtype);
+  CHECK(check_array(page_table, "page_table", 4));
+  CHECK(check_array(seq_lens, "seq_lens", 4));
+  if (misaligned_to(q_start, 4)) return fail(AQUAKV_EALIGN, "q_start is not 4-byte aligned");
+  CHECK(check_rows(q, "q", q_stride, row, eb));
+  CHECK(check_ptr(out, "out", true));
+  CHECK(check_ptr(workspace, "workspace", true));
+  if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;
+  const size_t need = aquakv_paged_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries);
+  if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
+  const PoolRanges pool = pool_ranges(L, pages);
+  const Params params = params_of(L);
+  const Range outs[] = {{out, (size_t)q_rows * row * eb, "out"}, {workspace, need, "workspace"}};
+  const Range ins[] = {pool.r[0], pool.r[1], pool.r[2], pool.r[3], {page_table, (size_t)batch * table_pages * sizeof(int32_t), "page_table"},
+                       {seq_lens, (size_t)batch * sizeof(int32_t), "seq_lens"},
+                       {q_start, q_start == nullptr ? 0 : ((size_t)batch + 1) * sizeof(int32_t), "q_start"},
+                       {q, rows_bytes(q_rows, q_stride, row, eb), "q"}, params.r[4], params.r[5], params.r[6]};
+  CHECK(check_no_alias(outs, 2, ins, 11));
+  aquakv::PagedAttendArgs a = {};
+  a.pool = pool_of(pages);
+  a.page_table = page_table; a.seq_lens = seq_lens; a.q_start = q_start;
+  a.table_pages = table_pages; a.batch = batch; a.max_queries = max_queries; a.H = L->kv_heads; a.q_heads = q_heads;
+  a.q_rows = q_rows; a.q_stride = q_stride; a.q = q; a.out = out; a.scale = score_scale;
+  a.signs_k = L->signs_k; a.signs_v = L->signs_v; a.codebook = L->codebook;
+  HIP_TRY(aquakv::launch_paged_attend(L->dtype, quantizer_id(L), a, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
+}
+
 }  // extern "C"

@@ -229,6 +229,43 @@ bool exact_gram_fits(int64_t tokens, int d0, int d1, int d_out);
 hipError_t launch_exact_gram(int64_t tokens, const void* x0, int d0, const void* x1, int d1, const void* Y, int d_out, double* G, void* columns,
                              int* flag, hipStream_t stream);
 
+// A layer's cache in pages of codes (paged_append.hip, paged_attend.hip): `rows` = n_pages * page_tokens rows of H heads in the
+// layout of the quantizers.
+struct PagedPool {
+  uint8_t* k_codes;
+  uint16_t* k_scales;
+  uint8_t* v_codes;
+  uint16_t* v_scales;
+  int64_t rows;
+  int n_pages, page_tokens;
+};
+struct PagedAppendArgs {
+  PagedPool pool;
+  const void *K, *V;                              // token t at + t * stride elements
+  int64_t k_stride, v_stride, tokens;             // tokens * H < 2^31
+  const int64_t* slots;                           // rows of the pool, others: the token is left out
+  const int32_t* positions;
+  const float *rope_cos, *rope_sin;               // nullable, [rope_rows, 64]
+  int rope_rows, H;
+  const int8_t *signs_k, *signs_v;
+  const float* codebook;
+  const uint32_t* table;                          // nullable
+  void *Khat, *Vhat;                              // nullable
+};
+hipError_t launch_paged_append(int dtype, int n_codewords, const PagedAppendArgs& a, hipStream_t stream);
+struct PagedAttendArgs {
+  PagedPool pool;
+  const int32_t *page_table, *seq_lens, *q_start; // [batch, table_pages], [batch], [batch + 1] or NULL: max_queries each
+  int table_pages, batch, max_queries, H, q_heads;
+  int64_t q_rows, q_stride;                       // query row r at + r * q_stride elements
+  const void* q;
+  void* out;                                      // [q_rows, q_heads, 128]
+  float scale;
+  const int8_t *signs_k, *signs_v;
+  const float* codebook;
+};
+hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
+
 // Device-to-device copies of n byte ranges, kCopyRangesPerLaunch per launch (3 KiB of kernel arguments).
 struct CopyRange { void* dst; const void* src; size_t bytes; };
 constexpr int kCopyRangesPerLaunch = 128;

@@ -1,0 +1,83 @@
+// New tokens of a cache that lives in pages of codes: keys rotated to their positions, keys and values quantized (Sect. 2 of the AQUA-KV
+// paper; no predictors), codes and scales to the rows `slots` names.  One launch for both tensors.
+//
+// A head's 128 values are held by eight lanes x 16 as in the stand-alone quantizer, whose body this is: the rotary embedding pairs
+// coordinates 64 apart, which sit in the same register of the lane whose position differs in the uppermost bit.
+#include "codec_core.h"
+#include "kernels.h"
+
+namespace aquakv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int N = 16, kLanes = kGroup / N, kGroups = kThreads / kLanes;      // values per lane, lanes per head group, groups per round
+
+// blockIdx.y: keys, values.  Rows whose slot or position lies outside are left out: nothing is written for them.
+template <typename T, int NCW>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void paged_append_kernel(const PagedAppendArgs a) {
+  const bool keys = blockIdx.y == 0;
+  const T* const X = static_cast<const T*>(keys ? a.K : a.V);
+  const int64_t x_stride = keys ? a.k_stride : a.v_stride;
+  T* const Xhat = static_cast<T*>(keys ? a.Khat : a.Vhat);
+  uint8_t* const codes = keys ? a.pool.k_codes : a.pool.v_codes;
+  uint16_t* const scales = keys ? a.pool.k_scales : a.pool.v_scales;
+  const int8_t* const signs = keys ? a.signs_k : a.signs_v;
+  const bool rope = keys && a.rope_cos != nullptr;
+  __shared__ Lds lds;
+  const int l = group_pos<N>(threadIdx.x), slot_in_block = threadIdx.x / kLanes;
+  if constexpr (!is_rtn(NCW)) {
+    TableRegs<kThreads> table_regs;
+    if (a.table != nullptr) table_regs.request(a.table);
+    load_codebook<NCW>(a.codebook, lds.cb);
+    if (a.table != nullptr) table_regs.store(lds.table);
+    __syncthreads();
+  }
+  const unsigned n_groups = (unsigned)a.tokens * (unsigned)a.H;
+  for (unsigned g0 = blockIdx.x * kGroups; g0 < n_groups; g0 += gridDim.x * kGroups) {
+    unsigned gid = g0 + slot_in_block;
+    const bool there = gid < n_groups;
+    if (!there) gid = n_groups - 1;                       // keep every lane in the DPP exchanges
+    const unsigned t = gid / (unsigned)a.H, head = gid - t * (unsigned)a.H;
+    const int64_t row = a.slots[t];
+    bool active = there && (uint64_t)row < (uint64_t)a.pool.rows;
+    int pos = 0;
+    if (rope) {
+      pos = a.positions[t];
+      if ((unsigned)pos >= (unsigned)a.rope_rows) { active = false; pos = 0; }
+    } else if (a.rope_cos != nullptr) {
+      active = active && (unsigned)a.positions[t] < (unsigned)a.rope_rows;      // (a token is left out as a whole)
+    }
+    float v[N], sf[N] = {};
+    Storage<T>::load(X + t * x_stride + head * kGroup + l * N, v);
+    if constexpr (!is_rtn(NCW)) load_signs(signs, (int)head, l, sf);
+    if (rope) rope128(v, l, a.rope_cos + (int64_t)pos * (kGroup / 2), a.rope_sin + (int64_t)pos * (kGroup / 2));
+    quantize_residual<NCW>(v, sf, l, lds.cb, a.table != nullptr ? lds.table : nullptr, active, row * a.H + head, codes, scales, Xhat != nullptr);
+    if (Xhat != nullptr) {
+      const float zero[N] = {};
+      finish_hat<NCW>(v, sf, zero);
+      if (active) Storage<T>::template store<false>(Xhat + (int64_t)gid * kGroup, l, v);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(int dtype, int n_codewords, const PagedAppendArgs& a, hipStream_t stream) {
+  const int64_t blocks = (a.tokens * a.H + kGroups - 1) / kGroups;
+  const dim3 grid((unsigned)(blocks < 512 ? blocks : 512), 2);
+#define AQUAKV_APPEND(T, NCW) paged_append_kernel<T, NCW><<<grid, kThreads, 0, stream>>>(a)
+#define AQUAKV_APPEND_T(T)                                    \
+  switch (n_codewords) {                                      \
+    case kRtn2: AQUAKV_APPEND(T, kRtn2); break;               \
+    case kRtn4: AQUAKV_APPEND(T, kRtn4); break;               \
+    case 16: AQUAKV_APPEND(T, 16); break;                     \
+    case 64: AQUAKV_APPEND(T, 64); break;                     \
+    default: AQUAKV_APPEND(T, 256);                           \
+  }
+  if (dtype == kBF16) { AQUAKV_APPEND_T(bf16_t) } else { AQUAKV_APPEND_T(float) }
+#undef AQUAKV_APPEND_T
+#undef AQUAKV_APPEND
+  return hipGetLastError();
+}
+
+}  // namespace aquakv
