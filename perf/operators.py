@@ -111,6 +111,13 @@ def grid(bits):
     return pts, nearest(pts.double()).to(torch.uint8)
 
 
+@functools.lru_cache(maxsize=None)
+def search_table(bits):
+    """Made once per grid, as a program does that appends."""
+    from paper_2501_19392_amd import binding as B
+    return B.build_search_table(grid(bits)[0])
+
+
 def randn(gen, *shape):
     return torch.randn(*shape, generator=gen, device="cuda")
 
@@ -133,7 +140,7 @@ def make_format(case, gen, dtype):
     if own:
         from paper_2501_19392_amd import binding as B
         if case["backbone"] == "grid":
-            s["handle"] = B.Layer(H, G, s["grid"], *s["signs"], dtype, search_table=B.build_search_table(s["grid"]))
+            s["handle"] = B.Layer(H, G, s["grid"], *s["signs"], dtype, search_table=search_table(case["bits"]) if case["kind"] == "append" else None)
         else:
             s["handle"] = B.Layer(H, G, None, None, None, dtype, rtn_bits=case["bits"])
     return s
