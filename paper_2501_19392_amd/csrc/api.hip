@@ -1675,10 +1675,10 @@ int check_paged_shape(const aquakv_layer* L, const aquakv_pages* pg, int32_t bat
     return fail(AQUAKV_EINVAL, "batch=%d table_pages=%d q_rows=%lld max_queries=%d", batch, table_pages, (long long)q_rows, max_queries);
   if (q_heads < 1 || q_heads % L->kv_heads) return fail(AQUAKV_EINVAL, "q_heads=%d must be a multiple of kv_heads=%d", q_heads, L->kv_heads);
   if (batch > 65535) return fail(AQUAKV_EUNSUPPORTED, "batch=%d: at most 65535 sequences", batch);
-  if ((int64_t)max_queries * q_heads > 0x7fffffffLL || q_rows > 0x7fffffffLL)
+  if ((int64_t)max_queries * q_heads >= (1 << 24) || (int64_t)max_queries * (q_heads / L->kv_heads) > 16 * 65535 || q_rows > 0x7fffffffLL)
     return fail(AQUAKV_EUNSUPPORTED, "%lld rows, %d queries of %d heads", (long long)q_rows, max_queries, q_heads);
-  if ((int64_t)table_pages * pg->page_tokens > 0x7fffffffLL - 4096)
-    return fail(AQUAKV_EUNSUPPORTED, "%d pages of %d tokens in a sequence", table_pages, pg->page_tokens);
+  if ((int64_t)table_pages * pg->page_tokens > 0x7fffffffLL - 4096 || (int64_t)table_pages * pg->page_tokens * (batch > 0 ? batch : 1) > ((int64_t)1 << 35))
+    return fail(AQUAKV_EUNSUPPORTED, "%d sequences of up to %d pages of %d tokens", batch, table_pages, pg->page_tokens);
   return AQUAKV_OK;
 }
 }  // namespace
@@ -1727,7 +1727,10 @@ int aquakv_paged_append(const aquakv_layer* L, const aquakv_pages* pages, int64_
 size_t aquakv_paged_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, int32_t table_pages,
                                     int64_t q_rows, int32_t max_queries) {
   if (check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries) != AQUAKV_OK) return 0;
-  return 16;
+  aquakv::PagedAttendArgs a = {};
+  a.pool = pool_of(pages);
+  a.batch = batch; a.table_pages = table_pages; a.max_queries = max_queries; a.q_heads = q_heads; a.H = L->kv_heads;
+  return (aquakv::paged_attend_workspace_bytes(a) + 255) / 256 * 256 + 256;
 }
 
 int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
@@ -1761,7 +1764,7 @@ int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_
   a.table_pages = table_pages; a.batch = batch; a.max_queries = max_queries; a.H = L->kv_heads; a.q_heads = q_heads;
   a.q_rows = q_rows; a.q_stride = q_stride; a.q = q; a.out = out; a.scale = score_scale;
   a.signs_k = L->signs_k; a.signs_v = L->signs_v; a.codebook = L->codebook;
-  HIP_TRY(aquakv::launch_paged_attend(L->dtype, quantizer_id(L), a, static_cast<hipStream_t>(stream)));
+  HIP_TRY(aquakv::launch_paged_attend(L->dtype, quantizer_id(L), a, workspace, static_cast<hipStream_t>(stream)));
   return AQUAKV_OK;
 }
 

@@ -263,8 +263,13 @@ struct PagedAttendArgs {
   float scale;
   const int8_t *signs_k, *signs_v;
   const float* codebook;
+  // set by the launcher
+  float *part, *stats;                            // [items, max_queries, q_heads, 128], [items, max_queries, q_heads, 2]
+  int slots, min_tiles;                           // pieces that fill the chip, tiles of a piece at least
+  uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
 };
-hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
+size_t paged_attend_workspace_bytes(const PagedAttendArgs& a);
+hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 
 // Device-to-device copies of n byte ranges, kCopyRangesPerLaunch per launch (3 KiB of kernel arguments).
 struct CopyRange { void* dst; const void* src; size_t bytes; };

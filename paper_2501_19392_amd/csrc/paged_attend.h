@@ -1,0 +1,517 @@
+// What the kernels that attend over pages of codes share: which rows and tokens they take, codes to fp16 operands of the matrix
+// instructions, the query's way in and the result's way out.
+//
+// Precision.  Operands are fp16 (11 bits): the rotated query times a power of two of its own, grid points times a power of two of
+// the grid's, weights times the token's scale relative to a running reference, all sums fp32.  fp32 layers hold each of them as two
+// fp16 numbers (22 bits) and take three products.  Uniform codes and zero points are exact: a code at the low end of a half-word is the
+// subnormal fp16 number code * 2^-24, which the matrix instructions take as it is, so that a mask is all the conversion there is.
+#pragma once
+#include "codec_core.h"
+#include "kernels.h"
+
+namespace aquakv {
+namespace paged {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(4))) int32_t* ConstInts;       // (scalar loads: what is read through it is not written meanwhile)
+inline __device__ ConstInts const_ints(const int32_t* p) { return (ConstInts)(uintptr_t)p; }
+
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kTile = 32;                    // tokens of a tile: four groups of 8, each within a page
+constexpr int kQueryExp = 14;                // largest coordinate of a row's query: 2^13 ... 2^14
+constexpr float kTopWeight = 0x1p15f;        // a weight beyond this moves the reference,
+constexpr float kStartExp = 8.0f;            // so that the largest is 2^kStartExp: what is 2^-33 of it still counts
+
+// ---------------------------------------------------------------- rows, pieces
+// What a sequence asks: `count` queries, its last tokens, rows first ... of q, of which n are answered; len tokens are cached.
+struct PagedQueries { int64_t first; int count, n, len; };
+__device__ __forceinline__ int length_of(const PagedAttendArgs& a, int len) {
+  return (int)min((int64_t)max(len, 0), (int64_t)a.table_pages * a.pool.page_tokens);
+}
+__device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, int b) {
+  PagedQueries w;
+  w.first = (int64_t)b * a.max_queries;
+  w.count = a.max_queries;
+  if (a.q_start != nullptr) {
+    const int64_t from = const_ints(a.q_start)[b], to = const_ints(a.q_start)[b + 1];
+    w.first = from < 0 ? 0 : from < a.q_rows ? from : a.q_rows;
+    const int64_t end = to < w.first ? w.first : to < a.q_rows ? to : a.q_rows;
+    w.count = (int)(end - w.first);
+  }
+  w.n = min(w.count, a.max_queries);
+  w.len = length_of(a, const_ints(a.seq_lens)[b]);
+  return w;
+}
+
+// The tokens of all sequences are cut into pieces of equally many tiles, so that about a.slots of them cover the batch whatever its
+// lengths (each sequence has one at least): item i of the launch is piece `piece` of `pieces` of sequence b (-1: behind the last).
+struct Share { int b, piece, pieces, tiles, items, first; };
+__device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
+  return b < a.batch ? max((length_of(a, a.seq_lens[b]) + kTile - 1) / kTile, 1) : 0;
+}
+// tiles per piece
+__device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int64_t total) {
+  const int64_t room = max(a.slots - a.batch, max(a.slots / 2, 1));
+  return (int)max((total + room - 1) / room, (int64_t)a.min_tiles);
+}
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
+  return x;
+}
+// by_item: of item `which`; else of sequence `which` (first: its first item)
+template <bool BY_ITEM> __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int which) {
+  Share s = {-1, 0, 1, 0, 0, 0};
+  if (a.batch == 1) {
+    const int n = max((length_of(a, const_ints(a.seq_lens)[0]) + kTile - 1) / kTile, 1);
+    s.tiles = piece_tiles(a, n);
+    s.items = s.pieces = (n + s.tiles - 1) / s.tiles;
+    if (!BY_ITEM || which < s.items) { s.b = 0; s.piece = which; }
+    return s;
+  }
+  int64_t total = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) total += wave_sum(tiles_of(a, b0 + lane));
+  s.tiles = piece_tiles(a, total);
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int mine = (tiles_of(a, b0 + lane) + s.tiles - 1) / s.tiles;
+    int end = mine;                                        // items up to and with this sequence
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const int add = __shfl_up(end, k);
+      end += lane >= k ? add : 0;
+    }
+    end += s.items;
+    const uint64_t past = BY_ITEM ? __builtin_amdgcn_ballot_w64(end > which) : b0 + 63 >= which ? ~0ull << (which - b0) : 0;
+    if (past != 0 && s.b < 0) {
+      const int l = __builtin_ctzll(past);
+      s.b = b0 + l;
+      s.pieces = __builtin_amdgcn_readlane(mine, l);
+      s.first = __builtin_amdgcn_readlane(end, l) - s.pieces;
+      s.piece = which - s.first;
+    }
+    s.items = __builtin_amdgcn_readlane(end, 63);
+  }
+  return s;
+}
+
+// Pool rows at which the four groups of 8 tokens of a tile start, -1: not there.
+struct Rows { int r[4]; };
+__device__ __forceinline__ Rows rows_of(const PagedAttendArgs& a, int b, int t) {
+  const ConstInts table = const_ints(a.page_table) + (int64_t)b * a.table_pages;
+  Rows out;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t group = (uint32_t)t / 8 + j;
+    uint32_t page = (uint32_t)(((uint64_t)group * a.page_magic) >> 32), in = group - page * a.page_groups;      // (one short at most)
+    if (in >= a.page_groups) { ++page; in -= a.page_groups; }
+    const int at = page < (uint32_t)a.table_pages ? table[page] : -1;
+    out.r[j] = (uint32_t)at < (uint32_t)a.pool.n_pages ? at * a.pool.page_tokens + (int)in * 8 : -1;
+  }
+  return out;
+}
+__device__ __forceinline__ unsigned there_of(const Rows& r) {
+  return (r.r[0] >= 0) | (r.r[1] >= 0) << 1 | (r.r[2] >= 0) << 2 | (r.r[3] >= 0) << 3;
+}
+__device__ __forceinline__ uint32_t row_of(const Rows& r, int j) {        // a row there is, in any case
+  const int r0 = r.r[0], r1 = r.r[1], r2 = r.r[2], r3 = r.r[3];           // (values: a choice between elements would be one between addresses)
+  const int lo = (j & 1) ? r1 : r0, hi = (j & 1) ? r3 : r2;
+  return (uint32_t)max((j & 2) ? hi : lo, 0);
+}
+
+// ---------------------------------------------------------------- columns: lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float column_max(float x) {
+  float y = x;
+  swap_lanes<16>(x, y);
+  x = fmaxf(x, y);
+  y = x;
+  swap_lanes<32>(x, y);
+  return fmaxf(x, y);
+}
+__device__ __forceinline__ float column_sum(float x) { return far_sum<32>(far_sum<16>(x)); }
+// The (unnormalised) transform of a row's 128 values, 32 g ... in lane group g.
+__device__ __forceinline__ void wht_columns(float (&v)[32]) {
+#pragma unroll
+  for (int h = 1; h < 32; h <<= 1) {
+#pragma unroll
+    for (int r = 0; r < 32; ++r) {
+      if ((r & h) == 0) {
+        const float x = v[r], y = v[r + h];
+        v[r] = x + y;
+        v[r + h] = x - y;
+      }
+    }
+  }
+  wht_swap_stage<16>(v);
+  wht_swap_stage<32>(v);
+}
+
+__device__ __forceinline__ uint32_t f16_pair(float x, float y) {
+  const f16x2 h = {(_Float16)x, (_Float16)y};
+  return __builtin_bit_cast(uint32_t, h);
+}
+// x as one fp16 number (TERMS = 1), or as the sum of two
+template <int TERMS> __device__ __forceinline__ void split_f16(const float (&x)[8], f16x8 (&out)[TERMS]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    out[0][i] = (_Float16)x[i];
+    if constexpr (TERMS == 2) out[1][i] = (_Float16)(x[i] - (float)out[0][i]);
+  }
+}
+__device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(f16x8, u32x4{a, b, c, d}); }
+
+// ---------------------------------------------------------------- codes
+template <int NCW, int TERMS> struct Codes {
+  static constexpr bool kRtn = is_rtn(NCW);
+  static constexpr int c = CodeBits<NCW>::c;               // bits per pair of values
+  static constexpr int kRow = kGroup / 2 * c / 8;          // bytes of a token's codes in one head
+  // The grid in LDS: a row of 256 bytes per point that holds it over and over (fp16 pair, or that and the rest of it), so that every
+  // lane finds its own copy in its own banks, and the byte offset of a look-up is (code << 8 | the lane's copy), put together by one byte permute.
+  static constexpr int kTableBytes = kRtn ? 0 : NCW * 256;
+  static constexpr int kEntry = 4 * TERMS;
+  static constexpr int kScaleBytes = kRtn ? 512 : 128;     // per wave
+  static constexpr int kVWords = kRtn || c == 6 ? 16 : 8;
+
+  // -> exponent e of the grid: it is held times 2^-e
+  static __device__ __forceinline__ int stage(const float* __restrict__ codebook, unsigned char* lds) {
+    if constexpr (kRtn) return 0;
+    float top = 0.f;
+    for (int j = threadIdx.x & 63; j < 2 * NCW; j += 64) top = fmaxf(top, fabsf(codebook[j]));
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    const int e = max(__builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top)), -100);
+    for (int i = threadIdx.x; i < NCW * 16; i += blockDim.x) {
+      const float x = __builtin_ldexpf(codebook[2 * (i / 16)], -e), y = __builtin_ldexpf(codebook[2 * (i / 16) + 1], -e);
+      const uint32_t hi = f16_pair(x, y);
+      uint32_t other = hi;
+      if constexpr (TERMS == 2) {
+        const f16x2 h = __builtin_bit_cast(f16x2, hi);
+        other = f16_pair(x - (float)h[0], y - (float)h[1]);
+      }
+      *reinterpret_cast<u32x4*>(lds + 16 * i) = u32x4{hi, other, hi, other};
+    }
+    return e;
+  }
+
+  // ---- the row's query: which coordinates lane group g holds, in which order
+  static __device__ __forceinline__ int coordinate(int g, int r) { return kRtn ? (r < 16 ? 16 * g + r : 64 + 16 * g + r - 16) : 32 * g + r; }
+  template <typename T> static __device__ __forceinline__ void load_query(const T* __restrict__ row, int g, float (&v)[32]) {
+    float half[16];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      Storage<T>::load(row + coordinate(g, 16 * k), half);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[16 * k + r] = half[r];
+    }
+  }
+  static __device__ __forceinline__ void pack_query(const float (&v)[32], f16x8 (&q)[TERMS][4], float (&qsum)[2]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = v[8 * j + i];
+      f16x8 part[TERMS];
+      split_f16<TERMS>(x, part);
+#pragma unroll
+      for (int n = 0; n < TERMS; ++n) {
+        if constexpr (!kRtn) {
+          q[n][j] = part[n];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) qsum[j >> 1] += (float)part[n][i];
+        }
+      }
+      if constexpr (kRtn) {
+#pragma unroll
+        for (int n = 0; n < TERMS; ++n) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            // value 8 (j & 1) + i of the half's 16: where its code comes up, and by how much it is too large there
+            const int r = 8 * (j & 1) + i;
+            const int to_j = NCW == kRtn4 ? j : 2 * (j >> 1) + ((r >> 2) & 1);
+            const int at = NCW == kRtn4 ? 2 * (i & 3) + (i >> 2) : 2 * (r & 3) + (r >> 3);
+            q[n][to_j][at] = part[n][i] * (_Float16)(1.0f / (float)field_scale(NCW == kRtn4 ? i & 1 : r & 3));
+          }
+        }
+      }
+    }
+    if constexpr (kRtn) {
+      qsum[0] = column_sum(qsum[0]) * 0x1p-24f;
+      qsum[1] = column_sum(qsum[1]) * 0x1p-24f;
+    }
+  }
+  // uniform: the k-th field of a half-word is masked in place, and so this many times its code
+  static constexpr int field_scale(int k) { return 1 << (NCW * k); }
+  static constexpr uint32_t field_mask(int k) { return 0x00010001u * (((1u << NCW) - 1u) << (NCW * k)); }
+  static constexpr int kFields = NCW == kRtn4 ? 2 : 4;     // fields of a byte
+
+  // ---- a tile's codes and scales on their way: keys of tokens 8 (m / 4) + m % 4 (+ 4), the lane group's share of the coordinates;
+  // values of tokens 8 g ..., 8 coordinates; the scale word of token lane % 32, lanes from 32 on: of the values
+  struct Words {
+    u32x4 k[2];
+    uint32_t v[kVWords];
+    u32x2 scale;
+  };
+  static __device__ __forceinline__ Words request(const PagedAttendArgs& a, const Rows& rows, int h, int lane) {
+    const int m = lane & 15, g = lane >> 4;
+    const uint32_t row_bytes = (uint32_t)a.H * kRow, head = (uint32_t)h * kRow;
+    Words w;
+    const uint8_t* k = a.pool.k_codes + (uint64_t)row_of(rows, m >> 2) * row_bytes + ((m & 3) * row_bytes + head);
+#pragma unroll
+    for (int p = 0; p < 2; ++p, k += 4 * row_bytes) {
+      if constexpr (NCW == kRtn4) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(k + 8 * g), y = *reinterpret_cast<const u32x2*>(k + 32 + 8 * g);
+        w.k[p] = u32x4{x.x, x.y, y.x, y.y};
+      } else if constexpr (NCW == kRtn2) {
+        w.k[p] = u32x4{*reinterpret_cast<const uint32_t*>(k + 4 * g), *reinterpret_cast<const uint32_t*>(k + 16 + 4 * g), 0, 0};
+      } else if constexpr (c == 8) {
+        w.k[p] = *reinterpret_cast<const u32x4*>(k + 16 * g);
+      } else if constexpr (c == 4) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(k + 8 * g);
+        w.k[p] = u32x4{x.x, x.y, 0, 0};
+      } else {
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(k + 12 * g);
+        w.k[p] = u32x4{x[0], x[1], x[2], 0};
+      }
+    }
+    const uint8_t* v = a.pool.v_codes + (uint64_t)row_of(rows, g) * row_bytes + head;
+#pragma unroll
+    for (int e = 0; e < 8; ++e, v += row_bytes) {
+      if constexpr (NCW == kRtn4) {
+        w.v[e] = *reinterpret_cast<const uint16_t*>(v + 2 * m);
+        w.v[8 + e] = *reinterpret_cast<const uint16_t*>(v + 32 + 2 * m);
+      } else if constexpr (NCW == kRtn2) {
+        w.v[e] = v[m];
+        w.v[8 + e] = v[16 + m];
+      } else if constexpr (c == 8) {
+        w.v[e] = *reinterpret_cast<const uint32_t*>(v + 4 * m);
+      } else if constexpr (c == 4) {
+        w.v[e] = *reinterpret_cast<const uint16_t*>(v + 2 * m);
+      } else {                                             // the two words that the lane's 24 bits lie in
+        w.v[e] = reinterpret_cast<const uint32_t*>(v)[(3 * m) >> 2];
+        w.v[8 + e] = reinterpret_cast<const uint32_t*>(v)[(3 * m + 2) >> 2];
+      }
+    }
+    const uint16_t* const scales = lane < 32 ? a.pool.k_scales : a.pool.v_scales;
+    const uint64_t at = (uint64_t)(row_of(rows, (lane >> 3) & 3) + (lane & 7)) * a.H + h;
+    if constexpr (kRtn) w.scale = reinterpret_cast<const u32x2*>(scales)[at];
+    else w.scale = u32x2{scales[at], 0};
+    return w;
+  }
+
+  // ---- scales: every lane's eight tokens 8 g ...
+  struct Scales { u32x4 ks[kRtn ? 2 : 1], kz[kRtn ? 2 : 1], vs[kRtn ? 2 : 1], vz[kRtn ? 2 : 1]; };      // 8 half-words each: scales (per half), zero points
+  static __device__ __forceinline__ void put_scales(const Words& w, unsigned char* lds, int lane) {
+    uint16_t* const to = reinterpret_cast<uint16_t*>(lds);
+    if constexpr (kRtn) {
+      uint16_t* const mine = to + (lane >> 5) * 128 + (lane & 31);
+      mine[0] = (uint16_t)w.scale.x; mine[32] = (uint16_t)(w.scale.x >> 16);
+      mine[64] = (uint16_t)w.scale.y; mine[96] = (uint16_t)(w.scale.y >> 16);
+    } else {
+      to[lane] = (uint16_t)w.scale.x;
+    }
+  }
+  static __device__ __forceinline__ Scales get_scales(const unsigned char* lds, int g) {
+    Scales s;
+    const auto at = [&](int i) { return *reinterpret_cast<const u32x4*>(lds + 64 * i + 16 * g); };
+    if constexpr (kRtn) {
+      s.ks[0] = at(0); s.kz[0] = at(1); s.ks[1] = at(2); s.kz[1] = at(3);
+      s.vs[0] = at(4); s.vz[0] = at(5); s.vs[1] = at(6); s.vz[1] = at(7);
+    } else {
+      s.ks[0] = at(0); s.vs[0] = at(1);
+    }
+    return s;
+  }
+  static __device__ __forceinline__ float half_at(const u32x4& w, int e) {
+    const f16x8 h = __builtin_bit_cast(f16x8, w);
+    return (float)h[e];
+  }
+  static __device__ __forceinline__ float int_at(const u32x4& w, int e) { return (float)((w[e >> 1] >> (16 * (e & 1))) & 0xffffu); }
+  static __device__ __forceinline__ void value_scales(const Scales& s, float (&sv)[kRtn ? 2 : 1][8]) {
+#pragma unroll
+    for (int k = 0; k < (kRtn ? 2 : 1); ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sv[k][e] = half_at(s.vs[k], e);
+  }
+  // zero points of the lane's tokens from `there` on are not used
+  static __device__ __forceinline__ void mask_zeros(Scales& s, int there) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t keep = (2 * i < there ? 0xffffu : 0u) | (2 * i + 1 < there ? 0xffff0000u : 0u);
+      s.vz[0][i] &= keep;
+      s.vz[kRtn ? 1 : 0][i] &= keep;
+    }
+  }
+
+  // ---- look-ups
+  template <int TERM = 0> static __device__ __forceinline__ uint32_t point(const unsigned char* lds, uint32_t offset) {
+    return *reinterpret_cast<const uint32_t*>(lds + offset + 4 * TERM);
+  }
+  // offset of the lane's copy (lane_at: 0 ... 255) of the point whose code is byte `k` of w
+  static __device__ __forceinline__ uint32_t offset_of_byte(uint32_t w, int k, uint32_t lane_at) {
+    return __builtin_amdgcn_perm(w, lane_at, 0x0c0c0400u + ((uint32_t)k << 8));
+  }
+  static __device__ __forceinline__ uint32_t lane_copy(int lane) { return (uint32_t)(lane * kEntry) & 255u; }
+  // code i (compile time) of the packed codes in w
+  template <int N> static __device__ __forceinline__ uint32_t offset(const uint32_t (&w)[N], int i, uint32_t lane_at) {
+    if constexpr (c == 8) {
+      return offset_of_byte(w[i >> 2], i & 3, lane_at);
+    } else if constexpr (c == 4) {
+      uint32_t x = (i & 1) ? w[i >> 3] >> 4 : w[i >> 3];
+      x &= 0x0f0f0f0fu;
+      return offset_of_byte(x, (i >> 1) & 3, lane_at);
+    } else {
+      const int bit = 6 * i, n = bit >> 5, sh = bit & 31;
+      uint32_t x = w[n] >> sh;
+      if (sh > 26) x |= w[n + 1 < N ? n + 1 : n] << (32 - sh);
+      return (x & 63u) << 8 | lane_at;
+    }
+  }
+
+  // ---- scores of product p: s[half][p] += keys * query
+  static __device__ __forceinline__ void scores(const Words& w, int p, const unsigned char* lds, int lane, const f16x8 (&q)[TERMS][4],
+                                                f32x4 (&s)[kRtn ? 2 : 1][2]) {
+    const uint32_t x[4] = {w.k[p].x, w.k[p].y, w.k[p].z, w.k[p].w};
+    if constexpr (kRtn) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t y[4];
+        const uint32_t d = NCW == kRtn4 ? x[j] : (j & 1) ? x[j >> 1] >> 8 : x[j >> 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = NCW == kRtn4 ? ((i & 2) ? d >> 8 : d) & field_mask(i & 1) : d & field_mask(i);
+        const f16x8 k = operand(y[0], y[1], y[2], y[3]);
+#pragma unroll
+        for (int n = 0; n < TERMS; ++n) s[j >> 1][p] = mfma(k, q[n][j], s[j >> 1][p]);
+      }
+    } else {
+      const uint32_t at = lane_copy(lane);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = offset(x, 4 * j + i, at);
+        const f16x8 k = operand(point(lds, o[0]), point(lds, o[1]), point(lds, o[2]), point(lds, o[3]));
+        s[0][p] = mfma(k, q[0][j], s[0][p]);
+        if constexpr (TERMS == 2) {
+          s[0][p] = mfma(k, q[1][j], s[0][p]);
+          s[0][p] = mfma(operand(point<1>(lds, o[0]), point<1>(lds, o[1]), point<1>(lds, o[2]), point<1>(lds, o[3])), q[0][j], s[0][p]);
+        }
+      }
+    }
+  }
+  // ... of the lane's eight tokens, times the scales
+  static __device__ __forceinline__ void scaled(const f32x4 (&s)[kRtn ? 2 : 1][2], const Scales& sc, const float (&qsum)[2], float (&y)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = s[0][e >> 2][e & 3];
+      if constexpr (kRtn) {
+        const float lo = __fmaf_rn(-int_at(sc.kz[0], e), qsum[0], y[e]), hi = __fmaf_rn(-int_at(sc.kz[1], e), qsum[1], s[1][e >> 2][e & 3]);
+        y[e] = __fmaf_rn(lo, half_at(sc.ks[0], e), hi * half_at(sc.ks[1], e));
+      } else {
+        y[e] *= half_at(sc.ks[0], e);
+      }
+    }
+  }
+
+  // ---- o[j] += values (coordinates: result()) * weights (per half)
+  static __device__ __forceinline__ void values(const Words& w, const Scales& sc, const float (&wt)[kRtn ? 2 : 1][8], const unsigned char* lds,
+                                                int lane, f32x4 (&o)[8], f32x4 (&oz)[2]) {
+    f16x8 b[kRtn ? 2 : 1][TERMS];
+#pragma unroll
+    for (int k = 0; k < (kRtn ? 2 : 1); ++k) split_f16<TERMS>(wt[k], b[k]);
+    if constexpr (kRtn) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f16x8 z = __builtin_bit_cast(f16x8, sc.vz[k]);
+#pragma unroll
+        for (int n = 0; n < TERMS; ++n) oz[k] = mfma(z, b[k][n], oz[k]);
+#pragma unroll
+        for (int byte = 0; byte < 4 / kFields; ++byte) {
+          uint32_t x[4];                                   // tokens 2 i and 2 i + 1 in the halves
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = w.v[8 * k + 2 * i], hi = w.v[8 * k + 2 * i + 1];
+            x[i] = NCW == kRtn4 ? __builtin_amdgcn_perm(hi, lo, byte == 0 ? 0x0c040c00u : 0x0c050c01u) : lo | hi << 16;
+          }
+#pragma unroll
+          for (int f = 0; f < kFields; ++f) {
+            const f16x8 v = operand(x[0] & field_mask(f), x[1] & field_mask(f), x[2] & field_mask(f), x[3] & field_mask(f));
+            const int j = 4 * k + kFields * byte + f;
+#pragma unroll
+            for (int n = 0; n < TERMS; ++n) o[j] = mfma(v, b[k][n], o[j]);
+          }
+        }
+      }
+    } else {
+      const uint32_t at = lane_copy(lane), m = lane & 15;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t d[TERMS][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t x[1] = {w.v[e]};
+          if constexpr (c == 6) x[0] = __builtin_amdgcn_alignbit(w.v[8 + e], w.v[e], 8 * ((3 * m) & 3));
+          const uint32_t off = offset(x, i, at);
+          d[0][e] = point(lds, off);
+          if constexpr (TERMS == 2) d[1][e] = point<1>(lds, off);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {                      // coordinates 2 i, 2 i + 1 of the lane's eight
+          f16x8 v[TERMS];
+#pragma unroll
+          for (int n = 0; n < TERMS; ++n) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_perm(d[n][2 * e + 1], d[n][2 * e], k == 0 ? 0x05040100u : 0x07060302u);
+            v[n] = operand(x[0], x[1], x[2], x[3]);
+          }
+          o[2 * i + k] = mfma(v[0], b[0][0], o[2 * i + k]);
+          if constexpr (TERMS == 2) {
+            o[2 * i + k] = mfma(v[0], b[0][1], o[2 * i + k]);
+            o[2 * i + k] = mfma(v[1], b[0][0], o[2 * i + k]);
+          }
+        }
+      }
+    }
+  }
+  // the lane's 32 coordinates, coordinate(g, r): product j's row 4 g + i is coordinate 8 (4 g + i) + j, or 4 (4 g + i) + j % 4 of half j / 4
+  static __device__ __forceinline__ void result(const f32x4 (&o)[8], const f32x4 (&oz)[2], int e, float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kRtn) v[16 * (j >> 2) + 4 * i + (j & 3)] = __builtin_ldexpf(o[j][i] * (1.0f / (float)field_scale(j % kFields)) - oz[j >> 2][i], e);
+        else v[8 * i + j] = __builtin_ldexpf(o[j][i], e);
+      }
+  }
+};
+
+// The lane's 32 coordinates of a row's result -> out.
+template <typename T, int NCW> __device__ __forceinline__ void finish(const PagedAttendArgs& a, float (&v)[32], float sum, int h, int g,
+                                                                      bool there, int64_t row, int qh) {
+  constexpr bool kRtn = is_rtn(NCW);
+  float by = sum == 0.f ? 0.f : 1.0f / sum;                // (no token: 0)
+  if constexpr (!kRtn) by *= kRsqrtG;
+#pragma unroll
+  for (int r = 0; r < 32; ++r) v[r] *= by;
+  if constexpr (!kRtn) {
+    float sf[32];
+    load_signs(a.signs_v, h, g, sf);
+    wht_columns(v);
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] *= sf[r];
+  }
+  if (!there) return;
+  T* const out = static_cast<T*>(a.out) + (row * a.q_heads + qh) * kGroup;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    float half[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) half[r] = v[16 * k + r];
+    Storage<T>::template store<false>(out + Codes<NCW, 1>::coordinate(g, 16 * k), 0, half);
+  }
+}
+
+}  // namespace paged
+}  // namespace aquakv

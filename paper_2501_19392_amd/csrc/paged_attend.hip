@@ -2,137 +2,267 @@
 // With the rotation R = H S / sqrt(128) of the quantizer (Sect. 2 of the AQUA-KV paper) a key is R^T (sigma C[codes]), so
 //   q . khat = sigma (R q) . C[codes],      sum_t p_t vhat_t = R^T sum_t (p_t sigma_t) C[codes_t]:
 // the query is rotated once, the result once, and in between a code is a look-up.  (Uniform backbone: no rotation, (code - zero) step.)
-//
-// One wave per query head of a query: a lane takes a token of 64 for the scores, two coordinates for the values.
-#include "codec_core.h"
-#include "kernels.h"
+#include "paged_attend.h"
+
+#include <algorithm>
 
 namespace aquakv {
 namespace {
 
-// What a sequence asks: `count` queries, its last tokens, rows first ... of q, of which n are answered; len tokens are cached.
-struct PagedQueries { int64_t first; int count, n, len; };
-__device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, int b) {
-  PagedQueries w;
-  w.first = (int64_t)b * a.max_queries;
-  w.count = a.max_queries;
-  if (a.q_start != nullptr) {
-    const int64_t from = a.q_start[b], to = a.q_start[b + 1];
-    w.first = from < 0 ? 0 : from < a.q_rows ? from : a.q_rows;
-    const int64_t end = to < w.first ? w.first : to < a.q_rows ? to : a.q_rows;
-    w.count = (int)(end - w.first);
-  }
-  w.n = min(w.count, a.max_queries);
-  const int64_t room = (int64_t)a.table_pages * a.pool.page_tokens;
-  w.len = (int)min((int64_t)max(a.seq_lens[b], 0), room);
-  return w;
-}
+using namespace paged;
 
-template <int NCW> __device__ __forceinline__ float2 pair_of(const uint8_t* __restrict__ row, int i, const float2* cb) {
-  constexpr int c = CodeBits<NCW>::c;
-  const int bit = c * i;
-  uint32_t w = row[bit >> 3];
-  if constexpr (c == 6) { if ((bit & 7) > 2) w |= (uint32_t)row[(bit >> 3) + 1] << 8; }
-  const uint32_t code = (w >> (bit & 7)) & ((1u << c) - 1u);
-  if constexpr (is_rtn(NCW)) return make_float2((float)(code & ((1u << NCW) - 1u)), (float)(code >> NCW));
-  else return cb[code];
-}
-
-// rotated coordinates 2 lane, 2 lane + 1 of a vector whose coordinates 2 lane, 2 lane + 1 are (x, y)
-__device__ __forceinline__ void wht_wave(float& x, float& y, int lane) {
-  const float s = x + y, d = x - y;
-  x = s; y = d;
-  for (int m = 1; m < 64; m <<= 1) {
-    const float px = __shfl_xor(x, m), py = __shfl_xor(y, m);
-    x = (lane & m) ? px - x : x + px;
-    y = (lane & m) ? py - y : y + py;
-  }
-}
-
+// One wave takes `tiles` tiles of 32 tokens of one kv head for up to 16 rows (query x query head of the kv head): soft-max in one pass with a
+// running reference, fp16 matrix instructions (16x16x32) with fp32 sums.  Lane l = 16 g + m:
+//   scores   S^T = K Q^T, two products of 16 tokens: A holds token 8 (m / 4) + m % 4 (+ 4 in the second), so that a lane gets the scores of
+//            tokens 8 g ... 8 g + 7 for row m, which is what the second product wants of it as its B operand, with no exchange between lanes;
+//   values   O^T = V^T P: A holds 8 tokens of one coordinate; a look-up gives two neighbouring coordinates, two permutes pair them up by
+//            token.  The 32 coordinates a lane ends with are consecutive, as the inverse transform wants them.
 template <typename T, int NCW>
-__global__ __launch_bounds__(64) void paged_attend_kernel(const PagedAttendArgs a) {
-  __shared__ float2 cb[is_rtn(NCW) ? 1 : NCW];
-  __shared__ float qs[kGroup];
-  const int lane = threadIdx.x, b = blockIdx.y, qi = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads, h = qh / (a.q_heads / a.H);
-  if constexpr (!is_rtn(NCW))
-    for (int j = lane; j < NCW; j += 64) cb[j] = make_float2(a.codebook[2 * j], a.codebook[2 * j + 1]);
+__global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAttendArgs a) {
+  constexpr int kTerms = sizeof(T) == 2 ? 1 : 2;
+  constexpr bool kRtn = is_rtn(NCW);
+  typedef Codes<NCW, kTerms> C;
+  __shared__ __align__(256) unsigned char lds[C::kTableBytes + kWaves * C::kScaleBytes];
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned char* const scale_lds = lds + C::kTableBytes + wave * C::kScaleBytes;
+
+  // which rows, kv head and piece of a sequence
+  const unsigned unit = blockIdx.x * kWaves + wave;
+  const int h = unit % a.H, item = unit / a.H;
+  const Share share = share_of<true>(a, lane, item);
+  if (blockIdx.x * kWaves / a.H >= (unsigned)share.items) return;         // (the whole workgroup is behind the last piece)
+  const int c_exp = C::stage(a.codebook, lds);
+  __syncthreads();
+  if (share.b < 0) return;
+  const int b = share.b, rep = a.q_heads / a.H;
+  const PagedQueries w = paged_queries(a, b);
+  const int n_rows = w.n * rep, row0 = blockIdx.y * 16;
+  if (row0 >= n_rows) return;
+  const int row = row0 + m, qi = row / rep, qh = h * rep + row % rep;
+  const bool row_there = row < n_rows;
+  // the last token the row sees; the tokens of this piece
+  const int limit = row_there ? w.len - w.count + qi : -1;
+  const int first_limit = w.len - w.count + row0 / rep, last_limit = w.len - w.count + min(row0 + 15, n_rows - 1) / rep;
+  const int t_begin = share.piece * share.tiles * kTile, t_end = min(min(t_begin + share.tiles * kTile, w.len), last_limit + 1);
+
+  // ---- the row's query: rotated, scaled to fp16's range
+  f16x8 q[kTerms][4];
+  float qsum[2] = {0.f, 0.f};                              // uniform: sum of the row's (rounded) query over each half
+  float f;                                                 // score in powers of two = f * sigma * sum
+  {
+    float v[32];
+    const T* const src = static_cast<const T*>(a.q) + (w.first + (row_there ? qi : 0)) * a.q_stride + (row_there ? qh : h * rep) * kGroup;
+    C::template load_query<T>(src, g, v);
+    if constexpr (!kRtn) {
+      float sf[32];
+      load_signs(a.signs_k, h, g, sf);
+#pragma unroll
+      for (int r = 0; r < 32; ++r) v[r] *= sf[r];
+      wht_columns(v);
+    }
+    const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
+    float top = 0.f;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) { v[r] *= by; top = fmaxf(top, fabsf(v[r])); }
+    const int e = max(__builtin_amdgcn_frexp_expf(column_max(top)), -100);
+    f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? 24 : c_exp), 126));
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] = __builtin_ldexpf(v[r], kQueryExp - e);
+    C::pack_query(v, q, qsum);
+  }
+
+  f32x4 o[8] = {};
+  f32x4 oz[2] = {};                                        // uniform: sums of the zero points, per half
+  float ref = -3.0e38f, sum = 0.f;                         // weights are 2^(score - ref)
+
+  const auto tile = [&](const typename C::Words& x, int t, unsigned there) {
+    // scales of the tile's 32 tokens to the lanes that need them
+    asm volatile("" ::: "memory");                         // (a wave's LDS accesses stay in order)
+    C::put_scales(x, scale_lds, lane);
+    asm volatile("" ::: "memory");
+    f32x4 s[kRtn ? 2 : 1][2] = {};                         // [half][product]
+    typename C::Scales sc = C::get_scales(scale_lds, g);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) C::scores(x, p, lds, lane, q, s);
+    float y[8];
+    C::scaled(s, sc, qsum, y);
+    float sv[kRtn ? 2 : 1][8];
+    C::value_scales(sc, sv);
+    const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;       // (t_end: of this piece, whole tiles but for the last)
+    if (masked) {
+      const int seen = (there >> g) & 1 ? limit - (t + 8 * g) : -1;        // tokens 0 ... seen of the lane's eight are seen
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e > seen) {
+          y[e] = -INFINITY;
+          sv[0][e] = 0.f;
+          if constexpr (kRtn) sv[1][e] = 0.f;
+        }
+      }
+      if constexpr (kRtn) C::mask_zeros(sc, (there >> g) & 1 ? min(w.len - (t + 8 * g), 8) : 0);
+    }
+    float p[8], wt[kRtn ? 2 : 1][8];
+    const auto weigh = [&] {
+      float top = 0.f, big = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref));
+        wt[0][e] = p[e] * sv[0][e];
+        top = fmaxf(top, wt[0][e]);
+        if constexpr (kRtn) { wt[1][e] = p[e] * sv[1][e]; top = fmaxf(top, wt[1][e]); }
+        big = fmaxf(big, p[e]);
+      }
+      return __builtin_amdgcn_ballot_w64(top > kTopWeight || big > 0x1p60f) != 0;
+    };
+    if (weigh()) {                                         // the reference follows: weights of the largest become 2^kStartExp
+      float top = -3.0e38f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float sg = sv[0][e];
+        if constexpr (kRtn) sg = fmaxf(sg, sv[1][e]);
+        top = fmaxf(top, y[e] * f + __builtin_amdgcn_logf(fmaxf(sg, 0x1p-24f)));
+      }
+      const float moved = fmaxf(ref, column_max(top) - kStartExp);
+      const float by = __builtin_amdgcn_exp2f(ref - moved);
+      ref = moved;
+      sum *= by;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] *= by;
+      if constexpr (kRtn) { oz[0] *= by; oz[1] *= by; }
+      weigh();
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += p[e];
+    C::values(x, sc, wt, lds, lane, o, oz);
+  };
+  // Codes are requested a tile ahead, the rows they are in two tiles ahead.
+  if (t_begin < t_end) {
+    typename C::Words even, odd;
+    Rows r0 = rows_of(a, b, t_begin), r1 = rows_of(a, b, t_begin + kTile);
+    even = C::request(a, r0, h, lane);
+    for (int t = t_begin;; t += 2 * kTile) {
+      Rows r2 = rows_of(a, b, t + 2 * kTile);
+      if (t + kTile < t_end) odd = C::request(a, r1, h, lane);
+      tile(even, t, there_of(r0));
+      if (t + kTile >= t_end) break;
+      r0 = rows_of(a, b, t + 3 * kTile);
+      if (t + 2 * kTile < t_end) even = C::request(a, r2, h, lane);
+      tile(odd, t + kTile, there_of(r1));
+      if (t + 2 * kTile >= t_end) break;
+      r1 = r0;
+      r0 = r2;
+    }
+  }
+
+  // ---- the lane's 32 coordinates of the row
+  sum = column_sum(sum);
+  float v[32];
+  C::result(o, oz, kRtn ? 24 : c_exp, v);
+  if (share.pieces == 1) {
+    finish<T, NCW>(a, v, sum, h, g, row_there, w.first + qi, qh);
+  } else if (row_there) {
+    const int64_t at = ((int64_t)item * a.max_queries + qi) * a.q_heads + qh;
+    float* const part = a.part + at * kGroup;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      *reinterpret_cast<f32x4*>(part + C::coordinate(g, 4 * r)) = f32x4{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
+    if (g == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
+  }
+}
+
+// out of one row from the pieces of its sequence: sum_i 2^(ref_i - top) part_i / sum_i 2^(ref_i - top) sum_i.
+// blockIdx = (query * q_heads + query head, sequence); threads of 32 take a piece, every eighth, 4 coordinates each.
+constexpr int kMergeThreads = 256, kMergeClasses = kMergeThreads / 32;
+template <typename T, bool RTN>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedAttendArgs a) {
+  __shared__ __align__(16) float red[kMergeClasses][kGroup];
+  __shared__ float refs[kMergeClasses], sums[kMergeClasses];
+  const int b = blockIdx.y, qi = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads, h = qh / (a.q_heads / a.H);
+  const Share share = share_of<false>(a, threadIdx.x & 63, b);
+  if (share.pieces == 1) return;
   const PagedQueries w = paged_queries(a, b);
   if (qi >= w.n) return;
-  const int64_t qrow = w.first + qi;
-  const int last = w.len - w.count + qi;                  // position of this query
-  const T* const q = static_cast<const T*>(a.q) + qrow * a.q_stride + qh * kGroup;
-  float x = (float)q[2 * lane], y = (float)q[2 * lane + 1];
-  if constexpr (!is_rtn(NCW)) {
-    x *= a.signs_k[h * kGroup + 2 * lane]; y *= a.signs_k[h * kGroup + 2 * lane + 1];
-    wht_wave(x, y, lane);
-    x *= kRsqrtG; y *= kRsqrtG;
+  const int k = threadIdx.x >> 5, l = threadIdx.x & 31;
+  const int64_t step = (int64_t)a.max_queries * a.q_heads, at = share.first * step + (int64_t)qi * a.q_heads + qh;
+  float ref = -3.0e38f, sum = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = k; i < share.pieces; i += kMergeClasses) {
+    const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * (at + i * step));
+    const f32x4 p = *reinterpret_cast<const f32x4*>(a.part + (at + i * step) * kGroup + 4 * l);
+    const float top = fmaxf(ref, st.x), keep = __builtin_amdgcn_exp2f(ref - top), by = __builtin_amdgcn_exp2f(st.x - top);
+    x = x * keep + p * by;
+    sum = sum * keep + st.y * by;
+    ref = top;
   }
-  qs[2 * lane] = x * a.scale; qs[2 * lane + 1] = y * a.scale;
+  *reinterpret_cast<f32x4*>(&red[k][4 * l]) = x;
+  if (l == 0) { refs[k] = ref; sums[k] = sum; }
   __syncthreads();
-  constexpr int kRow = kGroup / 2 * CodeBits<NCW>::c / 8;
-  float m = -INFINITY, sum = 0.f, ox = 0.f, oy = 0.f;
-  for (int t0 = 0; t0 <= last; t0 += 64) {
-    const int t = t0 + lane;
-    int64_t gid = -1;
-    if (t <= last) {
-      const int page = a.page_table[(int64_t)b * a.table_pages + t / a.pool.page_tokens];
-      if ((unsigned)page < (unsigned)a.pool.n_pages) gid = ((int64_t)page * a.pool.page_tokens + t % a.pool.page_tokens) * a.H + h;
-    }
-    float s = -INFINITY;
-    if (gid >= 0) {
-      float acc[2] = {0.f, 0.f};
-      float zero[2] = {0.f, 0.f}, step[2];
-      if constexpr (is_rtn(NCW)) {
-        for (int k = 0; k < 2; ++k) {
-          step[k] = half_bits_to_float(a.pool.k_scales[(gid * 2 + k) * 2]);
-          zero[k] = (float)a.pool.k_scales[(gid * 2 + k) * 2 + 1];
-        }
-      } else {
-        step[0] = step[1] = half_bits_to_float(a.pool.k_scales[gid]);
-      }
-      for (int i = 0; i < 64; ++i) {
-        const float2 c = pair_of<NCW>(a.pool.k_codes + gid * kRow, i, cb);
-        acc[i >> 5] += qs[2 * i] * (c.x - zero[i >> 5]) + qs[2 * i + 1] * (c.y - zero[i >> 5]);
-      }
-      s = acc[0] * step[0] + acc[1] * step[1];
-    }
-    float top = s;
-    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
-    if (top == -INFINITY) continue;
-    const float M = fmaxf(m, top), keep = expf(m - M), p = expf(s - M);
-    float part = p;
-    for (int k = 1; k < 64; k <<= 1) part += __shfl_xor(part, k);
-    sum = sum * keep + part; ox *= keep; oy *= keep; m = M;
-    for (int k = 0; k < 64; ++k) {
-      const float pk = __shfl(p, k);
-      const int64_t gk = __shfl(gid, k);
-      if (gk < 0) continue;
-      float zero = 0.f, step;
-      if constexpr (is_rtn(NCW)) {
-        step = half_bits_to_float(a.pool.v_scales[(gk * 2 + (lane >> 5)) * 2]);
-        zero = (float)a.pool.v_scales[(gk * 2 + (lane >> 5)) * 2 + 1];
-      } else {
-        step = half_bits_to_float(a.pool.v_scales[gk]);
-      }
-      const float2 c = pair_of<NCW>(a.pool.v_codes + gk * kRow, lane, cb);
-      ox += pk * step * (c.x - zero); oy += pk * step * (c.y - zero);
-    }
+  if (threadIdx.x >= 4) return;
+  // the row's result on a quad of lanes
+  const int q = threadIdx.x;
+  float top = refs[0];
+#pragma unroll
+  for (int i = 1; i < kMergeClasses; ++i) top = fmaxf(top, refs[i]);
+  float v[32] = {};
+  sum = 0.f;
+  for (int i = 0; i < kMergeClasses; ++i) {
+    const float by = __builtin_amdgcn_exp2f(refs[i] - top);
+    sum += sums[i] * by;
+    float p[32];
+    load_f32(&red[i][32 * q], p);
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] = __fmaf_rn(p[r], by, v[r]);
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;          // (no token: 0)
-  ox *= inv; oy *= inv;
-  if constexpr (!is_rtn(NCW)) {
-    wht_wave(ox, oy, lane);
-    ox *= kRsqrtG * a.signs_v[h * kGroup + 2 * lane]; oy *= kRsqrtG * a.signs_v[h * kGroup + 2 * lane + 1];
+  float norm = sum == 0.f ? 0.f : 1.0f / sum;
+  if constexpr (!RTN) {
+    float sf[32];
+    load_signs(a.signs_v, h, q, sf);
+    norm *= kRsqrtG * quad_sign(q);
+    wht128(v, q);
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] *= sf[r];
   }
-  T* const out = static_cast<T*>(a.out) + (qrow * a.q_heads + qh) * kGroup;
-  out[2 * lane] = (T)ox; out[2 * lane + 1] = (T)oy;
+#pragma unroll
+  for (int r = 0; r < 32; ++r) v[r] *= norm;
+  Storage<T>::template store<false>(static_cast<T*>(a.out) + ((w.first + qi) * a.q_heads + qh) * kGroup, q, v);
+}
+
+// How a launch is laid out, from sizes alone (lengths are on the device).
+struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles; int64_t items; bool merge; };
+constexpr int kMinTiles = 2;                               // a piece of fewer tokens costs more than it saves
+PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
+  PagedPlan p;
+  p.row_tiles = (unsigned)((max_queries * (q_heads / H) + 15) / 16);
+  p.min_tiles = kMinTiles;
+  // as many waves as the chip holds, two workgroups a CU
+  p.slots = (int)std::max<int64_t>(256 * 2 * kWaves / (H * p.row_tiles), 1);
+  const int64_t most = (table_pages * page_tokens + kTile - 1) / kTile;                       // tiles of a sequence
+  const int64_t each = std::max<int64_t>((most + kMinTiles - 1) / kMinTiles, 1);
+  p.items = std::min(batch * each, std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
+  p.blocks = (unsigned)((p.items * H + kWaves - 1) / kWaves);
+  p.merge = each > 1;
+  return p;
 }
 
 }  // namespace
 
-hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.max_queries * a.q_heads), (unsigned)a.batch);
-#define AQUAKV_ATTEND(T, NCW) paged_attend_kernel<T, NCW><<<grid, 64, 0, stream>>>(a)
+size_t paged_attend_workspace_bytes(const PagedAttendArgs& a) {
+  const PagedPlan p = paged_plan(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H);
+  return p.merge ? (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) : 0;
+}
+
+hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& args, void* workspace, hipStream_t stream) {
+  PagedAttendArgs a = args;
+  const PagedPlan plan = paged_plan(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H);
+  a.slots = plan.slots;
+  a.min_tiles = plan.min_tiles;
+  a.part = static_cast<float*>(workspace);
+  a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
+  a.page_groups = a.pool.page_tokens / 8;
+  a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
+#define AQUAKV_ATTEND(T, NCW) paged_attend_kernel<T, NCW><<<dim3(plan.blocks, plan.row_tiles), kThreads, 0, stream>>>(a)
 #define AQUAKV_ATTEND_T(T)                                    \
   switch (n_codewords) {                                      \
     case kRtn2: AQUAKV_ATTEND(T, kRtn2); break;               \
@@ -144,6 +274,17 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   if (dtype == kBF16) { AQUAKV_ATTEND_T(bf16_t) } else { AQUAKV_ATTEND_T(float) }
 #undef AQUAKV_ATTEND_T
 #undef AQUAKV_ATTEND
+  if (const hipError_t e = hipGetLastError()) return e;
+  if (!plan.merge) return hipSuccess;
+  const dim3 grid((unsigned)(a.max_queries * a.q_heads), (unsigned)a.batch);
+  const bool rtn = is_rtn(n_codewords);
+  if (dtype == kBF16) {
+    if (rtn) paged_merge_kernel<bf16_t, true><<<grid, kMergeThreads, 0, stream>>>(a);
+    else paged_merge_kernel<bf16_t, false><<<grid, kMergeThreads, 0, stream>>>(a);
+  } else {
+    if (rtn) paged_merge_kernel<float, true><<<grid, kMergeThreads, 0, stream>>>(a);
+    else paged_merge_kernel<float, false><<<grid, kMergeThreads, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 
