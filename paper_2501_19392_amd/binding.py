@@ -467,32 +467,38 @@ def aquakv_attend_cache(layers, shape, n_sink, n_compressed, n_recent, score_sca
                                     _ptr(rope_sin), score_scale, hats.buffer_info()[0], w, wb, _stream(stream)))
 
 
-def _rows(x, row: int):
-    """Rows of heads x 128 that may lie apart -> (address, elements from row to row); an address: one behind the other."""
-    if not isinstance(x, torch.Tensor):
-        return _ptr(x), row
-    if x.dim() != 3 or x.shape[1] * x.shape[2] != row or x.stride(2) != 1 or x.stride(1) != x.shape[2]:
-        raise ValueError(f"rows of {row} elements, each contiguous")
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else row
+# These are called once per layer and generated token, so looking at their tensors has to be cheap: shapes and strides are asked for once.
+def _rows(x, dtype, row: int, name: str):
+    """Rows of heads x 128 that may lie apart -> (address, elements from row to row, rows); an address: one behind the other."""
+    if x is None or isinstance(x, int):
+        return x, row, None
+    (n, heads, g), (step, head_step, one) = x.shape, x.stride()
+    if heads * g != row or one != 1 or (head_step != g and heads != 1) or x.dtype is not dtype:
+        raise ValueError(f"{name} must be rows of {row} elements, each contiguous, {dtype}")
+    return x.data_ptr(), step if n > 1 else row, n
 
 
-def _typed(x, dtype, name: str, shape=None):
-    if isinstance(x, torch.Tensor) and (x.dtype != dtype or (shape is not None and x.shape != shape)):
-        raise ValueError(f"{name} must be {dtype}{'' if shape is None else list(shape)}")
-    return _ptr(x)
+def _typed(x, dtype, n: int, name: str):
+    """A tensor of n elements, or an address."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.dtype is not dtype or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{name} must be {n} elements of {dtype}")
+    return x.data_ptr()
 
 
 def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_cos, rope_sin, Khat, Vhat, stream=None) -> None:
     """K, V: [tokens, kv_heads, 128], rows may lie apart; rope_cos, rope_sin: [rope_rows, 64] tensors (None: no rotation, positions unused)."""
-    row = layer.kv_heads * layer.head_dim
-    k, ks = _rows(K, row)
-    v, vs = _rows(V, row)
-    if any(isinstance(x, torch.Tensor) and (x.shape[0] != tokens or x.dtype != layer.dtype) for x in (K, V, Khat, Vhat)):
-        raise ValueError(f"{tokens} rows of {layer.dtype}")
-    rows = 0 if rope_cos is None else min(rope_cos.shape[0], rope_sin.shape[0])
-    _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, "slots", (tokens,)),
-                                    _typed(positions, torch.int32, "positions", (tokens,)), _typed(rope_cos, torch.float32, "rope_cos"),
-                                    _typed(rope_sin, torch.float32, "rope_sin"), rows, _ptr(Khat), _ptr(Vhat), _stream(stream)))
+    row, dtype = layer.d, layer.dtype
+    k, ks, nk = _rows(K, dtype, row, "K")
+    v, vs, nv = _rows(V, dtype, row, "V")
+    if (nk is not None and nk != tokens) or (nv is not None and nv != tokens):
+        raise ValueError(f"K and V must have {tokens} rows")
+    angles = 0 if rope_cos is None else rope_cos.numel()
+    _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, tokens, "slots"),
+                                    _typed(positions, torch.int32, tokens, "positions"), _typed(rope_cos, torch.float32, angles, "rope_cos"),
+                                    _typed(rope_sin, torch.float32, angles, "rope_sin"), angles // 64,
+                                    _typed(Khat, dtype, tokens * row, "Khat"), _typed(Vhat, dtype, tokens * row, "Vhat"), _stream(stream)))
 
 
 def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_pages: int, q_rows: int, max_queries: int) -> int:
@@ -502,16 +508,16 @@ def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_p
 def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
                         workspace, stream=None) -> None:
     """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence]."""
-    at, stride = _rows(q, q_heads * layer.head_dim)
+    row, dtype = q_heads * layer.head_dim, layer.dtype
+    at, stride, q_rows = _rows(q, dtype, row, "q")
     if page_table.dim() != 2 or page_table.shape[0] != batch:
         raise ValueError("page_table must be [batch, pages]")
-    if q.dtype != layer.dtype or out.dtype != layer.dtype or out.numel() != q.numel():
-        raise ValueError(f"q and out must be of one size, {layer.dtype}")
+    pages_each = page_table.shape[1]
     ws, nbytes = _ws(workspace)
-    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads, _typed(page_table, torch.int32, "page_table"),
-                                    page_table.shape[1], _typed(seq_lens, torch.int32, "seq_lens", (batch,)), q.shape[0], max_queries,
-                                    _typed(q_start, torch.int32, "q_start", (batch + 1,)), at, stride, score_scale, _ptr(out), ws, nbytes,
-                                    _stream(stream)))
+    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads, _typed(page_table, torch.int32, batch * pages_each, "page_table"),
+                                    pages_each, _typed(seq_lens, torch.int32, batch, "seq_lens"), q_rows, max_queries,
+                                    _typed(q_start, torch.int32, batch + 1, "q_start"), at, stride, score_scale,
+                                    _typed(out, dtype, q_rows * row, "out"), ws, nbytes, _stream(stream)))
 
 
 def aquakv_fit_workspace_bytes(d_in: int, d_out: int) -> int:

@@ -1730,7 +1730,7 @@ size_t aquakv_paged_workspace_bytes(const aquakv_layer* L, const aquakv_pages* p
   aquakv::PagedAttendArgs a = {};
   a.pool = pool_of(pages);
   a.batch = batch; a.table_pages = table_pages; a.max_queries = max_queries; a.q_heads = q_heads; a.H = L->kv_heads;
-  return (aquakv::paged_attend_workspace_bytes(a) + 255) / 256 * 256 + 256;
+  return (aquakv::paged_attend_workspace_bytes(L->dtype, quantizer_id(L), a) + 255) / 256 * 256 + 256;
 }
 
 int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,

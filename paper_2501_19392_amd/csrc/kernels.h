@@ -268,7 +268,7 @@ struct PagedAttendArgs {
   int slots, min_tiles;                           // pieces that fill the chip, tiles of a piece at least
   uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
 };
-size_t paged_attend_workspace_bytes(const PagedAttendArgs& a);
+size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 
 // Device-to-device copies of n byte ranges, kCopyRangesPerLaunch per launch (3 KiB of kernel arguments).

@@ -17,11 +17,12 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef const __attribute__((address_space(4))) int32_t* ConstInts;       // (scalar loads: what is read through it is not written meanwhile)
 inline __device__ ConstInts const_ints(const int32_t* p) { return (ConstInts)(uintptr_t)p; }
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kTile = 32;                    // tokens of a tile: four groups of 8, each within a page
 constexpr int kQueryExp = 14;                // largest coordinate of a row's query: 2^13 ... 2^14
 constexpr float kTopWeight = 0x1p15f;        // a weight beyond this moves the reference,
 constexpr float kStartExp = 8.0f;            // so that the largest is 2^kStartExp: what is 2^-33 of it still counts
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // ---------------------------------------------------------------- rows, pieces
 // What a sequence asks: `count` queries, its last tokens, rows first ... of q, of which n are answered; len tokens are cached.
@@ -39,6 +40,7 @@ __device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, 
     const int64_t end = to < w.first ? w.first : to < a.q_rows ? to : a.q_rows;
     w.count = (int)(end - w.first);
   }
+  w.count = uniform(w.count);
   w.n = min(w.count, a.max_queries);
   w.len = length_of(a, const_ints(a.seq_lens)[b]);
   return w;
@@ -58,7 +60,7 @@ __device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int64_t tot
 __device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
-  return x;
+  return uniform(x);
 }
 // by_item: of item `which`; else of sequence `which` (first: its first item)
 template <bool BY_ITEM> __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int which) {
@@ -92,6 +94,8 @@ template <bool BY_ITEM> __device__ __forceinline__ Share share_of(const PagedAtt
     }
     s.items = __builtin_amdgcn_readlane(end, 63);
   }
+  s.b = uniform(s.b); s.piece = uniform(s.piece); s.pieces = uniform(s.pieces); s.tiles = uniform(s.tiles); s.items = uniform(s.items);
+  s.first = uniform(s.first);
   return s;
 }
 
@@ -113,11 +117,12 @@ __device__ __forceinline__ Rows rows_of(const PagedAttendArgs& a, int b, int t) 
 __device__ __forceinline__ unsigned there_of(const Rows& r) {
   return (r.r[0] >= 0) | (r.r[1] >= 0) << 1 | (r.r[2] >= 0) << 2 | (r.r[3] >= 0) << 3;
 }
-__device__ __forceinline__ uint32_t row_of(const Rows& r, int j) {        // a row there is, in any case
+__device__ __forceinline__ int pick_of(const Rows& r, int j) {
   const int r0 = r.r[0], r1 = r.r[1], r2 = r.r[2], r3 = r.r[3];           // (values: a choice between elements would be one between addresses)
   const int lo = (j & 1) ? r1 : r0, hi = (j & 1) ? r3 : r2;
-  return (uint32_t)max((j & 2) ? hi : lo, 0);
+  return (j & 2) ? hi : lo;
 }
+__device__ __forceinline__ uint32_t row_of(const Rows& r, int j) { return (uint32_t)max(pick_of(r, j), 0); }      // a row there is, in any case
 
 // ---------------------------------------------------------------- columns: lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float column_max(float x) {
@@ -171,8 +176,7 @@ template <int NCW, int TERMS> struct Codes {
   static constexpr int kTableBytes = kRtn ? 0 : NCW * 256;
   static constexpr int kEntry = 4 * TERMS;
   static constexpr int kScaleBytes = kRtn ? 512 : 128;     // per wave
-  static constexpr int kVWords = kRtn || c == 6 ? 16 : 8;
-
+  
   // -> exponent e of the grid: it is held times 2^-e
   static __device__ __forceinline__ int stage(const float* __restrict__ codebook, unsigned char* lds) {
     if constexpr (kRtn) return 0;
@@ -194,13 +198,12 @@ template <int NCW, int TERMS> struct Codes {
     return e;
   }
 
-  // ---- the row's query: which coordinates lane group g holds, in which order
-  static __device__ __forceinline__ int coordinate(int g, int r) { return kRtn ? (r < 16 ? 16 * g + r : 64 + 16 * g + r - 16) : 32 * g + r; }
+  // ---- the row's query: lane group g holds coordinates 32 g ..., uniform: 16 g ... of both halves
   template <typename T> static __device__ __forceinline__ void load_query(const T* __restrict__ row, int g, float (&v)[32]) {
     float half[16];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      Storage<T>::load(row + coordinate(g, 16 * k), half);
+      Storage<T>::load(row + (kRtn ? 64 * k + 16 * g : 32 * g + 16 * k), half);
 #pragma unroll
       for (int r = 0; r < 16; ++r) v[16 * k + r] = half[r];
     }
@@ -248,100 +251,111 @@ template <int NCW, int TERMS> struct Codes {
 
   // ---- a tile's codes and scales on their way: keys of tokens 8 (m / 4) + m % 4 (+ 4), the lane group's share of the coordinates;
   // values of tokens 8 g ..., 8 coordinates; the scale word of token lane % 32, lanes from 32 on: of the values
-  struct Words {
+  struct Keys {
     u32x4 k[2];
-    uint32_t v[kVWords];
-    u32x2 scale;
+    std::conditional_t<kRtn, u32x2, uint32_t> scale;
   };
-  static __device__ __forceinline__ Words request(const PagedAttendArgs& a, const Rows& rows, int h, int lane) {
-    const int m = lane & 15, g = lane >> 4;
-    const uint32_t row_bytes = (uint32_t)a.H * kRow, head = (uint32_t)h * kRow;
-    Words w;
-    const uint8_t* k = a.pool.k_codes + (uint64_t)row_of(rows, m >> 2) * row_bytes + ((m & 3) * row_bytes + head);
-#pragma unroll
-    for (int p = 0; p < 2; ++p, k += 4 * row_bytes) {
-      if constexpr (NCW == kRtn4) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(k + 8 * g), y = *reinterpret_cast<const u32x2*>(k + 32 + 8 * g);
-        w.k[p] = u32x4{x.x, x.y, y.x, y.y};
-      } else if constexpr (NCW == kRtn2) {
-        w.k[p] = u32x4{*reinterpret_cast<const uint32_t*>(k + 4 * g), *reinterpret_cast<const uint32_t*>(k + 16 + 4 * g), 0, 0};
-      } else if constexpr (c == 8) {
-        w.k[p] = *reinterpret_cast<const u32x4*>(k + 16 * g);
-      } else if constexpr (c == 4) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(k + 8 * g);
-        w.k[p] = u32x4{x.x, x.y, 0, 0};
+  struct Values { uint32_t v[8]; };
+  // FAR: an array of the pool is larger than 4 GiB.  Otherwise a lane's place is a 32-bit offset from addresses that are the same for all lanes
+  // (the pool's, and those of its second to eighth row), which takes no vector instruction but the choice of its group's row.
+  template <bool FAR> struct Place {
+    const uint8_t* base;
+    std::conditional_t<FAR, uint64_t, uint32_t> at;
+    __device__ __forceinline__ Place(const void* pool, const Rows& rows, int j, uint32_t row_bytes, uint32_t lane_at) : base(static_cast<const uint8_t*>(pool)) {
+      if constexpr (FAR) {
+        at = (uint64_t)row_of(rows, j) * row_bytes + lane_at;
       } else {
-        const uint32_t* x = reinterpret_cast<const uint32_t*>(k + 12 * g);
-        w.k[p] = u32x4{x[0], x[1], x[2], 0};
+        Rows bytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bytes.r[i] = (int)((uint32_t)max(rows.r[i], 0) * row_bytes);
+        at = (uint32_t)pick_of(bytes, j) + lane_at;
       }
     }
-    const uint8_t* v = a.pool.v_codes + (uint64_t)row_of(rows, g) * row_bytes + head;
+    template <typename W> __device__ __forceinline__ W load(uint32_t more) const {       // `more`: the same for all lanes
+      uint64_t from = reinterpret_cast<uint64_t>(base) + more;
+      asm("" : "+s"(from));                                // (a sum in scalar registers, not one per lane)
+      W w;
+      __builtin_memcpy(&w, reinterpret_cast<const __attribute__((address_space(1))) uint8_t*>(from) + at, sizeof(W));
+      return w;
+    }
+  };
+  template <bool FAR> static __device__ __forceinline__ Keys request_keys(const PagedAttendArgs& a, const Rows& rows, int h, int lane) {
+    const int m = lane & 15, g = lane >> 4;
+    const uint32_t row_bytes = (uint32_t)a.H * kRow, head = (uint32_t)h * kRow;
+    Keys w;
+    const Place<FAR> k(a.pool.k_codes, rows, m >> 2, row_bytes, (m & 3) * row_bytes + (kRtn ? c : 2 * c) * g);
 #pragma unroll
-    for (int e = 0; e < 8; ++e, v += row_bytes) {
+    for (int p = 0; p < 2; ++p) {
+      const uint32_t more = head + 4 * p * row_bytes;
       if constexpr (NCW == kRtn4) {
-        w.v[e] = *reinterpret_cast<const uint16_t*>(v + 2 * m);
-        w.v[8 + e] = *reinterpret_cast<const uint16_t*>(v + 32 + 2 * m);
+        const u32x2 x = k.template load<u32x2>(more), y = k.template load<u32x2>(more + 32);
+        w.k[p] = u32x4{x.x, x.y, y.x, y.y};
       } else if constexpr (NCW == kRtn2) {
-        w.v[e] = v[m];
-        w.v[8 + e] = v[16 + m];
+        w.k[p] = u32x4{k.template load<uint32_t>(more), k.template load<uint32_t>(more + 16), 0, 0};
       } else if constexpr (c == 8) {
-        w.v[e] = *reinterpret_cast<const uint32_t*>(v + 4 * m);
+        w.k[p] = k.template load<u32x4>(more);
       } else if constexpr (c == 4) {
-        w.v[e] = *reinterpret_cast<const uint16_t*>(v + 2 * m);
-      } else {                                             // the two words that the lane's 24 bits lie in
-        w.v[e] = reinterpret_cast<const uint32_t*>(v)[(3 * m) >> 2];
-        w.v[8 + e] = reinterpret_cast<const uint32_t*>(v)[(3 * m + 2) >> 2];
+        const u32x2 x = k.template load<u32x2>(more);
+        w.k[p] = u32x4{x.x, x.y, 0, 0};
+      } else {
+        struct Three { uint32_t x, y, z; };
+        const Three x = k.template load<Three>(more);
+        w.k[p] = u32x4{x.x, x.y, x.z, 0};
       }
     }
     const uint16_t* const scales = lane < 32 ? a.pool.k_scales : a.pool.v_scales;
     const uint64_t at = (uint64_t)(row_of(rows, (lane >> 3) & 3) + (lane & 7)) * a.H + h;
     if constexpr (kRtn) w.scale = reinterpret_cast<const u32x2*>(scales)[at];
-    else w.scale = u32x2{scales[at], 0};
+    else w.scale = scales[at];
+    return w;
+  }
+  template <bool FAR> static __device__ __forceinline__ Values request_values(const PagedAttendArgs& a, const Rows& rows, int h, int lane) {
+    const int m = lane & 15, g = lane >> 4;
+    const uint32_t row_bytes = (uint32_t)a.H * kRow, head = (uint32_t)h * kRow;
+    Values w;
+    const Place<FAR> v(a.pool.v_codes, rows, g, row_bytes, c == 8 ? 4 * m : c == 4 ? 2 * m : max(3 * m - 1, 0));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t more = head + e * row_bytes;
+      if constexpr (c == 4) w.v[e] = v.template load<uint16_t>(more);
+      else w.v[e] = v.template load<uint32_t>(more);       // (6 bits: the lane's 3 bytes, and the one before them)
+    }
     return w;
   }
 
-  // ---- scales: every lane's eight tokens 8 g ...
-  struct Scales { u32x4 ks[kRtn ? 2 : 1], kz[kRtn ? 2 : 1], vs[kRtn ? 2 : 1], vz[kRtn ? 2 : 1]; };      // 8 half-words each: scales (per half), zero points
-  static __device__ __forceinline__ void put_scales(const Words& w, unsigned char* lds, int lane) {
+  // ---- scales: every lane's eight tokens 8 g ..., through LDS
+  static __device__ __forceinline__ void put_scales(const Keys& w, unsigned char* lds, int lane) {
     uint16_t* const to = reinterpret_cast<uint16_t*>(lds);
-    if constexpr (kRtn) {
+    if constexpr (kRtn) {                                  // keys, values: step and zero point of the lower half, of the upper half
       uint16_t* const mine = to + (lane >> 5) * 128 + (lane & 31);
       mine[0] = (uint16_t)w.scale.x; mine[32] = (uint16_t)(w.scale.x >> 16);
       mine[64] = (uint16_t)w.scale.y; mine[96] = (uint16_t)(w.scale.y >> 16);
     } else {
-      to[lane] = (uint16_t)w.scale.x;
+      to[lane] = (uint16_t)w.scale;
     }
   }
-  static __device__ __forceinline__ Scales get_scales(const unsigned char* lds, int g) {
-    Scales s;
-    const auto at = [&](int i) { return *reinterpret_cast<const u32x4*>(lds + 64 * i + 16 * g); };
-    if constexpr (kRtn) {
-      s.ks[0] = at(0); s.kz[0] = at(1); s.ks[1] = at(2); s.kz[1] = at(3);
-      s.vs[0] = at(4); s.vz[0] = at(5); s.vs[1] = at(6); s.vz[1] = at(7);
-    } else {
-      s.ks[0] = at(0); s.vs[0] = at(1);
-    }
-    return s;
-  }
+  static constexpr int kKeys = 0, kValues = kRtn ? 4 : 1;  // rows of 32 half-words
+  static __device__ __forceinline__ u32x4 eight(const unsigned char* lds, int row, int g) { return *reinterpret_cast<const u32x4*>(lds + 64 * row + 16 * g); }
   static __device__ __forceinline__ float half_at(const u32x4& w, int e) {
     const f16x8 h = __builtin_bit_cast(f16x8, w);
     return (float)h[e];
   }
   static __device__ __forceinline__ float int_at(const u32x4& w, int e) { return (float)((w[e >> 1] >> (16 * (e & 1))) & 0xffffu); }
-  static __device__ __forceinline__ void value_scales(const Scales& s, float (&sv)[kRtn ? 2 : 1][8]) {
+  // the values' scales of the lane's tokens, per half (kHalves), and their zero points: fp16 numbers (times 2^-24).  `there`: those from it on are 0
+  static constexpr int kHalves = kRtn ? 2 : 1;
+  static __device__ __forceinline__ void keep_first(u32x4& w, int there) {
 #pragma unroll
-    for (int k = 0; k < (kRtn ? 2 : 1); ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sv[k][e] = half_at(s.vs[k], e);
+    for (int i = 0; i < 4; ++i) w[i] &= (2 * i < there ? 0xffffu : 0u) | (2 * i + 1 < there ? 0xffff0000u : 0u);
   }
-  // zero points of the lane's tokens from `there` on are not used
-  static __device__ __forceinline__ void mask_zeros(Scales& s, int there) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t keep = (2 * i < there ? 0xffffu : 0u) | (2 * i + 1 < there ? 0xffff0000u : 0u);
-      s.vz[0][i] &= keep;
-      s.vz[kRtn ? 1 : 0][i] &= keep;
-    }
+  static __device__ __forceinline__ u32x4 value_scales(const unsigned char* lds, int k, int g) { return eight(lds, kValues + 2 * k, g); }
+  static __device__ __forceinline__ f16x8 zero_points(const unsigned char* lds, int k, int g, int there) {
+    u32x4 w = eight(lds, kValues + 2 * k + 1, g);
+    if (there < 8) keep_first(w, there);
+    return __builtin_bit_cast(f16x8, w);
+  }
+  // the larger one of a token's scales
+  static __device__ __forceinline__ float scale_at(const u32x4 (&vs)[kHalves], int e) {
+    return kRtn ? fmaxf(half_at(vs[0], e), half_at(vs[kHalves - 1], e)) : half_at(vs[0], e);
   }
 
   // ---- look-ups
@@ -370,7 +384,7 @@ template <int NCW, int TERMS> struct Codes {
   }
 
   // ---- scores of product p: s[half][p] += keys * query
-  static __device__ __forceinline__ void scores(const Words& w, int p, const unsigned char* lds, int lane, const f16x8 (&q)[TERMS][4],
+  static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const f16x8 (&q)[TERMS][4],
                                                 f32x4 (&s)[kRtn ? 2 : 1][2]) {
     const uint32_t x[4] = {w.k[p].x, w.k[p].y, w.k[p].z, w.k[p].w};
     if constexpr (kRtn) {
@@ -401,39 +415,49 @@ template <int NCW, int TERMS> struct Codes {
     }
   }
   // ... of the lane's eight tokens, times the scales
-  static __device__ __forceinline__ void scaled(const f32x4 (&s)[kRtn ? 2 : 1][2], const Scales& sc, const float (&qsum)[2], float (&y)[8]) {
+  static __device__ __forceinline__ void scaled(const f32x4 (&s)[kRtn ? 2 : 1][2], const unsigned char* lds, int g, const float (&qsum)[2], float (&y)[8]) {
+    const u32x4 ks = eight(lds, kKeys, g);
+    if constexpr (kRtn) {
+      const u32x4 kz = eight(lds, kKeys + 1, g), ks1 = eight(lds, kKeys + 2, g), kz1 = eight(lds, kKeys + 3, g);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = s[0][e >> 2][e & 3];
-      if constexpr (kRtn) {
-        const float lo = __fmaf_rn(-int_at(sc.kz[0], e), qsum[0], y[e]), hi = __fmaf_rn(-int_at(sc.kz[1], e), qsum[1], s[1][e >> 2][e & 3]);
-        y[e] = __fmaf_rn(lo, half_at(sc.ks[0], e), hi * half_at(sc.ks[1], e));
-      } else {
-        y[e] *= half_at(sc.ks[0], e);
+      for (int e = 0; e < 8; ++e) {
+        const float lo = __fmaf_rn(-int_at(kz, e), qsum[0], s[0][e >> 2][e & 3]), hi = __fmaf_rn(-int_at(kz1, e), qsum[1], s[1][e >> 2][e & 3]);
+        y[e] = __fmaf_rn(lo, half_at(ks, e), hi * half_at(ks1, e));
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = s[0][e >> 2][e & 3] * half_at(ks, e);
     }
   }
 
-  // ---- o[j] += values (coordinates: result()) * weights (per half)
-  static __device__ __forceinline__ void values(const Words& w, const Scales& sc, const float (&wt)[kRtn ? 2 : 1][8], const unsigned char* lds,
-                                                int lane, f32x4 (&o)[8], f32x4 (&oz)[2]) {
-    f16x8 b[kRtn ? 2 : 1][TERMS];
+  // ---- o[j] += values (coordinates: result()) * weights p * scale
+  static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, const float (&p)[8],
+                                                const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane, f32x4 (&o)[8], f32x4 (&oz)[2]) {
+    f16x8 b[kHalves][TERMS];
 #pragma unroll
-    for (int k = 0; k < (kRtn ? 2 : 1); ++k) split_f16<TERMS>(wt[k], b[k]);
+    for (int k = 0; k < kHalves; ++k) {
+      float weight[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) weight[e] = p[e] * half_at(vs[k], e);
+      split_f16<TERMS>(weight, b[k]);
+    }
     if constexpr (kRtn) {
+      // All rows of an operand have to be of one half (the weights are the half's): of the eight codes that a lane holds, lanes m and m ^ 8
+      // exchange four.  Lower half-word: coordinates of the lower half, upper one: of the upper half.
+      uint32_t d[8];
+      const uint32_t pick = c == 8 ? ((lane & 8) ? 0x07060302u : 0x01000504u) : ((lane & 8) ? 0x0c050c01u : 0x0c000c04u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = __builtin_amdgcn_perm(w.v[e], __float_as_uint(row_xor8(__uint_as_float(w.v[e]))), pick);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const f16x8 z = __builtin_bit_cast(f16x8, sc.vz[k]);
+        const f16x8 z = zero_points(scales, k, lane >> 4, there);
 #pragma unroll
         for (int n = 0; n < TERMS; ++n) oz[k] = mfma(z, b[k][n], oz[k]);
 #pragma unroll
         for (int byte = 0; byte < 4 / kFields; ++byte) {
           uint32_t x[4];                                   // tokens 2 i and 2 i + 1 in the halves
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = w.v[8 * k + 2 * i], hi = w.v[8 * k + 2 * i + 1];
-            x[i] = NCW == kRtn4 ? __builtin_amdgcn_perm(hi, lo, byte == 0 ? 0x0c040c00u : 0x0c050c01u) : lo | hi << 16;
-          }
+          for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(d[2 * i + 1], d[2 * i], 0x0c040c00u + 0x00010001u * (2 * k + byte));
 #pragma unroll
           for (int f = 0; f < kFields; ++f) {
             const f16x8 v = operand(x[0] & field_mask(f), x[1] & field_mask(f), x[2] & field_mask(f), x[3] & field_mask(f));
@@ -450,8 +474,7 @@ template <int NCW, int TERMS> struct Codes {
         uint32_t d[TERMS][8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          uint32_t x[1] = {w.v[e]};
-          if constexpr (c == 6) x[0] = __builtin_amdgcn_alignbit(w.v[8 + e], w.v[e], 8 * ((3 * m) & 3));
+          const uint32_t x[1] = {c == 6 ? w.v[e] >> (m != 0 ? 8 : 0) : w.v[e]};
           const uint32_t off = offset(x, i, at);
           d[0][e] = point(lds, off);
           if constexpr (TERMS == 2) d[1][e] = point<1>(lds, off);
@@ -475,7 +498,11 @@ template <int NCW, int TERMS> struct Codes {
       }
     }
   }
-  // the lane's 32 coordinates, coordinate(g, r): product j's row 4 g + i is coordinate 8 (4 g + i) + j, or 4 (4 g + i) + j % 4 of half j / 4
+  // the lane's 32 coordinates, in fours from coordinate(g, 4 i'): product j's row 4 g + i is coordinate 8 (4 g + i) + j, or (uniform) 8 ((4 g + i) % 8) +
+  // 4 (g / 2) + j % 4 of half j / 4
+  static __device__ __forceinline__ int coordinate(int g, int r) {
+    return kRtn ? 64 * (r >> 4) + 8 * ((4 * g + ((r >> 2) & 3)) & 7) + 4 * (g >> 1) : 32 * g + r;
+  }
   static __device__ __forceinline__ void result(const f32x4 (&o)[8], const f32x4 (&oz)[2], int e, float (&v)[32]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -505,11 +532,13 @@ template <typename T, int NCW> __device__ __forceinline__ void finish(const Page
   if (!there) return;
   T* const out = static_cast<T*>(a.out) + (row * a.q_heads + qh) * kGroup;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    float half[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) half[r] = v[16 * k + r];
-    Storage<T>::template store<false>(out + Codes<NCW, 1>::coordinate(g, 16 * k), 0, half);
+  for (int r = 0; r < 32; r += 4) {
+    T* const at = out + Codes<NCW, 1>::coordinate(g, r);
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<u32x2*>(at) = u32x2{Storage<T>::pack2(v[r], v[r + 1]), Storage<T>::pack2(v[r + 2], v[r + 3])};
+    } else {
+      *reinterpret_cast<f32x4*>(at) = f32x4{v[r], v[r + 1], v[r + 2], v[r + 3]};
+    }
   }
 }
 

@@ -17,8 +17,17 @@ using namespace paged;
 //            tokens 8 g ... 8 g + 7 for row m, which is what the second product wants of it as its B operand, with no exchange between lanes;
 //   values   O^T = V^T P: A holds 8 tokens of one coordinate; a look-up gives two neighbouring coordinates, two permutes pair them up by
 //            token.  The 32 coordinates a lane ends with are consecutive, as the inverse transform wants them.
-template <typename T, int NCW>
-__global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAttendArgs a) {
+// Waves of a workgroup, which share the copies of the grid, and waves per SIMD: with 128 registers four fit (two workgroups a CU, which is what LDS has
+// room for with 256 points); uniform codes need more for the two halves' scales, and no LDS to speak of; fp32 layers hold everything twice.
+template <typename T, int NCW> struct Shape {
+  static constexpr int kWaves = is_rtn(NCW) ? 4 : 8;
+  static constexpr int kPerSimd = is_rtn(NCW) ? 3 : sizeof(T) == 4 ? 2 : 4;
+  static constexpr int kThreads = 64 * kWaves, kSlots = 256 * 4 * kPerSimd;            // threads, waves on the chip
+};
+template <typename T, int NCW, bool FAR>
+__global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_waves_per_eu((Shape<T, NCW>::kPerSimd)))) void paged_attend_kernel(
+    const PagedAttendArgs a) {
+  constexpr int kWaves = Shape<T, NCW>::kWaves;
   constexpr int kTerms = sizeof(T) == 2 ? 1 : 2;
   constexpr bool kRtn = is_rtn(NCW);
   typedef Codes<NCW, kTerms> C;
@@ -29,7 +38,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAt
 
   // which rows, kv head and piece of a sequence
   const unsigned unit = blockIdx.x * kWaves + wave;
-  const int h = unit % a.H, item = unit / a.H;
+  const int h = uniform(unit % a.H), item = uniform(unit / a.H);
   const Share share = share_of<true>(a, lane, item);
   if (blockIdx.x * kWaves / a.H >= (unsigned)share.items) return;         // (the whole workgroup is behind the last piece)
   const int c_exp = C::stage(a.codebook, lds);
@@ -43,7 +52,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAt
   const bool row_there = row < n_rows;
   // the last token the row sees; the tokens of this piece
   const int limit = row_there ? w.len - w.count + qi : -1;
-  const int first_limit = w.len - w.count + row0 / rep, last_limit = w.len - w.count + min(row0 + 15, n_rows - 1) / rep;
+  const int first_limit = uniform(w.len - w.count + row0 / rep), last_limit = uniform(w.len - w.count + min(row0 + 15, n_rows - 1) / rep);
   const int t_begin = share.piece * share.tiles * kTile, t_end = min(min(t_begin + share.tiles * kTile, w.len), last_limit + 1);
 
   // ---- the row's query: rotated, scaled to fp16's range
@@ -76,41 +85,35 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAt
   f32x4 oz[2] = {};                                        // uniform: sums of the zero points, per half
   float ref = -3.0e38f, sum = 0.f;                         // weights are 2^(score - ref)
 
-  const auto tile = [&](const typename C::Words& x, int t, unsigned there) {
+  const auto tile = [&](const typename C::Keys& x, const typename C::Values& xv, int t, unsigned there) {
     // scales of the tile's 32 tokens to the lanes that need them
     asm volatile("" ::: "memory");                         // (a wave's LDS accesses stay in order)
     C::put_scales(x, scale_lds, lane);
     asm volatile("" ::: "memory");
     f32x4 s[kRtn ? 2 : 1][2] = {};                         // [half][product]
-    typename C::Scales sc = C::get_scales(scale_lds, g);
 #pragma unroll
     for (int p = 0; p < 2; ++p) C::scores(x, p, lds, lane, q, s);
     float y[8];
-    C::scaled(s, sc, qsum, y);
-    float sv[kRtn ? 2 : 1][8];
-    C::value_scales(sc, sv);
+    __builtin_amdgcn_sched_barrier(0);
+    C::scaled(s, scale_lds, g, qsum, y);
+    u32x4 vs[C::kHalves];
+#pragma unroll
+    for (int k = 0; k < C::kHalves; ++k) vs[k] = C::value_scales(scale_lds, k, g);
     const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;       // (t_end: of this piece, whole tiles but for the last)
     if (masked) {
-      const int seen = (there >> g) & 1 ? limit - (t + 8 * g) : -1;        // tokens 0 ... seen of the lane's eight are seen
+      const int seen = (there >> g) & 1 ? limit + 1 - (t + 8 * g) : 0;     // so many of the lane's eight tokens are seen
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (e > seen) {
-          y[e] = -INFINITY;
-          sv[0][e] = 0.f;
-          if constexpr (kRtn) sv[1][e] = 0.f;
-        }
-      }
-      if constexpr (kRtn) C::mask_zeros(sc, (there >> g) & 1 ? min(w.len - (t + 8 * g), 8) : 0);
+      for (int e = 0; e < 8; ++e) y[e] = e < seen ? y[e] : -INFINITY;
+#pragma unroll
+      for (int k = 0; k < C::kHalves; ++k) C::keep_first(vs[k], seen);
     }
-    float p[8], wt[kRtn ? 2 : 1][8];
+    float p[8];
     const auto weigh = [&] {
       float top = 0.f, big = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref));
-        wt[0][e] = p[e] * sv[0][e];
-        top = fmaxf(top, wt[0][e]);
-        if constexpr (kRtn) { wt[1][e] = p[e] * sv[1][e]; top = fmaxf(top, wt[1][e]); }
+        top = fmaxf(top, p[e] * C::scale_at(vs, e));
         big = fmaxf(big, p[e]);
       }
       return __builtin_amdgcn_ballot_w64(top > kTopWeight || big > 0x1p60f) != 0;
@@ -118,11 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAt
     if (weigh()) {                                         // the reference follows: weights of the largest become 2^kStartExp
       float top = -3.0e38f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float sg = sv[0][e];
-        if constexpr (kRtn) sg = fmaxf(sg, sv[1][e]);
-        top = fmaxf(top, y[e] * f + __builtin_amdgcn_logf(fmaxf(sg, 0x1p-24f)));
-      }
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, y[e] * f + __builtin_amdgcn_logf(fmaxf(C::scale_at(vs, e), 0x1p-24f)));
       const float moved = fmaxf(ref, column_max(top) - kStartExp);
       const float by = __builtin_amdgcn_exp2f(ref - moved);
       ref = moved;
@@ -134,35 +133,39 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attend_kernel(const PagedAt
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += p[e];
-    C::values(x, sc, wt, lds, lane, o, oz);
+    __builtin_amdgcn_sched_barrier(0);
+    C::values(xv, scale_lds, (there >> g) & 1 ? w.len - (t + 8 * g) : 0, p, vs, lds, lane, o, oz);
   };
-  // Codes are requested a tile ahead, the rows they are in two tiles ahead.
+  // Keys are requested a tile ahead, values behind the tile that takes their registers, the rows they are in two tiles ahead.
   if (t_begin < t_end) {
-    typename C::Words even, odd;
     Rows r0 = rows_of(a, b, t_begin), r1 = rows_of(a, b, t_begin + kTile);
-    even = C::request(a, r0, h, lane);
-    for (int t = t_begin;; t += 2 * kTile) {
-      Rows r2 = rows_of(a, b, t + 2 * kTile);
-      if (t + kTile < t_end) odd = C::request(a, r1, h, lane);
-      tile(even, t, there_of(r0));
-      if (t + kTile >= t_end) break;
-      r0 = rows_of(a, b, t + 3 * kTile);
-      if (t + 2 * kTile < t_end) even = C::request(a, r2, h, lane);
-      tile(odd, t + kTile, there_of(r1));
-      if (t + 2 * kTile >= t_end) break;
-      r1 = r0;
-      r0 = r2;
+    typename C::Keys k = C::template request_keys<FAR>(a, r0, h, lane), next = k;
+    typename C::Values v = C::template request_values<FAR>(a, r0, h, lane);
+#pragma unroll 1
+    for (int t = t_begin; t < t_end; t += kTile) {
+      const bool more = t + kTile < t_end;
+      if (more) next = C::template request_keys<FAR>(a, r1, h, lane);
+      const unsigned there = there_of(r0);
+      const Rows r2 = rows_of(a, b, t + 2 * kTile);
+      tile(k, v, t, there);
+      if (more) v = C::template request_values<FAR>(a, r1, h, lane);
+      k = next;
+      r0 = r1;
+      r1 = r2;
     }
   }
 
-  // ---- the lane's 32 coordinates of the row
+  // ---- the lane's 32 coordinates of the row (whose numbers are worked out anew: they are not worth registers in the loop)
+  int again = m;
+  asm volatile("" : "+v"(again));
+  const int row_out = row0 + again, qi_out = row_out / rep, qh_out = h * rep + row_out % rep;
   sum = column_sum(sum);
   float v[32];
   C::result(o, oz, kRtn ? 24 : c_exp, v);
   if (share.pieces == 1) {
-    finish<T, NCW>(a, v, sum, h, g, row_there, w.first + qi, qh);
-  } else if (row_there) {
-    const int64_t at = ((int64_t)item * a.max_queries + qi) * a.q_heads + qh;
+    finish<T, NCW>(a, v, sum, h, g, row_out < n_rows, w.first + qi_out, qh_out);
+  } else if (row_out < n_rows) {
+    const int64_t at = ((int64_t)item * a.max_queries + qi_out) * a.q_heads + qh_out;
     float* const part = a.part + at * kGroup;
 #pragma unroll
     for (int r = 0; r < 8; ++r)
@@ -232,48 +235,60 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedA
 // How a launch is laid out, from sizes alone (lengths are on the device).
 struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles; int64_t items; bool merge; };
 constexpr int kMinTiles = 2;                               // a piece of fewer tokens costs more than it saves
-PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
+template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
   PagedPlan p;
   p.row_tiles = (unsigned)((max_queries * (q_heads / H) + 15) / 16);
   p.min_tiles = kMinTiles;
-  // as many waves as the chip holds, two workgroups a CU
-  p.slots = (int)std::max<int64_t>(256 * 2 * kWaves / (H * p.row_tiles), 1);
+  // as many pieces as make all waves that the chip holds
+  p.slots = (int)std::max<int64_t>(Shape<T, NCW>::kSlots / (H * p.row_tiles), 1);
   const int64_t most = (table_pages * page_tokens + kTile - 1) / kTile;                       // tiles of a sequence
   const int64_t each = std::max<int64_t>((most + kMinTiles - 1) / kMinTiles, 1);
   p.items = std::min(batch * each, std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
-  p.blocks = (unsigned)((p.items * H + kWaves - 1) / kWaves);
+  p.blocks = (unsigned)((p.items * H + Shape<T, NCW>::kWaves - 1) / Shape<T, NCW>::kWaves);
   p.merge = each > 1;
   return p;
 }
 
 }  // namespace
 
-size_t paged_attend_workspace_bytes(const PagedAttendArgs& a) {
-  const PagedPlan p = paged_plan(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H);
+#define AQUAKV_PAGED(DT, NCW, CALL)                                            \
+  do {                                                                         \
+    if ((DT) == kBF16) { typedef bf16_t T; AQUAKV_PAGED_N(NCW, CALL); }        \
+    else { typedef float T; AQUAKV_PAGED_N(NCW, CALL); }                       \
+  } while (0)
+#define AQUAKV_PAGED_N(NCW, CALL)                                              \
+  do {                                                                         \
+    if ((NCW) == kRtn2) { constexpr int N = kRtn2; CALL; }                     \
+    else if ((NCW) == kRtn4) { constexpr int N = kRtn4; CALL; }                \
+    else if ((NCW) == 16) { constexpr int N = 16; CALL; }                      \
+    else if ((NCW) == 64) { constexpr int N = 64; CALL; }                      \
+    else { constexpr int N = 256; CALL; }                                      \
+  } while (0)
+
+static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a) {
+  PagedPlan p = {};
+  AQUAKV_PAGED(dtype, n_codewords, (p = paged_plan<T, N>(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H)));
+  return p;
+}
+
+size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a) {
+  const PagedPlan p = plan_of(dtype, n_codewords, a);
   return p.merge ? (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& args, void* workspace, hipStream_t stream) {
   PagedAttendArgs a = args;
-  const PagedPlan plan = paged_plan(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H);
+  const PagedPlan plan = plan_of(dtype, n_codewords, a);
   a.slots = plan.slots;
   a.min_tiles = plan.min_tiles;
   a.part = static_cast<float*>(workspace);
   a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
   a.page_groups = a.pool.page_tokens / 8;
   a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
-#define AQUAKV_ATTEND(T, NCW) paged_attend_kernel<T, NCW><<<dim3(plan.blocks, plan.row_tiles), kThreads, 0, stream>>>(a)
-#define AQUAKV_ATTEND_T(T)                                    \
-  switch (n_codewords) {                                      \
-    case kRtn2: AQUAKV_ATTEND(T, kRtn2); break;               \
-    case kRtn4: AQUAKV_ATTEND(T, kRtn4); break;               \
-    case 16: AQUAKV_ATTEND(T, 16); break;                     \
-    case 64: AQUAKV_ATTEND(T, 64); break;                     \
-    default: AQUAKV_ATTEND(T, 256);                           \
-  }
-  if (dtype == kBF16) { AQUAKV_ATTEND_T(bf16_t) } else { AQUAKV_ATTEND_T(float) }
-#undef AQUAKV_ATTEND_T
-#undef AQUAKV_ATTEND
+  const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
+  const dim3 blocks(plan.blocks, plan.row_tiles);
+  AQUAKV_PAGED(dtype, n_codewords, (far ? paged_attend_kernel<T, N, true><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)
+                                        : paged_attend_kernel<T, N, false><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)));
   if (const hipError_t e = hipGetLastError()) return e;
   if (!plan.merge) return hipSuccess;
   const dim3 grid((unsigned)(a.max_queries * a.q_heads), (unsigned)a.batch);
