@@ -265,6 +265,7 @@ struct PagedAttendArgs {
   const float* codebook;
   // set by the launcher
   float *part, *stats;                            // [items, max_queries, q_heads, 128], [items, max_queries, q_heads, 2]
+  int2* heads;                                    // [batch]: a sequence's first item, and how many
   int slots, min_tiles;                           // pieces that fill the chip, tiles of a piece at least
   uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
 };

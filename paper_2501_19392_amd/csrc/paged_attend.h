@@ -48,31 +48,30 @@ __device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, 
 
 // The tokens of all sequences are cut into pieces of equally many tiles, so that about a.slots of them cover the batch whatever its
 // lengths (each sequence has one at least): item i of the launch is piece `piece` of `pieces` of sequence b (-1: behind the last).
-struct Share { int b, piece, pieces, tiles, items, first; };
+struct Share { int b, piece, pieces, tiles, items; };
 __device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
   return b < a.batch ? max((length_of(a, a.seq_lens[b]) + kTile - 1) / kTile, 1) : 0;
 }
 // tiles per piece
-__device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int64_t total) {
-  const int64_t room = max(a.slots - a.batch, max(a.slots / 2, 1));
-  return (int)max((total + room - 1) / room, (int64_t)a.min_tiles);
+__device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int total) {
+  const uint32_t room = (uint32_t)max(a.slots - a.batch, max(a.slots / 2, 1));
+  return max((int)(((uint32_t)total + room - 1) / room), a.min_tiles);
 }
 __device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
   return uniform(x);
 }
-// by_item: of item `which`; else of sequence `which` (first: its first item)
-template <bool BY_ITEM> __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int which) {
-  Share s = {-1, 0, 1, 0, 0, 0};
+__device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
+  Share s = {-1, 0, 1, 0, 0};
   if (a.batch == 1) {
     const int n = max((length_of(a, const_ints(a.seq_lens)[0]) + kTile - 1) / kTile, 1);
     s.tiles = piece_tiles(a, n);
     s.items = s.pieces = (n + s.tiles - 1) / s.tiles;
-    if (!BY_ITEM || which < s.items) { s.b = 0; s.piece = which; }
+    if (item < s.items) { s.b = 0; s.piece = item; }
     return s;
   }
-  int64_t total = 0;
+  int total = 0;                                           // (all sequences' room is below 2^30 tiles)
   for (int b0 = 0; b0 < a.batch; b0 += 64) total += wave_sum(tiles_of(a, b0 + lane));
   s.tiles = piece_tiles(a, total);
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
@@ -84,18 +83,16 @@ template <bool BY_ITEM> __device__ __forceinline__ Share share_of(const PagedAtt
       end += lane >= k ? add : 0;
     }
     end += s.items;
-    const uint64_t past = BY_ITEM ? __builtin_amdgcn_ballot_w64(end > which) : b0 + 63 >= which ? ~0ull << (which - b0) : 0;
+    const uint64_t past = __builtin_amdgcn_ballot_w64(end > item);
     if (past != 0 && s.b < 0) {
       const int l = __builtin_ctzll(past);
       s.b = b0 + l;
       s.pieces = __builtin_amdgcn_readlane(mine, l);
-      s.first = __builtin_amdgcn_readlane(end, l) - s.pieces;
-      s.piece = which - s.first;
+      s.piece = item - (__builtin_amdgcn_readlane(end, l) - s.pieces);
     }
     s.items = __builtin_amdgcn_readlane(end, 63);
   }
   s.b = uniform(s.b); s.piece = uniform(s.piece); s.pieces = uniform(s.pieces); s.tiles = uniform(s.tiles); s.items = uniform(s.items);
-  s.first = uniform(s.first);
   return s;
 }
 
@@ -177,35 +174,77 @@ template <int NCW, int TERMS> struct Codes {
   static constexpr int kEntry = 4 * TERMS;
   static constexpr int kScaleBytes = kRtn ? 512 : 128;     // per wave
   
-  // -> exponent e of the grid: it is held times 2^-e
-  static __device__ __forceinline__ int stage(const float* __restrict__ codebook, unsigned char* lds) {
+  // A lane's points, kPoints l ... (fewer points than lanes: l modulo the points), on their way to LDS.
+  static constexpr int kPoints = NCW / 64 > 0 ? NCW / 64 : 1;
+  struct Points { float x[2 * kPoints]; };
+  static __device__ __forceinline__ Points request_points(const float* __restrict__ codebook, int lane) {
+    Points p = {};
+    if constexpr (!kRtn) __builtin_memcpy(&p, codebook + 2 * kPoints * (lane & (NCW / kPoints - 1)), sizeof(p));
+    return p;
+  }
+  // -> exponent e of the grid: it is held times 2^-e.  Wave `wave` of WAVES writes its share of every point's row; lanes start at different
+  // places of their rows, so that their banks differ.
+  template <int WAVES> static __device__ __forceinline__ int stage(const Points& p, unsigned char* lds, int lane, int wave) {
     if constexpr (kRtn) return 0;
     float top = 0.f;
-    for (int j = threadIdx.x & 63; j < 2 * NCW; j += 64) top = fmaxf(top, fabsf(codebook[j]));
 #pragma unroll
-    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
-    const int e = max(__builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top)), -100);
-    for (int i = threadIdx.x; i < NCW * 16; i += blockDim.x) {
-      const float x = __builtin_ldexpf(codebook[2 * (i / 16)], -e), y = __builtin_ldexpf(codebook[2 * (i / 16) + 1], -e);
+    for (int i = 0; i < 2 * kPoints; ++i) top = fmaxf(top, fabsf(p.x[i]));
+    top = column_max(top);
+    top = fmaxf(top, row_xor8(top));
+    top = fmaxf(top, octet_mirror(top));
+    top = fmaxf(top, quad_xor<1>(top));
+    top = fmaxf(top, quad_xor<2>(top));
+    const int e = max(uniform(__builtin_amdgcn_frexp_expf(top)), -100);
+    constexpr int kLanes = NCW / kPoints;                  // lanes that hold different points
+    constexpr int kChunks = 16 * kLanes / 64;              // 16-byte pieces of its points' rows that a lane of the workgroup writes, over the waves
+#pragma unroll
+    for (int i = 0; i < kPoints; ++i) {
+      const float x = __builtin_ldexpf(p.x[2 * i], -e), y = __builtin_ldexpf(p.x[2 * i + 1], -e);
       const uint32_t hi = f16_pair(x, y);
       uint32_t other = hi;
       if constexpr (TERMS == 2) {
         const f16x2 h = __builtin_bit_cast(f16x2, hi);
         other = f16_pair(x - (float)h[0], y - (float)h[1]);
       }
-      *reinterpret_cast<u32x4*>(lds + 16 * i) = u32x4{hi, other, hi, other};
+      const int point = kPoints * (lane & (kLanes - 1)) + i, turn = lane / kLanes;
+#pragma unroll
+      for (int k = 0; k < (kChunks + WAVES - 1) / WAVES; ++k) {
+        const int chunk = turn + (64 / kLanes) * (wave + WAVES * k);
+        if (kChunks % WAVES == 0 || wave + WAVES * k < kChunks)
+          *reinterpret_cast<u32x4*>(lds + 256 * point + 16 * ((chunk + lane) & 15)) = u32x4{hi, other, hi, other};
+      }
     }
     return e;
   }
 
   // ---- the row's query: lane group g holds coordinates 32 g ..., uniform: 16 g ... of both halves
-  template <typename T> static __device__ __forceinline__ void load_query(const T* __restrict__ row, int g, float (&v)[32]) {
-    float half[16];
+  template <typename T> struct Query { u32x4 w[2 * sizeof(T)], signs[kRtn ? 1 : 2]; };      // as loaded
+  template <typename T> static __device__ __forceinline__ Query<T> request_query(const T* __restrict__ row, const int8_t* signs, int h, int g) {
+    Query<T> q;
+    constexpr int kHalf = sizeof(T);                       // 16-byte words of 16 values
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      Storage<T>::load(row + (kRtn ? 64 * k + 16 * g : 32 * g + 16 * k), half);
+    for (int i = 0; i < 2 * kHalf; ++i)
+      q.w[i] = reinterpret_cast<const u32x4*>(row + (kRtn ? 64 * (i / kHalf) + 16 * g : 32 * g + 16 * (i / kHalf)))[i % kHalf];
+    if constexpr (!kRtn) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) v[16 * k + r] = half[r];
+      for (int i = 0; i < 2; ++i) q.signs[i] = reinterpret_cast<const u32x4*>(signs + h * kGroup + 32 * g)[i];
+    }
+    return q;
+  }
+  // (grids: with the signs)
+  template <typename T> static __device__ __forceinline__ void unpack_query(const Query<T>& q, float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+      if constexpr (sizeof(T) == 2) {
+        unpack_bf16x8(q.w[i], &v[8 * i]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[4 * i + k] = __uint_as_float(q.w[i][k]);
+      }
+    }
+    if constexpr (!kRtn) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) v[r] = __uint_as_float(__float_as_uint(v[r]) ^ ((q.signs[r >> 4][(r >> 2) & 3] << (24 - 8 * (r & 3))) & 0x80000000u));
     }
   }
   static __device__ __forceinline__ void pack_query(const float (&v)[32], f16x8 (&q)[TERMS][4], float (&qsum)[2]) {

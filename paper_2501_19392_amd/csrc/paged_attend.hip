@@ -36,49 +36,58 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned char* const scale_lds = lds + C::kTableBytes + wave * C::kScaleBytes;
 
+  // What is waited for at the start is a chain (lengths, then the piece's pages, then its codes); all else is requested beside it.
+  const typename C::Points points = C::request_points(a.codebook, lane);
   // which rows, kv head and piece of a sequence
   const unsigned unit = blockIdx.x * kWaves + wave;
   const int h = uniform(unit % a.H), item = uniform(unit / a.H);
-  const Share share = share_of<true>(a, lane, item);
+  const Share share = share_of(a, lane, item);
   if (blockIdx.x * kWaves / a.H >= (unsigned)share.items) return;         // (the whole workgroup is behind the last piece)
-  const int c_exp = C::stage(a.codebook, lds);
-  __syncthreads();
-  if (share.b < 0) return;
-  const int b = share.b, rep = a.q_heads / a.H;
+  const int b = max(share.b, 0), rep = a.q_heads / a.H;
   const PagedQueries w = paged_queries(a, b);
   const int n_rows = w.n * rep, row0 = blockIdx.y * 16;
-  if (row0 >= n_rows) return;
+  const bool idle = share.b < 0 || row0 >= n_rows;
   const int row = row0 + m, qi = row / rep, qh = h * rep + row % rep;
   const bool row_there = row < n_rows;
   // the last token the row sees; the tokens of this piece
   const int limit = row_there ? w.len - w.count + qi : -1;
   const int first_limit = uniform(w.len - w.count + row0 / rep), last_limit = uniform(w.len - w.count + min(row0 + 15, n_rows - 1) / rep);
-  const int t_begin = share.piece * share.tiles * kTile, t_end = min(min(t_begin + share.tiles * kTile, w.len), last_limit + 1);
+  const int t_begin = share.piece * share.tiles * kTile, t_end = idle ? 0 : min(min(t_begin + share.tiles * kTile, w.len), last_limit + 1);
+  const bool any = t_begin < t_end;
+  typename C::template Query<T> asked = {};
+  if (!idle)
+    asked = C::template request_query<T>(static_cast<const T*>(a.q) + (w.first + (row_there ? qi : 0)) * a.q_stride + (row_there ? qh : h * rep) * kGroup,
+                                         a.signs_k, h, g);
+  Rows r0 = {}, r1 = {};
+  typename C::Keys k = {}, next = {};
+  typename C::Values v = {};
+  if (any) {
+    r0 = rows_of(a, b, t_begin);
+    r1 = rows_of(a, b, t_begin + kTile);
+    k = C::template request_keys<FAR>(a, r0, h, lane);
+    v = C::template request_values<FAR>(a, r0, h, lane);
+  }
+  const int c_exp = C::template stage<kWaves>(points, lds, lane, wave);
+  __syncthreads();
+  if (idle) return;
 
   // ---- the row's query: rotated, scaled to fp16's range
   f16x8 q[kTerms][4];
   float qsum[2] = {0.f, 0.f};                              // uniform: sum of the row's (rounded) query over each half
   float f;                                                 // score in powers of two = f * sigma * sum
   {
-    float v[32];
-    const T* const src = static_cast<const T*>(a.q) + (w.first + (row_there ? qi : 0)) * a.q_stride + (row_there ? qh : h * rep) * kGroup;
-    C::template load_query<T>(src, g, v);
-    if constexpr (!kRtn) {
-      float sf[32];
-      load_signs(a.signs_k, h, g, sf);
-#pragma unroll
-      for (int r = 0; r < 32; ++r) v[r] *= sf[r];
-      wht_columns(v);
-    }
+    float x[32];
+    C::template unpack_query<T>(asked, x);
+    if constexpr (!kRtn) wht_columns(x);
     const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
     float top = 0.f;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) { v[r] *= by; top = fmaxf(top, fabsf(v[r])); }
+    for (int r = 0; r < 32; ++r) { x[r] *= by; top = fmaxf(top, fabsf(x[r])); }
     const int e = max(__builtin_amdgcn_frexp_expf(column_max(top)), -100);
     f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? 24 : c_exp), 126));
 #pragma unroll
-    for (int r = 0; r < 32; ++r) v[r] = __builtin_ldexpf(v[r], kQueryExp - e);
-    C::pack_query(v, q, qsum);
+    for (int r = 0; r < 32; ++r) x[r] = __builtin_ldexpf(x[r], kQueryExp - e);
+    C::pack_query(x, q, qsum);
   }
 
   f32x4 o[8] = {};
@@ -137,103 +146,123 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
     C::values(xv, scale_lds, (there >> g) & 1 ? w.len - (t + 8 * g) : 0, p, vs, lds, lane, o, oz);
   };
   // Keys are requested a tile ahead, values behind the tile that takes their registers, the rows they are in two tiles ahead.
-  if (t_begin < t_end) {
-    Rows r0 = rows_of(a, b, t_begin), r1 = rows_of(a, b, t_begin + kTile);
-    typename C::Keys k = C::template request_keys<FAR>(a, r0, h, lane), next = k;
-    typename C::Values v = C::template request_values<FAR>(a, r0, h, lane);
 #pragma unroll 1
-    for (int t = t_begin; t < t_end; t += kTile) {
-      const bool more = t + kTile < t_end;
-      if (more) next = C::template request_keys<FAR>(a, r1, h, lane);
-      const unsigned there = there_of(r0);
-      const Rows r2 = rows_of(a, b, t + 2 * kTile);
-      tile(k, v, t, there);
-      if (more) v = C::template request_values<FAR>(a, r1, h, lane);
-      k = next;
-      r0 = r1;
-      r1 = r2;
-    }
+  for (int t = t_begin; t < t_end; t += kTile) {
+    const bool more = t + kTile < t_end;
+    if (more) next = C::template request_keys<FAR>(a, r1, h, lane);
+    const unsigned there = there_of(r0);
+    const Rows r2 = rows_of(a, b, t + 2 * kTile);
+    tile(k, v, t, there);
+    if (more) v = C::template request_values<FAR>(a, r1, h, lane);
+    k = next;
+    r0 = r1;
+    r1 = r2;
   }
+
+  if (share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{item, share.pieces};
 
   // ---- the lane's 32 coordinates of the row (whose numbers are worked out anew: they are not worth registers in the loop)
   int again = m;
   asm volatile("" : "+v"(again));
   const int row_out = row0 + again, qi_out = row_out / rep, qh_out = h * rep + row_out % rep;
   sum = column_sum(sum);
-  float v[32];
-  C::result(o, oz, kRtn ? 24 : c_exp, v);
+  float x[32];
+  C::result(o, oz, kRtn ? 24 : c_exp, x);
   if (share.pieces == 1) {
-    finish<T, NCW>(a, v, sum, h, g, row_out < n_rows, w.first + qi_out, qh_out);
+    finish<T, NCW>(a, x, sum, h, g, row_out < n_rows, w.first + qi_out, qh_out);
   } else if (row_out < n_rows) {
     const int64_t at = ((int64_t)item * a.max_queries + qi_out) * a.q_heads + qh_out;
     float* const part = a.part + at * kGroup;
 #pragma unroll
     for (int r = 0; r < 8; ++r)
-      *reinterpret_cast<f32x4*>(part + C::coordinate(g, 4 * r)) = f32x4{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
+      *reinterpret_cast<f32x4*>(part + C::coordinate(g, 4 * r)) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
     if (g == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
   }
 }
 
 // out of one row from the pieces of its sequence: sum_i 2^(ref_i - top) part_i / sum_i 2^(ref_i - top) sum_i.
-// blockIdx = (query * q_heads + query head, sequence); threads of 32 take a piece, every eighth, 4 coordinates each.
-constexpr int kMergeThreads = 256, kMergeClasses = kMergeThreads / 32;
-template <typename T, bool RTN>
-__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedAttendArgs a) {
-  __shared__ __align__(16) float red[kMergeClasses][kGroup];
-  __shared__ float refs[kMergeClasses], sums[kMergeClasses];
+// blockIdx = (query * q_heads + query head, sequence); threads of 32 take a piece each, 4 coordinates a thread, and go on by as many pieces as there
+// are such groups: 8, or 32 where there are many pieces.  All partial results of a round are requested together, ahead of the sequence's numbers.
+template <typename T, bool RTN, int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendArgs a) {
+  constexpr int kClasses = THREADS / 32, kAhead = 4;
+  __shared__ __align__(16) float red[kClasses][kGroup];
+  __shared__ float refs[kClasses], sums[kClasses];
+  __shared__ __align__(16) float row[kGroup];
   const int b = blockIdx.y, qi = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads, h = qh / (a.q_heads / a.H);
-  const Share share = share_of<false>(a, threadIdx.x & 63, b);
-  if (share.pieces == 1) return;
+  const int2 head = a.heads[b];
+  const int pieces = uniform(head.y);
+  if (pieces == 1) return;
   const PagedQueries w = paged_queries(a, b);
   if (qi >= w.n) return;
   const int k = threadIdx.x >> 5, l = threadIdx.x & 31;
-  const int64_t step = (int64_t)a.max_queries * a.q_heads, at = share.first * step + (int64_t)qi * a.q_heads + qh;
+  const int64_t step = (int64_t)a.max_queries * a.q_heads, at = uniform(head.x) * step + (int64_t)qi * a.q_heads + qh;
   float ref = -3.0e38f, sum = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int i = k; i < share.pieces; i += kMergeClasses) {
-    const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * (at + i * step));
-    const f32x4 p = *reinterpret_cast<const f32x4*>(a.part + (at + i * step) * kGroup + 4 * l);
-    const float top = fmaxf(ref, st.x), keep = __builtin_amdgcn_exp2f(ref - top), by = __builtin_amdgcn_exp2f(st.x - top);
-    x = x * keep + p * by;
-    sum = sum * keep + st.y * by;
+  for (int i0 = k; i0 < pieces; i0 += kAhead * kClasses) {
+    f32x2 st[kAhead];
+    f32x4 p[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u * kClasses;
+      st[u] = f32x2{-3.0e38f, 0.f};
+      p[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (i < pieces) {
+        st[u] = *reinterpret_cast<const f32x2*>(a.stats + 2 * (at + i * step));
+        p[u] = *reinterpret_cast<const f32x4*>(a.part + (at + i * step) * kGroup + 4 * l);
+      }
+    }
+    float top = ref;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, st[u].x);
+    const float keep = __builtin_amdgcn_exp2f(ref - top);
+    x *= keep;
+    sum *= keep;
     ref = top;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const float by = __builtin_amdgcn_exp2f(st[u].x - top);
+      x += p[u] * by;
+      sum += st[u].y * by;
+    }
   }
   *reinterpret_cast<f32x4*>(&red[k][4 * l]) = x;
   if (l == 0) { refs[k] = ref; sums[k] = sum; }
   __syncthreads();
-  if (threadIdx.x >= 4) return;
-  // the row's result on a quad of lanes
-  const int q = threadIdx.x;
-  float top = refs[0];
+  if (threadIdx.x < kGroup) {                              // a thread per coordinate
+    float top = refs[0];
 #pragma unroll
-  for (int i = 1; i < kMergeClasses; ++i) top = fmaxf(top, refs[i]);
-  float v[32] = {};
-  sum = 0.f;
-  for (int i = 0; i < kMergeClasses; ++i) {
-    const float by = __builtin_amdgcn_exp2f(refs[i] - top);
-    sum += sums[i] * by;
-    float p[32];
-    load_f32(&red[i][32 * q], p);
+    for (int i = 1; i < kClasses; ++i) top = fmaxf(top, refs[i]);
+    float total = 0.f, value = 0.f;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) v[r] = __fmaf_rn(p[r], by, v[r]);
+    for (int i = 0; i < kClasses; ++i) {
+      const float by = __builtin_amdgcn_exp2f(refs[i] - top);
+      total += sums[i] * by;
+      value = __fmaf_rn(red[i][threadIdx.x], by, value);
+    }
+    row[threadIdx.x] = value * (total == 0.f ? 0.f : 1.0f / total);
   }
-  float norm = sum == 0.f ? 0.f : 1.0f / sum;
+  __syncthreads();
+  if (threadIdx.x >= 8) return;
+  // the row on eight lanes, as in the stand-alone inverse
+  const int q = group_pos<16>(threadIdx.x);
+  float v[16];
+  load_f32(&row[16 * q], v);
   if constexpr (!RTN) {
-    float sf[32];
+    float sf[16];
     load_signs(a.signs_v, h, q, sf);
-    norm *= kRsqrtG * quad_sign(q);
-    wht128(v, q);
+    const float norm = kRsqrtG * Rot<false>::sign(q);
 #pragma unroll
-    for (int r = 0; r < 32; ++r) v[r] *= sf[r];
+    for (int r = 0; r < 16; ++r) v[r] *= norm;
+    Rot<false>::iwht(v, q);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] *= sf[r];
   }
-#pragma unroll
-  for (int r = 0; r < 32; ++r) v[r] *= norm;
   Storage<T>::template store<false>(static_cast<T*>(a.out) + ((w.first + qi) * a.q_heads + qh) * kGroup, q, v);
 }
 
 // How a launch is laid out, from sizes alone (lengths are on the device).
-struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles; int64_t items; bool merge; };
+struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles; int64_t items; bool merge, many; };
 constexpr int kMinTiles = 2;                               // a piece of fewer tokens costs more than it saves
 template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
   PagedPlan p;
@@ -246,6 +275,7 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
   p.items = std::min(batch * each, std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
   p.blocks = (unsigned)((p.items * H + Shape<T, NCW>::kWaves - 1) / Shape<T, NCW>::kWaves);
   p.merge = each > 1;
+  p.many = p.items > 64 * batch;
   return p;
 }
 
@@ -273,7 +303,7 @@ static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a) {
 
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a) {
   const PagedPlan p = plan_of(dtype, n_codewords, a);
-  return p.merge ? (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) : 0;
+  return (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2);
 }
 
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& args, void* workspace, hipStream_t stream) {
@@ -283,6 +313,7 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   a.min_tiles = plan.min_tiles;
   a.part = static_cast<float*>(workspace);
   a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
+  a.heads = reinterpret_cast<int2*>(a.stats + plan.items * a.max_queries * a.q_heads * 2);
   a.page_groups = a.pool.page_tokens / 8;
   a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
   const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
@@ -293,13 +324,12 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   if (!plan.merge) return hipSuccess;
   const dim3 grid((unsigned)(a.max_queries * a.q_heads), (unsigned)a.batch);
   const bool rtn = is_rtn(n_codewords);
-  if (dtype == kBF16) {
-    if (rtn) paged_merge_kernel<bf16_t, true><<<grid, kMergeThreads, 0, stream>>>(a);
-    else paged_merge_kernel<bf16_t, false><<<grid, kMergeThreads, 0, stream>>>(a);
-  } else {
-    if (rtn) paged_merge_kernel<float, true><<<grid, kMergeThreads, 0, stream>>>(a);
-    else paged_merge_kernel<float, false><<<grid, kMergeThreads, 0, stream>>>(a);
-  }
+#define AQUAKV_MERGE(T, RTN)                                                                                  \
+  (plan.many ? paged_merge_kernel<T, RTN, 1024><<<grid, 1024, 0, stream>>>(a)                                  \
+             : paged_merge_kernel<T, RTN, 256><<<grid, 256, 0, stream>>>(a))
+  if (dtype == kBF16) { if (rtn) AQUAKV_MERGE(bf16_t, true); else AQUAKV_MERGE(bf16_t, false); }
+  else { if (rtn) AQUAKV_MERGE(float, true); else AQUAKV_MERGE(float, false); }
+#undef AQUAKV_MERGE
   return hipGetLastError();
 }
 
