@@ -148,6 +148,21 @@ __device__ __forceinline__ void wht_columns(float (&v)[32]) {
   wht_swap_stage<32>(v);
 }
 
+// The same transform of bf16 numbers (b[s]: values 8 s ... of the lane's 32) on the matrix cores, added to x: 32 instructions where the butterflies are 450,
+// which a wave that has little else to do runs once, from a cold instruction cache.  H = +-1 is made from the lane's number: row m of product R is
+// coordinate 32 (m / 4) + 4 R + m % 4, so that a lane ends with the coordinates it came with.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ void hadamard_columns(const bf16x8 (&b)[4], f32x4 (&x)[8], int lane) {
+  const uint32_t m = lane & 15, g = lane >> 4, flip = 0x80008000u;
+  const uint32_t p = 0x3f803f80u ^ ((m & 1) << 31) ^ ((__builtin_popcount((m >> 2) & g) & 1) ? flip : 0u), q = p ^ ((m & 2) ? flip : 0u);
+  const u32x4 rows[4] = {{p, q, p, q}, {p, q, p ^ flip, q ^ flip}, {p ^ flip, q ^ flip, p ^ flip, q ^ flip}, {p ^ flip, q ^ flip, p, q}};
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int R = 0; R < 8; ++R)
+      x[R] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows[(R & 1) + 2 * (__builtin_popcount((R >> 1) & s) & 1)]), b[s], x[R], 0, 0, 0);
+}
+
 __device__ __forceinline__ uint32_t f16_pair(float x, float y) {
   const f16x2 h = {(_Float16)x, (_Float16)y};
   return __builtin_bit_cast(uint32_t, h);
@@ -231,8 +246,26 @@ template <int NCW, int TERMS> struct Codes {
     }
     return q;
   }
-  // (grids: with the signs)
-  template <typename T> static __device__ __forceinline__ void unpack_query(const Query<T>& q, float (&v)[32]) {
+  // ... rotated (grids; without the factor 1 / sqrt(128))
+  static __device__ __forceinline__ uint32_t sign_bit(const u32x4 (&signs)[kRtn ? 1 : 2], int r) {      // bit 31: the sign of coordinate r of the lane's
+    return (signs[r >> 4][(r >> 2) & 3] << (24 - 8 * (r & 3))) & 0x80000000u;
+  }
+  template <typename T> static __device__ __forceinline__ void rotate_query(const Query<T>& q, int lane, float (&v)[32]) {
+    if constexpr (sizeof(T) == 2 && !kRtn) {
+      bf16x8 b[4];
+      f32x4 x[8] = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u32x4 w = q.w[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] ^= sign_bit(q.signs, 8 * i + 2 * k) >> 16 | sign_bit(q.signs, 8 * i + 2 * k + 1);
+        b[i] = __builtin_bit_cast(bf16x8, w);
+      }
+      hadamard_columns(b, x, lane);
+#pragma unroll
+      for (int r = 0; r < 32; ++r) v[r] = x[r >> 2][r & 3];
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
       if constexpr (sizeof(T) == 2) {
@@ -244,7 +277,8 @@ template <int NCW, int TERMS> struct Codes {
     }
     if constexpr (!kRtn) {
 #pragma unroll
-      for (int r = 0; r < 32; ++r) v[r] = __uint_as_float(__float_as_uint(v[r]) ^ ((q.signs[r >> 4][(r >> 2) & 3] << (24 - 8 * (r & 3))) & 0x80000000u));
+      for (int r = 0; r < 32; ++r) v[r] = __uint_as_float(__float_as_uint(v[r]) ^ sign_bit(q.signs, r));
+      wht_columns(v);
     }
   }
   static __device__ __forceinline__ void pack_query(const float (&v)[32], f16x8 (&q)[TERMS][4], float (&qsum)[2]) {
@@ -554,17 +588,34 @@ template <int NCW, int TERMS> struct Codes {
 };
 
 // The lane's 32 coordinates of a row's result -> out.
-template <typename T, int NCW> __device__ __forceinline__ void finish(const PagedAttendArgs& a, float (&v)[32], float sum, int h, int g,
+template <typename T, int NCW> __device__ __forceinline__ void finish(const PagedAttendArgs& a, float (&v)[32], float sum, int h, int lane,
                                                                       bool there, int64_t row, int qh) {
   constexpr bool kRtn = is_rtn(NCW);
   float by = sum == 0.f ? 0.f : 1.0f / sum;                // (no token: 0)
   if constexpr (!kRtn) by *= kRsqrtG;
 #pragma unroll
   for (int r = 0; r < 32; ++r) v[r] *= by;
+  if constexpr (!kRtn && sizeof(T) == 2) {                 // (as two bf16 numbers: 2^-17 of a value, far below the rounding of the result)
+    f32x4 x[8] = {};
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      bf16x8 b[4];
+#pragma unroll
+      for (int r = 0; r < 32; ++r) {
+        const bf16_t part = static_cast<bf16_t>(v[r]);
+        b[r >> 3][r & 7] = part;
+        v[r] -= static_cast<float>(part);
+      }
+      hadamard_columns(b, x, lane);
+    }
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] = x[r >> 2][r & 3];
+  } else if constexpr (!kRtn) {
+    wht_columns(v);
+  }
   if constexpr (!kRtn) {
     float sf[32];
-    load_signs(a.signs_v, h, g, sf);
-    wht_columns(v);
+    load_signs(a.signs_v, h, lane >> 4, sf);
 #pragma unroll
     for (int r = 0; r < 32; ++r) v[r] *= sf[r];
   }
@@ -572,7 +623,7 @@ template <typename T, int NCW> __device__ __forceinline__ void finish(const Page
   T* const out = static_cast<T*>(a.out) + (row * a.q_heads + qh) * kGroup;
 #pragma unroll
   for (int r = 0; r < 32; r += 4) {
-    T* const at = out + Codes<NCW, 1>::coordinate(g, r);
+    T* const at = out + Codes<NCW, 1>::coordinate(lane >> 4, r);
     if constexpr (sizeof(T) == 2) {
       *reinterpret_cast<u32x2*>(at) = u32x2{Storage<T>::pack2(v[r], v[r + 1]), Storage<T>::pack2(v[r + 2], v[r + 3])};
     } else {

@@ -77,16 +77,16 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
   float f;                                                 // score in powers of two = f * sigma * sum
   {
     float x[32];
-    C::template unpack_query<T>(asked, x);
-    if constexpr (!kRtn) wht_columns(x);
+    C::template rotate_query<T>(asked, lane, x);
     const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
     float top = 0.f;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) { x[r] *= by; top = fmaxf(top, fabsf(x[r])); }
-    const int e = max(__builtin_amdgcn_frexp_expf(column_max(top)), -100);
+    for (int r = 0; r < 32; ++r) top = fmaxf(top, fabsf(x[r]));
+    const int e = max(__builtin_amdgcn_frexp_expf(column_max(top) * fabsf(by)), -100);
     f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? 24 : c_exp), 126));
+    const float scaled = __builtin_ldexpf(by, kQueryExp - e);
 #pragma unroll
-    for (int r = 0; r < 32; ++r) x[r] = __builtin_ldexpf(x[r], kQueryExp - e);
+    for (int r = 0; r < 32; ++r) x[r] *= scaled;
     C::pack_query(x, q, qsum);
   }
 
@@ -162,21 +162,21 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
   if (share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{item, share.pieces};
 
   // ---- the lane's 32 coordinates of the row (whose numbers are worked out anew: they are not worth registers in the loop)
-  int again = m;
+  int again = lane;
   asm volatile("" : "+v"(again));
-  const int row_out = row0 + again, qi_out = row_out / rep, qh_out = h * rep + row_out % rep;
+  const int row_out = row0 + (again & 15), qi_out = row_out / rep, qh_out = h * rep + row_out % rep;
   sum = column_sum(sum);
   float x[32];
   C::result(o, oz, kRtn ? 24 : c_exp, x);
   if (share.pieces == 1) {
-    finish<T, NCW>(a, x, sum, h, g, row_out < n_rows, w.first + qi_out, qh_out);
+    finish<T, NCW>(a, x, sum, h, again, row_out < n_rows, w.first + qi_out, qh_out);
   } else if (row_out < n_rows) {
     const int64_t at = ((int64_t)item * a.max_queries + qi_out) * a.q_heads + qh_out;
     float* const part = a.part + at * kGroup;
 #pragma unroll
     for (int r = 0; r < 8; ++r)
-      *reinterpret_cast<f32x4*>(part + C::coordinate(g, 4 * r)) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
-    if (g == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
+      *reinterpret_cast<f32x4*>(part + C::coordinate(again >> 4, 4 * r)) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+    if (again < 16) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
   }
 }
 
