@@ -159,7 +159,7 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
     r1 = r2;
   }
 
-  if (share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{item, share.pieces};
+  if (a.heads != nullptr && share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{item, share.pieces};
 
   // ---- the lane's 32 coordinates of the row (whose numbers are worked out anew: they are not worth registers in the loop)
   int again = lane;
@@ -262,15 +262,24 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendA
 }
 
 // How a launch is laid out, from sizes alone (lengths are on the device).
-struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles; int64_t items; bool merge, many; };
+struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles, waves, row_blocks; int64_t items; bool merge, many; };
 constexpr int kMinTiles = 2;                               // a piece of fewer tokens costs more than it saves
+constexpr int kFewRows = 64;                               // rows of a kv head that waves of 16 rows take one after the other (bf16)
 template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
-  PagedPlan p;
-  p.row_tiles = (unsigned)((max_queries * (q_heads / H) + 15) / 16);
+  PagedPlan p = {};
+  const int64_t rows = max_queries * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
+  if (sizeof(T) == 2 && rows > kFewRows) {                 // workgroups of 128 or 256 rows, one a CU: the tokens in pieces if there are too few of them
+    p.waves = rows > 128 ? 8 : 4;
+    p.row_blocks = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+    p.slots = (int)std::max<int64_t>(std::min(256 / std::max<int64_t>(batch * H * p.row_blocks, 1), most / 8), 1);
+    p.items = batch * p.slots;
+    p.merge = p.slots > 1;
+    return p;
+  }
+  p.row_tiles = (unsigned)((rows + 15) / 16);
   p.min_tiles = kMinTiles;
   // as many pieces as make all waves that the chip holds
   p.slots = (int)std::max<int64_t>(Shape<T, NCW>::kSlots / (H * p.row_tiles), 1);
-  const int64_t most = (table_pages * page_tokens + kTile - 1) / kTile;                       // tiles of a sequence
   const int64_t each = std::max<int64_t>((most + kMinTiles - 1) / kMinTiles, 1);
   p.items = std::min(batch * each, std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
   p.blocks = (unsigned)((p.items * H + Shape<T, NCW>::kWaves - 1) / Shape<T, NCW>::kWaves);
@@ -303,6 +312,7 @@ static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a) {
 
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a) {
   const PagedPlan p = plan_of(dtype, n_codewords, a);
+  if (!p.merge) return 0;
   return (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2);
 }
 
@@ -311,16 +321,21 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   const PagedPlan plan = plan_of(dtype, n_codewords, a);
   a.slots = plan.slots;
   a.min_tiles = plan.min_tiles;
+  a.row_blocks = plan.row_blocks;
   a.part = static_cast<float*>(workspace);
   a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
-  a.heads = reinterpret_cast<int2*>(a.stats + plan.items * a.max_queries * a.q_heads * 2);
+  a.heads = plan.merge ? reinterpret_cast<int2*>(a.stats + plan.items * a.max_queries * a.q_heads * 2) : nullptr;
   a.page_groups = a.pool.page_tokens / 8;
   a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
-  const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
-  const dim3 blocks(plan.blocks, plan.row_tiles);
-  AQUAKV_PAGED(dtype, n_codewords, (far ? paged_attend_kernel<T, N, true><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)
-                                        : paged_attend_kernel<T, N, false><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)));
-  if (const hipError_t e = hipGetLastError()) return e;
+  if (plan.waves != 0) {
+    if (const hipError_t e = launch_paged_tiles(n_codewords, plan.waves, a, stream)) return e;
+  } else {
+    const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
+    const dim3 blocks(plan.blocks, plan.row_tiles);
+    AQUAKV_PAGED(dtype, n_codewords, (far ? paged_attend_kernel<T, N, true><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)
+                                          : paged_attend_kernel<T, N, false><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)));
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
   if (!plan.merge) return hipSuccess;
   const dim3 grid((unsigned)(a.max_queries * a.q_heads), (unsigned)a.batch);
   const bool rtn = is_rtn(n_codewords);

@@ -1,0 +1,402 @@
+// Attention of many queries over pages of codes (a chunk of a prompt behind what is cached): bf16 layers.
+//
+// A workgroup of 4 or 8 waves takes 32 rows (query x query head) a wave of one kv head and walks the tokens in tiles of 64.  The waves turn a tile's
+// codes into fp16 once, for all of them, keys [token][coordinate] and values [coordinate][token] in LDS (two buffers: the next tile is
+// written while this one is multiplied), and multiply with 32x32x16 matrix instructions: S^T = K Q^T, O^T += V^T P.  As in paged_attend.hip the lane
+// that gets scores holds them as the second product wants its operand: V's columns are in that order.
+#include "paged_attend.h"
+
+#include <algorithm>
+
+namespace aquakv {
+namespace paged {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr int kTokens = 64;                                // of a tile
+constexpr int kKeyBytes = kTokens * kGroup * 2, kBufferBytes = 2 * kKeyBytes + 2 * kTokens * 4;      // keys, values, scales of both
+
+// Coordinate (of 128) that row i of a 32-row operand R stands for, so that register n of lanes 32 hf ... of product R is coordinate
+// 16 (2 R + n / 8) + 8 hf + n % 8: what such a lane holds of a vector as the other operand.  (Swaps bits 2 and 3.)
+__device__ __forceinline__ int swapped(int d) { return (d & ~12) | (d & 4) << 1 | (d & 8) >> 1; }
+
+// LDS places: 16-byte pieces of a row are shuffled so that the lanes that read one piece of 16 rows (keys), or of 8 pairs of rows (values), use
+// different banks.
+__device__ __forceinline__ uint32_t key_place(int token, int piece) { return 256 * token + 16 * (piece ^ (token & 15)); }
+__device__ __forceinline__ uint32_t value_place(int row, int piece) { return 128 * row + 16 * (piece ^ ((row >> 1) & 7)); }
+
+// x += H b, columns of 128 bf16 numbers on two lanes (b[s]: coordinates 16 s + 8 hf ...)
+__device__ __forceinline__ void hadamard_pairs(const bf16x8 (&b)[8], f32x16 (&x)[4], int lane) {
+  const uint32_t r = lane & 31, hf = lane >> 5, flip = 0x80008000u;
+  const uint32_t p = 0x3f803f80u ^ ((r & 1) << 31) ^ (((r >> 2) & hf) ? flip : 0u), q = p ^ ((r & 2) ? flip : 0u);
+  const uint32_t p2 = p ^ ((r & 8) ? flip : 0u), q2 = q ^ ((r & 8) ? flip : 0u), odd = (r & 16) ? flip : 0u;
+  const u32x4 even = {p, q, p2, q2}, row[4] = {even, even ^ odd, even ^ flip, even ^ odd ^ flip};
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int R = 0; R < 4; ++R)
+      x[R] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, row[(s & 1) + 2 * (__builtin_popcount((s >> 1) & R) & 1)]), b[s], x[R], 0, 0, 0);
+}
+__device__ __forceinline__ float pair_max(float x) {       // over lanes l, l ^ 32
+  float y = x;
+  swap_lanes<32>(x, y);
+  return fmaxf(x, y);
+}
+
+// ---------------------------------------------------------------- codes of a tile
+// Wave `part` of the eight that a tile is shared out to: keys of tokens 8 part ... (a lane: 16 coordinates of a token), values of the eight tokens
+// that operand piece `part` holds, 16 (part / 2) + 4 (part % 2) + {0 ... 3, 8 ... 11} (a lane: 2 coordinates).
+template <int NCW> struct TileCodes {
+  typedef Codes<NCW, 1> C;
+  static constexpr bool kRtn = C::kRtn;
+  static constexpr int c = C::c, kRow = C::kRow;
+  u32x2 k;
+  uint32_t v[8];
+  u32x2 ks;                                                // the lane's token's scale word(s)
+  uint32_t vs[kRtn ? 8 : 1];                               // grids: scale of token lane % 8 of the piece; uniform: of each, the lane's half
+  int there[2];                                            // uniform: so many of the piece's first, second four tokens are there (the others hold anything)
+  static __device__ __forceinline__ int value_token(int part, int e) { return 16 * (part >> 1) + 4 * (part & 1) + (e & 3) + 8 * (e >> 2); }
+
+  __device__ __forceinline__ void request(const PagedAttendArgs& a, int b, int len, int h, int t, int part, int lane) {
+    const uint32_t row_bytes = (uint32_t)a.H * kRow;
+    const uint64_t key_row = (uint64_t)max(group_row(a, b, t / 8 + part), 0);
+    const int group[2] = {group_row(a, b, t / 8 + (part & ~1)), group_row(a, b, t / 8 + (part | 1))};
+    const uint64_t value_row[2] = {(uint64_t)max(group[0], 0) + 4 * (part & 1), (uint64_t)max(group[1], 0) + 4 * (part & 1)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) there[i] = group[i] < 0 ? 0 : len - (t + value_token(part, 4 * i));
+    const uint8_t* const kp = a.pool.k_codes + (key_row * row_bytes + h * kRow) + (uint32_t)(lane >> 3) * row_bytes;
+    if constexpr (c == 8) {
+      k = *reinterpret_cast<const u32x2*>(kp + 8 * (lane & 7));
+    } else if constexpr (c == 4) {
+      k = u32x2{*reinterpret_cast<const uint32_t*>(kp + 4 * (lane & 7)), 0};
+    } else {                                               // 6 bytes, from the second pieces on with the 2 before them
+      __builtin_memcpy(&k, kp + max(6 * (lane & 7) - 2, 0), 8);
+    }
+    const uint64_t key_group = (key_row + (lane >> 3)) * a.H + h;
+    if constexpr (kRtn) ks = reinterpret_cast<const u32x2*>(a.pool.k_scales)[key_group];
+    else ks = u32x2{a.pool.k_scales[key_group], 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint64_t row = value_row[e >> 2] + (e & 3);
+      const uint8_t* const vp = a.pool.v_codes + (row * row_bytes + h * kRow);
+      if constexpr (c == 8) {
+        v[e] = vp[lane];
+      } else if constexpr (c == 4) {
+        v[e] = vp[lane >> 1];
+      } else {
+        uint16_t two;
+        __builtin_memcpy(&two, vp + min((6 * lane) >> 3, 46), 2);
+        v[e] = two;
+      }
+      if constexpr (kRtn) vs[e] = reinterpret_cast<const uint32_t*>(a.pool.v_scales)[(row * a.H + h) * 2 + (lane >> 5)];
+    }
+    if constexpr (!kRtn) vs[0] = a.pool.v_scales[((lane & 4 ? value_row[1] : value_row[0]) + (lane & 3)) * a.H + h];
+  }
+  static __device__ __forceinline__ int group_row(const PagedAttendArgs& a, int b, uint32_t group) {
+    uint32_t page = (uint32_t)(((uint64_t)group * a.page_magic) >> 32), in = group - page * a.page_groups;
+    if (in >= a.page_groups) { ++page; in -= a.page_groups; }
+    const int at = page < (uint32_t)a.table_pages ? const_ints(a.page_table)[(int64_t)b * a.table_pages + page] : -1;
+    return (uint32_t)at < (uint32_t)a.pool.n_pages ? at * a.pool.page_tokens + (int)in * 8 : -1;
+  }
+
+  // a lane's keys and values to the buffer
+  __device__ __forceinline__ void store(const unsigned char* table, unsigned char* buffer, int part, int lane) const {
+    unsigned char* const values = buffer + kKeyBytes;
+    float* const scales = reinterpret_cast<float*>(buffer + 2 * kKeyBytes);
+    const int token = 8 * part + (lane >> 3), piece = 2 * (lane & 7);
+    u32x4 out[2];
+    if constexpr (kRtn) {
+      const bool upper = (lane & 7) >= 4;
+      const float s0 = half_bits_to_float((uint16_t)ks.x), s1 = half_bits_to_float((uint16_t)ks.y);
+      const int e = exponent(s0, s1);
+      const float step = __builtin_ldexpf(upper ? s1 : s0, -e);
+      const float zero = (float)((upper ? ks.y : ks.x) >> 16);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t w = NCW == kRtn4 ? (i < 4 ? k.x : k.y) >> (8 * (i & 3)) : k.x >> (4 * i);
+        const uint32_t low = w & ((1u << NCW) - 1u), high = (w >> NCW) & ((1u << NCW) - 1u);
+        out[i >> 2][i & 3] = f16_pair(((float)low - zero) * step, ((float)high - zero) * step);
+      }
+      if ((lane & 7) == 0) scales[token] = __builtin_ldexpf(1.0f, e);
+    } else {
+      const uint32_t at = C::lane_copy(lane);
+      const uint32_t w[2] = {c == 6 ? ((lane & 7) ? __builtin_amdgcn_alignbit(k.y, k.x, 16) : k.x) : k.x, c == 6 ? ((lane & 7) ? k.y >> 16 : k.y) : k.y};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[i >> 2][i & 3] = C::point(table, C::offset(w, i, at));
+      if ((lane & 7) == 0) scales[token] = half_bits_to_float((uint16_t)ks.x);
+    }
+    *reinterpret_cast<u32x4*>(buffer + key_place(token, piece)) = out[0];
+    *reinterpret_cast<u32x4*>(buffer + key_place(token, piece + 1)) = out[1];
+    // values: coordinates 2 lane, 2 lane + 1 of the piece's eight tokens
+    uint32_t d[8];
+    if constexpr (kRtn) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t word = (e & 3) < there[e >> 2] ? vs[e] : 0u;
+        const float mine = half_bits_to_float((uint16_t)word), other = __shfl_xor(mine, 32);
+        const int x = exponent(mine, other);
+        const float step = __builtin_ldexpf(mine, -x), zero = (float)(word >> 16);
+        const uint32_t w = NCW == kRtn4 ? v[e] : v[e] >> (4 * (lane & 1));
+        const uint32_t low = w & ((1u << NCW) - 1u), high = (w >> NCW) & ((1u << NCW) - 1u);
+        d[e] = f16_pair(((float)low - zero) * step, ((float)high - zero) * step);
+        if (lane == 0) scales[kTokens + value_token(part, e)] = __builtin_ldexpf(1.0f, x);
+      }
+    } else {
+      const uint32_t at = C::lane_copy(lane);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t code = c == 8 ? v[e] : c == 4 ? (v[e] >> (4 * (lane & 1))) & 15u : (v[e] >> (6 * lane - 8 * min((6 * lane) >> 3, 46))) & 63u;
+        d[e] = C::point(table, code << 8 | at);
+      }
+      if (lane < 8) scales[kTokens + value_token(part, lane)] = half_bits_to_float((uint16_t)vs[0]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t pick = i == 0 ? 0x05040100u : 0x07060302u;
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_perm(d[2 * e + 1], d[2 * e], pick);
+      *reinterpret_cast<u32x4*>(values + value_place(swapped(2 * lane + i), part)) = x;
+    }
+  }
+  // power of two behind which a token's two steps are held (so that products with codes stay in fp16's range)
+  static __device__ __forceinline__ int exponent(float s0, float s1) { return __builtin_amdgcn_frexp_expf(fmaxf(s0, s1)); }
+};
+
+// ---------------------------------------------------------------- the kernel
+template <int NCW, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVES / 4, WAVES / 4))) void paged_tiles_kernel(const PagedAttendArgs a) {
+  typedef Codes<NCW, 1> C;
+  constexpr bool kRtn = C::kRtn;
+  constexpr int kParts = 8 / WAVES;                        // shares of a tile's codes that a wave converts
+  __shared__ __align__(256) unsigned char lds[C::kTableBytes + 2 * kBufferBytes];
+  unsigned char* const buffers = lds + C::kTableBytes;
+  const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = uniform(threadIdx.x >> 6);
+  const typename C::Points points = C::request_points(a.codebook, lane);
+  // blockIdx: (piece, block of rows: the last ones, which see most tokens, first; kv head), sequence
+  const int h = blockIdx.x % a.H, piece = (blockIdx.x / a.H) % a.slots, block = a.row_blocks - 1 - blockIdx.x / a.H / a.slots, b = blockIdx.y;
+  const PagedQueries w = paged_queries(a, b);
+  const int rep = a.q_heads / a.H, n_rows = w.n * rep, row0 = block * 32 * WAVES;
+  if (row0 >= n_rows) return;
+  const int row = row0 + 32 * wave + col, qi = row / rep, qh = h * rep + row % rep;
+  const bool row_there = row < n_rows;
+  const int limit = row_there ? w.len - w.count + qi : -1;
+  const int wave_first = uniform(w.len - w.count + min(row0 + 32 * wave, n_rows - 1) / rep);      // smallest limit of the wave's rows
+  const int last_limit = uniform(w.len - w.count + min(row0 + 32 * WAVES - 1, n_rows - 1) / rep);
+  const int tiles = (last_limit + kTokens) / kTokens;      // (last_limit >= -len: 0 tiles where nothing is seen)
+  const int each = (max(tiles, 0) + a.slots - 1) / a.slots;
+  const int t_begin = piece * each * kTokens, t_end = min(t_begin + each * kTokens, last_limit + 1);
+
+  TileCodes<NCW> codes[kParts];
+  const auto request = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) codes[i].request(a, b, w.len, h, t, kParts * wave + i, lane);
+  };
+  const auto store = [&](int n) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) codes[i].store(lds, buffers + n * kBufferBytes, kParts * wave + i, lane);
+  };
+  if (t_begin < t_end) request(t_begin);
+  const int c_exp = C::template stage<WAVES>(points, lds, lane, wave);
+
+  // ---- the rows' queries
+  f16x8 q[8];
+  float f;
+  {
+    const bf16_t* const src = static_cast<const bf16_t*>(a.q) + (w.first + (row_there ? qi : 0)) * a.q_stride + (row_there ? qh : h * rep) * kGroup + 8 * hf;
+    float x[64];
+    u32x4 raw[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) raw[s] = *reinterpret_cast<const u32x4*>(src + 16 * s);
+    if constexpr (!kRtn) {
+      bf16x8 bq[8];
+      const int8_t* const signs = a.signs_k + h * kGroup + 8 * hf;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const u32x2 sg = *reinterpret_cast<const u32x2*>(signs + 16 * s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t two = i < 2 ? sg.x >> (16 * i) : sg.y >> (16 * (i - 2));
+          raw[s][i] ^= (two << 8 & 0x8000u) | (two << 16 & 0x80000000u);
+        }
+        bq[s] = __builtin_bit_cast(bf16x8, raw[s]);
+      }
+      f32x16 y[4] = {};
+      hadamard_pairs(bq, y, lane);
+#pragma unroll
+      for (int r = 0; r < 64; ++r) x[r] = y[r >> 4][r & 15];
+    } else {
+#pragma unroll
+      for (int s = 0; s < 8; ++s) unpack_bf16x8(raw[s], &x[8 * s]);
+    }
+    const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
+    float top = 0.f;
+#pragma unroll
+    for (int r = 0; r < 64; ++r) top = fmaxf(top, fabsf(x[r]));
+    const int e = max(__builtin_amdgcn_frexp_expf(pair_max(top) * fabsf(by)), -100);
+    f = __builtin_ldexpf(1.0f, min(e - kQueryExp + c_exp, 126));
+    const float scaled = __builtin_ldexpf(by, kQueryExp - e);
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[s][i] = (_Float16)(x[8 * s + i] * scaled);
+  }
+  __syncthreads();                                         // the grid's copies are there
+  f32x16 o[4] = {};
+  float ref = -3.0e38f, sum = 0.f;
+  if (t_begin < t_end) store(0);
+  __syncthreads();
+  if (t_begin + kTokens < t_end) request(t_begin + kTokens);
+  int n = 0;
+#pragma unroll 1
+  for (int t = t_begin; t < t_end; t += kTokens, n ^= 1) {
+    const unsigned char* const buffer = buffers + n * kBufferBytes;
+    const float* const scales = reinterpret_cast<const float*>(buffer + 2 * kKeyBytes);
+    unsigned there = 0;                                    // groups of 8 tokens whose page is in the pool
+#pragma unroll
+    for (int j = 0; j < 8; ++j) there |= (unsigned)(TileCodes<NCW>::group_row(a, b, t / 8 + j) >= 0) << j;
+    const bool masked = t + kTokens - 1 > wave_first || there != 255u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                          // 32 tokens each
+      f32x16 s = {};
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(buffer + key_place(32 * i + col, 2 * k + hf)), q[k], s, 0, 0, 0);
+      // the next tile's codes to the other buffer
+      if (i == 0 && t + kTokens < t_end) {
+        store(n ^ 1);
+        if (t + 2 * kTokens < t_end) request(t + 2 * kTokens);
+      }
+      // register 4 j + e is token 32 i + 8 j + 4 hf + e
+      f32x4 sv[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 sk = *reinterpret_cast<const f32x4*>(scales + 32 * i + 8 * j + 4 * hf);
+        sv[j] = *reinterpret_cast<const f32x4*>(scales + kTokens + 32 * i + 8 * j + 4 * hf);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * j + e] *= sk[e];
+      }
+      if (masked) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int seen = (there >> (4 * i + j)) & 1 ? limit + 1 - (t + 32 * i + 8 * j + 4 * hf) : 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[4 * j + e] = e < seen ? s[4 * j + e] : -INFINITY;
+            sv[j][e] = e < seen ? sv[j][e] : 0.f;
+          }
+        }
+      }
+      float p[16];
+      const auto weigh = [&] {
+        float top = 0.f, big = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], f, -ref));
+          top = fmaxf(top, p[r] * sv[r >> 2][r & 3]);
+          big = fmaxf(big, p[r]);
+        }
+        return __builtin_amdgcn_ballot_w64(top > kTopWeight || big > 0x1p60f) != 0;
+      };
+      if (weigh()) {
+        float top = -3.0e38f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r] * f + __builtin_amdgcn_logf(fmaxf(sv[r >> 2][r & 3], 0x1p-24f)));
+        const float moved = fmaxf(ref, pair_max(top) - kStartExp);
+        const float by = __builtin_amdgcn_exp2f(ref - moved);
+        ref = moved;
+        sum *= by;
+#pragma unroll
+        for (int R = 0; R < 4; ++R) o[R] *= by;
+        weigh();
+      }
+      const unsigned char* const values = buffer + kKeyBytes;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {                        // 16 tokens each
+        f16x8 weight;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sum += p[8 * k + e];
+          weight[e] = (_Float16)(p[8 * k + e] * sv[2 * k + (e >> 2)][e & 3]);
+        }
+#pragma unroll
+        for (int R = 0; R < 4; ++R)
+          o[R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(values + value_place(32 * R + col, 4 * i + 2 * k + hf)), weight, o[R], 0,
+                                                        0, 0);
+      }
+    }
+    __syncthreads();
+  }
+
+  // ---- results: register n of product R is coordinate 16 (2 R + n / 8) + 8 hf + n % 8
+  sum = far_sum<32>(sum);
+  if (a.slots > 1) {
+    if (block == 0 && h == 0 && piece == 0 && threadIdx.x == 0) a.heads[b] = int2{b * a.slots, a.slots};
+    if (!row_there) return;
+    const int64_t at = ((int64_t)(b * a.slots + piece) * a.max_queries + qi) * a.q_heads + qh;
+    float* const part = a.part + at * kGroup + 8 * hf;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_ldexpf(o[r >> 2][4 * (r & 3) + e], c_exp);
+      *reinterpret_cast<f32x4*>(part + 16 * (r >> 1) + 4 * (r & 1)) = x;
+    }
+    if (hf == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
+    return;
+  }
+  const float by = sum == 0.f ? 0.f : __builtin_ldexpf((kRtn ? 1.0f : kRsqrtG) / sum, c_exp);
+#pragma unroll
+  for (int R = 0; R < 4; ++R) o[R] *= by;
+  if constexpr (!kRtn) {
+    f32x16 y[4] = {};
+#pragma unroll
+    for (int term = 0; term < 2; ++term) {
+      bf16x8 bo[8];
+#pragma unroll
+      for (int r = 0; r < 64; ++r) {
+        const bf16_t part = static_cast<bf16_t>(o[r >> 4][r & 15]);
+        bo[r >> 3][r & 7] = part;
+        o[r >> 4][r & 15] -= static_cast<float>(part);
+      }
+      hadamard_pairs(bo, y, lane);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const u32x2 sg = *reinterpret_cast<const u32x2*>(a.signs_v + h * kGroup + 16 * s + 8 * hf);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        o[s >> 1][8 * (s & 1) + i] = __uint_as_float(__float_as_uint(y[s >> 1][8 * (s & 1) + i]) ^ ((i < 4 ? sg.x : sg.y) << (24 - 8 * (i & 3)) & 0x80000000u));
+    }
+  }
+  if (!row_there) return;
+  bf16_t* const out = static_cast<bf16_t*>(a.out) + ((w.first + qi) * a.q_heads + qh) * kGroup + 8 * hf;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    u32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = Storage<bf16_t>::pack2(o[s >> 1][8 * (s & 1) + 2 * i], o[s >> 1][8 * (s & 1) + 2 * i + 1]);
+    *reinterpret_cast<u32x4*>(out + 16 * s) = x;
+  }
+}
+
+}  // namespace
+}  // namespace paged
+
+hipError_t launch_paged_tiles(int n_codewords, int waves, const PagedAttendArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.H * a.slots * a.row_blocks), (unsigned)a.batch);
+#define AQUAKV_TILES(NCW)                                                                              \
+  (waves == 8 ? paged::paged_tiles_kernel<NCW, 8><<<grid, 512, 0, stream>>>(a)                         \
+              : paged::paged_tiles_kernel<NCW, 4><<<grid, 256, 0, stream>>>(a))
+  switch (n_codewords) {
+    case kRtn2: AQUAKV_TILES(kRtn2); break;
+    case kRtn4: AQUAKV_TILES(kRtn4); break;
+    case 16: AQUAKV_TILES(16); break;
+    case 64: AQUAKV_TILES(64); break;
+    default: AQUAKV_TILES(256);
+  }
+#undef AQUAKV_TILES
+  return hipGetLastError();
+}
+
+}  // namespace aquakv

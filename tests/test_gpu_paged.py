@@ -146,7 +146,7 @@ def attend(lg, pages, table, lens, q, counts, scale=SCALE, q_start=None, max_que
     ("bf16", 8, 32, [1], 16, 1), ("bf16", 2, 8, [31, 32, 33, 64, 65, 127], 8, 1), ("bf16", 1, 1, [700], 64, 1),
     ("bf16", 8, 64, [300, 1500, 5], 24, 1), ("bf16", 3, 15, [200, 90], 40, 1), ("bf16", 4, 16, [100, 17, 258], 16, 4),
     ("bf16", 2, 6, [130, 67], 8, 7), ("bf16", 1, 8, [530], 128, 40), ("bf16", 2, 8, [513, 300], 32, 97),
-    ("bf16", 1, 24, [60, 90], 16, 2), ("fp32", 2, 8, [1, 33, 150, 700], 16, 1), ("fp32", 3, 9, [260], 24, 5), ("fp32", 1, 4, [300], 32, 70)])
+    ("bf16", 1, 24, [60, 90], 16, 2), ("bf16", 2, 8, [1300, 25, 411], 8, 25), ("bf16", 8, 32, [640], 64, 80), ("bf16", 1, 4, [260], 24, 260), ("fp32", 2, 8, [1, 33, 150, 700], 16, 1), ("fp32", 3, 9, [260], 24, 5), ("fp32", 1, 4, [300], 32, 70)])
 def test_attention_over_pages(fmt, dtype, H, QH, lengths, page, queries):
     need_gpu()
     print(f"case attend {fmt} {dtype} H={H} QH={QH} lengths={lengths} page={page} queries={queries}", flush=True)
@@ -176,7 +176,7 @@ def test_rows_without_tokens_and_pages_outside_the_pool(dtype, fmt):
     assert (out[:6] == 0).all()
 
 
-@pytest.mark.parametrize("dtype,fmt,ragged,most", [("bf16", "grid256", [1, 0, 5, 2], 5), ("bf16", "rtn4", [40, 3, 0, 1], 40),
+@pytest.mark.parametrize("dtype,fmt,ragged,most", [("bf16", "grid256", [1, 0, 5, 2], 5), ("bf16", "rtn4", [40, 3, 0, 1], 40), ("bf16", "grid256", [15, 1, 14, 0], 15),
                                                     ("bf16", "grid64", [0, 70, 9, 1], 70), ("fp32", "grid16", [3, 0, 33, 1], 33)])
 def test_ragged_queries_leave_other_rows_alone(dtype, fmt, ragged, most):
     need_gpu()
