@@ -19,7 +19,7 @@ inline __device__ ConstInts const_ints(const int32_t* p) { return (ConstInts)(ui
 
 constexpr int kTile = 32;                    // tokens of a tile: four groups of 8, each within a page
 constexpr int kQueryExp = 14;                // largest coordinate of a row's query: 2^13 ... 2^14
-constexpr float kTopWeight = 0x1p15f;        // a weight beyond this moves the reference,
+constexpr float kTopExp = 15.0f, kTopWeight = 0x1p15f;      // a weight beyond 2^kTopExp moves the reference,
 constexpr float kStartExp = 8.0f;            // so that the largest is 2^kStartExp: what is 2^-33 of it still counts
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }

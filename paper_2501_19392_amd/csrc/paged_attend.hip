@@ -110,6 +110,7 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
     for (int k = 0; k < C::kHalves; ++k) vs[k] = C::value_scales(scale_lds, k, g);
     const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;       // (t_end: of this piece, whole tiles but for the last)
     if (masked) {
+      asm volatile("");                                    // (a branch, not selects that every tile would pay for)
       const int seen = (there >> g) & 1 ? limit + 1 - (t + 8 * g) : 0;     // so many of the lane's eight tokens are seen
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = e < seen ? y[e] : -INFINITY;

@@ -14,7 +14,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kTokens = 64;                                // of a tile
-constexpr int kKeyBytes = kTokens * kGroup * 2, kBufferBytes = 2 * kKeyBytes + 2 * kTokens * 4;      // keys, values, scales of both
+constexpr int kKeyBytes = kTokens * kGroup * 2, kBufferBytes = 2 * kKeyBytes + (2 * kTokens + 16) * 4;      // keys, values, scales of both, the largest of each eight of the values', pages that are not there
 
 // Coordinate (of 128) that row i of a 32-row operand R stands for, so that register n of lanes 32 hf ... of product R is coordinate
 // 16 (2 R + n / 8) + 8 hf + n % 8: what such a lane holds of a vector as the other operand.  (Swaps bits 2 and 3.)
@@ -54,12 +54,15 @@ template <int NCW> struct TileCodes {
   uint32_t v[8];
   u32x2 ks;                                                // the lane's token's scale word(s)
   uint32_t vs[kRtn ? 8 : 1];                               // grids: scale of token lane % 8 of the piece; uniform: of each, the lane's half
-  int there[2];                                            // uniform: so many of the piece's first, second four tokens are there (the others hold anything)
+  bool missing;                                            // the keys' page is not in the pool
+  int there[2];                                            // so many of the piece's first, second four tokens are there (the others hold anything)
   static __device__ __forceinline__ int value_token(int part, int e) { return 16 * (part >> 1) + 4 * (part & 1) + (e & 3) + 8 * (e >> 2); }
 
   __device__ __forceinline__ void request(const PagedAttendArgs& a, int b, int len, int h, int t, int part, int lane) {
     const uint32_t row_bytes = (uint32_t)a.H * kRow;
-    const uint64_t key_row = (uint64_t)max(group_row(a, b, t / 8 + part), 0);
+    const int key_group_row = group_row(a, b, t / 8 + part);
+    const uint64_t key_row = (uint64_t)max(key_group_row, 0);
+    missing = key_group_row < 0;
     const int group[2] = {group_row(a, b, t / 8 + (part & ~1)), group_row(a, b, t / 8 + (part | 1))};
     const uint64_t value_row[2] = {(uint64_t)max(group[0], 0) + 4 * (part & 1), (uint64_t)max(group[1], 0) + 4 * (part & 1)};
 #pragma unroll
@@ -127,8 +130,9 @@ template <int NCW> struct TileCodes {
     }
     *reinterpret_cast<u32x4*>(buffer + key_place(token, piece)) = out[0];
     *reinterpret_cast<u32x4*>(buffer + key_place(token, piece + 1)) = out[1];
-    // values: coordinates 2 lane, 2 lane + 1 of the piece's eight tokens
+    // values: coordinates 2 lane, 2 lane + 1 of the piece's eight tokens.  (Their scales bound the weights: those of tokens that are not there are 0.)
     uint32_t d[8];
+    float most = 0.f;
     if constexpr (kRtn) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -139,7 +143,9 @@ template <int NCW> struct TileCodes {
         const uint32_t w = NCW == kRtn4 ? v[e] : v[e] >> (4 * (lane & 1));
         const uint32_t low = w & ((1u << NCW) - 1u), high = (w >> NCW) & ((1u << NCW) - 1u);
         d[e] = f16_pair(((float)low - zero) * step, ((float)high - zero) * step);
-        if (lane == 0) scales[kTokens + value_token(part, e)] = __builtin_ldexpf(1.0f, x);
+        const float by = (e & 3) < there[e >> 2] ? __builtin_ldexpf(1.0f, x) : 0.f;
+        most = fmaxf(most, by);
+        if (lane == 0) scales[kTokens + value_token(part, e)] = by;
       }
     } else {
       const uint32_t at = C::lane_copy(lane);
@@ -148,7 +154,15 @@ template <int NCW> struct TileCodes {
         const uint32_t code = c == 8 ? v[e] : c == 4 ? (v[e] >> (4 * (lane & 1))) & 15u : (v[e] >> (6 * lane - 8 * min((6 * lane) >> 3, 46))) & 63u;
         d[e] = C::point(table, code << 8 | at);
       }
-      if (lane < 8) scales[kTokens + value_token(part, lane)] = half_bits_to_float((uint16_t)vs[0]);
+      most = (lane & 3) < (lane & 4 ? there[1] : there[0]) ? half_bits_to_float((uint16_t)vs[0]) : 0.f;
+      if (lane < 8) scales[kTokens + value_token(part, lane)] = most;
+      most = fmaxf(most, quad_xor<1>(most));
+      most = fmaxf(most, quad_xor<2>(most));
+      most = fmaxf(most, octet_mirror(most));
+    }
+    if (lane == 0) {
+      scales[2 * kTokens + part] = most;
+      scales[2 * kTokens + 8 + part] = missing ? 1.0f : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -252,10 +266,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
   for (int t = t_begin; t < t_end; t += kTokens, n ^= 1) {
     const unsigned char* const buffer = buffers + n * kBufferBytes;
     const float* const scales = reinterpret_cast<const float*>(buffer + 2 * kKeyBytes);
-    unsigned there = 0;                                    // groups of 8 tokens whose page is in the pool
-#pragma unroll
-    for (int j = 0; j < 8; ++j) there |= (unsigned)(TileCodes<NCW>::group_row(a, b, t / 8 + j) >= 0) << j;
-    const bool masked = t + kTokens - 1 > wave_first || there != 255u;
+    // groups of 8 tokens whose page is not in the pool
+    const uint32_t missing = (uint32_t)__builtin_amdgcn_ballot_w64(scales[2 * kTokens + 8 + (lane & 7)] != 0.f) & 255u;
+    const bool masked = t + kTokens - 1 > wave_first || missing != 0;
+    float lift;                                            // power of two of the tile's largest scale
+    {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(scales + 2 * kTokens), y = *reinterpret_cast<const f32x4*>(scales + 2 * kTokens + 4);
+      lift = __builtin_amdgcn_logf(fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))), 0x1p-24f));
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {                          // 32 tokens each
       f32x16 s = {};
@@ -268,56 +286,48 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
         if (t + 2 * kTokens < t_end) request(t + 2 * kTokens);
       }
       // register 4 j + e is token 32 i + 8 j + 4 hf + e
-      f32x4 sv[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const f32x4 sk = *reinterpret_cast<const f32x4*>(scales + 32 * i + 8 * j + 4 * hf);
-        sv[j] = *reinterpret_cast<const f32x4*>(scales + kTokens + 32 * i + 8 * j + 4 * hf);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * j + e] *= sk[e];
       }
       if (masked) {
+        asm volatile("");                                  // (a branch: the selects would cost every tile an instruction and a half per score)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int seen = (there >> (4 * i + j)) & 1 ? limit + 1 - (t + 32 * i + 8 * j + 4 * hf) : 0;
+          const int seen = !((missing >> (4 * i + j)) & 1) ? limit + 1 - (t + 32 * i + 8 * j + 4 * hf) : 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[4 * j + e] = e < seen ? s[4 * j + e] : -INFINITY;
-            sv[j][e] = e < seen ? sv[j][e] : 0.f;
-          }
+          for (int e = 0; e < 4; ++e) s[4 * j + e] = e < seen ? s[4 * j + e] : -INFINITY;
         }
       }
-      float p[16];
-      const auto weigh = [&] {
-        float top = 0.f, big = 0.f;
+      // the largest weight that the scores allow
+      float top = s[0];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], f, -ref));
-          top = fmaxf(top, p[r] * sv[r >> 2][r & 3]);
-          big = fmaxf(big, p[r]);
-        }
-        return __builtin_amdgcn_ballot_w64(top > kTopWeight || big > 0x1p60f) != 0;
-      };
-      if (weigh()) {
-        float top = -3.0e38f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r] * f + __builtin_amdgcn_logf(fmaxf(sv[r >> 2][r & 3], 0x1p-24f)));
-        const float moved = fmaxf(ref, pair_max(top) - kStartExp);
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+      if (__builtin_amdgcn_ballot_w64(__fmaf_rn(top, f, lift - ref) > kTopExp) != 0) {
+        const float moved = fmaxf(ref, pair_max(__fmaf_rn(top, f, lift)) - kStartExp);
         const float by = __builtin_amdgcn_exp2f(ref - moved);
         ref = moved;
         sum *= by;
 #pragma unroll
         for (int R = 0; R < 4; ++R) o[R] *= by;
-        weigh();
       }
+      float p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], f, -ref));
       const unsigned char* const values = buffer + kKeyBytes;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {                        // 16 tokens each
         f16x8 weight;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sum += p[8 * k + e];
-          weight[e] = (_Float16)(p[8 * k + e] * sv[2 * k + (e >> 2)][e & 3]);
+        for (int j = 0; j < 2; ++j) {
+          const f32x4 sv = *reinterpret_cast<const f32x4*>(scales + kTokens + 32 * i + 16 * k + 8 * j + 4 * hf);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sum += p[8 * k + 4 * j + e];
+            weight[4 * j + e] = (_Float16)(p[8 * k + 4 * j + e] * sv[e]);
+          }
         }
 #pragma unroll
         for (int R = 0; R < 4; ++R)
