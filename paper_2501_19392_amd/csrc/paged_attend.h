@@ -57,10 +57,15 @@ __device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int total) 
   const uint32_t room = (uint32_t)max(a.slots - a.batch, max(a.slots / 2, 1));
   return max((int)(((uint32_t)total + room - 1) / room), a.min_tiles);
 }
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
-  return uniform(x);
+// sums over the lanes up to and with this one
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111 /* row_shr:1 */, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142 /* row_bcast:15 */, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143 /* row_bcast:31 */, 0xc, 0xf, false);
+  return x;
 }
 __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
   Share s = {-1, 0, 1, 0, 0};
@@ -72,17 +77,16 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
     return s;
   }
   int total = 0;                                           // (all sequences' room is below 2^30 tiles)
-  for (int b0 = 0; b0 < a.batch; b0 += 64) total += wave_sum(tiles_of(a, b0 + lane));
+  int tiles = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    tiles = tiles_of(a, b0 + lane);
+    total += __builtin_amdgcn_readlane(wave_scan(tiles), 63);
+  }
   s.tiles = piece_tiles(a, total);
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const int mine = (tiles_of(a, b0 + lane) + s.tiles - 1) / s.tiles;
-    int end = mine;                                        // items up to and with this sequence
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const int add = __shfl_up(end, k);
-      end += lane >= k ? add : 0;
-    }
-    end += s.items;
+    if (a.batch > 64) tiles = tiles_of(a, b0 + lane);
+    const int mine = (tiles + s.tiles - 1) / s.tiles;
+    const int end = s.items + wave_scan(mine);             // items up to and with this sequence
     const uint64_t past = __builtin_amdgcn_ballot_w64(end > item);
     if (past != 0 && s.b < 0) {
       const int l = __builtin_ctzll(past);
@@ -282,6 +286,7 @@ template <int NCW, int TERMS> struct Codes {
     }
   }
   static __device__ __forceinline__ void pack_query(const float (&v)[32], f16x8 (&q)[TERMS][4], float (&qsum)[2]) {
+    qsum[0] = qsum[1] = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float x[8];
@@ -426,9 +431,18 @@ template <int NCW, int TERMS> struct Codes {
     if (there < 8) keep_first(w, there);
     return __builtin_bit_cast(f16x8, w);
   }
-  // the larger one of a token's scales
-  static __device__ __forceinline__ float scale_at(const u32x4 (&vs)[kHalves], int e) {
-    return kRtn ? fmaxf(half_at(vs[0], e), half_at(vs[kHalves - 1], e)) : half_at(vs[0], e);
+  // power of two of the largest scale of the lane's tokens (at least the smallest fp16 number's)
+  static __device__ __forceinline__ float lift_of(const u32x4 (&vs)[kHalves]) {
+    const auto pair = [&](int k, int i) {
+      const uint32_t w = vs[k][i];                         // (a cast of the element itself would take the vector's first)
+      return __builtin_bit_cast(f16x2, w);
+    };
+    f16x2 top = pair(0, 0);
+#pragma unroll
+    for (int k = 0; k < kHalves; ++k)
+#pragma unroll
+      for (int i = k == 0 ? 1 : 0; i < 4; ++i) top = __builtin_elementwise_max(top, pair(k, i));
+    return __builtin_amdgcn_logf(fmaxf(fmaxf((float)top[0], (float)top[1]), 0x1p-24f));
   }
 
   // ---- look-ups
@@ -456,9 +470,19 @@ template <int NCW, int TERMS> struct Codes {
     }
   }
 
-  // ---- scores of product p: s[half][p] += keys * query
-  static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const f16x8 (&q)[TERMS][4],
-                                                f32x4 (&s)[kRtn ? 2 : 1][2]) {
+  // What a lane keeps of one of its (one or two) rows.
+  struct Column {
+    f16x8 q[TERMS][4];
+    float qsum[2];                                         // uniform: sum of the row's (rounded) query over each half
+    float f;                                               // score in powers of two = f * sigma * sum
+    int limit;                                             // last token that the row sees
+    f32x4 o[8];
+    f32x4 oz[kRtn ? 2 : 1];                                // uniform: sums of the zero points, per half
+    float ref, sum;                                        // weights are 2^(score - ref)
+  };
+  // ---- scores of product p: s[column][half][p] += keys * query
+  template <int COLS> static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const Column (&col)[COLS],
+                                                                    f32x4 (&s)[COLS][kRtn ? 2 : 1][2]) {
     const uint32_t x[4] = {w.k[p].x, w.k[p].y, w.k[p].z, w.k[p].w};
     if constexpr (kRtn) {
 #pragma unroll
@@ -469,7 +493,9 @@ template <int NCW, int TERMS> struct Codes {
         for (int i = 0; i < 4; ++i) y[i] = NCW == kRtn4 ? ((i & 2) ? d >> 8 : d) & field_mask(i & 1) : d & field_mask(i);
         const f16x8 k = operand(y[0], y[1], y[2], y[3]);
 #pragma unroll
-        for (int n = 0; n < TERMS; ++n) s[j >> 1][p] = mfma(k, q[n][j], s[j >> 1][p]);
+        for (int n = 0; n < TERMS; ++n)
+#pragma unroll
+          for (int i = 0; i < COLS; ++i) s[i][j >> 1][p] = mfma(k, col[i].q[n][j], s[i][j >> 1][p]);
       }
     } else {
       const uint32_t at = lane_copy(lane);
@@ -479,10 +505,15 @@ template <int NCW, int TERMS> struct Codes {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = offset(x, 4 * j + i, at);
         const f16x8 k = operand(point(lds, o[0]), point(lds, o[1]), point(lds, o[2]), point(lds, o[3]));
-        s[0][p] = mfma(k, q[0][j], s[0][p]);
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) s[i][0][p] = mfma(k, col[i].q[0][j], s[i][0][p]);
         if constexpr (TERMS == 2) {
-          s[0][p] = mfma(k, q[1][j], s[0][p]);
-          s[0][p] = mfma(operand(point<1>(lds, o[0]), point<1>(lds, o[1]), point<1>(lds, o[2]), point<1>(lds, o[3])), q[0][j], s[0][p]);
+          const f16x8 rest = operand(point<1>(lds, o[0]), point<1>(lds, o[1]), point<1>(lds, o[2]), point<1>(lds, o[3]));
+#pragma unroll
+          for (int i = 0; i < COLS; ++i) {
+            s[i][0][p] = mfma(k, col[i].q[1][j], s[i][0][p]);
+            s[i][0][p] = mfma(rest, col[i].q[0][j], s[i][0][p]);
+          }
         }
       }
     }
@@ -504,16 +535,18 @@ template <int NCW, int TERMS> struct Codes {
   }
 
   // ---- o[j] += values (coordinates: result()) * weights p * scale
-  static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, const float (&p)[8],
-                                                const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane, f32x4 (&o)[8], f32x4 (&oz)[2]) {
-    f16x8 b[kHalves][TERMS];
+  template <int COLS> static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, const float (&p)[COLS][8],
+                                                                    const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane, Column (&col)[COLS]) {
+    f16x8 b[COLS][kHalves][TERMS];
 #pragma unroll
-    for (int k = 0; k < kHalves; ++k) {
-      float weight[8];
+    for (int n = 0; n < COLS; ++n)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) weight[e] = p[e] * half_at(vs[k], e);
-      split_f16<TERMS>(weight, b[k]);
-    }
+      for (int k = 0; k < kHalves; ++k) {
+        float weight[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) weight[e] = p[n][e] * half_at(vs[k], e);
+        split_f16<TERMS>(weight, b[n][k]);
+      }
     if constexpr (kRtn) {
       // All rows of an operand have to be of one half (the weights are the half's): of the eight codes that a lane holds, lanes m and m ^ 8
       // exchange four.  Lower half-word: coordinates of the lower half, upper one: of the upper half.
@@ -525,7 +558,9 @@ template <int NCW, int TERMS> struct Codes {
       for (int k = 0; k < 2; ++k) {
         const f16x8 z = zero_points(scales, k, lane >> 4, there);
 #pragma unroll
-        for (int n = 0; n < TERMS; ++n) oz[k] = mfma(z, b[k][n], oz[k]);
+        for (int i = 0; i < COLS; ++i)
+#pragma unroll
+          for (int n = 0; n < TERMS; ++n) col[i].oz[k] = mfma(z, b[i][k][n], col[i].oz[k]);
 #pragma unroll
         for (int byte = 0; byte < 4 / kFields; ++byte) {
           uint32_t x[4];                                   // tokens 2 i and 2 i + 1 in the halves
@@ -536,7 +571,9 @@ template <int NCW, int TERMS> struct Codes {
             const f16x8 v = operand(x[0] & field_mask(f), x[1] & field_mask(f), x[2] & field_mask(f), x[3] & field_mask(f));
             const int j = 4 * k + kFields * byte + f;
 #pragma unroll
-            for (int n = 0; n < TERMS; ++n) o[j] = mfma(v, b[k][n], o[j]);
+            for (int i = 0; i < COLS; ++i)
+#pragma unroll
+              for (int n = 0; n < TERMS; ++n) col[i].o[j] = mfma(v, b[i][k][n], col[i].o[j]);
           }
         }
       }
@@ -562,10 +599,14 @@ template <int NCW, int TERMS> struct Codes {
             for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_perm(d[n][2 * e + 1], d[n][2 * e], k == 0 ? 0x05040100u : 0x07060302u);
             v[n] = operand(x[0], x[1], x[2], x[3]);
           }
-          o[2 * i + k] = mfma(v[0], b[0][0], o[2 * i + k]);
-          if constexpr (TERMS == 2) {
-            o[2 * i + k] = mfma(v[0], b[0][1], o[2 * i + k]);
-            o[2 * i + k] = mfma(v[1], b[0][0], o[2 * i + k]);
+#pragma unroll
+          for (int n = 0; n < COLS; ++n) {
+            f32x4& o = col[n].o[2 * i + k];
+            o = mfma(v[0], b[n][0][0], o);
+            if constexpr (TERMS == 2) {
+              o = mfma(v[0], b[n][0][1], o);
+              o = mfma(v[1], b[n][0][0], o);
+            }
           }
         }
       }
@@ -576,13 +617,13 @@ template <int NCW, int TERMS> struct Codes {
   static __device__ __forceinline__ int coordinate(int g, int r) {
     return kRtn ? 64 * (r >> 4) + 8 * ((4 * g + ((r >> 2) & 3)) & 7) + 4 * (g >> 1) : 32 * g + r;
   }
-  static __device__ __forceinline__ void result(const f32x4 (&o)[8], const f32x4 (&oz)[2], int e, float (&v)[32]) {
+  static __device__ __forceinline__ void result(const Column& col, int e, float (&v)[32]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (kRtn) v[16 * (j >> 2) + 4 * i + (j & 3)] = __builtin_ldexpf(o[j][i] * (1.0f / (float)field_scale(j % kFields)) - oz[j >> 2][i], e);
-        else v[8 * i + j] = __builtin_ldexpf(o[j][i], e);
+        if constexpr (kRtn) v[16 * (j >> 2) + 4 * i + (j & 3)] = __builtin_ldexpf(col.o[j][i] * (1.0f / (float)field_scale(j % kFields)) - col.oz[j >> 2][i], e);
+        else v[8 * i + j] = __builtin_ldexpf(col.o[j][i], e);
       }
   }
 };

@@ -17,17 +17,18 @@ using namespace paged;
 //            tokens 8 g ... 8 g + 7 for row m, which is what the second product wants of it as its B operand, with no exchange between lanes;
 //   values   O^T = V^T P: A holds 8 tokens of one coordinate; a look-up gives two neighbouring coordinates, two permutes pair them up by
 //            token.  The 32 coordinates a lane ends with are consecutive, as the inverse transform wants them.
+// COLS = 2: 32 rows, on twice the registers; a tile's codes become operands once for both.
 // Waves of a workgroup, which share the copies of the grid, and waves per SIMD: with 128 registers four fit (two workgroups a CU, which is what LDS has
 // room for with 256 points); uniform codes need more for the two halves' scales, and no LDS to speak of; fp32 layers hold everything twice.
-template <typename T, int NCW> struct Shape {
-  static constexpr int kWaves = is_rtn(NCW) ? 4 : 8;
-  static constexpr int kPerSimd = is_rtn(NCW) ? 3 : sizeof(T) == 4 ? 2 : 4;
+template <typename T, int NCW, int COLS> struct Shape {
+  static constexpr int kWaves = is_rtn(NCW) || COLS == 2 ? 4 : 8;
+  static constexpr int kPerSimd = COLS == 2 ? 2 : is_rtn(NCW) ? 3 : sizeof(T) == 4 ? 2 : 4;
   static constexpr int kThreads = 64 * kWaves, kSlots = 256 * 4 * kPerSimd;            // threads, waves on the chip
 };
-template <typename T, int NCW, bool FAR>
-__global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_waves_per_eu((Shape<T, NCW>::kPerSimd)))) void paged_attend_kernel(
-    const PagedAttendArgs a) {
-  constexpr int kWaves = Shape<T, NCW>::kWaves;
+template <typename T, int NCW, int COLS, bool FAR>
+__global__ __launch_bounds__((Shape<T, NCW, COLS>::kThreads)) __attribute__((amdgpu_waves_per_eu((Shape<T, NCW, COLS>::kPerSimd)))) void
+paged_attend_kernel(const PagedAttendArgs a) {
+  constexpr int kWaves = Shape<T, NCW, COLS>::kWaves, kRows = 16 * COLS;
   constexpr int kTerms = sizeof(T) == 2 ? 1 : 2;
   constexpr bool kRtn = is_rtn(NCW);
   typedef Codes<NCW, kTerms> C;
@@ -45,19 +46,22 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
   if (blockIdx.x * kWaves / a.H >= (unsigned)share.items) return;         // (the whole workgroup is behind the last piece)
   const int b = max(share.b, 0), rep = a.q_heads / a.H;
   const PagedQueries w = paged_queries(a, b);
-  const int n_rows = w.n * rep, row0 = blockIdx.y * 16;
+  const int n_rows = w.n * rep, row0 = blockIdx.y * kRows;
   const bool idle = share.b < 0 || row0 >= n_rows;
-  const int row = row0 + m, qi = row / rep, qh = h * rep + row % rep;
-  const bool row_there = row < n_rows;
-  // the last token the row sees; the tokens of this piece
-  const int limit = row_there ? w.len - w.count + qi : -1;
-  const int first_limit = uniform(w.len - w.count + row0 / rep), last_limit = uniform(w.len - w.count + min(row0 + 15, n_rows - 1) / rep);
+  // the tokens of this piece
+  const int first_limit = uniform(w.len - w.count + row0 / rep), last_limit = uniform(w.len - w.count + min(row0 + kRows - 1, n_rows - 1) / rep);
   const int t_begin = share.piece * share.tiles * kTile, t_end = idle ? 0 : min(min(t_begin + share.tiles * kTile, w.len), last_limit + 1);
   const bool any = t_begin < t_end;
-  typename C::template Query<T> asked = {};
-  if (!idle)
-    asked = C::template request_query<T>(static_cast<const T*>(a.q) + (w.first + (row_there ? qi : 0)) * a.q_stride + (row_there ? qh : h * rep) * kGroup,
-                                         a.signs_k, h, g);
+  typename C::Column col[COLS];
+  typename C::template Query<T> asked[COLS] = {};
+  if (!idle) {
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) {                       // (rows that are not there: the last one again, which sees nothing)
+      const int row = row0 + 16 * i + m, there = min(row, n_rows - 1), qi = there / rep, qh = h * rep + there % rep;
+      col[i].limit = row < n_rows ? w.len - w.count + qi : -1;
+      asked[i] = C::template request_query<T>(static_cast<const T*>(a.q) + (w.first + qi) * a.q_stride + qh * kGroup, a.signs_k, h, g);
+    }
+  }
   Rows r0 = {}, r1 = {};
   typename C::Keys k = {}, next = {};
   typename C::Values v = {};
@@ -71,80 +75,88 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
   __syncthreads();
   if (idle) return;
 
-  // ---- the row's query: rotated, scaled to fp16's range
-  f16x8 q[kTerms][4];
-  float qsum[2] = {0.f, 0.f};                              // uniform: sum of the row's (rounded) query over each half
-  float f;                                                 // score in powers of two = f * sigma * sum
-  {
+  // ---- the rows' queries: rotated, scaled to fp16's range
+#pragma unroll
+  for (int i = 0; i < COLS; ++i) {
     float x[32];
-    C::template rotate_query<T>(asked, lane, x);
+    C::template rotate_query<T>(asked[i], lane, x);
     const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
     float top = 0.f;
 #pragma unroll
     for (int r = 0; r < 32; ++r) top = fmaxf(top, fabsf(x[r]));
     const int e = max(__builtin_amdgcn_frexp_expf(column_max(top) * fabsf(by)), -100);
-    f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? 24 : c_exp), 126));
+    col[i].f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? 24 : c_exp), 126));
     const float scaled = __builtin_ldexpf(by, kQueryExp - e);
 #pragma unroll
     for (int r = 0; r < 32; ++r) x[r] *= scaled;
-    C::pack_query(x, q, qsum);
+    C::pack_query(x, col[i].q, col[i].qsum);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) col[i].o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < C::kHalves; ++j) col[i].oz[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    col[i].ref = -3.0e38f;
+    col[i].sum = 0.f;
   }
-
-  f32x4 o[8] = {};
-  f32x4 oz[2] = {};                                        // uniform: sums of the zero points, per half
-  float ref = -3.0e38f, sum = 0.f;                         // weights are 2^(score - ref)
 
   const auto tile = [&](const typename C::Keys& x, const typename C::Values& xv, int t, unsigned there) {
     // scales of the tile's 32 tokens to the lanes that need them
     asm volatile("" ::: "memory");                         // (a wave's LDS accesses stay in order)
     C::put_scales(x, scale_lds, lane);
     asm volatile("" ::: "memory");
-    f32x4 s[kRtn ? 2 : 1][2] = {};                         // [half][product]
+    f32x4 s[COLS][C::kHalves][2] = {};                     // [column][half][product]
 #pragma unroll
-    for (int p = 0; p < 2; ++p) C::scores(x, p, lds, lane, q, s);
-    float y[8];
+    for (int p = 0; p < 2; ++p) C::scores(x, p, lds, lane, col, s);
     __builtin_amdgcn_sched_barrier(0);
-    C::scaled(s, scale_lds, g, qsum, y);
+    float p[COLS][8];
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) C::scaled(s[i], scale_lds, g, col[i].qsum, p[i]);
     u32x4 vs[C::kHalves];
 #pragma unroll
     for (int k = 0; k < C::kHalves; ++k) vs[k] = C::value_scales(scale_lds, k, g);
-    const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;       // (t_end: of this piece, whole tiles but for the last)
-    if (masked) {
+    const int held = (there >> g) & 1 ? w.len - (t + 8 * g) : 0;           // so many of the lane's eight tokens are there: the others hold anything
+    if (t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u) {      // (t_end: of this piece, whole tiles but for the last)
       asm volatile("");                                    // (a branch, not selects that every tile would pay for)
-      const int seen = (there >> g) & 1 ? limit + 1 - (t + 8 * g) : 0;     // so many of the lane's eight tokens are seen
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = e < seen ? y[e] : -INFINITY;
+      for (int i = 0; i < COLS; ++i) {
+        const int seen = min(col[i].limit + 1 - (t + 8 * g), held);
 #pragma unroll
-      for (int k = 0; k < C::kHalves; ++k) C::keep_first(vs[k], seen);
+        for (int e = 0; e < 8; ++e) p[i][e] = e < seen ? p[i][e] : -INFINITY;
+      }
+#pragma unroll
+      for (int k = 0; k < C::kHalves; ++k) C::keep_first(vs[k], held);
     }
-    float p[8];
-    const auto weigh = [&] {
-      float top = 0.f, big = 0.f;
+    // The reference follows where the largest weight that the scores allow is too large: such weights become 2^kStartExp.
+    const float lift = C::lift_of(vs);
+    float top[COLS];
+    bool high = false;
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) {
+      top[i] = p[i][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top[i] = fmaxf(top[i], p[i][e]);
+      high |= __fmaf_rn(top[i], col[i].f, lift - col[i].ref) > kTopExp;
+    }
+    if (__builtin_amdgcn_ballot_w64(high) != 0) {
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) {
+        const float moved = fmaxf(col[i].ref, column_max(__fmaf_rn(top[i], col[i].f, lift)) - kStartExp);
+        const float by = __builtin_amdgcn_exp2f(col[i].ref - moved);
+        col[i].ref = moved;
+        col[i].sum *= by;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) col[i].o[j] *= by;
+        if constexpr (kRtn) { col[i].oz[0] *= by; col[i].oz[1] *= by; }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < COLS; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref));
-        top = fmaxf(top, p[e] * C::scale_at(vs, e));
-        big = fmaxf(big, p[e]);
+        p[i][e] = __builtin_amdgcn_exp2f(__fmaf_rn(p[i][e], col[i].f, -col[i].ref));
+        col[i].sum += p[i][e];
       }
-      return __builtin_amdgcn_ballot_w64(top > kTopWeight || big > 0x1p60f) != 0;
-    };
-    if (weigh()) {                                         // the reference follows: weights of the largest become 2^kStartExp
-      float top = -3.0e38f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, y[e] * f + __builtin_amdgcn_logf(fmaxf(C::scale_at(vs, e), 0x1p-24f)));
-      const float moved = fmaxf(ref, column_max(top) - kStartExp);
-      const float by = __builtin_amdgcn_exp2f(ref - moved);
-      ref = moved;
-      sum *= by;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] *= by;
-      if constexpr (kRtn) { oz[0] *= by; oz[1] *= by; }
-      weigh();
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += p[e];
     __builtin_amdgcn_sched_barrier(0);
-    C::values(xv, scale_lds, (there >> g) & 1 ? w.len - (t + 8 * g) : 0, p, vs, lds, lane, o, oz);
+    C::values(xv, scale_lds, held, p, vs, lds, lane, col);
   };
   // Keys are requested a tile ahead, values behind the tile that takes their registers, the rows they are in two tiles ahead.
 #pragma unroll 1
@@ -165,19 +177,22 @@ __global__ __launch_bounds__((Shape<T, NCW>::kThreads)) __attribute__((amdgpu_wa
   // ---- the lane's 32 coordinates of the row (whose numbers are worked out anew: they are not worth registers in the loop)
   int again = lane;
   asm volatile("" : "+v"(again));
-  const int row_out = row0 + (again & 15), qi_out = row_out / rep, qh_out = h * rep + row_out % rep;
-  sum = column_sum(sum);
-  float x[32];
-  C::result(o, oz, kRtn ? 24 : c_exp, x);
-  if (share.pieces == 1) {
-    finish<T, NCW>(a, x, sum, h, again, row_out < n_rows, w.first + qi_out, qh_out);
-  } else if (row_out < n_rows) {
-    const int64_t at = ((int64_t)item * a.max_queries + qi_out) * a.q_heads + qh_out;
-    float* const part = a.part + at * kGroup;
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-      *reinterpret_cast<f32x4*>(part + C::coordinate(again >> 4, 4 * r)) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
-    if (again < 16) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
+  for (int i = 0; i < COLS; ++i) {
+    const int row = row0 + 16 * i + (again & 15), qi = row / rep, qh = h * rep + row % rep;
+    const float sum = column_sum(col[i].sum);
+    float x[32];
+    C::result(col[i], kRtn ? 24 : c_exp, x);
+    if (share.pieces == 1) {
+      finish<T, NCW>(a, x, sum, h, again, row < n_rows, w.first + qi, qh);
+    } else if (row < n_rows) {
+      const int64_t at = ((int64_t)item * a.max_queries + qi) * a.q_heads + qh;
+      float* const part = a.part + at * kGroup;
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        *reinterpret_cast<f32x4*>(part + C::coordinate(again >> 4, 4 * r)) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+      if (again < 16) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{col[i].ref, sum};
+    }
   }
 }
 
@@ -263,7 +278,7 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendA
 }
 
 // How a launch is laid out, from sizes alone (lengths are on the device).
-struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles, waves, row_blocks; int64_t items; bool merge, many; };
+struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles, waves, row_blocks; int64_t items; bool two, merge, many; };
 constexpr int kMinTiles = 2;                               // a piece of fewer tokens costs more than it saves
 constexpr int kFewRows = 64;                               // rows of a kv head that waves of 16 rows take one after the other (bf16)
 template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
@@ -277,13 +292,15 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
     p.merge = p.slots > 1;
     return p;
   }
-  p.row_tiles = (unsigned)((rows + 15) / 16);
+  p.two = sizeof(T) == 2 && rows > 16;
+  const int per_wave = p.two ? 32 : 16, waves = p.two ? Shape<T, NCW, 2>::kWaves : Shape<T, NCW, 1>::kWaves;
+  p.row_tiles = (unsigned)((rows + per_wave - 1) / per_wave);
   p.min_tiles = kMinTiles;
   // as many pieces as make all waves that the chip holds
-  p.slots = (int)std::max<int64_t>(Shape<T, NCW>::kSlots / (H * p.row_tiles), 1);
+  p.slots = (int)std::max<int64_t>((p.two ? Shape<T, NCW, 2>::kSlots : Shape<T, NCW, 1>::kSlots) / (H * p.row_tiles), 1);
   const int64_t each = std::max<int64_t>((most + kMinTiles - 1) / kMinTiles, 1);
   p.items = std::min(batch * each, std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
-  p.blocks = (unsigned)((p.items * H + Shape<T, NCW>::kWaves - 1) / Shape<T, NCW>::kWaves);
+  p.blocks = (unsigned)((p.items * H + waves - 1) / waves);
   p.merge = each > 1;
   p.many = p.items > 64 * batch;
   return p;
@@ -333,8 +350,16 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   } else {
     const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
     const dim3 blocks(plan.blocks, plan.row_tiles);
-    AQUAKV_PAGED(dtype, n_codewords, (far ? paged_attend_kernel<T, N, true><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)
-                                          : paged_attend_kernel<T, N, false><<<blocks, Shape<T, N>::kThreads, 0, stream>>>(a)));
+#define AQUAKV_ATTEND(T, N, COLS)                                                                                        \
+  (far ? paged_attend_kernel<T, N, COLS, true><<<blocks, Shape<T, N, COLS>::kThreads, 0, stream>>>(a)                     \
+       : paged_attend_kernel<T, N, COLS, false><<<blocks, Shape<T, N, COLS>::kThreads, 0, stream>>>(a))
+    if (plan.two) {
+      typedef bf16_t T;
+      AQUAKV_PAGED_N(n_codewords, (AQUAKV_ATTEND(T, N, 2)));
+    } else {
+      AQUAKV_PAGED(dtype, n_codewords, (AQUAKV_ATTEND(T, N, 1)));
+    }
+#undef AQUAKV_ATTEND
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (!plan.merge) return hipSuccess;
