@@ -266,7 +266,7 @@ struct PagedAttendArgs {
   // set by the launcher
   float *part, *stats;                            // [items, max_queries, q_heads, 128], [items, max_queries, q_heads, 2]
   int2* heads;                                    // [batch]: a sequence's first item, and how many
-  int slots, min_tiles;                           // pieces that fill the chip, tiles of a piece at least (blocks of rows: pieces of a sequence)
+  int slots;                                      // pieces that fill the chip (blocks of rows: pieces of a sequence)
   int row_blocks;                                 // blocks of 32 rows per wave (paged_tiles.hip)
   uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
 };

@@ -25,6 +25,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
   const bool rope = keys && a.rope_cos != nullptr;
   __shared__ Lds lds;
   const int l = group_pos<N>(threadIdx.x), slot_in_block = threadIdx.x / kLanes;
+  const unsigned n_groups = (unsigned)a.tokens * (unsigned)a.H, step = gridDim.x * kGroups;
+  float v[N];
+  int64_t row;
+  int pos = 0;
+  const auto request = [&](unsigned g0) {
+    const unsigned gid = min(g0 + slot_in_block, n_groups - 1), t = gid / (unsigned)a.H;      // (every lane stays in the DPP exchanges)
+    row = a.slots[t];
+    if (a.rope_cos != nullptr) pos = a.positions[t];
+    Storage<T>::load(X + t * x_stride + (gid - t * (unsigned)a.H) * kGroup + l * N, v);
+  };
+  request(blockIdx.x * kGroups);                          // on the way while the tables are
   if constexpr (!is_rtn(NCW)) {
     TableRegs<kThreads> table_regs;
     if (a.table != nullptr) table_regs.request(a.table);
@@ -32,23 +43,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     if (a.table != nullptr) table_regs.store(lds.table);
     __syncthreads();
   }
-  const unsigned n_groups = (unsigned)a.tokens * (unsigned)a.H;
-  for (unsigned g0 = blockIdx.x * kGroups; g0 < n_groups; g0 += gridDim.x * kGroups) {
-    unsigned gid = g0 + slot_in_block;
-    const bool there = gid < n_groups;
-    if (!there) gid = n_groups - 1;                       // keep every lane in the DPP exchanges
-    const unsigned t = gid / (unsigned)a.H, head = gid - t * (unsigned)a.H;
-    const int64_t row = a.slots[t];
-    bool active = there && (uint64_t)row < (uint64_t)a.pool.rows;
-    int pos = 0;
-    if (rope) {
-      pos = a.positions[t];
-      if ((unsigned)pos >= (unsigned)a.rope_rows) { active = false; pos = 0; }
-    } else if (a.rope_cos != nullptr) {
-      active = active && (unsigned)a.positions[t] < (unsigned)a.rope_rows;      // (a token is left out as a whole)
-    }
-    float v[N], sf[N] = {};
-    Storage<T>::load(X + t * x_stride + head * kGroup + l * N, v);
+  for (unsigned g0 = blockIdx.x * kGroups;;) {
+    const unsigned gid = min(g0 + slot_in_block, n_groups - 1), head = gid % (unsigned)a.H;
+    bool active = g0 + slot_in_block < n_groups && (uint64_t)row < (uint64_t)a.pool.rows;
+    if (a.rope_cos != nullptr && (unsigned)pos >= (unsigned)a.rope_rows) { active = false; pos = 0; }      // (a token is left out as a whole)
+    float sf[N] = {};
     if constexpr (!is_rtn(NCW)) load_signs(signs, (int)head, l, sf);
     if (rope) rope128(v, l, a.rope_cos + (int64_t)pos * (kGroup / 2), a.rope_sin + (int64_t)pos * (kGroup / 2));
     quantize_residual<NCW>(v, sf, l, lds.cb, a.table != nullptr ? lds.table : nullptr, active, row * a.H + head, codes, scales, Xhat != nullptr);
@@ -57,6 +56,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
       finish_hat<NCW>(v, sf, zero);
       if (active) Storage<T>::template store<false>(Xhat + (int64_t)gid * kGroup, l, v);
     }
+    if ((g0 += step) >= n_groups) break;
+    request(g0);
   }
 }
 

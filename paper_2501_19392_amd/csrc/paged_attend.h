@@ -55,7 +55,7 @@ __device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
 // tiles per piece
 __device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int total) {
   const uint32_t room = (uint32_t)max(a.slots - a.batch, max(a.slots / 2, 1));
-  return max((int)(((uint32_t)total + room - 1) / room), a.min_tiles);
+  return (int)(((uint32_t)total + room - 1) / room);
 }
 // sums over the lanes up to and with this one
 __device__ __forceinline__ int wave_scan(int x) {

@@ -23,6 +23,10 @@ using namespace paged;
 template <typename T, int NCW, int COLS> struct Shape {
   static constexpr int kWaves = is_rtn(NCW) || COLS == 2 ? 4 : 8;
   static constexpr int kPerSimd = COLS == 2 ? 2 : is_rtn(NCW) ? 3 : sizeof(T) == 4 ? 2 : 4;
+  // COLS = 2: a workgroup's waves take pieces of one kv head, one behind the other, and join their results (5 queries of 8 x 9999 tokens, 3 bits: 33.2 us,
+  // two waves of two heads each 34.5, every wave its own result 37.6).  With 16 rows they take all heads of the same tokens, whose codes share cache
+  // lines: 32 x 16 384 tokens 95.6 us, four waves of two heads joined 99.5, two of four heads 109, one head 113 (one sequence of 131 072: 47, 45, 47, 49).
+  static constexpr bool kJoined = COLS == 2;
   static constexpr int kThreads = 64 * kWaves, kSlots = 256 * 4 * kPerSimd;            // threads, waves on the chip
 };
 template <typename T, int NCW, int COLS, bool FAR>
@@ -32,18 +36,29 @@ paged_attend_kernel(const PagedAttendArgs a) {
   constexpr int kTerms = sizeof(T) == 2 ? 1 : 2;
   constexpr bool kRtn = is_rtn(NCW);
   typedef Codes<NCW, kTerms> C;
-  __shared__ __align__(256) unsigned char lds[C::kTableBytes + kWaves * C::kScaleBytes];
+  constexpr bool kJoined = Shape<T, NCW, COLS>::kJoined;
+  constexpr int kPiece = 16 * (kGroup + 2) * 4;            // bytes of 16 rows' sums, references and sums of weights
+  constexpr int kJoinBytes = kJoined ? (kWaves - 1) * COLS * kPiece : 0, kTable = kJoinBytes > C::kTableBytes ? kJoinBytes : C::kTableBytes;
+  __shared__ __align__(256) unsigned char lds[kTable + kWaves * C::kScaleBytes];
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  unsigned char* const scale_lds = lds + C::kTableBytes + wave * C::kScaleBytes;
+  unsigned char* const scale_lds = lds + kTable + wave * C::kScaleBytes;
 
   // What is waited for at the start is a chain (lengths, then the piece's pages, then its codes); all else is requested beside it.
   const typename C::Points points = C::request_points(a.codebook, lane);
   // which rows, kv head and piece of a sequence
-  const unsigned unit = blockIdx.x * kWaves + wave;
-  const int h = uniform(unit % a.H), item = uniform(unit / a.H);
+  int h, item;
+  if constexpr (kJoined) {                                 // workgroups go round the eight chiplets: those of the heads of a piece are eight apart
+    const unsigned turn = blockIdx.x >> 3;
+    h = turn % a.H;
+    item = (turn / a.H * 8 + (blockIdx.x & 7)) * kWaves + wave;
+  } else {
+    const unsigned unit = blockIdx.x * kWaves + wave;
+    h = uniform(unit % a.H);
+    item = uniform(unit / a.H);
+  }
   const Share share = share_of(a, lane, item);
-  if (blockIdx.x * kWaves / a.H >= (unsigned)share.items) return;         // (the whole workgroup is behind the last piece)
+  if ((kJoined ? item - wave : (int)(blockIdx.x * kWaves / a.H)) >= share.items) return;      // (the whole workgroup is behind the last piece)
   const int b = max(share.b, 0), rep = a.q_heads / a.H;
   const PagedQueries w = paged_queries(a, b);
   const int n_rows = w.n * rep, row0 = blockIdx.y * kRows;
@@ -73,11 +88,12 @@ paged_attend_kernel(const PagedAttendArgs a) {
   }
   const int c_exp = C::template stage<kWaves>(points, lds, lane, wave);
   __syncthreads();
-  if (idle) return;
+  if (!kJoined && idle) return;
 
   // ---- the rows' queries: rotated, scaled to fp16's range
 #pragma unroll
   for (int i = 0; i < COLS; ++i) {
+    if (idle) break;
     float x[32];
     C::template rotate_query<T>(asked[i], lane, x);
     const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
@@ -172,26 +188,70 @@ paged_attend_kernel(const PagedAttendArgs a) {
     r1 = r2;
   }
 
-  if (a.heads != nullptr && share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{item, share.pieces};
-
-  // ---- the lane's 32 coordinates of the row (whose numbers are worked out anew: they are not worth registers in the loop)
+  // Results of a sequence that others than this workgroup (wave) have: their number, and which this one's is.
+  int results = share.pieces, result = item;
+  int others = 0;                                          // waves behind this one whose results it takes
+  if constexpr (kJoined) {
+    const int first = item - share.piece, group = (item - wave) / kWaves;
+    results = (first + share.pieces - 1) / kWaves - first / kWaves + 1;
+    result = group + b;                                    // (two sequences that share a workgroup are neighbours)
+    others = min(kWaves - wave, share.pieces - share.piece) - 1;
+  }
+  if (a.heads != nullptr && !idle && share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{result, results};
+  // (worked out anew: lane and row numbers are not worth registers in the loop)
   int again = lane;
   asm volatile("" : "+v"(again));
+  const auto place = [&](int w, int i) { return reinterpret_cast<f32x4*>(lds + ((w - 1) * COLS + i) * kPiece); };
+  if constexpr (kJoined) {
+    // the first wave of each sequence takes the others' sums, which go where the grid was
+    const bool gives = wave != 0 && share.piece != 0;
+    __syncthreads();
+    if (gives && !idle) {
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) {
+        const float sum = column_sum(col[i].sum);
+        float x[32];
+        C::result(col[i], kRtn ? 24 : c_exp, x);
+        f32x4* const to = place(wave, i);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) to[64 * r + again] = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+        if (again < 16) reinterpret_cast<f32x2*>(to + 512)[again] = f32x2{col[i].ref, sum};
+      }
+    }
+    __syncthreads();
+    if (gives || idle) return;
+  }
+  // ---- the lane's 32 coordinates of the row
 #pragma unroll
   for (int i = 0; i < COLS; ++i) {
     const int row = row0 + 16 * i + (again & 15), qi = row / rep, qh = h * rep + row % rep;
-    const float sum = column_sum(col[i].sum);
-    float x[32];
+    float x[32], ref = col[i].ref, sum = column_sum(col[i].sum);
     C::result(col[i], kRtn ? 24 : c_exp, x);
-    if (share.pieces == 1) {
+    if constexpr (kJoined) {
+#pragma unroll 1
+      for (int n = 1; n <= others; ++n) {
+        const f32x4* const from = place(wave + n, i);
+        const f32x2 st = reinterpret_cast<const f32x2*>(from + 512)[again & 15];
+        const float top = fmaxf(ref, st.x), keep = __builtin_amdgcn_exp2f(ref - top), by = __builtin_amdgcn_exp2f(st.x - top);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const f32x4 y = from[64 * r + again];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * r + e] = __fmaf_rn(y[e], by, x[4 * r + e] * keep);
+        }
+        sum = __fmaf_rn(st.y, by, sum * keep);
+        ref = top;
+      }
+    }
+    if (results == 1) {
       finish<T, NCW>(a, x, sum, h, again, row < n_rows, w.first + qi, qh);
     } else if (row < n_rows) {
-      const int64_t at = ((int64_t)item * a.max_queries + qi) * a.q_heads + qh;
+      const int64_t at = ((int64_t)result * a.max_queries + qi) * a.q_heads + qh;
       float* const part = a.part + at * kGroup;
 #pragma unroll
       for (int r = 0; r < 8; ++r)
         *reinterpret_cast<f32x4*>(part + C::coordinate(again >> 4, 4 * r)) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
-      if (again < 16) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{col[i].ref, sum};
+      if (again < 16) *reinterpret_cast<f32x2*>(a.stats + 2 * at) = f32x2{ref, sum};
     }
   }
 }
@@ -278,8 +338,8 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendA
 }
 
 // How a launch is laid out, from sizes alone (lengths are on the device).
-struct PagedPlan { unsigned blocks, row_tiles; int slots, min_tiles, waves, row_blocks; int64_t items; bool two, merge, many; };
-constexpr int kMinTiles = 2;                               // a piece of fewer tokens costs more than it saves
+struct PagedPlan { unsigned blocks, row_tiles; int slots, waves, row_blocks; int64_t items; bool two, merge, many; };
+constexpr int kManyPieces = 64;                            // results of a sequence beyond which the merge has 1024 threads
 constexpr int kFewRows = 64;                               // rows of a kv head that waves of 16 rows take one after the other (bf16)
 template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
   PagedPlan p = {};
@@ -295,14 +355,21 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
   p.two = sizeof(T) == 2 && rows > 16;
   const int per_wave = p.two ? 32 : 16, waves = p.two ? Shape<T, NCW, 2>::kWaves : Shape<T, NCW, 1>::kWaves;
   p.row_tiles = (unsigned)((rows + per_wave - 1) / per_wave);
-  p.min_tiles = kMinTiles;
-  // as many pieces as make all waves that the chip holds
+  // As many pieces as make all waves that the chip holds, of one tile at least (4 kv heads x 16 384 tokens x 32 sequences: 95.7 us, half as many
+  // 111, twice as many 99; 5 queries of 8 x 9999 37.7, 42.8, 50.7; pieces of two tiles at least: one sequence of 700 tokens 12.4 for 11.1).
   p.slots = (int)std::max<int64_t>((p.two ? Shape<T, NCW, 2>::kSlots : Shape<T, NCW, 1>::kSlots) / (H * p.row_tiles), 1);
-  const int64_t each = std::max<int64_t>((most + kMinTiles - 1) / kMinTiles, 1);
-  p.items = std::min(batch * each, std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
-  p.blocks = (unsigned)((p.items * H + waves - 1) / waves);
-  p.merge = each > 1;
-  p.many = p.items > 64 * batch;
+  const int64_t pieces = std::min(batch * std::max<int64_t>(most, 1), std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
+  if (p.two) {                                             // (a workgroup has results of as many sequences as it has pieces of)
+    const int64_t groups = (pieces + waves - 1) / waves;
+    p.blocks = (unsigned)((groups + 7) / 8 * 8 * H);
+    p.items = groups + batch;
+    p.merge = groups > 1;
+  } else {
+    p.blocks = (unsigned)((pieces * H + waves - 1) / waves);
+    p.items = pieces;
+    p.merge = most > 1;
+  }
+  p.many = p.items > kManyPieces * batch;
   return p;
 }
 
@@ -338,7 +405,6 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   PagedAttendArgs a = args;
   const PagedPlan plan = plan_of(dtype, n_codewords, a);
   a.slots = plan.slots;
-  a.min_tiles = plan.min_tiles;
   a.row_blocks = plan.row_blocks;
   a.part = static_cast<float*>(workspace);
   a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
