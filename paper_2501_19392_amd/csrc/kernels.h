@@ -272,7 +272,7 @@ struct PagedAttendArgs {
 };
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a);
 // Many queries (bf16): `waves` (4 or 8) x 32 rows per workgroup.
-hipError_t launch_paged_tiles(int n_codewords, int waves, const PagedAttendArgs& a, hipStream_t stream);
+hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 
 // Device-to-device copies of n byte ranges, kCopyRangesPerLaunch per launch (3 KiB of kernel arguments).

@@ -18,6 +18,7 @@ typedef const __attribute__((address_space(4))) int32_t* ConstInts;       // (sc
 inline __device__ ConstInts const_ints(const int32_t* p) { return (ConstInts)(uintptr_t)p; }
 
 constexpr int kTile = 32;                    // tokens of a tile: four groups of 8, each within a page
+constexpr int kTileWaves = 8, kTileRows = 32 * kTileWaves;  // of a workgroup of paged_tiles
 constexpr int kQueryExp = 14;                // largest coordinate of a row's query: 2^13 ... 2^14
 constexpr float kTopExp = 15.0f, kTopWeight = 0x1p15f;      // a weight beyond 2^kTopExp moves the reference,
 constexpr float kStartExp = 8.0f;            // so that the largest is 2^kStartExp: what is 2^-33 of it still counts
@@ -52,10 +53,17 @@ struct Share { int b, piece, pieces, tiles, items; };
 __device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
   return b < a.batch ? max((length_of(a, a.seq_lens[b]) + kTile - 1) / kTile, 1) : 0;
 }
-// tiles per piece
+// tiles per piece with which ceil(tiles / piece) over all sequences is at most max(slots, slots / 2 + batch), whatever the lengths
 __device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int total) {
   const uint32_t room = (uint32_t)max(a.slots - a.batch, max(a.slots / 2, 1));
   return (int)(((uint32_t)total + room - 1) / room);
+}
+// Short pieces make half as many: two waves of one tile take as long as one of two, whose results are half as many to write and to join (one query of
+// 10 000 tokens, 313 tiles: 20.0 us in pieces of one tile, 15.9 of two; of 6000 14.9, 14.6; 5 queries of 2000 tokens of 8 sequences: 20.5 in pieces of two, 18.6 of
+// three, 19.7 of four).  Longer ones want all waves there are (32 x 16 384 tokens: 95 us, on half of the waves 111).
+__device__ __forceinline__ int short_piece(const PagedAttendArgs& a, int total) {
+  const uint32_t half = (uint32_t)max(a.slots / 2, 1);
+  return (int)min(((uint32_t)total + half - 1) / half, 4u);
 }
 // sums over the lanes up to and with this one
 __device__ __forceinline__ int wave_scan(int x) {
@@ -71,7 +79,7 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
   Share s = {-1, 0, 1, 0, 0};
   if (a.batch == 1) {
     const int n = max((length_of(a, const_ints(a.seq_lens)[0]) + kTile - 1) / kTile, 1);
-    s.tiles = piece_tiles(a, n);
+    s.tiles = max((n + a.slots - 1) / a.slots, short_piece(a, n));
     s.items = s.pieces = (n + s.tiles - 1) / s.tiles;
     if (item < s.items) { s.b = 0; s.piece = item; }
     return s;
@@ -83,9 +91,19 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
     total += __builtin_amdgcn_readlane(wave_scan(tiles), 63);
   }
   s.tiles = piece_tiles(a, total);
+  // The fewest tiles that do, where a wave has all lengths: 32 x 16 384 tokens are 512 pieces of 32 tiles then, not 480 of 35 (94.3 us for 95.6).
+  if (a.batch <= 64 && 2 * a.batch <= a.slots) {
+    int low = max((int)(((uint32_t)total + a.slots - 1) / a.slots), 1);
+    while (low < s.tiles) {
+      const int mid = (low + s.tiles) >> 1;
+      if (__builtin_amdgcn_readlane(wave_scan((int)(((uint32_t)tiles + mid - 1) / (uint32_t)mid)), 63) <= a.slots) s.tiles = mid;
+      else low = mid + 1;
+    }
+  }
+  s.tiles = max(s.tiles, short_piece(a, total));
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     if (a.batch > 64) tiles = tiles_of(a, b0 + lane);
-    const int mine = (tiles + s.tiles - 1) / s.tiles;
+    const int mine = (int)((uint32_t)(tiles + s.tiles - 1) / (uint32_t)s.tiles);
     const int end = s.items + wave_scan(mine);             // items up to and with this sequence
     const uint64_t past = __builtin_amdgcn_ballot_w64(end > item);
     if (past != 0 && s.b < 0) {

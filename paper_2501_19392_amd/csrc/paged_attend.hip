@@ -338,25 +338,30 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendA
 }
 
 // How a launch is laid out, from sizes alone (lengths are on the device).
-struct PagedPlan { unsigned blocks, row_tiles; int slots, waves, row_blocks; int64_t items; bool two, merge, many; };
-constexpr int kManyPieces = 64;                            // results of a sequence beyond which the merge has 1024 threads
-constexpr int kFewRows = 64;                               // rows of a kv head that waves of 16 rows take one after the other (bf16)
+struct PagedPlan { unsigned blocks, row_tiles; int slots, row_blocks; int64_t items; bool two, merge, many; };
+// Results of a sequence beyond which the merge has 1024 threads a row, of 256 (one query of 131 072 tokens 41.0 us, for 45.0; beyond 8: 32 x 4000 tokens
+// 37.4 for 34.4).
+constexpr int kManyPieces = 64;
+// Rows of a kv head up to which waves of 32 take them in turn (8 x 9999 tokens, 3 bits: 68 rows 108 us, in tiles of 256 rows 131; 128 rows 93, 135; 32 x 4000:
+// 167, 167 and 150, 170; one sequence of 12 288: 35, 31 and 31, 35; 192 rows of 8 x 9999: 230, 136).
+constexpr int kFewRows = 128;
 template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
   PagedPlan p = {};
   const int64_t rows = max_queries * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
-  if (sizeof(T) == 2 && rows > kFewRows) {                 // workgroups of 128 or 256 rows, one a CU: the tokens in pieces if there are too few of them
-    p.waves = rows > 128 ? 8 : 4;
-    p.row_blocks = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+  if (sizeof(T) == 2 && rows > kFewRows) {                 // workgroups of 256 rows, one a CU: the tokens in pieces if there are too few of them
+    p.row_blocks = (int)((rows + kTileRows - 1) / kTileRows);
     p.slots = (int)std::max<int64_t>(std::min(256 / std::max<int64_t>(batch * H * p.row_blocks, 1), most / 8), 1);
     p.items = batch * p.slots;
     p.merge = p.slots > 1;
     return p;
   }
-  p.two = sizeof(T) == 2 && rows > 16;
+  // 9 to 16 rows fill one column of a wave, but two columns take as long and join their results (16 rows of 8 x 9999 tokens, 3 bits: 37.3 us, in one column
+  // 39.7; of one sequence of 12 288: 18.9, 29.8; of 32 x 4000 46.1, 44.8); 8 rows do not (one sequence of 131 072: 46.5, 40.0).
+  p.two = sizeof(T) == 2 && rows > 8;
   const int per_wave = p.two ? 32 : 16, waves = p.two ? Shape<T, NCW, 2>::kWaves : Shape<T, NCW, 1>::kWaves;
   p.row_tiles = (unsigned)((rows + per_wave - 1) / per_wave);
-  // As many pieces as make all waves that the chip holds, of one tile at least (4 kv heads x 16 384 tokens x 32 sequences: 95.7 us, half as many
-  // 111, twice as many 99; 5 queries of 8 x 9999 37.7, 42.8, 50.7; pieces of two tiles at least: one sequence of 700 tokens 12.4 for 11.1).
+  // As many pieces as make all waves that the chip holds (32 x 16 384 tokens: 95.7 us, half as many 111, twice as many 99; 5 queries of 8 x 9999 37.7, 42.8,
+  // 50.7); the kernel makes fewer of short ones.
   p.slots = (int)std::max<int64_t>((p.two ? Shape<T, NCW, 2>::kSlots : Shape<T, NCW, 1>::kSlots) / (H * p.row_tiles), 1);
   const int64_t pieces = std::min(batch * std::max<int64_t>(most, 1), std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
   if (p.two) {                                             // (a workgroup has results of as many sequences as it has pieces of)
@@ -411,8 +416,8 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   a.heads = plan.merge ? reinterpret_cast<int2*>(a.stats + plan.items * a.max_queries * a.q_heads * 2) : nullptr;
   a.page_groups = a.pool.page_tokens / 8;
   a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
-  if (plan.waves != 0) {
-    if (const hipError_t e = launch_paged_tiles(n_codewords, plan.waves, a, stream)) return e;
+  if (plan.row_blocks != 0) {
+    if (const hipError_t e = launch_paged_tiles(n_codewords, a, stream)) return e;
   } else {
     const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
     const dim3 blocks(plan.blocks, plan.row_tiles);

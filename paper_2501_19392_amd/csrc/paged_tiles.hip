@@ -1,6 +1,6 @@
 // Attention of many queries over pages of codes (a chunk of a prompt behind what is cached): bf16 layers.
 //
-// A workgroup of 4 or 8 waves takes 32 rows (query x query head) a wave of one kv head and walks the tokens in tiles of 64.  The waves turn a tile's
+// A workgroup of 8 waves takes 32 rows (query x query head) a wave of one kv head and walks the tokens in tiles of 64.  The waves turn a tile's
 // codes into fp16 once, for all of them, keys [token][coordinate] and values [coordinate][token] in LDS (two buffers: the next tile is
 // written while this one is multiplied), and multiply with 32x32x16 matrix instructions: S^T = K Q^T, O^T += V^T P.  As in paged_attend.hip the lane
 // that gets scores holds them as the second product wants its operand: V's columns are in that order.
@@ -178,11 +178,10 @@ template <int NCW> struct TileCodes {
 };
 
 // ---------------------------------------------------------------- the kernel
-template <int NCW, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVES / 4, WAVES / 4))) void paged_tiles_kernel(const PagedAttendArgs a) {
+template <int NCW>
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tiles_kernel(const PagedAttendArgs a) {
   typedef Codes<NCW, 1> C;
   constexpr bool kRtn = C::kRtn;
-  constexpr int kParts = 8 / WAVES;                        // shares of a tile's codes that a wave converts
   __shared__ __align__(256) unsigned char lds[C::kTableBytes + 2 * kBufferBytes];
   unsigned char* const buffers = lds + C::kTableBytes;
   const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = uniform(threadIdx.x >> 6);
@@ -190,28 +189,22 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
   // blockIdx: (piece, block of rows: the last ones, which see most tokens, first; kv head), sequence
   const int h = blockIdx.x % a.H, piece = (blockIdx.x / a.H) % a.slots, block = a.row_blocks - 1 - blockIdx.x / a.H / a.slots, b = blockIdx.y;
   const PagedQueries w = paged_queries(a, b);
-  const int rep = a.q_heads / a.H, n_rows = w.n * rep, row0 = block * 32 * WAVES;
+  const int rep = a.q_heads / a.H, n_rows = w.n * rep, row0 = block * kTileRows;
   if (row0 >= n_rows) return;
   const int row = row0 + 32 * wave + col, qi = row / rep, qh = h * rep + row % rep;
   const bool row_there = row < n_rows;
   const int limit = row_there ? w.len - w.count + qi : -1;
   const int wave_first = uniform(w.len - w.count + min(row0 + 32 * wave, n_rows - 1) / rep);      // smallest limit of the wave's rows
-  const int last_limit = uniform(w.len - w.count + min(row0 + 32 * WAVES - 1, n_rows - 1) / rep);
+  const int last_limit = uniform(w.len - w.count + min(row0 + kTileRows - 1, n_rows - 1) / rep);
   const int tiles = (last_limit + kTokens) / kTokens;      // (last_limit >= -len: 0 tiles where nothing is seen)
   const int each = (max(tiles, 0) + a.slots - 1) / a.slots;
   const int t_begin = piece * each * kTokens, t_end = min(t_begin + each * kTokens, last_limit + 1);
 
-  TileCodes<NCW> codes[kParts];
-  const auto request = [&](int t) {
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) codes[i].request(a, b, w.len, h, t, kParts * wave + i, lane);
-  };
-  const auto store = [&](int n) {
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) codes[i].store(lds, buffers + n * kBufferBytes, kParts * wave + i, lane);
-  };
+  TileCodes<NCW> codes;
+  const auto request = [&](int t) { codes.request(a, b, w.len, h, t, wave, lane); };
+  const auto store = [&](int n) { codes.store(lds, buffers + n * kBufferBytes, wave, lane); };
   if (t_begin < t_end) request(t_begin);
-  const int c_exp = C::template stage<WAVES>(points, lds, lane, wave);
+  const int c_exp = C::template stage<kTileWaves>(points, lds, lane, wave);
 
   // ---- the rows' queries
   f16x8 q[8];
@@ -393,11 +386,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
 }  // namespace
 }  // namespace paged
 
-hipError_t launch_paged_tiles(int n_codewords, int waves, const PagedAttendArgs& a, hipStream_t stream) {
+hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)(a.H * a.slots * a.row_blocks), (unsigned)a.batch);
-#define AQUAKV_TILES(NCW)                                                                              \
-  (waves == 8 ? paged::paged_tiles_kernel<NCW, 8><<<grid, 512, 0, stream>>>(a)                         \
-              : paged::paged_tiles_kernel<NCW, 4><<<grid, 256, 0, stream>>>(a))
+#define AQUAKV_TILES(NCW) paged::paged_tiles_kernel<NCW><<<grid, 64 * paged::kTileWaves, 0, stream>>>(a)
   switch (n_codewords) {
     case kRtn2: AQUAKV_TILES(kRtn2); break;
     case kRtn4: AQUAKV_TILES(kRtn4); break;
