@@ -524,9 +524,9 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   page_tokens, row numbers to 0 ... q_rows, and tokens of a page that is not in the pool (page_table outside 0 ... n_pages - 1)
  *   are not seen.  page_table, seq_lens, q_start: aligned to 4 bytes.
  *   bf16: products in fp16 with fp32 sums (queries and grid points rounded to fp16 behind a power of two, weights likewise), results within a
- *   rounding of bf16; fp32: fp32 throughout.
- *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments), for the same arguments or any that are at least as
- *   large; the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same time, captured ones included,
+ *   rounding of bf16; fp32: each of them as the sum of two fp16 numbers (22 bits), fp32 sums.
+ *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments) for the same layer, pages and sizes (other sizes may
+ *   need more, smaller ones too); the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same time, captured ones included,
  *   need workspaces of their own.
  *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.

@@ -279,9 +279,10 @@ class Pages:
         rows = n_pages * page_tokens
         code_bytes, scale_words = rows * layer.kv_heads * layer.code_bytes_per_group, rows * layer.d // layer.rht_group * layer.scale_words_per_group
         for t, size in zip(given, (code_bytes, 2 * scale_words) * 2):
-            if t is None or not t.is_contiguous() or t.nbytes != size:
-                raise ValueError(f"codes and scales of {rows} rows, all four of them, contiguous")
+            if t is None or not t.is_contiguous() or t.nbytes != size or t.get_device() != given[0].get_device():
+                raise ValueError(f"codes and scales of {rows} rows, all four of them, contiguous, on one device")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = given
+        self.device = given[0].get_device()
         self.c = aquakv_pages(n_pages, page_tokens, *(t.data_ptr() for t in given))
 
 
@@ -468,37 +469,51 @@ def aquakv_attend_cache(layers, shape, n_sink, n_compressed, n_recent, score_sca
 
 
 # These are called once per layer and generated token, so looking at their tensors has to be cheap: shapes and strides are asked for once.
-def _rows(x, dtype, row: int, name: str):
+def _here() -> int:
+    """The current device, which tensors have to be on (-1 where there is none: arguments are looked at, nothing is launched)."""
+    return _get_device() if _gpu_ready else torch.cuda.current_device() if torch.cuda.is_available() else -1
+
+
+def _rows(x, dtype, row: int, name: str, device: int):
     """Rows of heads x 128 that may lie apart -> (address, elements from row to row, rows); an address: one behind the other."""
     if x is None or isinstance(x, int):
         return x, row, None
     (n, heads, g), (step, head_step, one) = x.shape, x.stride()
-    if heads * g != row or one != 1 or (head_step != g and heads != 1) or x.dtype is not dtype:
-        raise ValueError(f"{name} must be rows of {row} elements, each contiguous, {dtype}")
+    if heads * g != row or one != 1 or (head_step != g and heads != 1) or x.dtype is not dtype or x.get_device() != device:
+        raise ValueError(f"{name} must be rows of {row} elements, each contiguous, {dtype}, on the current device")
     return x.data_ptr(), step if n > 1 else row, n
 
 
-def _typed(x, dtype, n: int, name: str):
+def _typed(x, dtype, n: int, name: str, device: int):
     """A tensor of n elements, or an address."""
     if x is None or isinstance(x, int):
         return x
-    if x.dtype is not dtype or x.numel() != n or not x.is_contiguous():
-        raise ValueError(f"{name} must be {n} elements of {dtype}")
+    if x.dtype is not dtype or x.numel() != n or not x.is_contiguous() or x.get_device() != device:
+        raise ValueError(f"{name} must be {n} elements of {dtype} on the current device")
     return x.data_ptr()
 
 
+def _pool_here(pages, device: int) -> None:
+    if pages.__class__ is Pages and pages.device != device:
+        raise ValueError("the pages are not on the current device")
+
+
 def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_cos, rope_sin, Khat, Vhat, stream=None) -> None:
-    """K, V: [tokens, kv_heads, 128], rows may lie apart; rope_cos, rope_sin: [rope_rows, 64] tensors (None: no rotation, positions unused)."""
-    row, dtype = layer.d, layer.dtype
-    k, ks, nk = _rows(K, dtype, row, "K")
-    v, vs, nv = _rows(V, dtype, row, "V")
+    """K, V: [tokens, kv_heads, 128], rows may lie apart; rope_cos, rope_sin: [rope_rows, 64] tensors (None: no rotation, positions unused).
+    Tensors have to be on the current device (ValueError otherwise), whose current stream is taken unless one is given."""
+    row, dtype, here = layer.d, layer.dtype, _here()
+    _pool_here(pages, here)
+    k, ks, nk = _rows(K, dtype, row, "K", here)
+    v, vs, nv = _rows(V, dtype, row, "V", here)
     if (nk is not None and nk != tokens) or (nv is not None and nv != tokens):
         raise ValueError(f"K and V must have {tokens} rows")
     angles = 0 if rope_cos is None else rope_cos.numel()
-    _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, tokens, "slots"),
-                                    _typed(positions, torch.int32, tokens, "positions"), _typed(rope_cos, torch.float32, angles, "rope_cos"),
-                                    _typed(rope_sin, torch.float32, angles, "rope_sin"), angles // 64,
-                                    _typed(Khat, dtype, tokens * row, "Khat"), _typed(Vhat, dtype, tokens * row, "Vhat"), _stream(stream)))
+    _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, tokens, "slots", here),
+                                    _typed(positions, torch.int32, tokens, "positions", here),
+                                    _typed(rope_cos, torch.float32, angles, "rope_cos", here),
+                                    _typed(rope_sin, torch.float32, angles, "rope_sin", here), angles // 64,
+                                    _typed(Khat, dtype, tokens * row, "Khat", here), _typed(Vhat, dtype, tokens * row, "Vhat", here),
+                                    _stream(stream)))
 
 
 def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_pages: int, q_rows: int, max_queries: int) -> int:
@@ -507,17 +522,22 @@ def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_p
 
 def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
                         workspace, stream=None) -> None:
-    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence]."""
-    row, dtype = q_heads * layer.head_dim, layer.dtype
-    at, stride, q_rows = _rows(q, dtype, row, "q")
+    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence].  Tensors have to be on the current
+    device (ValueError otherwise), whose current stream is taken unless one is given."""
+    row, dtype, here = q_heads * layer.head_dim, layer.dtype, _here()
+    _pool_here(pages, here)
+    at, stride, q_rows = _rows(q, dtype, row, "q", here)
     if page_table.dim() != 2 or page_table.shape[0] != batch:
         raise ValueError("page_table must be [batch, pages]")
     pages_each = page_table.shape[1]
+    if workspace.__class__ is torch.Tensor and workspace.get_device() != here:
+        raise ValueError("workspace is not on the current device")
     ws, nbytes = _ws(workspace)
-    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads, _typed(page_table, torch.int32, batch * pages_each, "page_table"),
-                                    pages_each, _typed(seq_lens, torch.int32, batch, "seq_lens"), q_rows, max_queries,
-                                    _typed(q_start, torch.int32, batch + 1, "q_start"), at, stride, score_scale,
-                                    _typed(out, dtype, q_rows * row, "out"), ws, nbytes, _stream(stream)))
+    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads,
+                                    _typed(page_table, torch.int32, batch * pages_each, "page_table", here), pages_each,
+                                    _typed(seq_lens, torch.int32, batch, "seq_lens", here), q_rows, max_queries,
+                                    _typed(q_start, torch.int32, batch + 1, "q_start", here), at, stride, score_scale,
+                                    _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
 
 
 def aquakv_fit_workspace_bytes(d_in: int, d_out: int) -> int:

@@ -156,13 +156,14 @@ def test_attention_over_pages(fmt, dtype, H, QH, lengths, page, queries):
     print(f"  worst {P.check(out, want, bound, fmt):.3g} of the bound", flush=True)
 
 
+@pytest.mark.parametrize("queries", [1, 3, 40])
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "grid256"), ("bf16", "rtn4"), ("bf16", "grid16"), ("fp32", "grid256")])
-def test_rows_without_tokens_and_pages_outside_the_pool(dtype, fmt):
+def test_rows_without_tokens_and_pages_outside_the_pool(dtype, fmt, queries):
     """Empty and too short sequences (queries that see nothing: 0), lengths over the table's room or below zero, pages that are not
     there in the middle and at the end."""
     need_gpu()
     page, lengths = 8, [0, 2, 100, 40, 64]
-    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 2, 8, lengths, page, 3)
+    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 2, 8, lengths, page, queries)
     table[2, 3], table[2, 12] = -1, pages.n_pages
     table[3, :] = torch.tensor([1 << 30] * table.shape[1])                 # nothing of this sequence is there
     lens = torch.tensor([0, 2, 100, 40, 10 ** 9], dtype=torch.int32)       # ... the last: as much as the table has room for
@@ -170,10 +171,11 @@ def test_rows_without_tokens_and_pages_outside_the_pool(dtype, fmt):
     out = attend(lg, pages, table, lens, q, counts)
     want, bound = P.reference(lo, pages, table, lens, q, counts, SCALE, dtype)
     P.check(out, want, bound, fmt)
-    assert (out[:3] == 0).all() and (out[3] == 0).all() and (out[9:12] == 0).all()
+    n = queries
+    assert (out[:n] == 0).all() and (out[n:n + max(n - 2, 0)] == 0).all() and (out[3 * n:4 * n] == 0).all()
     lens[1] = -5
     out = attend(lg, pages, table, lens, q, counts)
-    assert (out[:6] == 0).all()
+    assert (out[:2 * n] == 0).all()
 
 
 @pytest.mark.parametrize("dtype,fmt,ragged,most", [("bf16", "grid256", [1, 0, 5, 2], 5), ("bf16", "rtn4", [40, 3, 0, 1], 40), ("bf16", "grid256", [15, 1, 14, 0], 15),
@@ -205,13 +207,14 @@ def test_ragged_queries_leave_other_rows_alone(dtype, fmt, ragged, most):
     attend(lg, pages, table, lens, joint[:, 4:], counts, q_start=wild, max_queries=1, out=out)
 
 
-@pytest.mark.parametrize("dtype,fmt", [("bf16", "grid256"), ("bf16", "rtn4"), ("bf16", "rtn2"), ("fp32", "grid256"), ("fp32", "rtn4")])
+@pytest.mark.parametrize("dtype,fmt,queries", [("bf16", "grid256", 2), ("bf16", "rtn4", 2), ("bf16", "rtn2", 2), ("fp32", "grid256", 2), ("fp32", "rtn4", 2),
+                                               ("bf16", "grid256", 5), ("bf16", "rtn4", 5), ("bf16", "grid256", 40), ("bf16", "rtn4", 40)])
 @pytest.mark.parametrize("kind", ["sink", "rising", "huge", "tiny", "zero", "outlier", "negative"])
-def test_scores_and_scales_of_any_size(dtype, fmt, kind):
+def test_scores_and_scales_of_any_size(dtype, fmt, queries, kind):
     """One token that outweighs all others, a maximum that grows to the end, scales at both ends of fp16, zero rows, one value row a
     thousand times the others', a negative score scale."""
     need_gpu()
-    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 1, 4, [600], 16, 2)
+    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 1, 4, [600], 16, queries)
     rows = P.sequence_rows(pages, table[0], 600)
     ks, vs = (t[..., 0] if lo.rtn_bits is not None else t for t in (pages.k_scales, pages.v_scales))
     set_to = lambda t, r, x: t.__setitem__(r.cuda(), torch.as_tensor(x).half().view(torch.int16).cuda().view(-1, *[1] * (t.dim() - 1)))
@@ -235,11 +238,12 @@ def test_scores_and_scales_of_any_size(dtype, fmt, kind):
     print(f"  {fmt} {kind}: worst {P.check(out, want, bound, kind):.3g} of the bound", flush=True)
 
 
-def test_queries_of_any_size_and_not_finite_ones_stay_among_themselves():
+@pytest.mark.parametrize("H,queries", [(2, 3), (1, 3), (1, 40)])
+def test_queries_of_any_size_and_not_finite_ones_stay_among_themselves(H, queries):
     """A query's size is no matter of the others': rows of 1e30, 1e-30 and zeros, and a row that is not finite gives such a row and no other."""
     need_gpu()
     for fmt in ("grid256", "rtn4"):
-        lo, lg, pages, table, lens, q, counts = build("bf16", fmt, 1, 4, [300], 16, 3)
+        lo, lg, pages, table, lens, q, counts = build("bf16", fmt, H, 4, [300], 16, queries)
         q[0, 0] = 0
         q[1, 1] *= 1e-30
         want, bound = P.reference(lo, pages, table, lens, q, counts, SCALE, "bf16")
@@ -254,6 +258,62 @@ def test_queries_of_any_size_and_not_finite_ones_stay_among_themselves():
         out = attend(lg, pages, table, lens, q, counts)
         want, _ = P.reference(lo, pages, table, lens, q, counts, SCALE, "bf16")
         P.check(out, want, 2.0 ** -8 * want.norm(dim=-1) + 2.0 ** -10 * want.norm(dim=-1) + 1e-6, fmt)
+
+
+@pytest.mark.parametrize("fmt", ["grid256", "rtn4"])
+@pytest.mark.parametrize("rows", [8, 9, 16, 17, 32, 33, 64, 65, 128, 129, 256, 257])
+def test_rows_of_a_kv_head(fmt, rows):
+    """As many rows as waves and workgroups hold, and one more; sequences that are cut into several pieces, end with them, have one, or none."""
+    need_gpu()
+    lo, lg, pages, table, lens, q, counts = build("bf16", fmt, 2, 2, [650, 64, 1, 0, 33, 2048], 64, rows)
+    P.check(attend(lg, pages, table, lens, q, counts), *P.reference(lo, pages, table, lens, q, counts, SCALE, "bf16"), f"{fmt} {rows}")
+
+
+@pytest.mark.parametrize("dtype,fmt,batch,QH,ragged", [("bf16", "grid256", 64, 4, False), ("bf16", "grid256", 65, 4, True), ("bf16", "rtn4", 130, 24, True),
+                                                       ("bf16", "grid16", 130, 24, False), ("fp32", "grid64", 70, 2, True), ("bf16", "rtn2", 70, 280, False)])
+def test_many_sequences_that_share_pages(dtype, fmt, batch, QH, ragged):
+    """More sequences than a wave has lanes, of any lengths, some without tokens or queries; all of them begin with the first one's pages."""
+    need_gpu()
+    gen = torch.Generator().manual_seed(batch + QH)
+    lengths = (torch.rand(batch, generator=gen) ** 3 * 300).long().tolist()
+    lengths[0], lengths[5], lengths[-1] = 333, 0, 1
+    most = 2 if ragged else 1
+    counts = torch.randint(0, most + 1, (batch,), generator=gen).tolist() if ragged else [1] * batch
+    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 2, QH, lengths, 32, 1, 3, ragged=counts)
+    for b in range(1, batch):
+        if lengths[b] >= 64:
+            table[b, :2] = table[0, :2]
+    start = torch.tensor([0, *np.cumsum(counts)], dtype=torch.int32, device="cuda") if ragged else None
+    out = attend(lg, pages, table, lens, q, counts, q_start=start, max_queries=most)
+    P.check(out, *P.reference(lo, pages, table, lens, q, counts, SCALE, dtype), f"{fmt} {batch}")
+
+
+@pytest.mark.parametrize("fmt,QH", [("grid256", 1), ("rtn4", 3), ("grid64", 10)])
+def test_a_long_sequence(fmt, QH):
+    need_gpu()
+    lo, lg, pages, table, lens, q, counts = build("bf16", fmt, 1, QH, [70001, 3], 256, 1)
+    P.check(attend(lg, pages, table, lens, q, counts), *P.reference(lo, pages, table, lens, q, counts, SCALE, "bf16"), fmt)
+
+
+def test_tensors_that_are_not_on_the_device():
+    need_gpu()
+    from paper_2501_19392_amd import binding as B
+    lo, lg, pages, table, lens, q, counts = build("bf16", "grid256", 2, 4, [50, 20], 16, 1)
+    ws = torch.empty(B.aquakv_paged_workspace_bytes(lg, pages, 2, 4, table.shape[1], 2, 1), dtype=torch.uint8, device="cuda")
+    good = dict(page_table=table.cuda(), seq_lens=lens.cuda(), q=q, q_start=None, out=torch.empty_like(q), workspace=ws)
+    for name, at in dict(page_table=table, seq_lens=lens, q=q.cpu(), q_start=torch.tensor([0, 1, 2], dtype=torch.int32), out=q.cpu(), workspace=ws.cpu()).items():
+        k = {**good, name: at}
+        with pytest.raises(ValueError, match="device"):
+            B.aquakv_paged_attend(lg, pages, 2, 4, k["page_table"], k["seq_lens"], k["q"], 1, k["q_start"], SCALE, k["out"], k["workspace"])
+    K = torch.zeros(2, 2, 128, dtype=torch.bfloat16, device="cuda")
+    cos, sin = angles(9)
+    good = dict(K=K, V=K, slots=torch.tensor([1, 2], device="cuda"), positions=torch.zeros(2, dtype=torch.int32, device="cuda"), cos=cos, sin=sin, Khat=None)
+    for name, t in dict(K=K.cpu(), V=K.cpu(), slots=torch.tensor([1, 2]), positions=torch.zeros(2, dtype=torch.int32), cos=cos.cpu(), sin=sin.cpu(), Khat=K.cpu()).items():
+        k = {**good, name: t}
+        with pytest.raises(ValueError, match="device"):
+            B.aquakv_paged_append(lg, pages, 2, k["K"], k["V"], k["slots"], k["positions"], k["cos"], k["sin"], k["Khat"], None)
+    with pytest.raises(ValueError, match="device"):
+        B.Pages(lg, pages.n_pages, 16, k_codes=pages.k_codes, k_scales=pages.k_scales, v_codes=pages.v_codes.cpu(), v_scales=pages.v_scales)
 
 
 def test_a_pool_beyond_32_bits():
