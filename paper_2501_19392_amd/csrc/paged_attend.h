@@ -4,7 +4,8 @@
 // Precision.  Operands are fp16 (11 bits): the rotated query times a power of two of its own, grid points times a power of two of
 // the grid's, weights times the token's scale relative to a running reference, all sums fp32.  fp32 layers hold each of them as two
 // fp16 numbers (22 bits) and take three products.  Uniform codes and zero points are exact: a code at the low end of a half-word is the
-// subnormal fp16 number code * 2^-24, which the matrix instructions take as it is, so that a mask is all the conversion there is.
+// subnormal fp16 number code * 2^-24, which the matrix instructions take as it is, so that a mask is all the conversion there is (fp32
+// layers make it a normal number, which sums need that are to be exact beyond 2^-17).
 #pragma once
 #include "codec_core.h"
 #include "kernels.h"
@@ -189,16 +190,26 @@ __device__ __forceinline__ uint32_t f16_pair(float x, float y) {
   const f16x2 h = {(_Float16)x, (_Float16)y};
   return __builtin_bit_cast(uint32_t, h);
 }
-// x as one fp16 number (TERMS = 1), or as the sum of two
+__device__ __forceinline__ f16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(f16x8, u32x4{a, b, c, d}); }
+// x as one fp16 number (TERMS = 1), or as the sum of two: the second is what the first leaves, of that very first number.  (The compiler would round x twice,
+// once from the product that x comes from and once from x, and the two may be neighbours: scores of such rows were off by 2^-13 of a coordinate.)
 template <int TERMS> __device__ __forceinline__ void split_f16(const float (&x)[8], f16x8 (&out)[TERMS]) {
+  uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    out[0][i] = (_Float16)x[i];
-    if constexpr (TERMS == 2) out[1][i] = (_Float16)(x[i] - (float)out[0][i]);
+  for (int i = 0; i < 4; ++i) w[i] = f16_pair(x[2 * i], x[2 * i + 1]);
+  if constexpr (TERMS == 2) {
+    uint32_t rest[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      asm("" : "+v"(w[i]));
+      const f16x2 h = __builtin_bit_cast(f16x2, w[i]);
+      rest[i] = f16_pair(x[2 * i] - (float)h[0], x[2 * i + 1] - (float)h[1]);
+    }
+    out[1] = operand(rest[0], rest[1], rest[2], rest[3]);
   }
+  out[0] = operand(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(f16x8, u32x4{a, b, c, d}); }
 
 // ---------------------------------------------------------------- codes
 template <int NCW, int TERMS> struct Codes {
@@ -237,9 +248,10 @@ template <int NCW, int TERMS> struct Codes {
 #pragma unroll
     for (int i = 0; i < kPoints; ++i) {
       const float x = __builtin_ldexpf(p.x[2 * i], -e), y = __builtin_ldexpf(p.x[2 * i + 1], -e);
-      const uint32_t hi = f16_pair(x, y);
+      uint32_t hi = f16_pair(x, y);
       uint32_t other = hi;
       if constexpr (TERMS == 2) {
+        asm("" : "+v"(hi));                                // (as in split_f16)
         const f16x2 h = __builtin_bit_cast(f16x2, hi);
         other = f16_pair(x - (float)h[0], y - (float)h[1]);
       }
@@ -336,13 +348,22 @@ template <int NCW, int TERMS> struct Codes {
       }
     }
     if constexpr (kRtn) {
-      qsum[0] = column_sum(qsum[0]) * 0x1p-24f;
-      qsum[1] = column_sum(qsum[1]) * 0x1p-24f;
+      qsum[0] = __builtin_ldexpf(column_sum(qsum[0]), -kFieldExp);
+      qsum[1] = __builtin_ldexpf(column_sum(qsum[1]), -kFieldExp);
     }
   }
   // uniform: the k-th field of a half-word is masked in place, and so this many times its code
   static constexpr int field_scale(int k) { return 1 << (NCW * k); }
   static constexpr uint32_t field_mask(int k) { return 0x00010001u * (((1u << NCW) - 1u) << (NCW * k)); }
+  // ... as fp16 numbers.  One term: the bits as they are, a subnormal number, times 2^-kFieldExp.  Two terms: a normal number, by way of 1024 + it (the
+  // matrix instructions align products by their exponents before they add them, and a subnormal number's is 10 above its bits: sums kept about 2^-17).
+  static constexpr int kFieldExp = TERMS == 1 ? 24 : 0;
+  static __device__ __forceinline__ uint32_t small_ints(uint32_t x) {
+    if constexpr (TERMS == 1) return x;
+    const f16x2 k = {(_Float16)1024.0f, (_Float16)1024.0f};
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x | 0x64006400u) - k);
+  }
+  static __device__ __forceinline__ uint32_t field(uint32_t x, int k) { return small_ints(x & field_mask(k)); }
   static constexpr int kFields = NCW == kRtn4 ? 2 : 4;     // fields of a byte
 
   // ---- a tile's codes and scales on their way: keys of tokens 8 (m / 4) + m % 4 (+ 4), the lane group's share of the coordinates;
@@ -437,7 +458,7 @@ template <int NCW, int TERMS> struct Codes {
     return (float)h[e];
   }
   static __device__ __forceinline__ float int_at(const u32x4& w, int e) { return (float)((w[e >> 1] >> (16 * (e & 1))) & 0xffffu); }
-  // the values' scales of the lane's tokens, per half (kHalves), and their zero points: fp16 numbers (times 2^-24).  `there`: those from it on are 0
+  // the values' scales of the lane's tokens, per half (kHalves), and their zero points: fp16 numbers (times 2^-kFieldExp).  `there`: those from it on are 0
   static constexpr int kHalves = kRtn ? 2 : 1;
   static __device__ __forceinline__ void keep_first(u32x4& w, int there) {
 #pragma unroll
@@ -447,7 +468,7 @@ template <int NCW, int TERMS> struct Codes {
   static __device__ __forceinline__ f16x8 zero_points(const unsigned char* lds, int k, int g, int there) {
     u32x4 w = eight(lds, kValues + 2 * k + 1, g);
     if (there < 8) keep_first(w, there);
-    return __builtin_bit_cast(f16x8, w);
+    return operand(small_ints(w.x), small_ints(w.y), small_ints(w.z), small_ints(w.w));
   }
   // power of two of the largest scale of the lane's tokens (at least the smallest fp16 number's)
   static __device__ __forceinline__ float lift_of(const u32x4 (&vs)[kHalves]) {
@@ -508,7 +529,7 @@ template <int NCW, int TERMS> struct Codes {
         uint32_t y[4];
         const uint32_t d = NCW == kRtn4 ? x[j] : (j & 1) ? x[j >> 1] >> 8 : x[j >> 1];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = NCW == kRtn4 ? ((i & 2) ? d >> 8 : d) & field_mask(i & 1) : d & field_mask(i);
+        for (int i = 0; i < 4; ++i) y[i] = NCW == kRtn4 ? field((i & 2) ? d >> 8 : d, i & 1) : field(d, i);
         const f16x8 k = operand(y[0], y[1], y[2], y[3]);
 #pragma unroll
         for (int n = 0; n < TERMS; ++n)
@@ -586,7 +607,7 @@ template <int NCW, int TERMS> struct Codes {
           for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(d[2 * i + 1], d[2 * i], 0x0c040c00u + 0x00010001u * (2 * k + byte));
 #pragma unroll
           for (int f = 0; f < kFields; ++f) {
-            const f16x8 v = operand(x[0] & field_mask(f), x[1] & field_mask(f), x[2] & field_mask(f), x[3] & field_mask(f));
+            const f16x8 v = operand(field(x[0], f), field(x[1], f), field(x[2], f), field(x[3], f));
             const int j = 4 * k + kFields * byte + f;
 #pragma unroll
             for (int i = 0; i < COLS; ++i)

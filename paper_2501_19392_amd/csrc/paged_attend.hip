@@ -101,7 +101,7 @@ paged_attend_kernel(const PagedAttendArgs a) {
 #pragma unroll
     for (int r = 0; r < 32; ++r) top = fmaxf(top, fabsf(x[r]));
     const int e = max(__builtin_amdgcn_frexp_expf(column_max(top) * fabsf(by)), -100);
-    col[i].f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? 24 : c_exp), 126));
+    col[i].f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? C::kFieldExp : c_exp), 126));
     const float scaled = __builtin_ldexpf(by, kQueryExp - e);
 #pragma unroll
     for (int r = 0; r < 32; ++r) x[r] *= scaled;
@@ -211,7 +211,7 @@ paged_attend_kernel(const PagedAttendArgs a) {
       for (int i = 0; i < COLS; ++i) {
         const float sum = column_sum(col[i].sum);
         float x[32];
-        C::result(col[i], kRtn ? 24 : c_exp, x);
+        C::result(col[i], kRtn ? C::kFieldExp : c_exp, x);
         f32x4* const to = place(wave, i);
 #pragma unroll
         for (int r = 0; r < 8; ++r) to[64 * r + again] = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
@@ -226,7 +226,7 @@ paged_attend_kernel(const PagedAttendArgs a) {
   for (int i = 0; i < COLS; ++i) {
     const int row = row0 + 16 * i + (again & 15), qi = row / rep, qh = h * rep + row % rep;
     float x[32], ref = col[i].ref, sum = column_sum(col[i].sum);
-    C::result(col[i], kRtn ? 24 : c_exp, x);
+    C::result(col[i], kRtn ? C::kFieldExp : c_exp, x);
     if constexpr (kJoined) {
 #pragma unroll 1
       for (int n = 1; n <= others; ++n) {

@@ -295,6 +295,61 @@ def test_a_long_sequence(fmt, QH):
     P.check(attend(lg, pages, table, lens, q, counts), *P.reference(lo, pages, table, lens, q, counts, SCALE, "bf16"), fmt)
 
 
+@pytest.mark.parametrize("fmt", ["grid256", "grid64", "grid16", "rtn4", "rtn2"])
+def test_scores_of_fp32_layers(fmt):
+    """4096 rows over two tokens, of which the second has a score of 0 and no value, so that a row gives sigmoid(score) v: what a score is off by shows.
+
+    Off by at most A (3 * 2^-22 + 44 * 2^-24), A = scale * sum |q_i| |k_i| (uniform: |q_i| step (code + zero)) over the products as they are taken: query and grid
+    point are two fp16 numbers each (2^-22 of either), the product of the two second ones is left out (2^-22), and 12 instructions add 32 products each
+    (44 roundings on a product's way).  Behind it, relative to the result: the exponent's argument, 2^-22 |score|, and all else, 2^-20."""
+    need_gpu()
+    lo, lg, pages, table, lens, q, counts = build("fp32", fmt, 1, 64, [2], 8, 1)
+    rtn = lo.rtn_bits is not None
+    first = int(table[0, 0]) * 8
+    for t in (pages.k_scales, pages.v_scales):
+        (t[..., 0] if rtn else t)[first + 1] = 0
+    gen = torch.Generator().manual_seed(21)
+    batch = 64
+    q = (1.5 * torch.randn(batch, 64, 128, generator=gen)).cuda()
+    out = attend(lg, pages, table.repeat(batch, 1), lens.repeat(batch), q, [1] * batch).double().cpu()
+    k, v = (P.held(lo, c[first:first + 1], s[first:first + 1], sg)[0, 0] for c, s, sg in
+            ((pages.k_codes, pages.k_scales, lo.signs_k), (pages.v_codes, pages.v_scales, lo.signs_v)))
+    x = q.double().cpu()
+    score = SCALE * (x @ k)
+    if rtn:
+        step, zero = (pages.k_scales[first, :, i].cpu() for i in (0, 1))
+        offset = (step.view(torch.float16).double() * zero.double()).repeat_interleave(64)
+        A = SCALE * (x.abs() @ (k.abs() + 2 * offset))
+    else:
+        d = torch.arange(128)
+        odd = sum((d[:, None] & d) >> i & 1 for i in range(7)) % 2
+        rot = (1.0 - 2.0 * odd.double()) / 128 ** 0.5 * torch.as_tensor(lo.signs_k).double().view(1, 128)
+        A = SCALE * ((x @ rot.T).abs() @ (rot @ k).abs())
+    p = torch.sigmoid(score)
+    off = (out - p[..., None] * v).norm(dim=-1) / (p * v.norm())
+    bound = (1 - p) * A * (3 * 2.0 ** -22 + 44 * 2.0 ** -24) + score.abs() * 2.0 ** -22 + 2.0 ** -20
+    print(f"  {fmt}: worst {(off / bound).max().item():.3g} of the bound, {off.max().item():.3g}", flush=True)
+    assert (off <= bound).all()
+
+
+@pytest.mark.parametrize("fmt", ["grid256", "grid16", "rtn4", "rtn2"])
+def test_fp32_layers_beside_plain_fp32(fmt):
+    """Errors like those of the same attention in plain fp32: what is rounded to 22 bits instead of 24 is off by four times as much, three such factors (query,
+    key, weight and value) by 4 sqrt(3) < 8, in the root mean square over 512 rows of 700 tokens."""
+    need_gpu()
+    lo, lg, pages, table, lens, q, counts = build("fp32", fmt, 1, 64, [700] * 8, 32, 1, spread=0.3)
+    out = attend(lg, pages, table, lens, q, counts).double().cpu()
+    want, _ = P.reference(lo, pages, table, lens, q, counts, SCALE, "fp32")
+    K, V = (P.held(lo, c, s, sg)[:, 0].float() for c, s, sg in ((pages.k_codes, pages.k_scales, lo.signs_k), (pages.v_codes, pages.v_scales, lo.signs_v)))
+    plain = torch.empty_like(want)
+    for b in range(8):
+        rows = P.sequence_rows(pages, table[b], 700)
+        plain[b] = (torch.softmax((q[b].cpu() @ K[rows].T) * SCALE, -1) @ V[rows]).double()
+    rms = [((x - want).norm(dim=-1) / want.norm(dim=-1)).square().mean().sqrt().item() for x in (out, plain)]
+    print(f"  {fmt}: {rms[0]:.3g}, plain {rms[1]:.3g}", flush=True)
+    assert rms[0] <= 8 * rms[1]
+
+
 def test_tensors_that_are_not_on_the_device():
     need_gpu()
     from paper_2501_19392_amd import binding as B
