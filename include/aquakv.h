@@ -526,8 +526,9 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   bf16: products in fp16 with fp32 sums (queries and grid points rounded to fp16 behind a power of two, weights likewise), results within a
  *   rounding of bf16; fp32: each of them as the sum of two fp16 numbers (22 bits), fp32 sums.
  *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments) for the same layer, pages and sizes (other sizes may
- *   need more, smaller ones too); the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same time, captured ones included,
- *   need workspaces of their own.
+ *   need more, smaller ones too); the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same
+ *   time, captured ones included, need workspaces of their own.  At most 65535 sequences, max_queries * q_heads < 2^22, batch *
+ *   kv_heads < 2^25, table_pages * page_tokens < 2^31 - 4096 and 2^35 over the batch: AQUAKV_EUNSUPPORTED beyond.
  *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.
  */

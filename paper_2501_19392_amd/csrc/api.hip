@@ -1675,7 +1675,9 @@ int check_paged_shape(const aquakv_layer* L, const aquakv_pages* pg, int32_t bat
     return fail(AQUAKV_EINVAL, "batch=%d table_pages=%d q_rows=%lld max_queries=%d", batch, table_pages, (long long)q_rows, max_queries);
   if (q_heads < 1 || q_heads % L->kv_heads) return fail(AQUAKV_EINVAL, "q_heads=%d must be a multiple of kv_heads=%d", q_heads, L->kv_heads);
   if (batch > 65535) return fail(AQUAKV_EUNSUPPORTED, "batch=%d: at most 65535 sequences", batch);
-  if ((int64_t)max_queries * q_heads >= (1 << 24) || (int64_t)max_queries * (q_heads / L->kv_heads) > 16 * 65535 || q_rows > 0x7fffffffLL)
+  // (threads of a launch: below 2^32, up to 1024 a row where results are joined, 64 a sequence and kv head, 16 rows a block of the other grid dimension)
+  if ((int64_t)max_queries * q_heads >= (1 << 22) || (int64_t)batch * L->kv_heads >= (1 << 25) ||
+      (int64_t)max_queries * (q_heads / L->kv_heads) > 16 * 65535 || q_rows > 0x7fffffffLL)
     return fail(AQUAKV_EUNSUPPORTED, "%lld rows, %d queries of %d heads", (long long)q_rows, max_queries, q_heads);
   if ((int64_t)table_pages * pg->page_tokens > 0x7fffffffLL - 4096 || (int64_t)table_pages * pg->page_tokens * (batch > 0 ? batch : 1) > ((int64_t)1 << 35))
     return fail(AQUAKV_EUNSUPPORTED, "%d sequences of up to %d pages of %d tokens", batch, table_pages, pg->page_tokens);

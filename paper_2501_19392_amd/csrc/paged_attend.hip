@@ -347,7 +347,7 @@ constexpr int kManyPieces = 64;
 constexpr int kFewRows = 128;
 template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
   PagedPlan p = {};
-  const int64_t rows = max_queries * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
+  const int64_t rows = std::max<int64_t>(max_queries, 1) * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
   if (sizeof(T) == 2 && rows > kFewRows) {                 // workgroups of 256 rows, one a CU: the tokens in pieces if there are too few of them
     p.row_blocks = (int)((rows + kTileRows - 1) / kTileRows);
     p.slots = (int)std::max<int64_t>(std::min(256 / std::max<int64_t>(batch * H * p.row_blocks, 1), most / 8), 1);

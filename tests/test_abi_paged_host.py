@@ -167,3 +167,19 @@ def test_the_binding_looks_at_its_tensors():
     for t, n, x, o in bad:
         with pytest.raises(ValueError):
             B.aquakv_paged_attend(lay, pages, 2, 4, t, n, x, 1, None, 1.0, o, slots)
+
+
+@pytest.mark.parametrize("name", ["batch", "q_rows", "max_queries"])
+def test_the_size_of_nothing(name):
+    c = Buffers()
+    c.n[name] = 0
+    assert c.size() > 0                                                     # (a call that has nothing to do still wants a workspace)
+
+
+@pytest.mark.parametrize("kw", [dict(max_queries=1 << 17, q_rows=1 << 17), dict(max_queries=1, q_heads=1 << 22, q_stride=128 << 22),
+                                dict(batch=65535, max_queries=1, q_heads=4096, q_stride=128 * 4096, kv_heads=4096)])
+def test_more_than_a_launch_holds(kw):
+    """Threads of one launch stay below 2^32."""
+    c = Buffers(**({"kv_heads": kw["kv_heads"]} if "kv_heads" in kw else {}))
+    c.n.update({k: v for k, v in kw.items() if k != "kv_heads"})
+    assert c.attend() == B.AQUAKV_EUNSUPPORTED and c.size() == 0

@@ -91,6 +91,28 @@ def test_rows_go_to_their_slots(dtype, fmt, H, tokens, page, rope, apart, hats):
             assert (got[out.numpy()] == 7.0).all()
 
 
+@pytest.mark.parametrize("fmt", ["grid16", "grid64", "grid256"])
+@pytest.mark.parametrize("hat", ["K", "V"])
+def test_without_a_search_table_the_codes_are_the_same(fmt, hat):
+    need_gpu()
+    from paper_2501_19392_amd import binding as B
+    lo, lg, pages = P.make(3, "bf16", fmt, 9, 8)
+    other = B.Layer(3, 128, lg.codebook, lg.signs_k, lg.signs_v, torch.bfloat16)
+    pools = [pages, B.Pages(other, 9, 8)]
+    gen = torch.Generator().manual_seed(3)
+    K, V = ((torch.randn(67, 3, 128, generator=gen) * torch.randn(3, 128, generator=gen).exp()).bfloat16().cuda() for _ in range(2))
+    slots, hats = torch.randperm(72, generator=gen)[:67].cuda(), []
+    for layer, p in zip((lg, other), pools):
+        for t in (p.k_codes, p.v_codes, p.k_scales, p.v_scales):
+            t.zero_()
+        hats.append(torch.empty_like(K))
+        B.aquakv_paged_append(layer, p, 67, K, V, slots, None, None, None, hats[-1] if hat == "K" else None, hats[-1] if hat == "V" else None)
+    torch.cuda.synchronize()
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        assert torch.equal(getattr(pools[0], name), getattr(pools[1], name)), name
+    assert torch.equal(*hats)
+
+
 def test_zero_rows_and_no_tokens():
     need_gpu()
     from paper_2501_19392_amd import binding as B
@@ -209,10 +231,10 @@ def test_ragged_queries_leave_other_rows_alone(dtype, fmt, ragged, most):
 
 @pytest.mark.parametrize("dtype,fmt,queries", [("bf16", "grid256", 2), ("bf16", "rtn4", 2), ("bf16", "rtn2", 2), ("fp32", "grid256", 2), ("fp32", "rtn4", 2),
                                                ("bf16", "grid256", 5), ("bf16", "rtn4", 5), ("bf16", "grid256", 40), ("bf16", "rtn4", 40)])
-@pytest.mark.parametrize("kind", ["sink", "rising", "huge", "tiny", "zero", "outlier", "negative"])
+@pytest.mark.parametrize("kind", ["sink", "rising", "huge", "tiny", "zero", "outlier", "negative", "flat"])
 def test_scores_and_scales_of_any_size(dtype, fmt, queries, kind):
     """One token that outweighs all others, a maximum that grows to the end, scales at both ends of fp16, zero rows, one value row a
-    thousand times the others', a negative score scale."""
+    thousand times the others', a score scale that is negative, or 0."""
     need_gpu()
     lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 1, 4, [600], 16, queries)
     rows = P.sequence_rows(pages, table[0], 600)
@@ -232,7 +254,7 @@ def test_scores_and_scales_of_any_size(dtype, fmt, queries, kind):
     elif kind == "outlier":
         set_to(vs, rows[300:301], [1000.0]); set_to(vs, rows[:64], [1e-6] * 64)
     else:
-        scale = -SCALE
+        scale = -SCALE if kind == "negative" else 0.0
     out = attend(lg, pages, table, lens, q, counts, scale)
     want, bound = P.reference(lo, pages, table, lens, q, counts, scale, dtype)
     print(f"  {fmt} {kind}: worst {P.check(out, want, bound, kind):.3g} of the bound", flush=True)
@@ -386,13 +408,15 @@ def test_a_pool_beyond_32_bits():
     Kh, Vh = torch.empty_like(K), torch.empty_like(V)
     B.aquakv_paged_append(lg, pages, T, K, V, slots.cuda(), None, None, None, Kh, Vh)
     table, lens = torch.tensor([far], dtype=torch.int32), torch.tensor([T], dtype=torch.int32)
-    q = (1.5 * torch.randn(1, 16, 128, generator=gen)).bfloat16().cuda()
-    out = attend(lg, pages, table, lens, q, [1])
     rows = slots.cuda()
     k, v = (P.held(lo, c[rows], s[rows], sg) for c, s, sg in ((pages.k_codes, pages.k_scales, lo.signs_k), (pages.v_codes, pages.v_scales, lo.signs_v)))
-    for h in range(16):
-        want, bound = P.attention(q[:, h].double().cpu(), k[:, h // 2], v[:, h // 2], SCALE, torch.ones(1, T, dtype=torch.bool), "bf16")
-        P.check(out[:, h], want, bound, f"head {h}")
+    for n in (1, 8, 80):                                                   # 2, 16 and 160 rows of a kv head
+        q = (1.5 * torch.randn(n, 16, 128, generator=gen)).bfloat16().cuda()
+        out = attend(lg, pages, table, lens, q, [n])
+        seen = torch.arange(T)[None] <= T - n + torch.arange(n)[:, None]
+        for h in range(16):
+            want, bound = P.attention(q[:, h].double().cpu(), k[:, h // 2], v[:, h // 2], SCALE, seen, "bf16")
+            P.check(out[:, h], want, bound, f"{n} queries, head {h}")
     U.assert_close_storage(Kh, k.numpy(), "bf16", "keys")
 
 
