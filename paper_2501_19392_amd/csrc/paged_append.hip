@@ -3,6 +3,12 @@
 //
 // A head's 128 values are held by eight lanes x 16 as in the stand-alone quantizer, whose body this is: the rotary embedding pairs
 // coordinates 64 apart, which sit in the same register of the lane whose position differs in the uppermost bit.
+//
+// Bound by the vector pipes: 8192 tokens of 8 heads, 256 points, with the rows read back, take 33.5 us (80 MB at 2.4 TB/s) and 840 instructions
+// for 16 values of a lane, 82 % of the cycles; the rotations there and back are 224 of them, the search 280.  A few tokens are one chain of waits (arguments,
+// rows and tables, barrier, rotation, search): one token 5.0 us in a trace.  What came out no faster: rows of a round requested during the one before
+// (36.2 us, for registers); 32 values a lane in columns, with the way back on the matrix cores and the grid 16 times in LDS, which takes
+// bank conflicts from 58 to 22 % of the LDS cycles (34.5 us: 15 % fewer instructions, and 6 more of 64 KB to fill; one token 7.9).
 #include "codec_core.h"
 #include "kernels.h"
 
@@ -35,7 +41,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
     if (a.rope_cos != nullptr) pos = a.positions[t];
     Storage<T>::load(X + t * x_stride + (gid - t * (unsigned)a.H) * kGroup + l * N, v);
   };
-  request(blockIdx.x * kGroups);                          // on the way while the tables are
+  request(blockIdx.x * kGroups);                          // on the way while the tables are (one token 5.5 us a call in a graph, behind them 5.7)
   if constexpr (!is_rtn(NCW)) {
     TableRegs<kThreads> table_regs;
     if (a.table != nullptr) table_regs.request(a.table);

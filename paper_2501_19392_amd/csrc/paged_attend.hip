@@ -18,6 +18,14 @@ using namespace paged;
 //   values   O^T = V^T P: A holds 8 tokens of one coordinate; a look-up gives two neighbouring coordinates, two permutes pair them up by
 //            token.  The 32 coordinates a lane ends with are consecutive, as the inverse transform wants them.
 // COLS = 2: 32 rows, on twice the registers; a tile's codes become operands once for both.
+// No tile is staged: a wave reads its codes with wide loads a tile ahead and turns them into operands in registers, by a look-up (one permute for the
+// address, one LDS read, no bank conflicts) for two coordinates.  Why one wave a piece and not a workgroup: nothing is shared but the grid, and no wave
+// waits for another.
+//
+// Bound by memory for long sequences: 32 x 16 384 tokens, 4 query heads a kv head, 88 us in the kernel, 4.6 TB/s of codes and scales (a copy reaches 5.1),
+// vector pipes busy in 60 % of the cycles.  Few tokens: by the chain at its start (lengths, pages, codes, grid, rotated query: 3 us to
+// the first score) and the second launch, 4 us: one sequence of 700 tokens 11.1 us a call.  Many rows (8 x 9999 tokens, 5 queries, 3 bits: 33 us): by the vector
+// pipes, 54 % busy, and the waits between a tile's two products at two waves a SIMD.
 // Waves of a workgroup, which share the copies of the grid, and waves per SIMD: with 128 registers four fit (two workgroups a CU, which is what LDS has
 // room for with 256 points); uniform codes need more for the two halves' scales, and no LDS to speak of; fp32 layers hold everything twice.
 template <typename T, int NCW, int COLS> struct Shape {
@@ -259,6 +267,7 @@ paged_attend_kernel(const PagedAttendArgs a) {
 // out of one row from the pieces of its sequence: sum_i 2^(ref_i - top) part_i / sum_i 2^(ref_i - top) sum_i.
 // blockIdx = (query * q_heads + query head, sequence); threads of 32 take a piece each, 4 coordinates a thread, and go on by as many pieces as there
 // are such groups: 8, or 32 where there are many pieces.  All partial results of a round are requested together, ahead of the sequence's numbers.
+// A chain of waits of 3 to 5 us whatever its size (24 sequences in some 19 pieces each: 4.8 us) but for one long sequence's (512 pieces of 64 heads, 17 MB: 8.8 us).
 template <typename T, bool RTN, int THREADS>
 __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendArgs a) {
   constexpr int kClasses = THREADS / 32, kAhead = 4;
