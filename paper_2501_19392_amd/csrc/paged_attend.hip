@@ -264,13 +264,64 @@ paged_attend_kernel(const PagedAttendArgs a) {
   }
 }
 
+// results from, from + by, ... below `pieces` of the row at `at` (results `step` rows apart): four coordinates of the sum, the reference, the sum of weights
+struct Joined { f32x4 x; float ref, sum; };
+__device__ __forceinline__ Joined join_results(const PagedAttendArgs& a, int64_t at, int64_t step, int from, int by, int pieces, int l) {
+  constexpr int kAhead = 4;
+  Joined j = {f32x4{0.f, 0.f, 0.f, 0.f}, -3.0e38f, 0.f};
+  for (int i0 = from; i0 < pieces; i0 += kAhead * by) {
+    f32x2 st[kAhead];
+    f32x4 p[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u * by;
+      st[u] = f32x2{-3.0e38f, 0.f};
+      p[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (i < pieces) {
+        st[u] = *reinterpret_cast<const f32x2*>(a.stats + 2 * (at + i * step));
+        p[u] = *reinterpret_cast<const f32x4*>(a.part + (at + i * step) * kGroup + 4 * l);
+      }
+    }
+    float top = j.ref;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, st[u].x);
+    const float keep = __builtin_amdgcn_exp2f(j.ref - top);
+    j.x *= keep;
+    j.sum *= keep;
+    j.ref = top;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const float by2 = __builtin_amdgcn_exp2f(st[u].x - top);
+      j.x += p[u] * by2;
+      j.sum += st[u].y * by2;
+    }
+  }
+  return j;
+}
+// a joined row, 16 coordinates on each of eight lanes as in the stand-alone inverse -> out
+template <typename T, bool RTN> __device__ __forceinline__ void finish_joined(const PagedAttendArgs& a, const float* row, int lane, int h, int64_t to) {
+  const int q = group_pos<16>(lane);
+  float v[16];
+  load_f32(row + 16 * q, v);
+  if constexpr (!RTN) {
+    float sf[16];
+    load_signs(a.signs_v, h, q, sf);
+    const float norm = kRsqrtG * Rot<false>::sign(q);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] *= norm;
+    Rot<false>::iwht(v, q);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] *= sf[r];
+  }
+  Storage<T>::template store<false>(static_cast<T*>(a.out) + to * kGroup, q, v);
+}
 // out of one row from the pieces of its sequence: sum_i 2^(ref_i - top) part_i / sum_i 2^(ref_i - top) sum_i.
 // blockIdx = (query * q_heads + query head, sequence); threads of 32 take a piece each, 4 coordinates a thread, and go on by as many pieces as there
 // are such groups: 8, or 32 where there are many pieces.  All partial results of a round are requested together, ahead of the sequence's numbers.
 // A chain of waits of 3 to 5 us whatever its size (24 sequences in some 19 pieces each: 4.8 us) but for one long sequence's (512 pieces of 64 heads, 17 MB: 8.8 us).
 template <typename T, bool RTN, int THREADS>
 __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendArgs a) {
-  constexpr int kClasses = THREADS / 32, kAhead = 4;
+  constexpr int kClasses = THREADS / 32;
   __shared__ __align__(16) float red[kClasses][kGroup];
   __shared__ float refs[kClasses], sums[kClasses];
   __shared__ __align__(16) float row[kGroup];
@@ -282,37 +333,9 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendA
   if (qi >= w.n) return;
   const int k = threadIdx.x >> 5, l = threadIdx.x & 31;
   const int64_t step = (int64_t)a.max_queries * a.q_heads, at = uniform(head.x) * step + (int64_t)qi * a.q_heads + qh;
-  float ref = -3.0e38f, sum = 0.f;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = k; i0 < pieces; i0 += kAhead * kClasses) {
-    f32x2 st[kAhead];
-    f32x4 p[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int i = i0 + u * kClasses;
-      st[u] = f32x2{-3.0e38f, 0.f};
-      p[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (i < pieces) {
-        st[u] = *reinterpret_cast<const f32x2*>(a.stats + 2 * (at + i * step));
-        p[u] = *reinterpret_cast<const f32x4*>(a.part + (at + i * step) * kGroup + 4 * l);
-      }
-    }
-    float top = ref;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, st[u].x);
-    const float keep = __builtin_amdgcn_exp2f(ref - top);
-    x *= keep;
-    sum *= keep;
-    ref = top;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const float by = __builtin_amdgcn_exp2f(st[u].x - top);
-      x += p[u] * by;
-      sum += st[u].y * by;
-    }
-  }
-  *reinterpret_cast<f32x4*>(&red[k][4 * l]) = x;
-  if (l == 0) { refs[k] = ref; sums[k] = sum; }
+  const Joined j = join_results(a, at, step, k, kClasses, pieces, l);
+  *reinterpret_cast<f32x4*>(&red[k][4 * l]) = j.x;
+  if (l == 0) { refs[k] = j.ref; sums[k] = j.sum; }
   __syncthreads();
   if (threadIdx.x < kGroup) {                              // a thread per coordinate
     float top = refs[0];
@@ -329,25 +352,35 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(const PagedAttendA
   }
   __syncthreads();
   if (threadIdx.x >= 8) return;
-  // the row on eight lanes, as in the stand-alone inverse
-  const int q = group_pos<16>(threadIdx.x);
-  float v[16];
-  load_f32(&row[16 * q], v);
-  if constexpr (!RTN) {
-    float sf[16];
-    load_signs(a.signs_v, h, q, sf);
-    const float norm = kRsqrtG * Rot<false>::sign(q);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] *= norm;
-    Rot<false>::iwht(v, q);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] *= sf[r];
+  finish_joined<T, RTN>(a, row, threadIdx.x, h, (w.first + qi) * a.q_heads + qh);
+}
+// The same for many rows of few pieces: eight rows a workgroup, 32 threads each, so that the way back takes a whole wave (1000 queries of 32 heads over 1000
+// tokens: 50 us, a row a workgroup 77; 512 over 6000: 92, 104; 130 sequences of 700 tokens 33, 36; where rows have some 20 pieces the loop over them
+// is the longer chain: 24 x 3000 tokens 28.8, 27.0).
+template <typename T, bool RTN>
+__global__ __launch_bounds__(256) void paged_merge_rows_kernel(const PagedAttendArgs a) {
+  __shared__ __align__(16) float rows[8][kGroup];
+  const int b = blockIdx.y, first = 8 * blockIdx.x;         // rows of the sequence: query * q_heads + query head
+  const int2 head = a.heads[b];
+  const int pieces = uniform(head.y);
+  if (pieces == 1) return;
+  const PagedQueries w = paged_queries(a, b);
+  const int n_rows = w.n * a.q_heads;
+  if (first >= n_rows) return;
+  const int k = threadIdx.x >> 5, l = threadIdx.x & 31;
+  const int64_t step = (int64_t)a.max_queries * a.q_heads, at = uniform(head.x) * step + min(first + k, n_rows - 1);
+  const Joined j = join_results(a, at, step, 0, 1, pieces, l);
+  *reinterpret_cast<f32x4*>(&rows[k][4 * l]) = j.x * (j.sum == 0.f ? 0.f : 1.0f / j.sum);
+  __syncthreads();
+  const int r = first + (threadIdx.x >> 3);
+  if (threadIdx.x < 64) {                                  // (rows that are not there stay for the exchanges of lanes)
+    const int there = min(r, n_rows - 1);
+    finish_joined<T, RTN>(a, rows[there - first], threadIdx.x & 7, there % a.q_heads / (a.q_heads / a.H), w.first * a.q_heads + there);
   }
-  Storage<T>::template store<false>(static_cast<T*>(a.out) + ((w.first + qi) * a.q_heads + qh) * kGroup, q, v);
 }
 
 // How a launch is laid out, from sizes alone (lengths are on the device).
-struct PagedPlan { unsigned blocks, row_tiles; int slots, row_blocks; int64_t items; bool two, merge, many; };
+struct PagedPlan { unsigned blocks, row_tiles; int slots, row_blocks; int64_t items; bool two, merge, many, by_rows; };
 // Results of a sequence beyond which the merge has 1024 threads a row, of 256 (one query of 131 072 tokens 41.0 us, for 45.0; beyond 8: 32 x 4000 tokens
 // 37.4 for 34.4).
 constexpr int kManyPieces = 64;
@@ -359,9 +392,13 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
   const int64_t rows = std::max<int64_t>(max_queries, 1) * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
   if (sizeof(T) == 2 && rows > kFewRows) {                 // workgroups of 256 rows, one a CU: the tokens in pieces if there are too few of them
     p.row_blocks = (int)((rows + kTileRows - 1) / kTileRows);
-    p.slots = (int)std::max<int64_t>(std::min(256 / std::max<int64_t>(batch * H * p.row_blocks, 1), most / 8), 1);
+    // ... of 4 tiles of 64 at least, of 2 where there is one block of rows and so little to join (180 rows over 700 tokens: 28.0 us, 22.2; 160 over 6000: 34.3, 31.5;
+    // 1200 rows over 300: 23.3, 26.2)
+    p.slots = (int)std::max<int64_t>(std::min(256 / std::max<int64_t>(batch * H * p.row_blocks, 1), most / (p.row_blocks == 1 ? 4 : 8)), 1);
     p.items = batch * p.slots;
     p.merge = p.slots > 1;
+    p.by_rows = p.slots <= 16;
+    p.many = p.slots > kManyPieces;
     return p;
   }
   // 9 to 16 rows fill one column of a wave, but two columns take as long and join their results (16 rows of 8 x 9999 tokens, 3 bits: 37.3 us, in one column
@@ -384,6 +421,7 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
     p.merge = most > 1;
   }
   p.many = p.items > kManyPieces * batch;
+  p.by_rows = p.items <= 8 * batch && batch * max_queries * q_heads >= 512;
   return p;
 }
 
@@ -445,8 +483,10 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   if (!plan.merge) return hipSuccess;
   const dim3 grid((unsigned)(a.max_queries * a.q_heads), (unsigned)a.batch);
   const bool rtn = is_rtn(n_codewords);
+  const dim3 by_rows((unsigned)((a.max_queries * a.q_heads + 7) / 8), (unsigned)a.batch);
 #define AQUAKV_MERGE(T, RTN)                                                                                  \
-  (plan.many ? paged_merge_kernel<T, RTN, 1024><<<grid, 1024, 0, stream>>>(a)                                  \
+  (plan.by_rows ? paged_merge_rows_kernel<T, RTN><<<by_rows, 256, 0, stream>>>(a)                              \
+   : plan.many ? paged_merge_kernel<T, RTN, 1024><<<grid, 1024, 0, stream>>>(a)                                  \
              : paged_merge_kernel<T, RTN, 256><<<grid, 256, 0, stream>>>(a))
   if (dtype == kBF16) { if (rtn) AQUAKV_MERGE(bf16_t, true); else AQUAKV_MERGE(bf16_t, false); }
   else { if (rtn) AQUAKV_MERGE(float, true); else AQUAKV_MERGE(float, false); }

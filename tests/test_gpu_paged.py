@@ -310,6 +310,23 @@ def test_many_sequences_that_share_pages(dtype, fmt, batch, QH, ragged):
     P.check(out, *P.reference(lo, pages, table, lens, q, counts, SCALE, dtype), f"{fmt} {batch}")
 
 
+@pytest.mark.parametrize("dtype,fmt,batch,H,QH", [("bf16", "grid64", 130, 8, 8), ("fp32", "rtn4", 70, 8, 24), ("bf16", "rtn2", 100, 16, 16), ("fp32", "grid16", 70, 8, 8)])
+def test_many_rows_of_few_pieces(dtype, fmt, batch, H, QH):
+    need_gpu()
+    gen = torch.Generator().manual_seed(batch)
+    lengths = (torch.rand(batch, generator=gen) ** 4 * 700).long().tolist()
+    lengths[3], lengths[7], lengths[8] = 700, 0, 31
+    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, H, QH, lengths, 64, 1, 4)
+    P.check(attend(lg, pages, table, lens, q, counts), *P.reference(lo, pages, table, lens, q, counts, SCALE, dtype), fmt)
+
+
+@pytest.mark.parametrize("fmt,lengths,queries", [("grid256", [5000], 150), ("rtn4", [20000], 140), ("grid16", [1100, 200, 0], 300)])
+def test_many_queries_over_tokens_in_pieces(fmt, lengths, queries):
+    need_gpu()
+    lo, lg, pages, table, lens, q, counts = build("bf16", fmt, 1, 1, lengths, 128, queries)
+    P.check(attend(lg, pages, table, lens, q, counts), *P.reference(lo, pages, table, lens, q, counts, SCALE, "bf16"), fmt)
+
+
 @pytest.mark.parametrize("fmt,QH", [("grid256", 1), ("rtn4", 3), ("grid64", 10)])
 def test_a_long_sequence(fmt, QH):
     need_gpu()
