@@ -476,7 +476,7 @@ def _here() -> int:
 
 def _rows(x, dtype, row: int, name: str, device: int):
     """Rows of heads x 128 that may lie apart -> (address, elements from row to row, rows); an address: one behind the other."""
-    if x is None or isinstance(x, int):
+    if x is None or x.__class__ is int:
         return x, row, None
     (n, heads, g), (step, head_step, one) = x.shape, x.stride()
     if heads * g != row or one != 1 or (head_step != g and heads != 1) or x.dtype is not dtype or x.get_device() != device:
@@ -486,9 +486,9 @@ def _rows(x, dtype, row: int, name: str, device: int):
 
 def _typed(x, dtype, n: int, name: str, device: int):
     """A tensor of n elements, or an address."""
-    if x is None or isinstance(x, int):
+    if x is None or x.__class__ is int:
         return x
-    if x.dtype is not dtype or x.numel() != n or not x.is_contiguous() or x.get_device() != device:
+    if not (x.dtype is dtype and x.numel() == n and x.is_contiguous() and x.get_device() == device):
         raise ValueError(f"{name} must be {n} elements of {dtype} on the current device")
     return x.data_ptr()
 
