@@ -9,6 +9,7 @@
 #pragma once
 #include "codec_core.h"
 #include "kernels.h"
+#include "paged_split.h"
 
 namespace aquakv {
 namespace paged {
@@ -52,19 +53,7 @@ __device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, 
 // lengths (each sequence has one at least): item i of the launch is piece `piece` of `pieces` of sequence b (-1: behind the last).
 struct Share { int b, piece, pieces, tiles, items; };
 __device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
-  return b < a.batch ? max((length_of(a, a.seq_lens[b]) + kTile - 1) / kTile, 1) : 0;
-}
-// tiles per piece with which ceil(tiles / piece) over all sequences is at most max(slots, slots / 2 + batch), whatever the lengths
-__device__ __forceinline__ int piece_tiles(const PagedAttendArgs& a, int total) {
-  const uint32_t room = (uint32_t)max(a.slots - a.batch, max(a.slots / 2, 1));
-  return (int)(((uint32_t)total + room - 1) / room);
-}
-// Short pieces make half as many: two waves of one tile take as long as one of two, whose results are half as many to write and to join (one query of
-// 10 000 tokens, 313 tiles: 20.0 us in pieces of one tile, 15.9 of two; of 6000 14.9, 14.6; 5 queries of 2000 tokens of 8 sequences: 20.5 in pieces of two, 18.6 of
-// three, 19.7 of four).  Longer ones want all waves there are (32 x 16 384 tokens: 95 us, on half of the waves 111).
-__device__ __forceinline__ int short_piece(const PagedAttendArgs& a, int total) {
-  const uint32_t half = (uint32_t)max(a.slots / 2, 1);
-  return (int)min(((uint32_t)total + half - 1) / half, 4u);
+  return b < a.batch ? max(tiles_of_tokens(length_of(a, a.seq_lens[b]), kTile), 1) : 0;
 }
 // sums over the lanes up to and with this one
 __device__ __forceinline__ int wave_scan(int x) {
@@ -79,8 +68,8 @@ __device__ __forceinline__ int wave_scan(int x) {
 __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
   Share s = {-1, 0, 1, 0, 0};
   if (a.batch == 1) {
-    const int n = max((length_of(a, const_ints(a.seq_lens)[0]) + kTile - 1) / kTile, 1);
-    s.tiles = max((n + a.slots - 1) / a.slots, short_piece(a, n));
+    const int n = max(tiles_of_tokens(length_of(a, const_ints(a.seq_lens)[0]), kTile), 1);
+    s.tiles = max((n + a.slots - 1) / a.slots, short_piece(n, a.slots));
     s.items = s.pieces = (n + s.tiles - 1) / s.tiles;
     if (item < s.items) { s.b = 0; s.piece = item; }
     return s;
@@ -91,7 +80,7 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
     tiles = tiles_of(a, b0 + lane);
     total += __builtin_amdgcn_readlane(wave_scan(tiles), 63);
   }
-  s.tiles = piece_tiles(a, total);
+  s.tiles = piece_tiles(total, a.slots, a.batch);
   // The fewest tiles that do, where a wave has all lengths: 32 x 16 384 tokens are 512 pieces of 32 tiles then, not 480 of 35 (94.3 us for 95.6).
   if (a.batch <= 64 && 2 * a.batch <= a.slots) {
     int low = max((int)(((uint32_t)total + a.slots - 1) / a.slots), 1);
@@ -101,7 +90,7 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
       else low = mid + 1;
     }
   }
-  s.tiles = max(s.tiles, short_piece(a, total));
+  s.tiles = max(s.tiles, short_piece(total, a.slots));
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     if (a.batch > 64) tiles = tiles_of(a, b0 + lane);
     const int mine = (int)((uint32_t)(tiles + s.tiles - 1) / (uint32_t)s.tiles);

@@ -73,7 +73,8 @@ paged_attend_kernel(const PagedAttendArgs a) {
   const bool idle = share.b < 0 || row0 >= n_rows;
   // the tokens of this piece
   const int first_limit = uniform(w.len - w.count + row0 / rep), last_limit = uniform(w.len - w.count + min(row0 + kRows - 1, n_rows - 1) / rep);
-  const int t_begin = share.piece * share.tiles * kTile, t_end = idle ? 0 : min(min(t_begin + share.tiles * kTile, w.len), last_limit + 1);
+  const TokenRange range = piece_range(share.piece, share.tiles, kTile, idle ? 0 : last_limit + 1);
+  const int t_begin = range.begin, t_end = range.end;
   const bool any = t_begin < t_end;
   typename C::Column col[COLS];
   typename C::template Query<T> asked[COLS] = {};

@@ -201,9 +201,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
   const int limit = row_there ? w.len - w.count + qi : -1;
   const int wave_first = uniform(w.len - w.count + min(row0 + 32 * wave, n_rows - 1) / rep);      // smallest limit of the wave's rows
   const int last_limit = uniform(w.len - w.count + min(row0 + kTileRows - 1, n_rows - 1) / rep);
-  const int tiles = (last_limit + kTokens) / kTokens;      // (last_limit >= -len: 0 tiles where nothing is seen)
-  const int each = (max(tiles, 0) + a.slots - 1) / a.slots;
-  const int t_begin = piece * each * kTokens, t_end = min(t_begin + each * kTokens, last_limit + 1);
+  const TokenRange range = piece_range(piece, (tiles_of_tokens(last_limit + 1, kTokens) + a.slots - 1) / a.slots, kTokens, last_limit + 1);
+  const int t_begin = range.begin, t_end = range.end;
 
   TileCodes<NCW> codes;
   const auto request = [&](int t) { codes.request(a, b, w.len, h, t, wave, lane); };
