@@ -507,11 +507,16 @@ def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_
     v, vs, nv = _rows(V, dtype, row, "V", here)
     if (nk is not None and nk != tokens) or (nv is not None and nv != tokens):
         raise ValueError(f"K and V must have {tokens} rows")
-    angles = 0 if rope_cos is None else rope_cos.numel()
+    rope_rows = 0
+    if rope_cos is not None:                                # (numbers of elements are not enough: a table of both halves' angles would be one of twice the rows)
+        if (rope_cos.__class__ is int or rope_sin.__class__ is int or rope_cos.dim() != 2 or rope_cos.shape[1] != 64 or
+                (rope_sin is not None and rope_sin.shape != rope_cos.shape)):
+            raise ValueError("rope_cos and rope_sin must be tensors [positions, 64]")
+        rope_rows = rope_cos.shape[0]
     _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, tokens, "slots", here),
                                     _typed(positions, torch.int32, tokens, "positions", here),
-                                    _typed(rope_cos, torch.float32, angles, "rope_cos", here),
-                                    _typed(rope_sin, torch.float32, angles, "rope_sin", here), angles // 64,
+                                    _typed(rope_cos, torch.float32, 64 * rope_rows, "rope_cos", here),
+                                    _typed(rope_sin, torch.float32, 64 * rope_rows, "rope_sin", here), rope_rows,
                                     _typed(Khat, dtype, tokens * row, "Khat", here), _typed(Vhat, dtype, tokens * row, "Vhat", here),
                                     _stream(stream)))
 
