@@ -209,6 +209,7 @@ class Layer:
             self.signs_k = signs_k.to(torch.int8).contiguous().reshape(-1)
             self.signs_v = signs_v.to(torch.int8).contiguous().reshape(-1)
             self.n_codewords, self.vq_dim = self.codebook.shape
+        self.row_layout = (kv_heads, head_dim, self.vq_dim, self.n_codewords, self.rht_group)      # what decides how a row's codes and scales lie
         self.w_k = None if w_k is None else w_k.to(dtype).contiguous()
         self.w_v = None if w_v is None else w_v.to(dtype).contiguous()
         self.b_k = None if b_k is None else b_k.to(torch.float32).contiguous()
@@ -272,7 +273,7 @@ class Pages:
     C struct that points at them."""
 
     def __init__(self, layer: Layer, n_pages: int, page_tokens: int, device="cuda", k_codes=None, k_scales=None, v_codes=None, v_scales=None):
-        self.n_pages, self.page_tokens = n_pages, page_tokens
+        self.n_pages, self.page_tokens, self.row_layout = n_pages, page_tokens, layer.row_layout
         given = (k_codes, k_scales, v_codes, v_scales)
         if all(t is None for t in given):
             given = (*layer.alloc_codes(n_pages * page_tokens, device), *layer.alloc_codes(n_pages * page_tokens, device))
@@ -493,16 +494,19 @@ def _typed(x, dtype, n: int, name: str, device: int):
     return x.data_ptr()
 
 
-def _pool_here(pages, device: int) -> None:
-    if pages.__class__ is Pages and pages.device != device:
-        raise ValueError("the pages are not on the current device")
+def _pool_here(layer, pages, device: int) -> None:
+    if isinstance(pages, Pages):
+        if pages.device != device:
+            raise ValueError("the pages are not on the current device")
+        if pages.row_layout != layer.row_layout:
+            raise ValueError("the pages were made for rows of another layout than this layer's")
 
 
 def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_cos, rope_sin, Khat, Vhat, stream=None) -> None:
     """K, V: [tokens, kv_heads, 128], rows may lie apart; rope_cos, rope_sin: [rope_rows, 64] tensors (None: no rotation, positions unused).
     Tensors have to be on the current device (ValueError otherwise), whose current stream is taken unless one is given."""
     row, dtype, here = layer.d, layer.dtype, _here()
-    _pool_here(pages, here)
+    _pool_here(layer, pages, here)
     k, ks, nk = _rows(K, dtype, row, "K", here)
     v, vs, nv = _rows(V, dtype, row, "V", here)
     if (nk is not None and nk != tokens) or (nv is not None and nv != tokens):
@@ -530,7 +534,7 @@ def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_
     """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence].  Tensors have to be on the current
     device (ValueError otherwise), whose current stream is taken unless one is given."""
     row, dtype, here = q_heads * layer.head_dim, layer.dtype, _here()
-    _pool_here(pages, here)
+    _pool_here(layer, pages, here)
     at, stride, q_rows = _rows(q, dtype, row, "q", here)
     if page_table.dim() != 2 or page_table.shape[0] != batch:
         raise ValueError("page_table must be [batch, pages]")

@@ -22,3 +22,28 @@ def test_rotary_tables_have_64_angles_a_row():
     for cos, sin in ((wide, wide), (good, wide), (wide, good), (good, good[:5]), (good[0], good[0]), (good.view(-1), good.view(-1)),
                      (good[None], good[None]), (1 << 20, good), (good, 1 << 20)):
         refused_append(lay, pages, K, slots, pos, cos, sin, r"\[positions, 64\]")
+
+
+def test_pages_of_another_layout():
+    """Rows of other sizes would be written behind the end of the tensors."""
+    grid = lambda n, heads=2: B.Layer(heads, 128, torch.zeros(n, 2), torch.ones(heads * 128), torch.ones(heads * 128), torch.bfloat16)
+    layers = [layer(), layer(rtn_bits=2), grid(16), grid(64), grid(256), grid(256, 4)]
+    for lay in layers:
+        for other in layers:
+            pages = B.Pages(other, 3, 8, device="cpu")
+            K = torch.zeros(4, lay.kv_heads, 128, dtype=torch.bfloat16)
+            q, table, lens = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+            if other is lay:
+                with pytest.raises(B.AquaKVError):                          # as far as the library, which wants slots
+                    B.aquakv_paged_append(lay, pages, 4, K, K, None, None, None, None, None, None)
+                continue
+            refused_append(lay, pages, K, torch.zeros(4, dtype=torch.int64), None, None, None, "another layout")
+            with pytest.raises(ValueError, match="another layout"):
+                B.aquakv_paged_attend(lay, pages, 2, 4, table, lens, q, 1, None, 1.0, q.clone(), None)
+    # a layer of the same layout may read another one's pages; a class of one's own is looked at as well
+
+    class Mine(B.Pages):
+        pass
+    refused_append(layers[0], Mine(layers[1], 3, 8, device="cpu"), torch.zeros(4, 2, 128, dtype=torch.bfloat16), None, None, None, None, "another layout")
+    with pytest.raises(B.AquaKVError):
+        B.aquakv_paged_append(layers[0], B.Pages(layer(), 3, 8, device="cpu"), 4, *[torch.zeros(4, 2, 128, dtype=torch.bfloat16)] * 2, *[None] * 6)
