@@ -215,6 +215,8 @@ class Layer:
         self.b_k = None if b_k is None else b_k.to(torch.float32).contiguous()
         self.b_v = None if b_v is None else b_v.to(torch.float32).contiguous()
         self.search_table = search_table
+        held = {t.get_device() for t in (self.codebook, self.signs_k, self.signs_v, search_table) if t is not None}
+        self.quantizer_device = None if not held else held.pop() if len(held) == 1 else "several"
         if self.w_k is not None and self.w_k.shape[0] != self.d:
             raise ValueError("w_k must be [D, d_in_k]")
         if self.w_v is not None and self.w_v.shape[0] != self.d:
@@ -495,6 +497,8 @@ def _typed(x, dtype, n: int, name: str, device: int):
 
 
 def _pool_here(layer, pages, device: int) -> None:
+    if layer.quantizer_device is not None and layer.quantizer_device != device:
+        raise ValueError("the layer's grid, signs and search table are not on the current device")
     if isinstance(pages, Pages):
         if pages.device != device:
             raise ValueError("the pages are not on the current device")

@@ -47,3 +47,19 @@ def test_pages_of_another_layout():
     refused_append(layers[0], Mine(layers[1], 3, 8, device="cpu"), torch.zeros(4, 2, 128, dtype=torch.bfloat16), None, None, None, None, "another layout")
     with pytest.raises(B.AquaKVError):
         B.aquakv_paged_append(layers[0], B.Pages(layer(), 3, 8, device="cpu"), 4, *[torch.zeros(4, 2, 128, dtype=torch.bfloat16)] * 2, *[None] * 6)
+
+
+def test_the_layers_tensors_are_on_the_current_device(monkeypatch):
+    """... as those of the call are (the current device is named here: pages and tensors as addresses, which nothing is known of)"""
+    pool = B.aquakv_pages(3, 8, 1 << 32, 2 << 32, 3 << 32, 4 << 32)
+    grid = B.Layer(2, 128, torch.zeros(16, 2), torch.ones(256), torch.ones(256), torch.bfloat16)
+    call = lambda lay: B.aquakv_paged_append(lay, pool, 4, 5 << 32, 6 << 32, None, None, None, None, None, None)
+    with pytest.raises(B.AquaKVError):                                      # (no slots)
+        call(grid)
+    monkeypatch.setattr(B, "_here", lambda: 0)
+    with pytest.raises(ValueError, match="current device"):
+        call(grid)
+    with pytest.raises(ValueError, match="current device"):
+        B.aquakv_paged_attend(grid, pool, 2, 4, None, None, 5 << 32, 1, None, 1.0, None, None)
+    with pytest.raises(B.AquaKVError):                                      # uniform: it has none
+        call(layer())
