@@ -540,6 +540,8 @@ def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_
     row, dtype, here = q_heads * layer.head_dim, layer.dtype, _here()
     _pool_here(layer, pages, here)
     at, stride, q_rows = _rows(q, dtype, row, "q", here)
+    if q_rows is None or page_table is None or page_table.__class__ is int:
+        raise ValueError("q and page_table must be tensors: their shapes say how many rows and pages there are")
     if page_table.dim() != 2 or page_table.shape[0] != batch:
         raise ValueError("page_table must be [batch, pages]")
     pages_each = page_table.shape[1]

@@ -63,3 +63,15 @@ def test_the_layers_tensors_are_on_the_current_device(monkeypatch):
         B.aquakv_paged_attend(grid, pool, 2, 4, None, None, 5 << 32, 1, None, 1.0, None, None)
     with pytest.raises(B.AquaKVError):                                      # uniform: it has none
         call(layer())
+
+
+def test_addresses_have_no_shape():
+    """Rows of q and pages of a sequence are counted from the tensors, so that an address will not do (for the other arguments it will)."""
+    lay = layer()
+    pages = B.Pages(lay, 3, 8, device="cpu")
+    q, table, lens = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for x, t in ((q.data_ptr(), table), (None, table), (q, table.data_ptr()), (q, None)):
+        with pytest.raises(ValueError, match="must be tensors"):
+            B.aquakv_paged_attend(lay, pages, 2, 4, t, lens, x, 1, None, 1.0, q.clone(), None)
+    with pytest.raises(B.AquaKVError, match="workspace"):
+        B.aquakv_paged_attend(lay, pages, 2, 4, table, 1 << 32, q, 1, None, 1.0, 2 << 32, None)
