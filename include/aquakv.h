@@ -530,7 +530,8 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   time, captured ones included, need workspaces of their own.  At most 65535 sequences, max_queries * q_heads < 2^22, batch *
  *   kv_heads < 2^25, table_pages * page_tokens < 2^31 - 4096 and 2^35 over the batch: AQUAKV_EUNSUPPORTED beyond.
  *
- * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.
+ * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens
+ * (tokens = 0), sequences or queries (batch, q_rows or max_queries = 0) nothing is done, and buffers but the pool's may be NULL.
  */
 typedef struct aquakv_pages {
   int32_t n_pages, page_tokens;

@@ -1691,6 +1691,7 @@ int aquakv_paged_append(const aquakv_layer* L, const aquakv_pages* pages, int64_
   CHECK(check_pages(L, pages));
   if (tokens < 0) return fail(AQUAKV_EINVAL, "tokens=%lld", (long long)tokens);
   if (tokens > 0x7fffffffLL / L->kv_heads) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, L->kv_heads);
+  if (tokens == 0) return AQUAKV_OK;                              // (before the buffers are looked at: those without elements may be NULL)
   const int64_t D = (int64_t)L->kv_heads * 128;
   const size_t eb = elem_bytes(L->dtype);
   CHECK(check_rows(K, "K", k_stride, D, eb));
@@ -1705,7 +1706,6 @@ int aquakv_paged_append(const aquakv_layer* L, const aquakv_pages* pages, int64_
   }
   CHECK(check_ptr(Khat, "Khat", false));
   CHECK(check_ptr(Vhat, "Vhat", false));
-  if (tokens == 0) return AQUAKV_OK;
   const PoolRanges pool = pool_ranges(L, pages);
   const Params params = params_of(L);
   const size_t hat = (size_t)tokens * D * eb, angles = rope_cos == nullptr ? 0 : (size_t)rope_rows * 64 * sizeof(float);
@@ -1741,6 +1741,7 @@ int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_
   CHECK(check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries));
   if (q_start == nullptr && q_rows != (int64_t)batch * max_queries)
     return fail(AQUAKV_EINVAL, "q_rows=%lld: without q_start every one of %d sequences has %d", (long long)q_rows, batch, max_queries);
+  if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;      // (as above)
   const int64_t row = (int64_t)q_heads * 128;
   const size_t eb = elem_bytes(L->dtype);
   CHECK(check_array(page_table, "page_table", 4));
@@ -1749,7 +1750,6 @@ int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_
   CHECK(check_rows(q, "q", q_stride, row, eb));
   CHECK(check_ptr(out, "out", true));
   CHECK(check_ptr(workspace, "workspace", true));
-  if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;
   const size_t need = aquakv_paged_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries);
   if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
   const PoolRanges pool = pool_ranges(L, pages);

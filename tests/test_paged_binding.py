@@ -75,3 +75,28 @@ def test_addresses_have_no_shape():
             B.aquakv_paged_attend(lay, pages, 2, 4, t, lens, x, 1, None, 1.0, q.clone(), None)
     with pytest.raises(B.AquaKVError, match="workspace"):
         B.aquakv_paged_attend(lay, pages, 2, 4, table, 1 << 32, q, 1, None, 1.0, 2 << 32, None)
+
+
+def test_nothing_to_do():
+    """A step without tokens or queries: tensors without elements have no address."""
+    lay = layer()
+    pages = B.Pages(lay, 3, 8, device="cpu")
+    K, slots, pos, cos = torch.zeros(0, 2, 128, dtype=torch.bfloat16), torch.zeros(0, dtype=torch.int64), torch.zeros(0, dtype=torch.int32), torch.zeros(9, 64)
+    assert K.data_ptr() == 0
+    B.aquakv_paged_append(lay, pages, 0, K, K, slots, None, None, None, None, None)
+    B.aquakv_paged_append(lay, pages, 0, K, K, slots, pos, cos, cos, K.clone(), K.clone())
+    q, table, lens = torch.zeros(0, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    start, ws = torch.zeros(3, dtype=torch.int32), torch.zeros(0, dtype=torch.uint8)
+    B.aquakv_paged_attend(lay, pages, 2, 4, table, lens, q, 0, None, 1.0, q.clone(), ws)
+    B.aquakv_paged_attend(lay, pages, 2, 4, table, lens, q, 5, start, 1.0, q.clone(), ws)
+    B.aquakv_paged_attend(lay, pages, 0, 4, table[:0], lens[:0], q, 1, None, 1.0, q.clone(), ws)
+    B.aquakv_paged_attend(lay, pages, 0, 4, table[:0], lens[:0], q, 1, start[:1], 1.0, q.clone(), ws)
+    with pytest.raises(B.AquaKVError):                                      # sizes are looked at all the same
+        B.aquakv_paged_attend(lay, pages, 2, 5, table, lens, torch.zeros(0, 5, 128, dtype=torch.bfloat16), 0, None, 1.0, None, ws)
+    # with addresses and a workspace of no bytes
+    p = B.aquakv_pages(3, 8, 1 << 32, 2 << 32, 3 << 32, 4 << 32)
+    none = [None] * 4
+    assert B._lib.aquakv_paged_append(lay.c, p, 0, None, 256, None, 256, *none, 0, None, None, None) == B.AQUAKV_OK
+    for batch, rows, most in ((0, 6, 2), (3, 0, 2), (3, 6, 0)):
+        start = 8 << 32
+        assert B._lib.aquakv_paged_attend(lay.c, p, batch, 4, 5 << 32, 3, 6 << 32, rows, most, start, 7 << 32, 512, 1.0, 9 << 32, None, 0, None) == B.AQUAKV_OK
