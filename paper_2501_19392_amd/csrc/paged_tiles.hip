@@ -14,7 +14,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kTokens = 64;                                // of a tile
-constexpr int kKeyBytes = kTokens * kGroup * 2, kBufferBytes = 2 * kKeyBytes + (2 * kTokens + 16) * 4;      // keys, values, scales of both, the largest of each eight of the values', pages that are not there
+constexpr int kKeyBytes = kTokens * kGroup * 2;             // (values: as many)
 
 // Coordinate (of 128) that row i of a 32-row operand R stands for, so that register n of lanes 32 hf ... of product R is coordinate
 // 16 (2 R + n / 8) + 8 hf + n % 8: what such a lane holds of a vector as the other operand.  (Swaps bits 2 and 3.)
@@ -46,9 +46,13 @@ __device__ __forceinline__ float pair_max(float x) {       // over lanes l, l ^ 
 // ---------------------------------------------------------------- codes of a tile
 // Wave `part` of the eight that a tile is shared out to: keys of tokens 8 part ... (a lane: 16 coordinates of a token), values of the eight tokens
 // that operand piece `part` holds, 16 (part / 2) + 4 (part % 2) + {0 ... 3, 8 ... 11} (a lane: 2 coordinates).
+// Operands are grid points, or (uniform) code - zero point, exact; scales stay fp32, a uniform row's one for each half of the coordinates.
 template <int NCW> struct TileCodes {
   typedef Codes<NCW, 1> C;
   static constexpr bool kRtn = C::kRtn;
+  // behind keys and values, fp32: scales of the keys, of the values (rows of kTokens; uniform: lower half, upper half), the largest of each eight of the
+  // values', pages that are not there
+  static constexpr int kHalves = C::kHalves, kLargest = 2 * kHalves * kTokens, kMissing = kLargest + 8, kBufferBytes = 2 * kKeyBytes + (kMissing + 8) * 4;
   static constexpr int c = C::c, kRow = C::kRow;
   u32x2 k;
   uint32_t v[8];
@@ -110,17 +114,11 @@ template <int NCW> struct TileCodes {
     u32x4 out[2];
     if constexpr (kRtn) {
       const bool upper = (lane & 7) >= 4;
-      const float s0 = half_bits_to_float((uint16_t)ks.x), s1 = half_bits_to_float((uint16_t)ks.y);
-      const int e = exponent(s0, s1);
-      const float step = __builtin_ldexpf(upper ? s1 : s0, -e);
-      const float zero = (float)((upper ? ks.y : ks.x) >> 16);
+      const uint32_t word = upper ? ks.y : ks.x;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t w = NCW == kRtn4 ? (i < 4 ? k.x : k.y) >> (8 * (i & 3)) : k.x >> (4 * i);
-        const uint32_t low = w & ((1u << NCW) - 1u), high = (w >> NCW) & ((1u << NCW) - 1u);
-        out[i >> 2][i & 3] = f16_pair(((float)low - zero) * step, ((float)high - zero) * step);
-      }
-      if ((lane & 7) == 0) scales[token] = __builtin_ldexpf(1.0f, e);
+      for (int i = 0; i < 8; ++i)
+        out[i >> 2][i & 3] = NCW == kRtn4 ? less_zero<0>(i < 4 ? k.x : k.y, i & 3, word) : (i & 1) ? less_zero<2>(k.x, i >> 1, word) : less_zero<0>(k.x, i >> 1, word);
+      if ((lane & 3) == 0) scales[(upper ? kTokens : 0) + token] = half_bits_to_float((uint16_t)word);
     } else {
       const uint32_t at = C::lane_copy(lane);
       const uint32_t w[2] = {c == 6 ? ((lane & 7) ? __builtin_amdgcn_alignbit(k.y, k.x, 16) : k.x) : k.x, c == 6 ? ((lane & 7) ? k.y >> 16 : k.y) : k.y};
@@ -137,16 +135,12 @@ template <int NCW> struct TileCodes {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t word = (e & 3) < there[e >> 2] ? vs[e] : 0u;
-        const float mine = half_bits_to_float((uint16_t)word), other = __shfl_xor(mine, 32);
-        const int x = exponent(mine, other);
-        const float step = __builtin_ldexpf(mine, -x), zero = (float)(word >> 16);
-        const uint32_t w = NCW == kRtn4 ? v[e] : v[e] >> (4 * (lane & 1));
-        const uint32_t low = w & ((1u << NCW) - 1u), high = (w >> NCW) & ((1u << NCW) - 1u);
-        d[e] = f16_pair(((float)low - zero) * step, ((float)high - zero) * step);
-        const float by = (e & 3) < there[e >> 2] ? __builtin_ldexpf(1.0f, x) : 0.f;
-        most = fmaxf(most, by);
-        if (lane == 0) scales[kTokens + value_token(part, e)] = by;
+        const float step = half_bits_to_float((uint16_t)word);
+        d[e] = less_zero<0>(NCW == kRtn4 ? v[e] : v[e] >> (4 * (lane & 1)), 0, word);
+        most = fmaxf(most, step);
+        if ((lane & 31) == 0) scales[(2 + (lane >> 5)) * kTokens + value_token(part, e)] = step;
       }
+      most = pair_max(most);
     } else {
       const uint32_t at = C::lane_copy(lane);
 #pragma unroll
@@ -155,14 +149,14 @@ template <int NCW> struct TileCodes {
         d[e] = C::point(table, code << 8 | at);
       }
       most = (lane & 3) < (lane & 4 ? there[1] : there[0]) ? half_bits_to_float((uint16_t)vs[0]) : 0.f;
-      if (lane < 8) scales[kTokens + value_token(part, lane)] = most;
+      if (lane < 8) scales[kHalves * kTokens + value_token(part, lane)] = most;
       most = fmaxf(most, quad_xor<1>(most));
       most = fmaxf(most, quad_xor<2>(most));
       most = fmaxf(most, octet_mirror(most));
     }
     if (lane == 0) {
-      scales[2 * kTokens + part] = most;
-      scales[2 * kTokens + 8 + part] = missing ? 1.0f : 0.0f;
+      scales[kLargest + part] = most;
+      scales[kMissing + part] = missing ? 1.0f : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -173,8 +167,18 @@ template <int NCW> struct TileCodes {
       *reinterpret_cast<u32x4*>(values + value_place(swapped(2 * lane + i), part)) = x;
     }
   }
-  // power of two behind which a token's two steps are held (so that products with codes stay in fp16's range)
-  static __device__ __forceinline__ int exponent(float s0, float s1) { return __builtin_amdgcn_frexp_expf(fmaxf(s0, s1)); }
+  // uniform: fields F and F + 1 of byte `byte` of x, less the zero point in the upper half of `word`.  A field that is masked in place is 2^s times its code; behind
+  // the bits of 1024 it is an fp16 number, 2^-s times which is 2^(10 - s) + code: one instruction takes that and the zero point off.  All of it is exact (zero
+  // points up to 1023, as in the other kernel).
+  template <int F> static __device__ __forceinline__ uint32_t less_zero(uint32_t x, int byte, uint32_t word) {
+    constexpr uint32_t s0 = NCW * F, s1 = NCW * (F + 1), mask = (1u << NCW) - 1u;
+    constexpr float by0 = 1.0f / (1 << s0), by1 = 1.0f / (1 << s1);
+    constexpr f16x2 by = {(_Float16)by0, (_Float16)by1}, less = {(_Float16)(-1024.0f * by0), (_Float16)(-1024.0f * by1)};
+    const uint32_t both = __builtin_amdgcn_perm(x, x, 0x0c000c00u + 0x00010001u * (uint32_t)byte);
+    const uint32_t y = (both & (mask << s0 | mask << (16 + s1))) | 0x64006400u;
+    const _Float16 zero = (_Float16)(uint16_t)(word >> 16);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, y), by, less - f16x2{zero, zero}));
+  }
 };
 
 // ---------------------------------------------------------------- the kernel
@@ -186,7 +190,9 @@ template <int NCW> struct TileCodes {
 template <int NCW>
 __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tiles_kernel(const PagedAttendArgs a) {
   typedef Codes<NCW, 1> C;
+  typedef TileCodes<NCW> Tile;
   constexpr bool kRtn = C::kRtn;
+  constexpr int kHalves = Tile::kHalves, kBufferBytes = Tile::kBufferBytes;
   __shared__ __align__(256) unsigned char lds[C::kTableBytes + 2 * kBufferBytes];
   unsigned char* const buffers = lds + C::kTableBytes;
   const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = uniform(threadIdx.x >> 6);
@@ -204,7 +210,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
   const TokenRange range = piece_range(piece, (tiles_of_tokens(last_limit + 1, kTokens) + a.slots - 1) / a.slots, kTokens, last_limit + 1);
   const int t_begin = range.begin, t_end = range.end;
 
-  TileCodes<NCW> codes;
+  Tile codes;
   const auto request = [&](int t) { codes.request(a, b, w.len, h, t, wave, lane); };
   const auto store = [&](int n) { codes.store(lds, buffers + n * kBufferBytes, wave, lane); };
   if (t_begin < t_end) request(t_begin);
@@ -264,30 +270,39 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     const unsigned char* const buffer = buffers + n * kBufferBytes;
     const float* const scales = reinterpret_cast<const float*>(buffer + 2 * kKeyBytes);
     // groups of 8 tokens whose page is not in the pool
-    const uint32_t missing = (uint32_t)__builtin_amdgcn_ballot_w64(scales[2 * kTokens + 8 + (lane & 7)] != 0.f) & 255u;
+    const uint32_t missing = (uint32_t)__builtin_amdgcn_ballot_w64(scales[Tile::kMissing + (lane & 7)] != 0.f) & 255u;
     const bool masked = t + kTokens - 1 > wave_first || missing != 0;
     float lift;                                            // power of two of the tile's largest scale
     {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(scales + 2 * kTokens), y = *reinterpret_cast<const f32x4*>(scales + 2 * kTokens + 4);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(scales + Tile::kLargest), y = *reinterpret_cast<const f32x4*>(scales + Tile::kLargest + 4);
       lift = __builtin_amdgcn_logf(fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))), 0x1p-24f));
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {                          // 32 tokens each
-      f32x16 s = {};
+      f32x16 part[kHalves] = {};
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(buffer + key_place(32 * i + col, 2 * k + hf)), q[k], s, 0, 0, 0);
+      for (int k = 0; k < 8; ++k) {
+        f32x16& x = part[k * kHalves / 8];
+        x = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(buffer + key_place(32 * i + col, 2 * k + hf)), q[k], x, 0, 0, 0);
+      }
       // the next tile's codes to the other buffer
       if (i == 0 && t + kTokens < t_end) {
         store(n ^ 1);
         if (t + 2 * kTokens < t_end) request(t + 2 * kTokens);
       }
       // register 4 j + e is token 32 i + 8 j + 4 hf + e
+      f32x16& s = part[0];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const f32x4 sk = *reinterpret_cast<const f32x4*>(scales + 32 * i + 8 * j + 4 * hf);
+        const float* const at = scales + 32 * i + 8 * j + 4 * hf;
+        const f32x4 sk = *reinterpret_cast<const f32x4*>(at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * j + e] *= sk[e];
+        if constexpr (kRtn) {
+          const f32x4 upper = *reinterpret_cast<const f32x4*>(at + kTokens);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * j + e] = __fmaf_rn(part[1][4 * j + e], upper[e], s[4 * j + e]);
+        }
       }
       if (masked) {
         asm volatile("");                                  // (a branch: the selects would cost every tile an instruction and a half per score)
@@ -316,20 +331,22 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
       const unsigned char* const values = buffer + kKeyBytes;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {                        // 16 tokens each
-        f16x8 weight;
+        f16x8 weight[kHalves];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const f32x4 sv = *reinterpret_cast<const f32x4*>(scales + kTokens + 32 * i + 16 * k + 8 * j + 4 * hf);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            sum += p[8 * k + 4 * j + e];
-            weight[4 * j + e] = (_Float16)(p[8 * k + 4 * j + e] * sv[e]);
+          for (int half = 0; half < kHalves; ++half) {
+            const f32x4 sv = *reinterpret_cast<const f32x4*>(scales + (kHalves + half) * kTokens + 32 * i + 16 * k + 8 * j + 4 * hf);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) weight[half][4 * j + e] = (_Float16)(p[8 * k + 4 * j + e] * sv[e]);
           }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum += p[8 * k + 4 * j + e];
         }
 #pragma unroll
         for (int R = 0; R < 4; ++R)
-          o[R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(values + value_place(32 * R + col, 4 * i + 2 * k + hf)), weight, o[R], 0,
-                                                        0, 0);
+          o[R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(values + value_place(32 * R + col, 4 * i + 2 * k + hf)),
+                                                        weight[R * kHalves / 4], o[R], 0, 0, 0);
       }
     }
     __syncthreads();

@@ -36,3 +36,57 @@ def test_a_sequence_of_almost_2_31_tokens(fmt, QH, queries):
     bound = (size * (2 * 2.0 ** -11 + 2 * 2128 * 2.0 ** -24) + (2.0 ** -5 + 2.0 ** -8) * want[:, 0].norm(dim=-1))[:, None].expand(queries, QH)
     P.check(out, want, bound, fmt)
     assert (bound < 0.5 * want.norm(dim=-1)).all()                          # (a lost half of them would show)
+
+
+@pytest.mark.parametrize("fmt", ["rtn4", "rtn2"])
+@pytest.mark.parametrize("dtype,QH", [("bf16", 8), ("bf16", 20), ("bf16", 160), ("fp32", 8)])
+def test_uniform_steps_of_a_heads_halves_far_apart(dtype, fmt, QH):
+    """Each half of a head keeps its own bits, however much larger the other one's step is: keys whose halves are 2^20 apart under queries the other way round, so
+    that both count, and values whose halves are 2^22 apart, looked at one by one.  16 sequences of two tokens, the second with a score of 0 and no value: a row is
+    sigmoid(score) v.
+
+    A score is off by A (u + 64 s + t), A = scale * sum |q_i| step (code + zero) over the products as they are taken: queries are rounded to u (bf16 layers: fp16,
+    2^-11; fp32 layers: two fp16 numbers, 2^-22), codes and zero points are not, sums have 64 roundings of s = 2^-24 on a product's way, and the matrix
+    instructions keep codes that are subnormal numbers to t = 2^-17 (bf16 layers).  Besides, fp16 ends at 2^-24: a row's query is held with its largest coordinate at
+    2^13 or above, divided by up to 2^bits or 2^(3 * 2) where codes are masked in place (4, 2 bits), so that any coordinate is off by half of 2^-24 * that, which is
+    2^-38 * that of the largest one: a 2^-12 of a coordinate that is 2^22 times smaller, as some here are.  (This term was added when fp32 layers had come out at 1.6
+    times the bound without it.)  A weight then, relative: (1 - p) of that, 2^-22 |score| of the exponent's argument, and its rounding u (with the step in it).  Weights
+    with their steps are fp16 numbers (one, or two) too, and the largest of a row is 2^8 or above, so that each is off by half of 2^-24, 2^-33 of the largest:
+    relative to one of a half whose step is r times smaller, of a token that is not the likelier one, 2^-33 r max(1, e^-score).  (Added when that half of fp32
+    layers had come out at 2^-11, as it says.)  The rest is below 2^-20, at the end one rounding."""
+    need_gpu()
+    u, t, last = (2.0 ** -11, 2.0 ** -17, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -22, 0.0, 2.0 ** -24)
+    batch, scale = 16, 0.02
+    lo, lg, pages = P.make(1, dtype, fmt, batch, 8)
+    gen = torch.Generator().manual_seed(QH)
+    P.fill(lo, pages, gen, 0.3)
+    first = 8 * torch.arange(batch)
+    step = lambda x: torch.as_tensor(x).half().view(torch.int16).cuda()
+    unit = 2.0 / (2 ** lo.rtn_bits - 1)
+    for scales, halves in ((pages.k_scales, (2.0 ** 12, 2.0 ** -8)), (pages.v_scales, (2.0 ** 10, 2.0 ** -12))):
+        for i, size in enumerate(halves):
+            scales[first.cuda(), i, 0] = step(size * unit * (1 + torch.rand(batch, generator=gen)))
+        scales[first.cuda() + 1, :, 0] = 0
+    q = 1.5 * torch.randn(batch, QH, 128, generator=gen)
+    q[..., :64] *= 2.0 ** -12
+    q[..., 64:] *= 2.0 ** 8
+    q = q.to(P.storage(dtype)).cuda()
+    table, lens = torch.arange(batch, dtype=torch.int32)[:, None], torch.full((batch,), 2, dtype=torch.int32)
+    out = attend(lg, pages, table, lens, q, [1] * batch, scale).double().cpu()
+    k, v = (P.held(lo, c, s, None)[first, 0] for c, s in ((pages.k_codes, pages.k_scales), (pages.v_codes, pages.v_scales)))
+    x = q.double().cpu()
+    steps, zeros = (pages.k_scales[first.cuda(), :, i].cpu().contiguous() for i in (0, 1))
+    offset = (steps.view(torch.float16).double() * zeros.double()).repeat_interleave(64, 1)
+    A = scale * (x.abs() @ (k.abs() + 2 * offset)[:, :, None])[..., 0]
+    end = scale * x.abs().amax(-1) * 2.0 ** -38 * (16 if lo.rtn_bits == 4 else 64) * (k.abs() + 2 * offset).sum(-1)[:, None]
+    score = scale * (x @ k[:, :, None])[..., 0]
+    p = torch.sigmoid(score)
+    bound = (1 - p) * (A * (u + 64 * 2.0 ** -24 + t) + end) + score.abs() * 2.0 ** -22 + u + 2.0 ** -20 + last
+    assert (A.mean() < 40) and (bound.mean() < 0.05)                        # (else nothing would show)
+    v_steps = pages.v_scales[first.cuda(), :, 0].cpu().contiguous().view(torch.float16).double()
+    for i, half in enumerate((slice(0, 64), slice(64, 128))):
+        bound_half = bound + 2.0 ** -33 * (v_steps.amax(1) / v_steps[:, i])[:, None] * torch.exp(-score).clamp(min=1)
+        want = p[..., None] * v[:, None, half]
+        off = (out[..., half] - want).norm(dim=-1) / want.norm(dim=-1)
+        print(f"  {dtype} {fmt} {QH} {half.start}: worst {(off / bound_half).max().item():.3g} of the bound, {off.max().item():.3g}; A {A.mean().item():.3g}", flush=True)
+        assert (off <= bound_half).all()
