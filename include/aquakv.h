@@ -516,7 +516,8 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   out[r, qh, :] = sum_t p_t vhat_t,  p = softmax over t of score_scale * q[r, qh, :] . khat_t, of kv head qh / (q_heads / kv_heads),
  *   khat, vhat what codes and scales stand for, unrounded.  Sequence b has seq_lens[b] tokens in the cache, token t in page
  *   page_table[b, t / page_tokens]; its queries are its last tokens: query i of n sees the tokens t <= seq_lens[b] - n + i, which
- *   must have been appended already.  A query that sees no token gives 0.  Queries are taken as already rotated.
+ *   must have been appended already.  A query that sees no token gives 0; what it does not see has no effect on it, scales that are
+ *   not finite included.  Queries are taken as already rotated.
  *   q [q_rows, q_heads, 128], row r at q + r * q_stride elements (16-byte aligned rows); out [q_rows, q_heads, 128]; both dtype.
  *   q_start NULL: max_queries queries of every sequence, q_rows = batch * max_queries.  Else device int32 [batch + 1], ascending:
  *   sequence b has the rows q_start[b] ... q_start[b + 1] - 1, at most max_queries (rows beyond that, and rows of no sequence, are

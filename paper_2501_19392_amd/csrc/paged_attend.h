@@ -562,9 +562,11 @@ template <int NCW, int TERMS> struct Codes {
     }
   }
 
-  // ---- o[j] += values (coordinates: result()) * weights p * scale
-  template <int COLS> static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, const float (&p)[COLS][8],
-                                                                    const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane, Column (&col)[COLS]) {
+  // ---- o[j] += values (coordinates: result()) * weights p * scale.  `there` of the lane's tokens are; masked: a row sees the first seen[] of them, and what the
+  // scales of the others are is no matter (0 times a number that is not finite would be).
+  template <int COLS> static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, bool masked, const int (&seen)[COLS],
+                                                                    const float (&p)[COLS][8], const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane,
+                                                                    Column (&col)[COLS]) {
     f16x8 b[COLS][kHalves][TERMS];
 #pragma unroll
     for (int n = 0; n < COLS; ++n)
@@ -575,6 +577,19 @@ template <int NCW, int TERMS> struct Codes {
         for (int e = 0; e < 8; ++e) weight[e] = p[n][e] * half_at(vs[k], e);
         split_f16<TERMS>(weight, b[n][k]);
       }
+    if (masked) {
+      asm volatile("");
+#pragma unroll
+      for (int n = 0; n < COLS; ++n)
+#pragma unroll
+        for (int k = 0; k < kHalves; ++k)
+#pragma unroll
+          for (int i = 0; i < TERMS; ++i) {
+            u32x4 x = __builtin_bit_cast(u32x4, b[n][k][i]);
+            keep_first(x, seen[n]);
+            b[n][k][i] = __builtin_bit_cast(f16x8, x);
+          }
+    }
     if constexpr (kRtn) {
       // All rows of an operand have to be of one half (the weights are the half's): of the eight codes that a lane holds, lanes m and m ^ 8
       // exchange four.  Lower half-word: coordinates of the lower half, upper one: of the upper half.

@@ -139,19 +139,25 @@ paged_attend_kernel(const PagedAttendArgs a) {
 #pragma unroll
     for (int k = 0; k < C::kHalves; ++k) vs[k] = C::value_scales(scale_lds, k, g);
     const int held = (there >> g) & 1 ? w.len - (t + 8 * g) : 0;           // so many of the lane's eight tokens are there: the others hold anything
-    if (t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u) {      // (t_end: of this piece, whole tiles but for the last)
+    const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;      // (t_end: of this piece, whole tiles but for the last)
+    float lift[COLS];
+    lift[0] = C::lift_of(vs);
+#pragma unroll
+    for (int i = 1; i < COLS; ++i) lift[i] = lift[0];
+    if (masked) {
       asm volatile("");                                    // (a branch, not selects that every tile would pay for)
 #pragma unroll
       for (int i = 0; i < COLS; ++i) {
         const int seen = min(col[i].limit + 1 - (t + 8 * g), held);
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[i][e] = e < seen ? p[i][e] : -INFINITY;
-      }
+        u32x4 own[C::kHalves];
 #pragma unroll
-      for (int k = 0; k < C::kHalves; ++k) C::keep_first(vs[k], held);
+        for (int k = 0; k < C::kHalves; ++k) { own[k] = vs[k]; C::keep_first(own[k], seen); }
+        lift[i] = C::lift_of(own);
+      }
     }
     // The reference follows where the largest weight that the scores allow is too large: such weights become 2^kStartExp.
-    const float lift = C::lift_of(vs);
     float top[COLS];
     bool high = false;
 #pragma unroll
@@ -159,12 +165,12 @@ paged_attend_kernel(const PagedAttendArgs a) {
       top[i] = p[i][0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top[i] = fmaxf(top[i], p[i][e]);
-      high |= __fmaf_rn(top[i], col[i].f, lift - col[i].ref) > kTopExp;
+      high |= __fmaf_rn(top[i], col[i].f, lift[i] - col[i].ref) > kTopExp;
     }
     if (__builtin_amdgcn_ballot_w64(high) != 0) {
 #pragma unroll
       for (int i = 0; i < COLS; ++i) {
-        const float moved = fmaxf(col[i].ref, column_max(__fmaf_rn(top[i], col[i].f, lift)) - kStartExp);
+        const float moved = fmaxf(col[i].ref, column_max(__fmaf_rn(top[i], col[i].f, lift[i])) - kStartExp);
         const float by = __builtin_amdgcn_exp2f(col[i].ref - moved);
         col[i].ref = moved;
         col[i].sum *= by;
@@ -181,7 +187,10 @@ paged_attend_kernel(const PagedAttendArgs a) {
         col[i].sum += p[i][e];
       }
     __builtin_amdgcn_sched_barrier(0);
-    C::values(xv, scale_lds, held, p, vs, lds, lane, col);
+    int seen[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) seen[i] = min(col[i].limit + 1 - (t + 8 * g), held);
+    C::values(xv, scale_lds, held, masked, seen, p, vs, lds, lane, col);
   };
   // Keys are requested a tile ahead, values behind the tile that takes their registers, the rows they are in two tiles ahead.
 #pragma unroll 1

@@ -304,21 +304,33 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
           for (int e = 0; e < 4; ++e) s[4 * j + e] = __fmaf_rn(part[1][4 * j + e], upper[e], s[4 * j + e]);
         }
       }
+      // of tokens 32 i + 8 j + 4 hf ... the row sees so many
+      const auto seen_of = [&](int j) { return !((missing >> (4 * i + j)) & 1) ? limit + 1 - (t + 32 * i + 8 * j + 4 * hf) : 0; };
+      const auto value_scales = [&](int half, int j) { return *reinterpret_cast<const f32x4*>(scales + (kHalves + half) * kTokens + 32 * i + 8 * j + 4 * hf); };
+      float own_lift = lift;
       if (masked) {
         asm volatile("");                                  // (a branch: the selects would cost every tile an instruction and a half per score)
+        float most = 0x1p-24f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int seen = !((missing >> (4 * i + j)) & 1) ? limit + 1 - (t + 32 * i + 8 * j + 4 * hf) : 0;
+          const int seen = seen_of(j);
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[4 * j + e] = e < seen ? s[4 * j + e] : -INFINITY;
+#pragma unroll
+          for (int half = 0; half < kHalves; ++half) {
+            const f32x4 sv = value_scales(half, j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = fmaxf(most, e < seen ? sv[e] : 0.f);
+          }
         }
+        own_lift = __builtin_amdgcn_logf(most);
       }
       // the largest weight that the scores allow
       float top = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-      if (__builtin_amdgcn_ballot_w64(__fmaf_rn(top, f, lift - ref) > kTopExp) != 0) {
-        const float moved = fmaxf(ref, pair_max(__fmaf_rn(top, f, lift)) - kStartExp);
+      if (__builtin_amdgcn_ballot_w64(__fmaf_rn(top, f, own_lift - ref) > kTopExp) != 0) {
+        const float moved = fmaxf(ref, pair_max(__fmaf_rn(top, f, own_lift)) - kStartExp);
         const float by = __builtin_amdgcn_exp2f(ref - moved);
         ref = moved;
         sum *= by;
@@ -336,12 +348,23 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
           for (int half = 0; half < kHalves; ++half) {
-            const f32x4 sv = *reinterpret_cast<const f32x4*>(scales + (kHalves + half) * kTokens + 32 * i + 16 * k + 8 * j + 4 * hf);
+            const f32x4 sv = value_scales(half, 2 * k + j);
 #pragma unroll
             for (int e = 0; e < 4; ++e) weight[half][4 * j + e] = (_Float16)(p[8 * k + 4 * j + e] * sv[e]);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum += p[8 * k + 4 * j + e];
+        }
+        if (masked) {                                      // (a scale that is not finite, of a token that the row does not see, would make its weight NaN)
+          asm volatile("");
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int seen = seen_of(2 * k + j);
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) weight[half][4 * j + e] = e < seen ? weight[half][4 * j + e] : (_Float16)0.f;
+          }
         }
 #pragma unroll
         for (int R = 0; R < 4; ++R)

@@ -90,3 +90,27 @@ def test_uniform_steps_of_a_heads_halves_far_apart(dtype, fmt, QH):
         off = (out[..., half] - want).norm(dim=-1) / want.norm(dim=-1)
         print(f"  {dtype} {fmt} {QH} {half.start}: worst {(off / bound_half).max().item():.3g} of the bound, {off.max().item():.3g}; A {A.mean().item():.3g}", flush=True)
         assert (off <= bound_half).all()
+
+
+@pytest.mark.parametrize("dtype,fmt,QH,queries", [("bf16", "grid256", 2, 3), ("bf16", "rtn4", 2, 3), ("bf16", "grid64", 4, 20), ("bf16", "rtn2", 4, 20),
+                                                  ("bf16", "grid16", 4, 70), ("bf16", "rtn4", 4, 70), ("fp32", "grid256", 4, 20), ("fp32", "rtn2", 4, 20)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("which", ["keys", "values", "both"])
+def test_what_a_query_does_not_see_is_no_matter(dtype, fmt, QH, queries, bad, which):
+    """Rows that are not finite, among the last tokens: the queries before them are as if they were not there, those behind them are not finite."""
+    need_gpu()
+    from tests.test_gpu_paged import build
+    lo, lg, pages, table, lens, q, counts = build(dtype, fmt, 1, QH, [150, 97], 16, queries)
+    want, bound = P.reference(lo, pages, table, lens, q, counts, SCALE, dtype)            # (finite: what the queries before them see stays the same)
+    bad_from = queries // 3
+    for b in range(2):
+        row = int(P.sequence_rows(pages, table[b], int(lens[b]))[int(lens[b]) - queries + bad_from])
+        for name, t in (("keys", pages.k_scales), ("values", pages.v_scales)):
+            if which in (name, "both"):
+                (t[..., 0] if lo.rtn_bits is not None else t)[row] = int(torch.tensor(bad).half().view(torch.int16))
+    out = attend(lg, pages, table, lens, q, counts)
+    for b in range(2):
+        own = slice(b * queries, b * queries + bad_from)
+        P.check(out[own], want[own], bound[own], f"{fmt} {b}")
+        if bad != bad or which != "keys":                                   # (an infinite key has a score of -inf, and so no weight, with half of all queries)
+            assert (~torch.isfinite(out[b * queries + bad_from:(b + 1) * queries].double())).any(-1).all()
