@@ -100,3 +100,18 @@ def test_nothing_to_do():
     for batch, rows, most in ((0, 6, 2), (3, 0, 2), (3, 6, 0)):
         start = 8 << 32
         assert B._lib.aquakv_paged_attend(lay.c, p, batch, 4, 5 << 32, 3, 6 << 32, rows, most, start, 7 << 32, 512, 1.0, 9 << 32, None, 0, None) == B.AQUAKV_OK
+
+
+def test_the_workspace_of_nothing_and_of_something():
+    """A call that has nothing to do takes a workspace of no bytes, any other one not (the binding hands over how many there are)."""
+    lay = layer()
+    pages = B.Pages(lay, 3, 8, device="cpu")
+    q, table, lens = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    at = 1 << 33
+    B.aquakv_paged_attend(lay, pages, 2, 4, table, lens, q, 0, torch.zeros(3, dtype=torch.int32), 1.0, q.clone(), (at, 0))
+    need = B.aquakv_paged_workspace_bytes(lay, pages, 2, 4, 3, 2, 1)
+    assert need > 0
+    for nbytes in (0, need - 1):
+        with pytest.raises(B.AquaKVError) as e:
+            B.aquakv_paged_attend(lay, pages, 2, 4, table, lens, q, 1, None, 1.0, q.clone(), (at, nbytes))
+        assert e.value.status == B.AQUAKV_EWORKSPACE
