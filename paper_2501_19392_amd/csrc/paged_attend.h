@@ -142,6 +142,14 @@ __device__ __forceinline__ float column_max(float x) {
   swap_lanes<32>(x, y);
   return fmaxf(x, y);
 }
+// a tile's weights, by pairs: one after the other, a lane's millions of equal weights would be off by 2^-24 of the sum each, all to one side (2^21 tokens: 1.2 %)
+template <int N> __device__ __forceinline__ float sum_of(const float (&x)[N]) {
+  float y[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) y[i] = x[2 * i] + x[2 * i + 1];
+  if constexpr (N == 2) return y[0];
+  else return sum_of(y);
+}
 __device__ __forceinline__ float column_sum(float x) { return far_sum<32>(far_sum<16>(x)); }
 // The (unnormalised) transform of a row's 128 values, 32 g ... in lane group g.
 __device__ __forceinline__ void wht_columns(float (&v)[32]) {

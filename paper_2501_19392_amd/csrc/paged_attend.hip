@@ -180,12 +180,11 @@ paged_attend_kernel(const PagedAttendArgs a) {
       }
     }
 #pragma unroll
-    for (int i = 0; i < COLS; ++i)
+    for (int i = 0; i < COLS; ++i) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[i][e] = __builtin_amdgcn_exp2f(__fmaf_rn(p[i][e], col[i].f, -col[i].ref));
-        col[i].sum += p[i][e];
-      }
+      for (int e = 0; e < 8; ++e) p[i][e] = __builtin_amdgcn_exp2f(__fmaf_rn(p[i][e], col[i].f, -col[i].ref));
+      col[i].sum += sum_of(p[i]);
+    }
     __builtin_amdgcn_sched_barrier(0);
     int seen[COLS];
 #pragma unroll

@@ -340,6 +340,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
       float p[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], f, -ref));
+      sum += sum_of(p);
       const unsigned char* const values = buffer + kKeyBytes;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {                        // 16 tokens each
@@ -352,8 +353,6 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int e = 0; e < 4; ++e) weight[half][4 * j + e] = (_Float16)(p[8 * k + 4 * j + e] * sv[e]);
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum += p[8 * k + 4 * j + e];
         }
         if (masked) {                                      // (a scale that is not finite, of a token that the row does not see, would make its weight NaN)
           asm volatile("");

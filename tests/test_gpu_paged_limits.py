@@ -30,10 +30,10 @@ def test_a_sequence_of_almost_2_31_tokens(fmt, QH, queries):
     total = P.held(lo, pages.v_codes[rows.cuda()], pages.v_scales[rows.cuda()], lo.signs_v)[:, 0].sum(0)
     seen = 2 * page - (queries - 1 - torch.arange(queries)).double()                     # (tokens that a query does not see have no value)
     want = (2 * total[None] / seen[:, None])[:, None].expand(queries, QH, 128)
-    # Weights and grid points are rounded to fp16 (2^-11 each), 2128 values are added in fp32.  A lane adds the weights of half a page, 2^19 of them, one after
-    # the other in fp32, each by a rounding of at most 2^-24 of the sum: 2^-5.  At the end one rounding to bf16.
+    # Weights and grid points are rounded to fp16 (2^-11 each), 2128 values are added in fp32.  A lane adds the weights of a tile, and
+    # the sums of a page's tiles, 2^15 of them, one after the other in fp32, each by a rounding of at most 2^-24 of the sum: 2^-9.  At the end one rounding to bf16.
     size = 2 * P.held(lo, pages.v_codes[rows.cuda()], pages.v_scales[rows.cuda()], lo.signs_v)[:, 0].norm(dim=-1).sum() / seen
-    bound = (size * (2 * 2.0 ** -11 + 2 * 2128 * 2.0 ** -24) + (2.0 ** -5 + 2.0 ** -8) * want[:, 0].norm(dim=-1))[:, None].expand(queries, QH)
+    bound = (size * (2 * 2.0 ** -11 + 2 * 2128 * 2.0 ** -24) + (2.0 ** -9 + 2.0 ** -8) * want[:, 0].norm(dim=-1))[:, None].expand(queries, QH)
     P.check(out, want, bound, fmt)
     assert (bound < 0.5 * want.norm(dim=-1)).all()                          # (a lost half of them would show)
 
@@ -114,3 +114,31 @@ def test_what_a_query_does_not_see_is_no_matter(dtype, fmt, QH, queries, bad, wh
         P.check(out[own], want[own], bound[own], f"{fmt} {b}")
         if bad != bad or which != "keys":                                   # (an infinite key has a score of -inf, and so no weight, with half of all queries)
             assert (~torch.isfinite(out[b * queries + bad_from:(b + 1) * queries].double())).any(-1).all()
+
+
+@pytest.mark.parametrize("batch,queries", [(256, 130), (256, 1), (200, 20)])
+@pytest.mark.parametrize("step", [0.55, 0.7, 0.95])
+def test_equal_weights_of_two_million_tokens(batch, queries, step):
+    """Sequences of 2^21 tokens (the same page over and over) with scores of 0, so that a row is the mean of the page.  So many sequences that one workgroup, or a
+    few waves, take a whole one each: a lane adds up the weights of 2^19 to 2^20 tokens, all alike.
+
+    Codes, steps and weights with their steps are exact here (2^8), so are sums of values but for 2^-24 of them for each addition; the weights of a tile are added
+    first and then to the sum: 2^16 additions, 2^-24 of it each, 2^-8 in all, where one after the other would be 2^20 of them.  One rounding to bf16, 2^-8 of a
+    coordinate at most.  Values: additions of 32 products a tile, 2^16 of those or half as many, 2^-8."""
+    need_gpu()
+    page, pages_each = 2048, 1024
+    lo, lg, pages = P.make(1, "bf16", "rtn4", 1, page)
+    gen = torch.Generator().manual_seed(3)
+    P.fill(lo, pages, gen)
+    for t in (pages.k_scales, pages.v_scales):
+        t[..., 0] = int(torch.tensor(step).half().view(torch.int16))
+        t[..., 1] = 0
+    q = torch.zeros(batch * queries, 1, 128, dtype=torch.bfloat16, device="cuda")
+    table, lens = torch.zeros(batch, pages_each, dtype=torch.int32), torch.full((batch,), page * pages_each, dtype=torch.int32)
+    print(f"case two million tokens batch={batch} queries={queries}", flush=True)
+    out = attend(lg, pages, table, lens, q, [queries] * batch).double().cpu()[:, 0]
+    want = P.held(lo, pages.v_codes, pages.v_scales, None)[:, 0].mean(0)
+    off = ((out - want).norm(dim=-1) / want.norm()).max().item()
+    print(f"  off by {off:.3g}", flush=True)
+    # (a query sees up to 130 tokens less of 2^21, 2^-14 of them)
+    assert off <= 3 * 2.0 ** -8 + 2.0 ** -13
