@@ -496,6 +496,20 @@ def _typed(x, dtype, n: int, name: str, device: int):
     return x.data_ptr()
 
 
+def _rope_tables(cos, sin, device: int):
+    """Two tensors [positions, 64] -> (addresses, positions).  (The number of elements is not enough: a table of both halves' angles would be one of twice the rows.)"""
+    if cos is None and sin is None:
+        return None, None, 0
+    if cos.__class__ is int or sin.__class__ is int or cos is None or sin is None:
+        raise ValueError("rope_cos and rope_sin must be tensors [positions, 64], both of them")
+    shape, at, at_sin = cos.shape, cos.get_device(), sin.get_device()
+    if len(shape) != 2 or shape[1] != 64 or sin.shape != shape:
+        raise ValueError("rope_cos and rope_sin must be tensors [positions, 64]")
+    if cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or at != device or at_sin != device or not cos.is_contiguous() or not sin.is_contiguous():
+        raise ValueError("rope_cos and rope_sin must be contiguous, torch.float32, on the current device")
+    return cos.data_ptr(), sin.data_ptr(), shape[0]
+
+
 def _pool_here(layer, pages, device: int) -> None:
     if layer.quantizer_device is not None and layer.quantizer_device != device:
         raise ValueError("the layer's grid, signs and search table are not on the current device")
@@ -515,16 +529,10 @@ def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_
     v, vs, nv = _rows(V, dtype, row, "V", here)
     if (nk is not None and nk != tokens) or (nv is not None and nv != tokens):
         raise ValueError(f"K and V must have {tokens} rows")
-    rope_rows = 0
-    if rope_cos is not None:                                # (numbers of elements are not enough: a table of both halves' angles would be one of twice the rows)
-        if (rope_cos.__class__ is int or rope_sin.__class__ is int or rope_cos.dim() != 2 or rope_cos.shape[1] != 64 or
-                (rope_sin is not None and rope_sin.shape != rope_cos.shape)):
-            raise ValueError("rope_cos and rope_sin must be tensors [positions, 64]")
-        rope_rows = rope_cos.shape[0]
+    cos, sin, rope_rows = _rope_tables(rope_cos, rope_sin, here)
     _check(_lib.aquakv_paged_append(_layer_ref(layer), _pages_ref(pages), tokens, k, ks, v, vs, _typed(slots, torch.int64, tokens, "slots", here),
                                     _typed(positions, torch.int32, tokens, "positions", here),
-                                    _typed(rope_cos, torch.float32, 64 * rope_rows, "rope_cos", here),
-                                    _typed(rope_sin, torch.float32, 64 * rope_rows, "rope_sin", here), rope_rows,
+                                    cos, sin, rope_rows,
                                     _typed(Khat, dtype, tokens * row, "Khat", here), _typed(Vhat, dtype, tokens * row, "Vhat", here),
                                     _stream(stream)))
 
