@@ -524,12 +524,17 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   left as they were).  Counts are read on the device, so a captured call follows them: lengths are cut to 0 ... table_pages *
  *   page_tokens, row numbers to 0 ... q_rows, and tokens of a page that is not in the pool (page_table outside 0 ... n_pages - 1)
  *   are not seen.  page_table, seq_lens, q_start: aligned to 4 bytes.
- *   bf16: products in fp16 with fp32 sums (queries and grid points rounded to fp16 behind a power of two, weights likewise), results within a
- *   rounding of bf16; fp32: each of them as the sum of two fp16 numbers (22 bits), fp32 sums.
+ *   bf16: products in fp16 with fp32 sums: rotated queries, grid points and weights times the value's scale are rounded to fp16 behind
+ *   powers of two, uniform codes are exact (up to 128 rows of a kv head their sums keep 2^-17 of the largest product); a weight times its
+ *   value's scale is kept to 2^-33 of a row's largest.  Errors are 1 to 1.5 times those of rounding the exact result to bf16.  fp32: each of
+ *   the factors as the sum of two fp16 numbers (22 bits, the product of the two second ones left out), fp32 sums.
+ *   A call is laid out by max_queries: sequences of few queries beside one of more than 128 rows (queries x query heads of a kv head) take
+ *   many times what they take in a call of their own.
  *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments) for the same layer, pages and sizes (other sizes may
  *   need more, smaller ones too); the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same
- *   time, captured ones included, need workspaces of their own.  At most 65535 sequences, max_queries * q_heads < 2^22, batch *
- *   kv_heads < 2^25, table_pages * page_tokens < 2^31 - 4096 and 2^35 over the batch: AQUAKV_EUNSUPPORTED beyond.
+ *   time, captured ones included, need workspaces of their own.  At most 65535 sequences, max_queries * q_heads < 2^22, max_queries *
+ *   (q_heads / kv_heads) <= 16 * 65535, q_rows < 2^31, batch * kv_heads < 2^25, table_pages * page_tokens < 2^31 - 4096 and 2^35 over
+ *   the batch: AQUAKV_EUNSUPPORTED beyond.
  *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens
  * (tokens = 0), sequences or queries (batch, q_rows or max_queries = 0) nothing is done, and buffers but the pool's may be NULL.

@@ -267,11 +267,11 @@ struct PagedAttendArgs {
   float *part, *stats;                            // [items, max_queries, q_heads, 128], [items, max_queries, q_heads, 2]
   int2* heads;                                    // [batch]: a sequence's first item, and how many
   int slots;                                      // pieces that fill the chip (blocks of rows: pieces of a sequence)
-  int row_blocks;                                 // blocks of 32 rows per wave (paged_tiles.hip)
+  int row_blocks;                                 // blocks of 256 rows (paged_tiles.hip), 0: not in such blocks
   uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
 };
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a);
-// Many queries (bf16): `waves` (4 or 8) x 32 rows per workgroup.
+// Many queries (bf16): 8 waves x 32 rows per workgroup.
 hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 

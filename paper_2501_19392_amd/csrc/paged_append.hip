@@ -4,9 +4,11 @@
 // A head's 128 values are held by eight lanes x 16 as in the stand-alone quantizer, whose body this is: the rotary embedding pairs
 // coordinates 64 apart, which sit in the same register of the lane whose position differs in the uppermost bit.
 //
-// Bound by the vector pipes: 8192 tokens of 8 heads, 256 points, with the rows read back, take 33.5 us (80 MB at 2.4 TB/s) and 840 instructions
-// for 16 values of a lane, 82 % of the cycles; the rotations there and back are 224 of them, the search 280.  A few tokens are one chain of waits (arguments,
-// rows and tables, barrier, rotation, search): one token 5.0 us in a trace.  What came out no faster: rows of a round requested during the one before
+// Bound by the vector pipes and LDS: 8192 tokens of 8 heads, 256 points, with the rows read back, take 33.7 us (80 MB at 2.4 TB/s) and 840 instructions
+// for 16 values of a lane, 82 % of the cycles; the rotations there and back are 224 of them, the search 280.  LDS is busy in 81 % of the cycles with the search's
+// look-ups, 58 % of that for bank conflicts.  Uniform codes, which have neither, are bound by memory (15.5 us, at a copy's rate).  A few tokens are one chain of waits (arguments,
+// rows and tables, grid and search table to LDS, barrier, rotation, search): one token 5.0 us in a trace (a call in a graph 6.0, with
+// uniform codes, which stage nothing, 3.3).  What came out no faster: rows of a round requested during the one before
 // (36.2 us, for registers); 32 values a lane in columns, with the way back on the matrix cores and the grid 16 times in LDS, which takes
 // bank conflicts from 58 to 22 % of the LDS cycles (34.5 us: 15 % fewer instructions, and 6 more of 64 KB to fill; one token 7.9).
 #include "codec_core.h"

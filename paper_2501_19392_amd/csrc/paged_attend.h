@@ -3,9 +3,13 @@
 //
 // Precision.  Operands are fp16 (11 bits): the rotated query times a power of two of its own, grid points times a power of two of
 // the grid's, weights times the token's scale relative to a running reference, all sums fp32.  fp32 layers hold each of them as two
-// fp16 numbers (22 bits) and take three products.  Uniform codes and zero points are exact: a code at the low end of a half-word is the
-// subnormal fp16 number code * 2^-24, which the matrix instructions take as it is, so that a mask is all the conversion there is (fp32
-// layers make it a normal number, which sums need that are to be exact beyond 2^-17).
+// fp16 numbers (22 bits) and take three products.  Uniform codes and zero points are exact operands: a code at the low end of a half-word is the
+// subnormal fp16 number code * 2^-24, which the matrix instructions take as it is, so that a mask is all the conversion there is.  They align such products
+// by the exponent, 10 above the code's bits, so that a sum keeps 2^-17 of its largest one, far below the rounding of query and weights; fp32 layers, and
+// paged_tiles.hip, which converts codes once for many rows, make them normal numbers, whose sums are fp32's.
+//
+// fp16 ends at 2^-24: coordinates of a query below 2^-27 of its largest (uniform codes, which are masked in place: 2^-23, 2 bits 2^-21), and weights with their
+// scales below 2^-22 of a row's largest, have fewer bits than 11, down to 2^-38 (2^-34, 2^-32) and 2^-33.
 #pragma once
 #include "codec_core.h"
 #include "kernels.h"
@@ -571,7 +575,7 @@ template <int NCW, int TERMS> struct Codes {
   }
 
   // ---- o[j] += values (coordinates: result()) * weights p * scale.  `there` of the lane's tokens are; masked: a row sees the first seen[] of them, and what the
-  // scales of the others are is no matter (0 times a number that is not finite would be).
+  // scales of the others are is no matter (0 times a number that is not finite would be): with one row a lane they are 0 already, with two the weights become 0.
   template <int COLS> static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, bool masked, const int (&seen)[COLS],
                                                                     const float (&p)[COLS][8], const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane,
                                                                     Column (&col)[COLS]) {
@@ -585,7 +589,7 @@ template <int NCW, int TERMS> struct Codes {
         for (int e = 0; e < 8; ++e) weight[e] = p[n][e] * half_at(vs[k], e);
         split_f16<TERMS>(weight, b[n][k]);
       }
-    if (masked) {
+    if (COLS > 1 && masked) {
       asm volatile("");
 #pragma unroll
       for (int n = 0; n < COLS; ++n)

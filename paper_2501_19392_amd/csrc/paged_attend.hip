@@ -26,6 +26,8 @@ using namespace paged;
 // vector pipes busy in 60 % of the cycles.  Few tokens: by the chain at its start (lengths, pages, codes, grid, rotated query: 3 us to
 // the first score) and the second launch, 4 us: one sequence of 700 tokens 11.1 us a call.  Many rows (8 x 9999 tokens, 5 queries, 3 bits: 33 us): by the vector
 // pipes, 54 % busy, and the waits between a tile's two products at two waves a SIMD.
+// Times of these three are of calls whose inputs change; those beside the rules below, of the same call again and again in a captured graph, whose codes may stay in
+// the caches (one sequence of 131 072 tokens, 8 rows a kv head: 46.4 us with other inputs each time, 41.9 with the same).  All of 8 kv heads.
 // Waves of a workgroup, which share the copies of the grid, and waves per SIMD: with 128 registers four fit (two workgroups a CU, which is what LDS has
 // room for with 256 points); uniform codes need more for the two halves' scales, and no LDS to speak of; fp32 layers hold everything twice.
 template <typename T, int NCW, int COLS> struct Shape {
@@ -140,10 +142,11 @@ paged_attend_kernel(const PagedAttendArgs a) {
     for (int k = 0; k < C::kHalves; ++k) vs[k] = C::value_scales(scale_lds, k, g);
     const int held = (there >> g) & 1 ? w.len - (t + 8 * g) : 0;           // so many of the lane's eight tokens are there: the others hold anything
     const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;      // (t_end: of this piece, whole tiles but for the last)
-    float lift[COLS];
-    lift[0] = C::lift_of(vs);
+    float lift[COLS];                                      // power of two of the largest scale of the lane's tokens that the row sees
+    if constexpr (COLS > 1) {
 #pragma unroll
-    for (int i = 1; i < COLS; ++i) lift[i] = lift[0];
+      for (int i = 0; i < COLS; ++i) lift[i] = C::lift_of(vs);
+    }
     if (masked) {
       asm volatile("");                                    // (a branch, not selects that every tile would pay for)
 #pragma unroll
@@ -153,10 +156,15 @@ paged_attend_kernel(const PagedAttendArgs a) {
         for (int e = 0; e < 8; ++e) p[i][e] = e < seen ? p[i][e] : -INFINITY;
         u32x4 own[C::kHalves];
 #pragma unroll
-        for (int k = 0; k < C::kHalves; ++k) { own[k] = vs[k]; C::keep_first(own[k], seen); }
-        lift[i] = C::lift_of(own);
+        for (int k = 0; k < C::kHalves; ++k) {
+          own[k] = vs[k];
+          C::keep_first(own[k], seen);
+          if constexpr (COLS == 1) vs[k] = own[k];
+        }
+        if constexpr (COLS > 1) lift[i] = C::lift_of(own);
       }
     }
+    if constexpr (COLS == 1) lift[0] = C::lift_of(vs);
     // The reference follows where the largest weight that the scores allow is too large: such weights become 2^kStartExp.
     float top[COLS];
     bool high = false;
@@ -388,7 +396,9 @@ __global__ __launch_bounds__(256) void paged_merge_rows_kernel(const PagedAttend
   }
 }
 
-// How a launch is laid out, from sizes alone (lengths are on the device).
+// How a launch is laid out, from sizes alone (lengths and counts of queries are on the device): by max_queries, whatever the sequences have.  So single queries
+// beside a chunk are walked by one workgroup a kv head each, as a block of 256 rows is: 31 over 16 384 tokens and a chunk of 512, 32 heads, 2.1 ms, in a call of
+// their own 94 us, the chunk by itself 99.
 struct PagedPlan { unsigned blocks, row_tiles; int slots, row_blocks; int64_t items; bool two, merge, many, by_rows; };
 // Results of a sequence beyond which the merge has 1024 threads a row, of 256 (one query of 131 072 tokens 41.0 us, for 45.0; beyond 8: 32 x 4000 tokens
 // 37.4 for 34.4).
@@ -411,7 +421,8 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
     return p;
   }
   // 9 to 16 rows fill one column of a wave, but two columns take as long and join their results (16 rows of 8 x 9999 tokens, 3 bits: 37.3 us, in one column
-  // 39.7; of one sequence of 12 288: 18.9, 29.8; of 32 x 4000 46.1, 44.8); 8 rows do not (one sequence of 131 072: 46.5, 40.0).
+  // 39.7; of one sequence of 12 288: 18.9, 29.8; of 32 x 4000 46.1, 44.8); 8 rows do not (one sequence of 131 072: 49.0, 41.9; 32 x 16 384: 138, 101; 8 x 9999 31.3,
+  // 30.4; but one of 16 384 18.0, 19.8).
   p.two = sizeof(T) == 2 && rows > 8;
   const int per_wave = p.two ? 32 : 16, waves = p.two ? Shape<T, NCW, 2>::kWaves : Shape<T, NCW, 1>::kWaves;
   p.row_tiles = (unsigned)((rows + per_wave - 1) / per_wave);

@@ -182,8 +182,9 @@ template <int NCW> struct TileCodes {
 };
 
 // ---------------------------------------------------------------- the kernel
-// 2048 queries of 32 heads over 12 288 tokens of 8 kv heads, 256 points: 505 to 518 us, 729 to 748 TFLOP/s (a library product of fp16 matrices of 8192 reaches 1319).
-// One workgroup a CU, two waves a SIMD (accumulators, query and a tile's codes in 242 registers): matrix cores busy in a third of the cycles, vector
+// 2048 queries of 32 heads over 12 288 tokens of 8 kv heads, 256 points: 503 to 523 us, 722 to 752 TFLOP/s (a library product of fp16 matrices of 8192 reaches 1319);
+// 64 points 539, 16 points 511, uniform 4 bits 604, 2 bits 620 (weights and scores of each half).
+// One workgroup a CU, two waves a SIMD (accumulators, query and a tile's codes in 236 to 248 registers): matrix cores busy in a third of the cycles, vector
 // pipes in half of them; a wave's chain of products, maximum, exponentials and conversion is what is left, and the two waves of a SIMD do not hide it for each
 // other.  Without the conversion of codes it would take 410 us, without the operands' LDS reads 465, without the exponentials 475.  Slower: 64 rows a
 // wave (1010 us: accumulators moved between register files), waves in turns by barriers (703), operands requested ahead by hand (515, spills).
