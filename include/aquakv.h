@@ -525,9 +525,10 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   page_tokens, row numbers to 0 ... q_rows, and tokens of a page that is not in the pool (page_table outside 0 ... n_pages - 1)
  *   are not seen.  page_table, seq_lens, q_start: aligned to 4 bytes.
  *   bf16: products in fp16 with fp32 sums: rotated queries, grid points and weights times the value's scale are rounded to fp16 behind
- *   powers of two, uniform codes are exact (up to 128 rows of a kv head their sums keep 2^-17 of the largest product); a weight times its
- *   value's scale is kept to 2^-33 of a row's largest.  Errors are 1 to 1.5 times those of rounding the exact result to bf16.  fp32: each of
- *   the factors as the sum of two fp16 numbers (22 bits, the product of the two second ones left out), fp32 sums.
+ *   powers of two, uniform codes are exact (up to 128 rows of a kv head their sums keep 2^-17 of the largest product).  Errors are 1 to
+ *   1.5 times those of rounding the exact result to bf16.  fp32: each of the factors as the sum of two fp16 numbers (22 bits, the product
+ *   of the two second ones left out), fp32 sums.  Both: p_t times a scale is kept to 2^-33 of the largest p times the largest scale beside
+ *   it (of 64 tokens), with all its bits down to 2^-22 of that.
  *   A call is laid out by max_queries: sequences of few queries beside one of more than 128 rows (queries x query heads of a kv head) take
  *   many times what they take in a call of their own.
  *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments) for the same layer, pages and sizes (other sizes may

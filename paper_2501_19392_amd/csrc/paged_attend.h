@@ -9,7 +9,8 @@
 // paged_tiles.hip, which converts codes once for many rows, make them normal numbers, whose sums are fp32's.
 //
 // fp16 ends at 2^-24: coordinates of a query below 2^-27 of its largest (uniform codes, which are masked in place: 2^-23, 2 bits 2^-21), and weights with their
-// scales below 2^-22 of a row's largest, have fewer bits than 11, down to 2^-38 (2^-34, 2^-32) and 2^-33.
+// scales below 2^-22 of the largest that scores and scales of a tile allow (each for itself: a weight's token may have a smaller scale than its neighbours), have
+// fewer bits than 11, down to 2^-38 (2^-34, 2^-32) and 2^-33.
 #pragma once
 #include "codec_core.h"
 #include "kernels.h"
