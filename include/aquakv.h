@@ -537,6 +537,13 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   (q_heads / kv_heads) <= 16 * 65535, q_rows < 2^31, batch * kv_heads < 2^25, table_pages * page_tokens < 2^31 - 4096 and 2^35 over
  *   the batch: AQUAKV_EUNSUPPORTED beyond.
  *
+ * aquakv_paged_attend_tree -- the same for drafted tokens that form a tree: the n queries of a sequence are its last n tokens, which must have
+ *   been appended already, and query i sees all tokens before them and, of the n, those whose bit is set: tree [q_rows, tree_words], bit j (of
+ *   value 2^(j % 32) of word j / 32) of row r: r sees token seq_lens[b] - n + j.  A draft that is to see itself has its own bit set; nothing else is
+ *   made of the bits, so that any mask of the last tokens can be given.  tree_words >= max_queries / 32, rounded up; tokens that have no bit
+ *   in a row's words (a sequence of more rows than 32 * tree_words) are not seen.  A row without bits, with nothing cached before the drafts, gives 0.
+ *   tree: aligned to 4 bytes, at most 2^17 words a row.  Layout, limits, workspace and precision are those of aquakv_paged_attend.
+ *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens
  * (tokens = 0), sequences or queries (batch, q_rows or max_queries = 0) nothing is done, and buffers but the pool's may be NULL.
  */
@@ -556,6 +563,10 @@ int aquakv_paged_attend(const aquakv_layer* layer, const aquakv_pages* pages, in
                         int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
                         const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes,
                         void* stream);
+int aquakv_paged_attend_tree(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                             int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
+                             const uint32_t* tree, int32_t tree_words, const void* q, int64_t q_stride, float score_scale, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

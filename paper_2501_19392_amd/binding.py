@@ -42,7 +42,7 @@ EXPORTS = [
     "aquakv_fit_workspace_bytes", "aquakv_fit_predictor",
     "aquakv_softmax", "aquakv_weighted_workspace_bytes", "aquakv_decode_values_weighted", "aquakv_decode_values_attend",
     "aquakv_attend_raw", "aquakv_copy_ranges", "aquakv_encode_layers", "aquakv_attend_cache_workspace_bytes", "aquakv_attend_cache",
-    "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend",
+    "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend", "aquakv_paged_attend_tree",
 ]
 
 
@@ -126,7 +126,8 @@ _lib.aquakv_paged_append.argtypes = [_LP, _PP, _I64, _P, _I64, _P, _I64, _P, _P,
 _lib.aquakv_paged_workspace_bytes.restype = ctypes.c_size_t
 _lib.aquakv_paged_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, _I32]
 _lib.aquakv_paged_attend.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
-for _n in ("aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
+_lib.aquakv_paged_attend_tree.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I32, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
+for _n in ("aquakv_paged_attend_tree", "aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
            "aquakv_decode_attn_scores", "aquakv_decode_attn_scores_rope", "aquakv_decode_attn_scores_folded",
            "aquakv_decode_attn_scores_folded_static", "aquakv_encode_keys", "aquakv_encode_values",
            "aquakv_decode_values", "aquakv_fit_predictor"):
@@ -541,10 +542,8 @@ def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_p
     return _lib.aquakv_paged_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table_pages, q_rows, max_queries)
 
 
-def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
-                        workspace, stream=None) -> None:
-    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence].  Tensors have to be on the current
-    device (ValueError otherwise), whose current stream is taken unless one is given."""
+def _asked(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, q_start, workspace):
+    """What the calls that attend over pages have in common -> (the current device, arguments as the C calls take them, by name)"""
     row, dtype, here = q_heads * layer.head_dim, layer.dtype, _here()
     _pool_here(layer, pages, here)
     at, stride, q_rows = _rows(q, dtype, row, "q", here)
@@ -555,12 +554,32 @@ def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_
     pages_each = page_table.shape[1]
     if workspace.__class__ is torch.Tensor and workspace.get_device() != here:
         raise ValueError("workspace is not on the current device")
+    return (here, row, dtype, _typed(page_table, torch.int32, batch * pages_each, "page_table", here), pages_each,
+            _typed(seq_lens, torch.int32, batch, "seq_lens", here), q_rows, _typed(q_start, torch.int32, batch + 1, "q_start", here), at, stride)
+
+
+def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
+                        workspace, stream=None) -> None:
+    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence].  Tensors have to be on the current
+    device (ValueError otherwise), whose current stream is taken unless one is given."""
+    here, row, dtype, table, pages_each, lens, q_rows, start, at, stride = _asked(layer, pages, batch, q_heads, page_table, seq_lens, q, q_start, workspace)
     ws, nbytes = _ws(workspace)
-    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads,
-                                    _typed(page_table, torch.int32, batch * pages_each, "page_table", here), pages_each,
-                                    _typed(seq_lens, torch.int32, batch, "seq_lens", here), q_rows, max_queries,
-                                    _typed(q_start, torch.int32, batch + 1, "q_start", here), at, stride, score_scale,
-                                    _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
+    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table, pages_each, lens, q_rows, max_queries, start, at, stride,
+                                    score_scale, _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
+
+
+def aquakv_paged_attend_tree(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, tree, score_scale: float,
+                             out, workspace, stream=None) -> None:
+    """tree: int32 [q_rows, words], bit j % 32 of word j / 32 of a row: it sees the j-th of its sequence's queries' own tokens; the rest as in
+    aquakv_paged_attend."""
+    here, row, dtype, table, pages_each, lens, q_rows, start, at, stride = _asked(layer, pages, batch, q_heads, page_table, seq_lens, q, q_start, workspace)
+    if tree is None or tree.__class__ is int or tree.dim() != 2 or tree.shape[0] != q_rows:
+        raise ValueError(f"tree must be a tensor of {q_rows} rows of words")
+    words = tree.shape[1]
+    ws, nbytes = _ws(workspace)
+    _check(_lib.aquakv_paged_attend_tree(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table, pages_each, lens, q_rows, max_queries, start,
+                                         _typed(tree, torch.int32, q_rows * words, "tree", here), words, at, stride, score_scale,
+                                         _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
 
 
 def aquakv_fit_workspace_bytes(d_in: int, d_out: int) -> int:

@@ -1735,18 +1735,25 @@ size_t aquakv_paged_workspace_bytes(const aquakv_layer* L, const aquakv_pages* p
   return (aquakv::paged_attend_workspace_bytes(L->dtype, quantizer_id(L), a) + 255) / 256 * 256 + 256;
 }
 
-int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
-                        int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
-                        const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+namespace {
+// (with_tree: rows see of their sequence's queries' own tokens those that the bits say, otherwise those up to their own)
+int paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table, int32_t table_pages,
+                 const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start, bool with_tree, const uint32_t* tree,
+                 int32_t tree_words, const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes,
+                 void* stream) {
   CHECK(check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries));
   if (q_start == nullptr && q_rows != (int64_t)batch * max_queries)
     return fail(AQUAKV_EINVAL, "q_rows=%lld: without q_start every one of %d sequences has %d", (long long)q_rows, batch, max_queries);
+  if (with_tree && (tree_words < 0 || tree_words < max_queries / 32 + (max_queries % 32 != 0)))
+    return fail(AQUAKV_EINVAL, "tree_words=%d: a bit for each of %d queries", tree_words, max_queries);
+  if (with_tree && tree_words > (1 << 17)) return fail(AQUAKV_EUNSUPPORTED, "tree_words=%d", tree_words);
   if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;      // (as above)
   const int64_t row = (int64_t)q_heads * 128;
   const size_t eb = elem_bytes(L->dtype);
   CHECK(check_array(page_table, "page_table", 4));
   CHECK(check_array(seq_lens, "seq_lens", 4));
   if (misaligned_to(q_start, 4)) return fail(AQUAKV_EALIGN, "q_start is not 4-byte aligned");
+  if (with_tree) CHECK(check_array(tree, "tree", 4));
   CHECK(check_rows(q, "q", q_stride, row, eb));
   CHECK(check_ptr(out, "out", true));
   CHECK(check_ptr(workspace, "workspace", true));
@@ -1758,16 +1765,34 @@ int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_
   const Range ins[] = {pool.r[0], pool.r[1], pool.r[2], pool.r[3], {page_table, (size_t)batch * table_pages * sizeof(int32_t), "page_table"},
                        {seq_lens, (size_t)batch * sizeof(int32_t), "seq_lens"},
                        {q_start, q_start == nullptr ? 0 : ((size_t)batch + 1) * sizeof(int32_t), "q_start"},
-                       {q, rows_bytes(q_rows, q_stride, row, eb), "q"}, params.r[4], params.r[5], params.r[6]};
-  CHECK(check_no_alias(outs, 2, ins, 11));
+                       {q, rows_bytes(q_rows, q_stride, row, eb), "q"}, {tree, with_tree ? (size_t)q_rows * tree_words * sizeof(uint32_t) : 0, "tree"},
+                       params.r[4], params.r[5], params.r[6]};
+  CHECK(check_no_alias(outs, 2, ins, 12));
   aquakv::PagedAttendArgs a = {};
   a.pool = pool_of(pages);
   a.page_table = page_table; a.seq_lens = seq_lens; a.q_start = q_start;
   a.table_pages = table_pages; a.batch = batch; a.max_queries = max_queries; a.H = L->kv_heads; a.q_heads = q_heads;
   a.q_rows = q_rows; a.q_stride = q_stride; a.q = q; a.out = out; a.scale = score_scale;
+  if (with_tree) { a.tree = tree; a.tree_words = tree_words; }
   a.signs_k = L->signs_k; a.signs_v = L->signs_v; a.codebook = L->codebook;
   HIP_TRY(aquakv::launch_paged_attend(L->dtype, quantizer_id(L), a, workspace, static_cast<hipStream_t>(stream)));
   return AQUAKV_OK;
+}
+}  // namespace
+
+int aquakv_paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                        int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
+                        const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_attend(L, pages, batch, q_heads, page_table, table_pages, seq_lens, q_rows, max_queries, q_start, false, nullptr, 0, q, q_stride,
+                      score_scale, out, workspace, workspace_bytes, stream);
+}
+
+int aquakv_paged_attend_tree(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                             int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
+                             const uint32_t* tree, int32_t tree_words, const void* q, int64_t q_stride, float score_scale, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_attend(L, pages, batch, q_heads, page_table, table_pages, seq_lens, q_rows, max_queries, q_start, true, tree, tree_words, q, q_stride,
+                      score_scale, out, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -269,10 +269,14 @@ struct PagedAttendArgs {
   int slots;                                      // pieces that fill the chip (blocks of rows: pieces of a sequence)
   int row_blocks;                                 // blocks of 256 rows (paged_tiles.hip), 0: not in such blocks
   uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
+  const uint32_t* tree;                           // nullable, [q_rows, tree_words]: bit j of row r: it sees draft j of its sequence (paged_tree.hip)
+  int tree_words;
 };
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a);
 // Many queries (bf16): 8 waves x 32 rows per workgroup.
 hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
+hipError_t launch_paged_tree_rows(int dtype, int n_codewords, bool two, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream);
+hipError_t launch_paged_tree_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 
 // Device-to-device copies of n byte ranges, kCopyRangesPerLaunch per launch (3 KiB of kernel arguments).

@@ -113,6 +113,33 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
   return s;
 }
 
+// Which of up to eight consecutive tokens a row sees: the first n, or (drafts of a tree) those whose bit is set.
+template <bool TREE> struct SeenOf {
+  int n;
+  __device__ __forceinline__ bool has(int e) const { return e < n; }
+  __device__ __forceinline__ void keep(u32x4& w) const {   // half-words of the others become 0
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] &= (has(2 * i) ? 0xffffu : 0u) | (has(2 * i + 1) ? 0xffff0000u : 0u);
+  }
+};
+template <> struct SeenOf<true> {
+  uint32_t bits;
+  __device__ __forceinline__ bool has(int e) const { return (bits >> e) & 1; }
+  __device__ __forceinline__ void keep(u32x4& w) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] &= (has(2 * i) ? 0xffffu : 0u) | (has(2 * i + 1) ? 0xffff0000u : 0u);
+  }
+};
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 8 ? 255u : n <= 0 ? 0u : (1u << n) - 1u; }
+// Bits draft ... draft + 7 of query row `row` of a tree: tokens ahead of the drafts (below 0) are seen, drafts behind the row's words are not.
+__device__ __forceinline__ uint32_t tree_bits(const PagedAttendArgs& a, int64_t row, int draft) {
+  if (draft <= -8) return 255u;
+  const uint32_t* const words = a.tree + row * a.tree_words;
+  const int at = draft >> 5;                               // (-1: ahead of the first)
+  const uint32_t lo = at < 0 ? 0xffffffffu : at < a.tree_words ? words[at] : 0u, hi = at + 1 < a.tree_words ? words[at + 1] : 0u;
+  return __builtin_amdgcn_alignbit(hi, lo, (uint32_t)draft & 31u) & 255u;
+}
+
 // Pool rows at which the four groups of 8 tokens of a tile start, -1: not there.
 struct Rows { int r[4]; };
 __device__ __forceinline__ Rows rows_of(const PagedAttendArgs& a, int b, int t) {
@@ -462,14 +489,12 @@ template <int NCW, int TERMS> struct Codes {
   static __device__ __forceinline__ float int_at(const u32x4& w, int e) { return (float)((w[e >> 1] >> (16 * (e & 1))) & 0xffffu); }
   // the values' scales of the lane's tokens, per half (kHalves), and their zero points: fp16 numbers (times 2^-kFieldExp).  `there`: those from it on are 0
   static constexpr int kHalves = kRtn ? 2 : 1;
-  static __device__ __forceinline__ void keep_first(u32x4& w, int there) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] &= (2 * i < there ? 0xffffu : 0u) | (2 * i + 1 < there ? 0xffff0000u : 0u);
-  }
   static __device__ __forceinline__ u32x4 value_scales(const unsigned char* lds, int k, int g) { return eight(lds, kValues + 2 * k, g); }
-  static __device__ __forceinline__ f16x8 zero_points(const unsigned char* lds, int k, int g, int there) {
+  // BOUNDED: those that are none (beyond 1023, of tokens whose rows hold anything) are made finite, as their weight of 0 asks for
+  template <bool BOUNDED> static __device__ __forceinline__ f16x8 zero_points(const unsigned char* lds, int k, int g, int there) {
     u32x4 w = eight(lds, kValues + 2 * k + 1, g);
-    if (there < 8) keep_first(w, there);
+    if (there < 8) SeenOf<false>{there}.keep(w);
+    if constexpr (BOUNDED) w &= 0x03ff03ffu;
     return operand(small_ints(w.x), small_ints(w.y), small_ints(w.z), small_ints(w.w));
   }
   // power of two of the largest scale of the lane's tokens (at least the smallest fp16 number's)
@@ -577,7 +602,7 @@ template <int NCW, int TERMS> struct Codes {
 
   // ---- o[j] += values (coordinates: result()) * weights p * scale.  `there` of the lane's tokens are; masked: a row sees the first seen[] of them, and what the
   // scales of the others are is no matter (0 times a number that is not finite would be): with one row a lane they are 0 already, with two the weights become 0.
-  template <int COLS> static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, bool masked, const int (&seen)[COLS],
+  template <int COLS, typename Seen> static __device__ __forceinline__ void values(const Values& w, const unsigned char* scales, int there, bool masked, const Seen (&seen)[COLS],
                                                                     const float (&p)[COLS][8], const u32x4 (&vs)[kHalves], const unsigned char* lds, int lane,
                                                                     Column (&col)[COLS]) {
     f16x8 b[COLS][kHalves][TERMS];
@@ -599,7 +624,7 @@ template <int NCW, int TERMS> struct Codes {
 #pragma unroll
           for (int i = 0; i < TERMS; ++i) {
             u32x4 x = __builtin_bit_cast(u32x4, b[n][k][i]);
-            keep_first(x, seen[n]);
+            seen[n].keep(x);
             b[n][k][i] = __builtin_bit_cast(f16x8, x);
           }
     }
@@ -612,7 +637,7 @@ template <int NCW, int TERMS> struct Codes {
       for (int e = 0; e < 8; ++e) d[e] = __builtin_amdgcn_perm(w.v[e], __float_as_uint(row_xor8(__uint_as_float(w.v[e]))), pick);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const f16x8 z = zero_points(scales, k, lane >> 4, there);
+        const f16x8 z = zero_points<std::is_same<Seen, SeenOf<true>>::value>(scales, k, lane >> 4, there);
 #pragma unroll
         for (int i = 0; i < COLS; ++i)
 #pragma unroll
