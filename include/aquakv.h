@@ -544,6 +544,21 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   in a row's words (a sequence of more rows than 32 * tree_words) are not seen.  A row without bits, with nothing cached before the drafts, gives 0.
  *   tree: aligned to 4 bytes, at most 2^17 words a row.  Layout, limits, workspace and precision are those of aquakv_paged_attend.
  *
+ * aquakv_paged_select -- which tokens of a cache are kept: of each sequence the `budget` tokens with the largest mass, its first n_first and last
+ *   n_last ones (n_first + n_last <= budget) whatever theirs is.  mass: fp32 [n_pages, kv_heads, page_tokens] as aquakv_paged_weights accumulates
+ *   it; a token's is the sum over the heads, in 32 bits, head after head.  Of equal ones the first is kept; what is no number comes last, behind it
+ *   tokens of a page that is not in the pool.  kept [batch, budget]: token numbers, ascending, -1 behind the n_kept[b] = min(seq_lens[b], budget)
+ *   that there are; n_kept [batch].  Counts and tables as in aquakv_paged_attend.  workspace: aquakv_paged_select_workspace_bytes() bytes.
+ *
+ * aquakv_paged_keep -- token kept[b, i] of sequence b becomes its token first[b] + i (first NULL: i), i < n_kept[b] (at most max_kept): codes, scales and, if
+ *   given, mass.  kept [batch, max_kept], n_kept, first [batch]: device int32, aligned to 4 bytes.  So an eviction is select and keep, and drafts that were
+ *   accepted are kept with first = the tokens ahead of the drafts; the caller's sequence then has first[b] + n_kept[b] tokens.  to_table NULL: in the
+ *   pages that page_table names; all rows of a sequence are read before any is written, so entries may be in any order and may repeat.  Else to
+ *   pages that to_table [batch, to_pages] names, which may not be ones that the call reads.  What goes from or to a token outside its table
+ *   or a page that is not in the pool is left out.  Two entries, or two sequences, that name the same row to write to leave anything there; no sequence may read
+ *   rows that the call writes for another one.  Keys keep the rotation that they have.
+ *   workspace: aquakv_paged_keep_workspace_bytes() bytes for the same layer, pages and sizes (with_mass: 0, or 1 where mass is given).
+ *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens
  * (tokens = 0), sequences or queries (batch, q_rows or max_queries = 0) nothing is done, and buffers but the pool's may be NULL.
  */
@@ -567,6 +582,37 @@ int aquakv_paged_attend_tree(const aquakv_layer* layer, const aquakv_pages* page
                              int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
                              const uint32_t* tree, int32_t tree_words, const void* q, int64_t q_stride, float score_scale, void* out,
                              void* workspace, size_t workspace_bytes, void* stream);
+size_t aquakv_paged_select_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t table_pages, int32_t budget);
+int aquakv_paged_select(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, const int32_t* page_table, int32_t table_pages,
+                        const int32_t* seq_lens, const float* mass, int32_t budget, int32_t n_first, int32_t n_last, int32_t* kept, int32_t* n_kept,
+                        void* workspace, size_t workspace_bytes, void* stream);
+size_t aquakv_paged_keep_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t max_kept, int32_t with_mass);
+int aquakv_paged_keep(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, const int32_t* page_table, int32_t table_pages, int32_t max_kept,
+                      const int32_t* kept, const int32_t* n_kept, const int32_t* first, const int32_t* to_table, int32_t to_pages, float* mass,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * aquakv_rotary -- rows of heads x 128 (queries, keys, or both where they lie side by side in a joint product) rotated to their positions: of each
+ *   head the first rotary_dim coordinates (a multiple of 16, at most 128), the others copied.  Coordinates that form a pair (x, y): i and
+ *   rotary_dim / 2 + i (AQUAKV_ROTARY_HALVES, the convention of the other calls), or 2 i and 2 i + 1 (AQUAKV_ROTARY_PAIRS); with c, s = row positions[t] of rope_cos,
+ *   rope_sin (fp32 [rope_rows, rotary_dim / 2]), column i:  (x, y) -> (x c - y s, y c + x s);  transposed != 0: (x c + y s, y c - x s), which is
+ *   the way back for tables of magnitude 1, and the gradient for any.  fp32 arithmetic, one rounding to dtype.
+ *   Token t is at x + t * x_stride elements and goes to out + t * out_stride (rows contiguous, 16-byte aligned).  out = x with the same stride: in place;
+ *   otherwise they may not overlap.  A token whose position is outside the tables is left out: its row of `out` stays as it was.  positions: int32 [tokens].
+ *   tokens * heads < 2^30.
+ *
+ * aquakv_rotary_tables -- rope_cos, rope_sin [rows, rotary_dim / 2] for positions first ... first + rows - 1 (below 2^31):
+ *   magnitude * cos, sin(position * w_i),  w_i = base^(-2 i / rotary_dim) (k_i + (1 - k_i) / factor):
+ *   factor 1: plain frequencies.  Otherwise, for contexts `factor` times as long, original_len 0: k_i = 0, all frequencies alike; original_len > 0:
+ *   k_i = (r_i - low_turns) / (high_turns - low_turns) cut to 0 ... 1, r_i = the turns that frequency i makes over original_len positions, so that fast
+ *   frequencies stay and slow ones are stretched.  magnitude: 1, or what scores are scaled by (both of query and key).  Angles in 64 bits.
+ */
+typedef enum { AQUAKV_ROTARY_HALVES = 0, AQUAKV_ROTARY_PAIRS = 1 } aquakv_rotary_layout;
+int aquakv_rotary(int32_t dtype, int64_t tokens, int32_t heads, const void* x, int64_t x_stride, const int32_t* positions, const float* rope_cos,
+                  const float* rope_sin, int32_t rope_rows, int32_t rotary_dim, int32_t layout, int32_t transposed, void* out, int64_t out_stride,
+                  void* stream);
+int aquakv_rotary_tables(int64_t rows, int64_t first, int32_t rotary_dim, double base, double factor, double original_len, double low_turns,
+                         double high_turns, float magnitude, float* rope_cos, float* rope_sin, void* stream);
 
 #ifdef __cplusplus
 }

@@ -43,6 +43,8 @@ EXPORTS = [
     "aquakv_softmax", "aquakv_weighted_workspace_bytes", "aquakv_decode_values_weighted", "aquakv_decode_values_attend",
     "aquakv_attend_raw", "aquakv_copy_ranges", "aquakv_encode_layers", "aquakv_attend_cache_workspace_bytes", "aquakv_attend_cache",
     "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend", "aquakv_paged_attend_tree",
+    "aquakv_paged_select_workspace_bytes", "aquakv_paged_select", "aquakv_paged_keep_workspace_bytes", "aquakv_paged_keep",
+    "aquakv_rotary", "aquakv_rotary_tables",
 ]
 
 
@@ -127,7 +129,15 @@ _lib.aquakv_paged_workspace_bytes.restype = ctypes.c_size_t
 _lib.aquakv_paged_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, _I32]
 _lib.aquakv_paged_attend.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
 _lib.aquakv_paged_attend_tree.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I32, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
-for _n in ("aquakv_paged_attend_tree", "aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
+_F32, _F64, _SZ = ctypes.c_float, ctypes.c_double, ctypes.c_size_t
+_lib.aquakv_paged_select_workspace_bytes.restype = _lib.aquakv_paged_keep_workspace_bytes.restype = _SZ
+_lib.aquakv_paged_select_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32]
+_lib.aquakv_paged_select.argtypes = [_LP, _PP, _I32, _P, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _P, _SZ, _P]
+_lib.aquakv_paged_keep_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32]
+_lib.aquakv_paged_keep.argtypes = [_LP, _PP, _I32, _P, _I32, _I32, _P, _P, _P, _P, _I32, _P, _P, _SZ, _P]
+_lib.aquakv_rotary.argtypes = [_I32, _I64, _I32, _P, _I64, _P, _P, _P, _I32, _I32, _I32, _I32, _P, _I64, _P]
+_lib.aquakv_rotary_tables.argtypes = [_I64, _I64, _I32, _F64, _F64, _F64, _F64, _F64, _F32, _P, _P, _P]
+for _n in ("aquakv_paged_select", "aquakv_paged_keep", "aquakv_rotary", "aquakv_rotary_tables", "aquakv_paged_attend_tree", "aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
            "aquakv_decode_attn_scores", "aquakv_decode_attn_scores_rope", "aquakv_decode_attn_scores_folded",
            "aquakv_decode_attn_scores_folded_static", "aquakv_encode_keys", "aquakv_encode_values",
            "aquakv_decode_values", "aquakv_fit_predictor"):
@@ -580,6 +590,98 @@ def aquakv_paged_attend_tree(layer, pages, batch: int, q_heads: int, page_table,
     _check(_lib.aquakv_paged_attend_tree(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table, pages_each, lens, q_rows, max_queries, start,
                                          _typed(tree, torch.int32, q_rows * words, "tree", here), words, at, stride, score_scale,
                                          _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
+
+
+def _table(x, batch: int, name: str, device: int):
+    """A page table [batch, pages] -> (address, pages)"""
+    if x is None or x.__class__ is int or x.dim() != 2 or x.shape[0] != batch:
+        raise ValueError(f"{name} must be a tensor [batch, pages]")
+    pages = x.shape[1]
+    return _typed(x, torch.int32, batch * pages, name, device), pages
+
+
+def _mass(x, layer, pages, device: int):
+    """[n_pages, kv_heads, page_tokens]"""
+    c = pages.c if isinstance(pages, Pages) else pages
+    return _typed(x, torch.float32, c.n_pages * c.page_tokens * layer.kv_heads, "mass", device)
+
+
+def _space(workspace, device: int):
+    if workspace.__class__ is torch.Tensor and workspace.get_device() != device:
+        raise ValueError("workspace is not on the current device")
+    return _ws(workspace)
+
+
+def aquakv_paged_select_workspace_bytes(layer, pages, batch: int, table_pages: int, budget: int) -> int:
+    return _lib.aquakv_paged_select_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, table_pages, budget)
+
+
+def aquakv_paged_select(layer, pages, batch: int, page_table, seq_lens, mass, budget: int, n_first: int, n_last: int, kept, n_kept, workspace,
+                        stream=None) -> None:
+    """mass: fp32 [n_pages, kv_heads, page_tokens]; kept: int32 [batch, budget], n_kept: int32 [batch], both written.  Tensors have to be on the
+    current device (ValueError otherwise), whose current stream is taken unless one is given."""
+    here = _here()
+    _pool_here(layer, pages, here)
+    table, pages_each = _table(page_table, batch, "page_table", here)
+    ws, nbytes = _space(workspace, here)
+    _check(_lib.aquakv_paged_select(_layer_ref(layer), _pages_ref(pages), batch, table, pages_each, _typed(seq_lens, torch.int32, batch, "seq_lens", here),
+                                    _mass(mass, layer, pages, here), budget, n_first, n_last, _typed(kept, torch.int32, batch * budget, "kept", here),
+                                    _typed(n_kept, torch.int32, batch, "n_kept", here), ws, nbytes, _stream(stream)))
+
+
+def aquakv_paged_keep_workspace_bytes(layer, pages, batch: int, max_kept: int, with_mass: bool) -> int:
+    return _lib.aquakv_paged_keep_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, max_kept, int(with_mass))
+
+
+def aquakv_paged_keep(layer, pages, batch: int, page_table, kept, n_kept, first, to_table, mass, workspace, stream=None) -> None:
+    """kept: int32 [batch, max_kept] token numbers; first: int32 [batch] or None; to_table: another page table [batch, pages], or None: in place.
+    Tensors have to be on the current device (ValueError otherwise), whose current stream is taken unless one is given."""
+    here = _here()
+    _pool_here(layer, pages, here)
+    table, pages_each = _table(page_table, batch, "page_table", here)
+    to, to_pages = (None, 0) if to_table is None else _table(to_table, batch, "to_table", here)
+    entries, most = _table(kept, batch, "kept", here)
+    ws, nbytes = _space(workspace, here)
+    _check(_lib.aquakv_paged_keep(_layer_ref(layer), _pages_ref(pages), batch, table, pages_each, most, entries,
+                                  _typed(n_kept, torch.int32, batch, "n_kept", here), _typed(first, torch.int32, batch, "first", here), to, to_pages,
+                                  _mass(mass, layer, pages, here), ws, nbytes, _stream(stream)))
+
+
+ROTARY_LAYOUTS = {"half": 0, "pairs": 1}
+
+
+def aquakv_rotary(x, positions, rope_cos, rope_sin, rotary_dim: int, layout: str, out, transposed: bool = False, stream=None) -> None:
+    """x, out: [tokens, heads, 128], rows may lie apart (out = x: in place); positions: int32 [tokens]; rope_cos, rope_sin: fp32
+    [rows, rotary_dim / 2]; layout: "half" or "pairs".  Tensors have to be on the current device (ValueError otherwise), whose current stream is
+    taken unless one is given."""
+    here = _here()
+    if x.dim() != 3 or out.shape != x.shape:
+        raise ValueError("x and out must be tensors [tokens, heads, 128] of one shape")
+    if layout not in ROTARY_LAYOUTS:
+        raise ValueError(f"layout {layout!r}: one of {sorted(ROTARY_LAYOUTS)}")
+    tokens, heads, g = x.shape
+    if g != 128:
+        raise ValueError("x and out must be tensors [tokens, heads, 128] of one shape")
+    at, stride, _ = _rows(x, x.dtype, heads * 128, "x", here)
+    to, to_stride, _ = _rows(out, x.dtype, heads * 128, "out", here)
+    if rope_cos.dim() != 2 or rope_cos.shape[1] * 2 != rotary_dim or rope_sin.shape != rope_cos.shape:
+        raise ValueError("rope_cos and rope_sin must be tensors [rows, rotary_dim / 2]")
+    rows, n = rope_cos.shape[0], rope_cos.numel()
+    _check(_lib.aquakv_rotary(_dtype_code(x.dtype), tokens, heads, at, stride, _typed(positions, torch.int32, tokens, "positions", here),
+                              _typed(rope_cos, torch.float32, n, "rope_cos", here), _typed(rope_sin, torch.float32, n, "rope_sin", here), rows,
+                              rotary_dim, ROTARY_LAYOUTS[layout], int(transposed), to, to_stride, _stream(stream)))
+
+
+def aquakv_rotary_tables(rope_cos, rope_sin, base: float, first: int = 0, factor: float = 1.0, original_len: float = 0.0, low_turns: float = 0.0,
+                         high_turns: float = 0.0, magnitude: float = 1.0, stream=None) -> None:
+    """rope_cos, rope_sin: fp32 [rows, rotary_dim / 2], written for positions first ... first + rows - 1."""
+    here = _here()
+    if rope_cos.dim() != 2 or rope_sin.shape != rope_cos.shape:
+        raise ValueError("rope_cos and rope_sin must be tensors [rows, rotary_dim / 2]")
+    (rows, pairs), n = rope_cos.shape, rope_cos.numel()
+    _check(_lib.aquakv_rotary_tables(rows, first, 2 * pairs, base, factor, original_len, low_turns, high_turns, magnitude,
+                                     _typed(rope_cos, torch.float32, n, "rope_cos", here), _typed(rope_sin, torch.float32, n, "rope_sin", here),
+                                     _stream(stream)))
 
 
 def aquakv_fit_workspace_bytes(d_in: int, d_out: int) -> int:

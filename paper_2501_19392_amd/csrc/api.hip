@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 #include <memory>
 #include <mutex>
 #include <new>
@@ -1793,6 +1794,149 @@ int aquakv_paged_attend_tree(const aquakv_layer* L, const aquakv_pages* pages, i
                              void* workspace, size_t workspace_bytes, void* stream) {
   return paged_attend(L, pages, batch, q_heads, page_table, table_pages, seq_lens, q_rows, max_queries, q_start, true, tree, tree_words, q, q_stride,
                       score_scale, out, workspace, workspace_bytes, stream);
+}
+
+size_t aquakv_paged_select_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t table_pages, int32_t budget) {
+  if (check_paged_shape(L, pages, batch, L == nullptr ? 1 : L->kv_heads, table_pages, 0, 0) != AQUAKV_OK || budget < 0) return 0;
+  return aquakv::paged_select_workspace_bytes(batch, table_pages, pages->page_tokens) + 256;
+}
+
+int aquakv_paged_select(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, const int32_t* page_table, int32_t table_pages,
+                        const int32_t* seq_lens, const float* mass, int32_t budget, int32_t n_first, int32_t n_last, int32_t* kept, int32_t* n_kept,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  CHECK(check_paged_shape(L, pages, batch, L == nullptr ? 1 : L->kv_heads, table_pages, 0, 0));
+  if (budget < 0 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > budget)
+    return fail(AQUAKV_EINVAL, "budget=%d n_first=%d n_last=%d: those that are always kept have to fit", budget, n_first, n_last);
+  if (batch == 0) return AQUAKV_OK;
+  CHECK(check_array(page_table, "page_table", 4));
+  CHECK(check_array(seq_lens, "seq_lens", 4));
+  CHECK(check_ptr(mass, "mass", true));
+  if (budget > 0 || kept != nullptr) CHECK(check_array(kept, "kept", 4));
+  CHECK(check_array(n_kept, "n_kept", 4));
+  CHECK(check_ptr(workspace, "workspace", true));
+  const size_t need = aquakv_paged_select_workspace_bytes(L, pages, batch, table_pages, budget);
+  if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
+  const size_t tokens = (size_t)pages->n_pages * pages->page_tokens;
+  const Range outs[] = {{kept, (size_t)batch * budget * sizeof(int32_t), "kept"}, {n_kept, (size_t)batch * sizeof(int32_t), "n_kept"},
+                        {workspace, need, "workspace"}};
+  const Range ins[] = {{page_table, (size_t)batch * table_pages * sizeof(int32_t), "page_table"}, {seq_lens, (size_t)batch * sizeof(int32_t), "seq_lens"},
+                       {mass, tokens * L->kv_heads * sizeof(float), "mass"}};
+  CHECK(check_no_alias(outs, 3, ins, 3));
+  aquakv::PagedSelectArgs a = {};
+  a.page_table = page_table; a.seq_lens = seq_lens; a.mass = mass; a.kept = kept; a.n_kept = n_kept; a.keys = static_cast<uint32_t*>(workspace);
+  a.table_pages = table_pages; a.batch = batch; a.H = L->kv_heads; a.n_pages = pages->n_pages; a.page_tokens = pages->page_tokens;
+  a.budget = budget; a.n_first = n_first; a.n_last = n_last;
+  HIP_TRY(aquakv::launch_paged_select(a, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
+}
+
+namespace {
+int check_keep_shape(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t max_kept) {
+  CHECK(check_pages(L, pages));
+  if (batch < 0 || max_kept < 0) return fail(AQUAKV_EINVAL, "batch=%d max_kept=%d", batch, max_kept);
+  if (batch > 65535) return fail(AQUAKV_EUNSUPPORTED, "batch=%d: at most 65535 sequences", batch);
+  // (threads of a launch: below 2^32, one per 16 bytes of a row, or per head)
+  if ((int64_t)max_kept * std::max<int64_t>(make_plan(L, 1).code_row, L->kv_heads) >= ((int64_t)1 << 31) * 8)
+    return fail(AQUAKV_EUNSUPPORTED, "max_kept=%d rows of %d heads", max_kept, L->kv_heads);
+  return AQUAKV_OK;
+}
+}  // namespace
+
+size_t aquakv_paged_keep_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t max_kept, int32_t with_mass) {
+  if (check_keep_shape(L, pages, batch, max_kept) != AQUAKV_OK) return 0;
+  return aquakv::paged_keep_workspace_bytes(batch, max_kept, (int64_t)make_plan(L, 1).code_row, (int64_t)scale_row_bytes(L), L->kv_heads, with_mass != 0) + 256;
+}
+
+int aquakv_paged_keep(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, const int32_t* page_table, int32_t table_pages, int32_t max_kept,
+                      const int32_t* kept, const int32_t* n_kept, const int32_t* first, const int32_t* to_table, int32_t to_pages, float* mass,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  CHECK(check_keep_shape(L, pages, batch, max_kept));
+  CHECK(check_paged_shape(L, pages, batch, L->kv_heads, table_pages, 0, 0));
+  if (to_table != nullptr) CHECK(check_paged_shape(L, pages, batch, L->kv_heads, to_pages, 0, 0));
+  if (batch == 0 || max_kept == 0) return AQUAKV_OK;
+  CHECK(check_array(page_table, "page_table", 4));
+  CHECK(check_array(kept, "kept", 4));
+  CHECK(check_array(n_kept, "n_kept", 4));
+  if (misaligned_to(first, 4)) return fail(AQUAKV_EALIGN, "first is not 4-byte aligned");
+  if (misaligned_to(to_table, 4)) return fail(AQUAKV_EALIGN, "to_table is not 4-byte aligned");
+  CHECK(check_ptr(mass, "mass", false));
+  CHECK(check_ptr(workspace, "workspace", true));
+  const size_t need = aquakv_paged_keep_workspace_bytes(L, pages, batch, max_kept, mass != nullptr);
+  if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
+  const PoolRanges pool = pool_ranges(L, pages);
+  const size_t tokens = (size_t)pages->n_pages * pages->page_tokens, ints = (size_t)batch * sizeof(int32_t);
+  const Range outs[] = {pool.r[0], pool.r[1], pool.r[2], pool.r[3], {mass, mass == nullptr ? 0 : tokens * L->kv_heads * sizeof(float), "mass"},
+                        {workspace, need, "workspace"}};
+  const Range ins[] = {{page_table, ints * table_pages, "page_table"}, {kept, ints * max_kept, "kept"}, {n_kept, ints, "n_kept"},
+                       {first, first == nullptr ? 0 : ints, "first"}, {to_table, to_table == nullptr ? 0 : ints * to_pages, "to_table"}};
+  CHECK(check_no_alias(outs, 6, ins, 5));
+  aquakv::PagedKeepArgs a = {};
+  a.pool = pool_of(pages);
+  a.page_table = page_table; a.kept = kept; a.n_kept = n_kept; a.first = first; a.to_table = to_table; a.mass = mass;
+  a.table_pages = table_pages; a.to_pages = to_pages; a.batch = batch; a.max_kept = max_kept; a.H = L->kv_heads;
+  a.code_row = (int)make_plan(L, 1).code_row; a.scale_row = (int)scale_row_bytes(L);
+  HIP_TRY(aquakv::launch_paged_keep(a, workspace, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
+}
+
+// ---- rotary positions --------------------------------------------------------------------------------------------
+int aquakv_rotary(int32_t dtype, int64_t tokens, int32_t heads, const void* x, int64_t x_stride, const int32_t* positions, const float* rope_cos,
+                  const float* rope_sin, int32_t rope_rows, int32_t rotary_dim, int32_t layout, int32_t transposed, void* out, int64_t out_stride,
+                  void* stream) {
+  if (dtype != AQUAKV_BF16 && dtype != AQUAKV_FP32) return fail(AQUAKV_EINVAL, "dtype=%d", dtype);
+  if (tokens < 0 || heads < 1 || rope_rows < 1) return fail(AQUAKV_EINVAL, "tokens=%lld heads=%d rope_rows=%d", (long long)tokens, heads, rope_rows);
+  if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return fail(AQUAKV_EINVAL, "rotary_dim=%d of heads of 128", rotary_dim);
+  if (rotary_dim % 16) return fail(AQUAKV_EUNSUPPORTED, "rotary_dim=%d: multiples of 16 are built", rotary_dim);
+  if (layout != AQUAKV_ROTARY_HALVES && layout != AQUAKV_ROTARY_PAIRS) return fail(AQUAKV_EINVAL, "layout=%d", layout);
+  if (tokens > (1LL << 31) || tokens * heads >= (1LL << 30)) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, heads);
+  if (tokens == 0) return AQUAKV_OK;
+  const int64_t row = (int64_t)heads * 128;
+  const size_t eb = elem_bytes(dtype), angles = (size_t)rope_rows * (rotary_dim / 2) * sizeof(float);
+  CHECK(check_rows(x, "x", x_stride, row, eb));
+  CHECK(check_rows(out, "out", out_stride, row, eb));
+  CHECK(check_array(positions, "positions", 4));
+  CHECK(check_ptr(rope_cos, "rope_cos", true));
+  CHECK(check_ptr(rope_sin, "rope_sin", true));
+  const bool in_place = x == out && x_stride == out_stride;
+  const size_t x_bytes = rows_bytes(tokens, x_stride, row, eb);
+  const Range outs[] = {{out, rows_bytes(tokens, out_stride, row, eb), "out"}};
+  const Range ins[] = {{x, in_place ? 0 : x_bytes, "x"}, {positions, (size_t)tokens * sizeof(int32_t), "positions"},
+                       {rope_cos, angles, "rope_cos"}, {rope_sin, angles, "rope_sin"}};
+  CHECK(check_no_alias(outs, 1, ins, 4));
+  aquakv::RotaryArgs a = {};
+  a.x = x; a.out = out; a.x_stride = x_stride; a.out_stride = out_stride; a.tokens = tokens; a.positions = positions;
+  a.cos = rope_cos; a.sin = rope_sin; a.heads = heads; a.dim = rotary_dim; a.rope_rows = rope_rows;
+  a.in_place = in_place; a.transposed = transposed != 0;
+  HIP_TRY(aquakv::launch_rotary(dtype, layout == AQUAKV_ROTARY_PAIRS, a, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
+}
+
+int aquakv_rotary_tables(int64_t rows, int64_t first, int32_t rotary_dim, double base, double factor, double original_len, double low_turns,
+                         double high_turns, float magnitude, float* rope_cos, float* rope_sin, void* stream) {
+  if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return fail(AQUAKV_EINVAL, "rotary_dim=%d of heads of 128", rotary_dim);
+  if (rotary_dim % 16) return fail(AQUAKV_EUNSUPPORTED, "rotary_dim=%d: multiples of 16 are built", rotary_dim);
+  if (rows < 0 || first < 0 || rows > 0x7fffffffLL || first > 0x7fffffffLL - rows)
+    return fail(AQUAKV_EINVAL, "positions %lld ... of %lld rows", (long long)first, (long long)rows);
+  if (!(base > 0) || !std::isfinite(base) || !(factor > 0) || !std::isfinite(factor) || !std::isfinite(magnitude))
+    return fail(AQUAKV_EINVAL, "base=%g factor=%g magnitude=%g", base, factor, (double)magnitude);
+  if (!(original_len >= 0) || !std::isfinite(original_len)) return fail(AQUAKV_EINVAL, "original_len=%g", original_len);
+  if (original_len > 0 && (!(low_turns >= 0) || !(high_turns > low_turns) || !std::isfinite(high_turns)))
+    return fail(AQUAKV_EINVAL, "low_turns=%g high_turns=%g", low_turns, high_turns);
+  if (rows == 0) return AQUAKV_OK;
+  CHECK(check_ptr(rope_cos, "rope_cos", true));
+  CHECK(check_ptr(rope_sin, "rope_sin", true));
+  const size_t bytes = (size_t)rows * (rotary_dim / 2) * sizeof(float);
+  const Range outs[] = {{rope_cos, bytes, "rope_cos"}, {rope_sin, bytes, "rope_sin"}};
+  CHECK(check_no_alias(outs, 2, nullptr, 0));
+  aquakv::RotaryTablesArgs a = {};
+  a.cos = rope_cos; a.sin = rope_sin; a.rows = rows; a.first = first; a.pairs = rotary_dim / 2; a.magnitude = magnitude;
+  for (int i = 0; i < a.pairs; ++i) {
+    const double turns = std::pow(base, -2.0 * i / rotary_dim) / 6.283185307179586476925;
+    const double kept = original_len > 0 ? std::min(std::max((original_len * turns - low_turns) / (high_turns - low_turns), 0.0), 1.0) : 0.0;
+    a.turns[i] = turns * (kept + (1.0 - kept) / factor);
+  }
+  HIP_TRY(aquakv::launch_rotary_tables(a, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
 }
 
 }  // extern "C"

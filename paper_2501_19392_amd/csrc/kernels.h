@@ -279,6 +279,48 @@ hipError_t launch_paged_tree_rows(int dtype, int n_codewords, bool two, dim3 blo
 hipError_t launch_paged_tree_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 
+// The tokens of each sequence that have most mass (paged_evict.hip): kept [batch, budget] ascending, -1 behind n_kept [batch].
+struct PagedSelectArgs {
+  const int32_t *page_table, *seq_lens;           // [batch, table_pages], [batch]
+  const float* mass;                              // [n_pages, H, page_tokens]
+  int32_t *kept, *n_kept;
+  uint32_t* keys;                                 // [batch, table_pages * page_tokens]
+  int table_pages, batch, H, n_pages, page_tokens, budget, n_first, n_last;
+};
+size_t paged_select_workspace_bytes(int64_t batch, int64_t table_pages, int64_t page_tokens);
+hipError_t launch_paged_select(const PagedSelectArgs& a, hipStream_t stream);
+// Token kept[b][i] of a sequence becomes its token first[b] + i, in pages of the same table or (to_table) of another one.
+struct PagedKeepArgs {
+  PagedPool pool;
+  const int32_t *page_table, *kept, *n_kept;      // [batch, table_pages], [batch, max_kept], [batch]
+  const int32_t *first, *to_table;                // nullable: [batch], [batch, to_pages]
+  float* mass;                                    // nullable, [n_pages, H, page_tokens]
+  int table_pages, to_pages, batch, max_kept, H;
+  int code_row, scale_row;                        // bytes of a row's codes, scales
+};
+size_t paged_keep_workspace_bytes(int64_t batch, int64_t max_kept, int64_t code_row, int64_t scale_row, int64_t H, bool mass);
+hipError_t launch_paged_keep(const PagedKeepArgs& a, void* workspace, hipStream_t stream);
+
+// Rotary positions (rotary.hip): rows of heads x 128 by tables [rope_rows, dim / 2]; tables of given frequencies (turns per position).
+struct RotaryArgs {
+  const void* x;                                  // token t at + t * x_stride elements
+  void* out;
+  int64_t x_stride, out_stride, tokens;
+  const int32_t* positions;                       // outside the tables: the row is left as it was
+  const float *cos, *sin;
+  int heads, dim, rope_rows;
+  bool in_place, transposed;
+};
+hipError_t launch_rotary(int dtype, bool pairs, const RotaryArgs& a, hipStream_t stream);
+struct RotaryTablesArgs {
+  float *cos, *sin;                               // [rows, pairs]
+  int64_t rows, first, step;                      // (step: set by the launcher)
+  int pairs;                                      // a multiple of 8 up to 64
+  float magnitude;
+  double turns[64];
+};
+hipError_t launch_rotary_tables(const RotaryTablesArgs& a, hipStream_t stream);
+
 // Device-to-device copies of n byte ranges, kCopyRangesPerLaunch per launch (3 KiB of kernel arguments).
 struct CopyRange { void* dst; const void* src; size_t bytes; };
 constexpr int kCopyRangesPerLaunch = 128;
