@@ -544,6 +544,16 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   in a row's words (a sequence of more rows than 32 * tree_words) are not seen.  A row without bits, with nothing cached before the drafts, gives 0.
  *   tree: aligned to 4 bytes, at most 2^17 words a row.  Layout, limits, workspace and precision are those of aquakv_paged_attend.
  *
+ * aquakv_paged_weights -- the attention weight that each cached token gets, accumulated per kv head in mass, fp32 [n_pages, kv_heads, page_tokens]:
+ *   mass[t] = keep * mass[t] + sum over the sequence's queries r and the query heads of kv head h of p_{r, qh, t},  p as in aquakv_paged_attend,
+ *   whose arguments these are.  Tokens of the queries themselves (the last n) have had no weight before: what mass holds for them is not read, so new
+ *   tokens need no clearing; with keep = 0 it is not read for any.  Sequences without queries, tokens behind a sequence and pages that are not in the pool are left
+ *   as they were; where a sequence has more than max_queries rows, those that are not answered add nothing.  A page that two sequences name has
+ *   anything in its mass afterwards.  After drafts were accepted (aquakv_paged_keep) the accepted ones are the last tokens, and their queries are taken here.
+ *   Both dtypes: products of two fp16 numbers for each factor (22 bits), fp32 sums in a fixed order: the same bits each time.  Beyond the limits of
+ *   aquakv_paged_attend: table_pages * page_tokens * kv_heads < 2^32.  workspace: aquakv_paged_weights_workspace_bytes() bytes, which hold the scores of all
+ *   tokens there is room for where a kv head has at most 8 rows (queries x query heads).
+ *
  * aquakv_paged_select -- which tokens of a cache are kept: of each sequence the `budget` tokens with the largest mass, its first n_first and last
  *   n_last ones (n_first + n_last <= budget) whatever theirs is.  mass: fp32 [n_pages, kv_heads, page_tokens] as aquakv_paged_weights accumulates
  *   it; a token's is the sum over the heads, in 32 bits, head after head.  Of equal ones the first is kept; what is no number comes last, behind it
@@ -582,6 +592,11 @@ int aquakv_paged_attend_tree(const aquakv_layer* layer, const aquakv_pages* page
                              int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
                              const uint32_t* tree, int32_t tree_words, const void* q, int64_t q_stride, float score_scale, void* out,
                              void* workspace, size_t workspace_bytes, void* stream);
+size_t aquakv_paged_weights_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads,
+                                            int32_t table_pages, int64_t q_rows, int32_t max_queries);
+int aquakv_paged_weights(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                         int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start, const void* q,
+                         int64_t q_stride, float score_scale, float keep, float* mass, void* workspace, size_t workspace_bytes, void* stream);
 size_t aquakv_paged_select_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t table_pages, int32_t budget);
 int aquakv_paged_select(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, const int32_t* page_table, int32_t table_pages,
                         const int32_t* seq_lens, const float* mass, int32_t budget, int32_t n_first, int32_t n_last, int32_t* kept, int32_t* n_kept,

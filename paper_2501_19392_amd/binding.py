@@ -43,6 +43,7 @@ EXPORTS = [
     "aquakv_softmax", "aquakv_weighted_workspace_bytes", "aquakv_decode_values_weighted", "aquakv_decode_values_attend",
     "aquakv_attend_raw", "aquakv_copy_ranges", "aquakv_encode_layers", "aquakv_attend_cache_workspace_bytes", "aquakv_attend_cache",
     "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend", "aquakv_paged_attend_tree",
+    "aquakv_paged_weights_workspace_bytes", "aquakv_paged_weights",
     "aquakv_paged_select_workspace_bytes", "aquakv_paged_select", "aquakv_paged_keep_workspace_bytes", "aquakv_paged_keep",
     "aquakv_rotary", "aquakv_rotary_tables",
 ]
@@ -130,6 +131,9 @@ _lib.aquakv_paged_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, 
 _lib.aquakv_paged_attend.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
 _lib.aquakv_paged_attend_tree.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I32, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
 _F32, _F64, _SZ = ctypes.c_float, ctypes.c_double, ctypes.c_size_t
+_lib.aquakv_paged_weights_workspace_bytes.restype = _SZ
+_lib.aquakv_paged_weights_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, _I32]
+_lib.aquakv_paged_weights.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I64, _F32, _F32, _P, _P, _SZ, _P]
 _lib.aquakv_paged_select_workspace_bytes.restype = _lib.aquakv_paged_keep_workspace_bytes.restype = _SZ
 _lib.aquakv_paged_select_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32]
 _lib.aquakv_paged_select.argtypes = [_LP, _PP, _I32, _P, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _P, _SZ, _P]
@@ -137,7 +141,7 @@ _lib.aquakv_paged_keep_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32]
 _lib.aquakv_paged_keep.argtypes = [_LP, _PP, _I32, _P, _I32, _I32, _P, _P, _P, _P, _I32, _P, _P, _SZ, _P]
 _lib.aquakv_rotary.argtypes = [_I32, _I64, _I32, _P, _I64, _P, _P, _P, _I32, _I32, _I32, _I32, _P, _I64, _P]
 _lib.aquakv_rotary_tables.argtypes = [_I64, _I64, _I32, _F64, _F64, _F64, _F64, _F64, _F32, _P, _P, _P]
-for _n in ("aquakv_paged_select", "aquakv_paged_keep", "aquakv_rotary", "aquakv_rotary_tables", "aquakv_paged_attend_tree", "aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
+for _n in ("aquakv_paged_weights", "aquakv_paged_select", "aquakv_paged_keep", "aquakv_rotary", "aquakv_rotary_tables", "aquakv_paged_attend_tree", "aquakv_paged_append", "aquakv_paged_attend", "aquakv_attend_cache", "aquakv_encode_layers", "aquakv_copy_ranges", "aquakv_attend_raw", "aquakv_softmax", "aquakv_decode_values_weighted", "aquakv_decode_values_attend", "aquakv_predict", "aquakv_quantize", "aquakv_dequantize", "aquakv_encode_layer", "aquakv_decode_layer",
            "aquakv_decode_attn_scores", "aquakv_decode_attn_scores_rope", "aquakv_decode_attn_scores_folded",
            "aquakv_decode_attn_scores_folded_static", "aquakv_encode_keys", "aquakv_encode_values",
            "aquakv_decode_values", "aquakv_fit_predictor"):
@@ -610,6 +614,19 @@ def _space(workspace, device: int):
     if workspace.__class__ is torch.Tensor and workspace.get_device() != device:
         raise ValueError("workspace is not on the current device")
     return _ws(workspace)
+
+
+def aquakv_paged_weights_workspace_bytes(layer, pages, batch: int, q_heads: int, table_pages: int, q_rows: int, max_queries: int) -> int:
+    return _lib.aquakv_paged_weights_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table_pages, q_rows, max_queries)
+
+
+def aquakv_paged_weights(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, keep: float,
+                         mass, workspace, stream=None) -> None:
+    """mass: fp32 [n_pages, kv_heads, page_tokens], updated; the rest as in aquakv_paged_attend."""
+    here, _, _, table, pages_each, lens, q_rows, start, at, stride = _asked(layer, pages, batch, q_heads, page_table, seq_lens, q, q_start, workspace)
+    ws, nbytes = _ws(workspace)
+    _check(_lib.aquakv_paged_weights(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table, pages_each, lens, q_rows, max_queries, start, at, stride,
+                                     score_scale, keep, _mass(mass, layer, pages, here), ws, nbytes, _stream(stream)))
 
 
 def aquakv_paged_select_workspace_bytes(layer, pages, batch: int, table_pages: int, budget: int) -> int:

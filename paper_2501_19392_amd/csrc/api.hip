@@ -1796,6 +1796,54 @@ int aquakv_paged_attend_tree(const aquakv_layer* L, const aquakv_pages* pages, i
                       score_scale, out, workspace, workspace_bytes, stream);
 }
 
+size_t aquakv_paged_weights_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, int32_t table_pages,
+                                            int64_t q_rows, int32_t max_queries) {
+  if (check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries) != AQUAKV_OK) return 0;
+  aquakv::PagedAttendArgs a = {};
+  a.pool = pool_of(pages);
+  a.batch = batch; a.table_pages = table_pages; a.max_queries = max_queries; a.q_heads = q_heads; a.H = L->kv_heads;
+  return aquakv::paged_weights_workspace_bytes(L->dtype, quantizer_id(L), a) + 256;
+}
+
+int aquakv_paged_weights(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
+                         int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start, const void* q,
+                         int64_t q_stride, float score_scale, float keep, float* mass, void* workspace, size_t workspace_bytes, void* stream) {
+  CHECK(check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries));
+  if (q_start == nullptr && q_rows != (int64_t)batch * max_queries)
+    return fail(AQUAKV_EINVAL, "q_rows=%lld: without q_start every one of %d sequences has %d", (long long)q_rows, batch, max_queries);
+  if (!std::isfinite(keep)) return fail(AQUAKV_EINVAL, "keep=%g", (double)keep);
+  // (threads of a launch: below 2^32, a fourth of the tokens of each kv head)
+  if ((int64_t)table_pages * pages->page_tokens * L->kv_heads >= ((int64_t)1 << 32))
+    return fail(AQUAKV_EUNSUPPORTED, "%d pages of %d tokens of %d heads", table_pages, pages->page_tokens, L->kv_heads);
+  if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;
+  const int64_t row = (int64_t)q_heads * 128;
+  const size_t eb = elem_bytes(L->dtype);
+  CHECK(check_array(page_table, "page_table", 4));
+  CHECK(check_array(seq_lens, "seq_lens", 4));
+  if (misaligned_to(q_start, 4)) return fail(AQUAKV_EALIGN, "q_start is not 4-byte aligned");
+  CHECK(check_rows(q, "q", q_stride, row, eb));
+  CHECK(check_ptr(mass, "mass", true));
+  CHECK(check_ptr(workspace, "workspace", true));
+  const size_t need = aquakv_paged_weights_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries);
+  if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
+  const PoolRanges pool = pool_ranges(L, pages);
+  const Params params = params_of(L);
+  const Range outs[] = {{mass, (size_t)pages->n_pages * pages->page_tokens * L->kv_heads * sizeof(float), "mass"}, {workspace, need, "workspace"}};
+  const Range ins[] = {pool.r[0], pool.r[1], pool.r[2], pool.r[3], {page_table, (size_t)batch * table_pages * sizeof(int32_t), "page_table"},
+                       {seq_lens, (size_t)batch * sizeof(int32_t), "seq_lens"},
+                       {q_start, q_start == nullptr ? 0 : ((size_t)batch + 1) * sizeof(int32_t), "q_start"},
+                       {q, rows_bytes(q_rows, q_stride, row, eb), "q"}, params.r[4], params.r[5], params.r[6]};
+  CHECK(check_no_alias(outs, 2, ins, 11));
+  aquakv::PagedAttendArgs a = {};
+  a.pool = pool_of(pages);
+  a.page_table = page_table; a.seq_lens = seq_lens; a.q_start = q_start;
+  a.table_pages = table_pages; a.batch = batch; a.max_queries = max_queries; a.H = L->kv_heads; a.q_heads = q_heads;
+  a.q_rows = q_rows; a.q_stride = q_stride; a.q = q; a.scale = score_scale;
+  a.signs_k = L->signs_k; a.signs_v = L->signs_v; a.codebook = L->codebook;
+  HIP_TRY(aquakv::launch_paged_weights(L->dtype, quantizer_id(L), a, keep, mass, workspace, static_cast<hipStream_t>(stream)));
+  return AQUAKV_OK;
+}
+
 size_t aquakv_paged_select_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t table_pages, int32_t budget) {
   if (check_paged_shape(L, pages, batch, L == nullptr ? 1 : L->kv_heads, table_pages, 0, 0) != AQUAKV_OK || budget < 0) return 0;
   return aquakv::paged_select_workspace_bytes(batch, table_pages, pages->page_tokens) + 256;

@@ -425,7 +425,7 @@ template <int NCW, int TERMS> struct Codes {
       return w;
     }
   };
-  template <bool FAR> static __device__ __forceinline__ Keys request_keys(const PagedAttendArgs& a, const Rows& rows, int h, int lane) {
+  template <bool FAR, bool VALUES = true> static __device__ __forceinline__ Keys request_keys(const PagedAttendArgs& a, const Rows& rows, int h, int lane) {
     const int m = lane & 15, g = lane >> 4;
     const uint32_t row_bytes = (uint32_t)a.H * kRow, head = (uint32_t)h * kRow;
     Keys w;
@@ -449,7 +449,7 @@ template <int NCW, int TERMS> struct Codes {
         w.k[p] = u32x4{x.x, x.y, x.z, 0};
       }
     }
-    const uint16_t* const scales = lane < 32 ? a.pool.k_scales : a.pool.v_scales;
+    const uint16_t* const scales = !VALUES || lane < 32 ? a.pool.k_scales : a.pool.v_scales;
     const uint64_t at = (uint64_t)(row_of(rows, (lane >> 3) & 3) + (lane & 7)) * a.H + h;
     if constexpr (kRtn) w.scale = reinterpret_cast<const u32x2*>(scales)[at];
     else w.scale = scales[at];
@@ -547,7 +547,7 @@ template <int NCW, int TERMS> struct Codes {
     float ref, sum;                                        // weights are 2^(score - ref)
   };
   // ---- scores of product p: s[column][half][p] += keys * query
-  template <int COLS> static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const Column (&col)[COLS],
+  template <int COLS, typename Col> static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const Col (&col)[COLS],
                                                                     f32x4 (&s)[COLS][kRtn ? 2 : 1][2]) {
     const uint32_t x[4] = {w.k[p].x, w.k[p].y, w.k[p].z, w.k[p].w};
     if constexpr (kRtn) {
