@@ -267,7 +267,9 @@ struct PagedAttendArgs {
   float *part, *stats;                            // [items, max_queries, q_heads, 128], [items, max_queries, q_heads, 2]
   int2* heads;                                    // [batch]: a sequence's first item, and how many
   int slots;                                      // pieces that fill the chip (blocks of rows: pieces of a sequence)
-  int row_blocks;                                 // blocks of 256 rows (paged_tiles.hip), 0: not in such blocks
+  int row_blocks;                                 // blocks of 256 rows (paged_tiles.h), 0: not in such blocks
+  // trees: at most so many pieces of all sequences (in such blocks); tiles of rows (not in such blocks), and whether those of a piece go to different chiplets
+  int items, row_tiles, rows_apart;
   uint32_t page_groups, page_magic;               // page_tokens / 8, 2^32 / that
   const uint32_t* tree;                           // nullable, [q_rows, tree_words]: bit j of row r: it sees draft j of its sequence (paged_tree.hip)
   int tree_words;
@@ -275,7 +277,7 @@ struct PagedAttendArgs {
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a);
 // Many queries (bf16): 8 waves x 32 rows per workgroup.
 hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
-hipError_t launch_paged_tree_rows(int dtype, int n_codewords, bool two, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream);
+hipError_t launch_paged_tree_rows(int dtype, int n_codewords, int cols, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_tree_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
 // Attention weights added to mass [n_pages, H, page_tokens] (paged_weights.hip); of the arguments out, tree and values are not used.

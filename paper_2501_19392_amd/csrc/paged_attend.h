@@ -57,8 +57,8 @@ __device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, 
 // The tokens of all sequences are cut into pieces of equally many tiles, so that about a.slots of them cover the batch whatever its
 // lengths (each sequence has one at least): item i of the launch is piece `piece` of `pieces` of sequence b (-1: behind the last).
 struct Share { int b, piece, pieces, tiles, items; };
-__device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
-  return b < a.batch ? max(tiles_of_tokens(length_of(a, a.seq_lens[b]), kTile), 1) : 0;
+template <int TILE> __device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
+  return b < a.batch ? max(tiles_of_tokens(length_of(a, a.seq_lens[b]), TILE), 1) : 0;
 }
 // sums over the lanes up to and with this one
 __device__ __forceinline__ int wave_scan(int x) {
@@ -70,10 +70,10 @@ __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143 /* row_bcast:31 */, 0xc, 0xf, false);
   return x;
 }
-__device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
+template <int TILE = kTile> __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
   Share s = {-1, 0, 1, 0, 0};
   if (a.batch == 1) {
-    const int n = max(tiles_of_tokens(length_of(a, const_ints(a.seq_lens)[0]), kTile), 1);
+    const int n = max(tiles_of_tokens(length_of(a, const_ints(a.seq_lens)[0]), TILE), 1);
     s.tiles = max((n + a.slots - 1) / a.slots, short_piece(n, a.slots));
     s.items = s.pieces = (n + s.tiles - 1) / s.tiles;
     if (item < s.items) { s.b = 0; s.piece = item; }
@@ -82,7 +82,7 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
   int total = 0;                                           // (all sequences' room is below 2^30 tiles)
   int tiles = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    tiles = tiles_of(a, b0 + lane);
+    tiles = tiles_of<TILE>(a, b0 + lane);
     total += __builtin_amdgcn_readlane(wave_scan(tiles), 63);
   }
   s.tiles = piece_tiles(total, a.slots, a.batch);
@@ -97,7 +97,7 @@ __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, in
   }
   s.tiles = max(s.tiles, short_piece(total, a.slots));
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    if (a.batch > 64) tiles = tiles_of(a, b0 + lane);
+    if (a.batch > 64) tiles = tiles_of<TILE>(a, b0 + lane);
     const int mine = (int)((uint32_t)(tiles + s.tiles - 1) / (uint32_t)s.tiles);
     const int end = s.items + wave_scan(mine);             // items up to and with this sequence
     const uint64_t past = __builtin_amdgcn_ballot_w64(end > item);

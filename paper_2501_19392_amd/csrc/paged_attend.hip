@@ -129,17 +129,39 @@ __global__ __launch_bounds__(256) void paged_merge_rows_kernel(const PagedAttend
 // How a launch is laid out, from sizes alone (lengths and counts of queries are on the device): by max_queries, whatever the sequences have.  So single queries
 // beside a chunk are walked by one workgroup a kv head each, as a block of 256 rows is: 31 over 16 384 tokens and a chunk of 512, 32 heads, 2.1 ms, in a call of
 // their own 94 us, the chunk by itself 99.
-struct PagedPlan { unsigned blocks, row_tiles; int slots, row_blocks; int64_t items; bool two, merge, many, by_rows; };
+struct PagedPlan { unsigned blocks, row_tiles, rows_apart; int slots, row_blocks; int64_t items; int cols; bool merge, many, by_rows; };
 // Results of a sequence beyond which the merge has 1024 threads a row, of 256 (one query of 131 072 tokens 41.0 us, for 45.0; beyond 8: 32 x 4000 tokens
 // 37.4 for 34.4).
 constexpr int kManyPieces = 64;
 // Rows of a kv head up to which waves of 32 take them in turn (8 x 9999 tokens, 3 bits: 68 rows 108 us, in tiles of 256 rows 131; 128 rows 93, 135; 32 x 4000:
 // 167, 167 and 150, 170; one sequence of 12 288: 35, 31 and 31, 35; 192 rows of 8 x 9999: 230, 136).
 constexpr int kFewRows = 128;
-template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H) {
+// Trees: columns of 16 rows that a wave has, by the rows of a kv head and the tiles of all sequences and heads.  Three take the codes to operands once where two would do it
+// twice, on all registers there are (uniform codes need too many): 36 rows of 32 x 8000 tokens (256 points) 83 us, with two 119; 80 rows 149, 187; 144 rows 215, 436; 64
+// rows, two tiles either way, 148, 122.  Where a wave has few tiles, more waves are better: 36 rows of 16 000 tokens 23.9, 22.5; of 2000 16.4, 14.6.
+int tree_columns(int64_t rows, bool rtn, int64_t tiles) {
+  if (rows <= 8) return 1;
+  return !rtn && tiles >= 8192 && (rows + 47) / 48 < (rows + 31) / 32 ? 3 : 2;
+}
+// ... from which on workgroups of 256 rows take them: 192 rows of 32 x 8000 tokens 327 us, in waves 302; 256: 334, 460 (uniform codes: 144 rows 397, 463; 128: 395, 294).
+// Not over few tokens: 256 rows of 2000 31 us, in waves 21.
+bool tree_in_blocks(int64_t rows, bool rtn, int64_t tiles) { return rows > (rtn ? 128 : 192) && (tiles >= 4096 || rows > 512); }
+template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table_pages, int64_t page_tokens, int64_t max_queries, int64_t q_heads, int64_t H, bool tree) {
   PagedPlan p = {};
   const int64_t rows = std::max<int64_t>(max_queries, 1) * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
-  if (sizeof(T) == 2 && rows > kFewRows) {                 // workgroups of 256 rows, one a CU: the tokens in pieces if there are too few of them
+  if (sizeof(T) == 2 && tree && tree_in_blocks(rows, is_rtn(NCW), batch * most * H)) {      // one workgroup a CU, pieces of equal size over all sequences
+    const int row_blocks = (int)((rows + kTileRows - 1) / kTileRows), slots = (int)std::max<int64_t>(256 / (H * row_blocks), 1);
+    const int64_t tiles = std::max<int64_t>((table_pages * page_tokens + 63) / 64, 1);
+    const int64_t items = std::min(batch * tiles, std::max<int64_t>(slots - batch, std::max(slots / 2, 1)) + batch);
+    if (items * H < (1 << 22)) {                           // (threads of a launch: below 2^32)
+      p.row_blocks = row_blocks; p.slots = slots; p.items = items;
+      p.merge = tiles > 1;
+      p.by_rows = items <= 16 * batch;
+      p.many = items > kManyPieces * batch;
+      return p;
+    }
+  }
+  if (sizeof(T) == 2 && !tree && rows > kFewRows) {                 // workgroups of 256 rows, one a CU: the tokens in pieces if there are too few of them
     p.row_blocks = (int)((rows + kTileRows - 1) / kTileRows);
     // ... of 4 tiles of 64 at least, of 2 where there is one block of rows and so little to join (180 rows over 700 tokens: 28.0 us, 22.2; 160 over 6000: 34.3, 31.5;
     // 1200 rows over 300: 23.3, 26.2)
@@ -153,16 +175,24 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
   // 9 to 16 rows fill one column of a wave, but two columns take as long and join their results (16 rows of 8 x 9999 tokens, 3 bits: 37.3 us, in one column
   // 39.7; of one sequence of 12 288: 18.9, 29.8; of 32 x 4000 46.1, 44.8); 8 rows do not (one sequence of 131 072: 49.0, 41.9; 32 x 16 384: 138, 101; 8 x 9999 31.3,
   // 30.4; but one of 16 384 18.0, 19.8).
-  p.two = sizeof(T) == 2 && rows > 8;
-  const int per_wave = p.two ? 32 : 16, waves = p.two ? Shape<T, NCW, 2>::kWaves : Shape<T, NCW, 1>::kWaves;
+  p.cols = sizeof(T) == 4 ? 1 : tree ? tree_columns(rows, is_rtn(NCW), batch * most * H) : rows > 8 ? 2 : 1;
+  // (threads of a launch: below 2^32, where row tiles share a grid dimension with the pieces)
+  if (tree && (batch + 512) * H * ((rows + 31) / 32) >= (1 << 22)) p.cols = 1;
+  const int per_wave = 16 * p.cols, waves = p.cols > 1 ? Shape<T, NCW, 2>::kWaves : Shape<T, NCW, 1>::kWaves;
   p.row_tiles = (unsigned)((rows + per_wave - 1) / per_wave);
   // As many pieces as make all waves that the chip holds (32 x 16 384 tokens: 95.7 us, half as many 111, twice as many 99; 5 queries of 8 x 9999 37.7, 42.8,
   // 50.7); the kernel makes fewer of short ones.
-  p.slots = (int)std::max<int64_t>((p.two ? Shape<T, NCW, 2>::kSlots : Shape<T, NCW, 1>::kSlots) / (H * p.row_tiles), 1);
+  p.slots = (int)std::max<int64_t>((p.cols > 1 ? Shape<T, NCW, 2>::kSlots : Shape<T, NCW, 1>::kSlots) / (H * p.row_tiles), 1);
+  if (tree && p.cols > 1) {                                // (whole workgroups of pieces: no more of them than run at once)
+    const int64_t at_once = Shape<T, NCW, 2>::kSlots / Shape<T, NCW, 2>::kWaves, groups = std::max<int64_t>(at_once / (H * p.row_tiles), 1);
+    p.slots = (int)groups * Shape<T, NCW, 2>::kWaves;
+    p.rows_apart = groups % 8 != 0 || batch * most < 4 * p.slots;      // (few tiles a wave: 104 rows over 2000 tokens 16.7 us, on the same CUs 19.6)
+  }
   const int64_t pieces = std::min(batch * std::max<int64_t>(most, 1), std::max<int64_t>(p.slots - batch, std::max(p.slots / 2, 1)) + batch);
-  if (p.two) {                                             // (a workgroup has results of as many sequences as it has pieces of)
+  if (p.cols > 1) {                                        // (a workgroup has results of as many sequences as it has pieces of)
     const int64_t groups = (pieces + waves - 1) / waves;
     p.blocks = (unsigned)((groups + 7) / 8 * 8 * H);
+    if (p.rows_apart) p.blocks = (unsigned)((groups * p.row_tiles + 7) / 8 * 8 * H);
     p.items = groups + batch;
     p.merge = groups > 1;
   } else {
@@ -177,23 +207,29 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
 
 }  // namespace
 
-static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a) {
+static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a, bool tree) {
   PagedPlan p = {};
-  AQUAKV_PAGED(dtype, n_codewords, (p = paged_plan<T, N>(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H)));
+  AQUAKV_PAGED(dtype, n_codewords, (p = paged_plan<T, N>(a.batch, a.table_pages, a.pool.page_tokens, a.max_queries, a.q_heads, a.H, tree)));
   return p;
 }
 
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a) {
-  const PagedPlan p = plan_of(dtype, n_codewords, a);
-  if (!p.merge) return 0;
-  return (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2);
+  size_t most = 0;                                         // (one size for calls with and without a tree)
+  for (const bool tree : {false, true}) {
+    const PagedPlan p = plan_of(dtype, n_codewords, a, tree);
+    if (p.merge) most = std::max(most, (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2));
+  }
+  return most;
 }
 
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& args, void* workspace, hipStream_t stream) {
   PagedAttendArgs a = args;
-  const PagedPlan plan = plan_of(dtype, n_codewords, a);
+  const PagedPlan plan = plan_of(dtype, n_codewords, a, a.tree != nullptr);
   a.slots = plan.slots;
   a.row_blocks = plan.row_blocks;
+  a.items = (int)plan.items;
+  a.row_tiles = (int)plan.row_tiles;
+  a.rows_apart = (int)plan.rows_apart;
   a.part = static_cast<float*>(workspace);
   a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
   a.heads = plan.merge ? reinterpret_cast<int2*>(a.stats + plan.items * a.max_queries * a.q_heads * 2) : nullptr;
@@ -203,9 +239,9 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
     const hipError_t e = a.tree != nullptr ? launch_paged_tree_tiles(n_codewords, a, stream) : launch_paged_tiles(n_codewords, a, stream);
     if (e) return e;
   } else {
-    const dim3 blocks(plan.blocks, plan.row_tiles);
-    const hipError_t e = a.tree != nullptr ? launch_paged_tree_rows(dtype, n_codewords, plan.two, blocks, a, stream)
-                                           : launch_rows<false>(dtype, n_codewords, plan.two, blocks, a, stream);
+    const dim3 blocks(plan.blocks, plan.rows_apart ? 1u : plan.row_tiles);
+    const hipError_t e = a.tree != nullptr ? launch_paged_tree_rows(dtype, n_codewords, plan.cols, blocks, a, stream)
+                                           : launch_rows<false>(dtype, n_codewords, plan.cols, blocks, a, stream);
     if (e) return e;
   }
   if (!plan.merge) return hipSuccess;

@@ -25,12 +25,12 @@ namespace paged {
 // Waves of a workgroup, which share the copies of the grid, and waves per SIMD: with 128 registers four fit (two workgroups a CU, which is what LDS has
 // room for with 256 points); uniform codes need more for the two halves' scales, and no LDS to speak of; fp32 layers hold everything twice.
 template <typename T, int NCW, int COLS> struct Shape {
-  static constexpr int kWaves = is_rtn(NCW) || COLS == 2 ? 4 : 8;
-  static constexpr int kPerSimd = COLS == 2 ? 2 : is_rtn(NCW) ? 3 : sizeof(T) == 4 ? 2 : 4;
+  static constexpr int kWaves = is_rtn(NCW) || COLS >= 2 ? 4 : 8;
+  static constexpr int kPerSimd = COLS >= 2 ? 2 : is_rtn(NCW) ? 3 : sizeof(T) == 4 ? 2 : 4;
   // COLS = 2: a workgroup's waves take pieces of one kv head, one behind the other, and join their results (5 queries of 8 x 9999 tokens, 3 bits: 33.2 us,
   // two waves of two heads each 34.5, every wave its own result 37.6).  With 16 rows they take all heads of the same tokens, whose codes share cache
   // lines: 32 x 16 384 tokens 95.6 us, four waves of two heads joined 99.5, two of four heads 109, one head 113 (one sequence of 131 072: 47, 45, 47, 49).
-  static constexpr bool kJoined = COLS == 2;
+  static constexpr bool kJoined = COLS >= 2;
   static constexpr int kThreads = 64 * kWaves, kSlots = 256 * 4 * kPerSimd;            // threads, waves on the chip
 };
 template <typename T, int NCW, int COLS, bool FAR, bool TREE>
@@ -52,10 +52,21 @@ paged_attend_kernel(const PagedAttendArgs a) {
   const typename C::Points points = C::request_points(a.codebook, lane);
   // which rows, kv head and piece of a sequence
   int h, item;
+  unsigned row_tile = blockIdx.y;
   if constexpr (kJoined) {                                 // workgroups go round the eight chiplets: those of the heads of a piece are eight apart
     const unsigned turn = blockIdx.x >> 3;
+    unsigned group = turn / a.H * 8 + (blockIdx.x & 7);
     h = turn % a.H;
-    item = (turn / a.H * 8 + (blockIdx.x & 7)) * kWaves + wave;
+    if constexpr (TREE) {
+      // Row tiles of a piece come to the same CU, one behind the other, where the pieces fill all chiplets alike (4 tiles, 32 x 8000 tokens: 246 us, else 262);
+      // otherwise they go round the chiplets with the pieces (3 tiles, 21 groups of pieces: 187 us, else 297, as five chiplets would have 72 workgroups, for 64 that
+      // run at once).
+      if (a.rows_apart) {
+        row_tile = group % a.row_tiles;
+        group /= a.row_tiles;
+      }
+    }
+    item = group * kWaves + wave;
   } else {
     const unsigned unit = blockIdx.x * kWaves + wave;
     h = uniform(unit % a.H);
@@ -65,7 +76,7 @@ paged_attend_kernel(const PagedAttendArgs a) {
   if ((kJoined ? item - wave : (int)(blockIdx.x * kWaves / a.H)) >= share.items) return;      // (the whole workgroup is behind the last piece)
   const int b = max(share.b, 0), rep = a.q_heads / a.H;
   const PagedQueries w = paged_queries(a, b);
-  const int n_rows = w.n * rep, row0 = blockIdx.y * kRows;
+  const int n_rows = w.n * rep, row0 = row_tile * kRows;
   const bool idle = share.b < 0 || row0 >= n_rows;
   // the tokens of this piece
   const int past = w.len - w.count;                        // tokens ahead of the queries' own
@@ -226,7 +237,7 @@ paged_attend_kernel(const PagedAttendArgs a) {
     result = group + b;                                    // (two sequences that share a workgroup are neighbours)
     others = min(kWaves - wave, share.pieces - share.piece) - 1;
   }
-  if (a.heads != nullptr && !idle && share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) a.heads[b] = int2{result, results};
+  if (a.heads != nullptr && !idle && share.piece == 0 && h == 0 && row_tile == 0 && lane == 0) a.heads[b] = int2{result, results};
   // (worked out anew: lane and row numbers are not worth registers in the loop)
   int again = lane;
   asm volatile("" : "+v"(again));
@@ -299,14 +310,21 @@ paged_attend_kernel(const PagedAttendArgs a) {
     else { constexpr int N = 256; CALL; }                                      \
   } while (0)
 
-template <bool TREE> hipError_t launch_rows(int dtype, int n_codewords, bool two, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream) {
+template <bool TREE> hipError_t launch_rows(int dtype, int n_codewords, int cols, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream) {
   const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;      // (codes take half a byte per value at most)
 #define AQUAKV_ATTEND(T, N, COLS)                                                                                             \
   (far ? paged_attend_kernel<T, N, COLS, true, TREE><<<blocks, Shape<T, N, COLS>::kThreads, 0, stream>>>(a)                    \
        : paged_attend_kernel<T, N, COLS, false, TREE><<<blocks, Shape<T, N, COLS>::kThreads, 0, stream>>>(a))
-  if (two) {
+  if (cols == 2) {
     typedef bf16_t T;
     AQUAKV_PAGED_N(n_codewords, (AQUAKV_ATTEND(T, N, 2)));
+  } else if (cols == 3) {                                  // (trees, grids)
+    if constexpr (TREE) {
+      typedef bf16_t T;
+      if (n_codewords == 16) AQUAKV_ATTEND(T, 16, 3);
+      else if (n_codewords == 64) AQUAKV_ATTEND(T, 64, 3);
+      else AQUAKV_ATTEND(T, 256, 3);
+    }
   } else {
     AQUAKV_PAGED(dtype, n_codewords, (AQUAKV_ATTEND(T, N, 1)));
   }

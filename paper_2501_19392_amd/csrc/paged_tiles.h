@@ -197,8 +197,20 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
   unsigned char* const buffers = lds + C::kTableBytes;
   const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const typename C::Points points = C::request_points(a.codebook, lane);
-  // blockIdx: (piece, block of rows: the last ones, which see most tokens, first; kv head), sequence
-  const int h = blockIdx.x % a.H, piece = (blockIdx.x / a.H) % a.slots, block = a.row_blocks - 1 - blockIdx.x / a.H / a.slots, b = blockIdx.y;
+  const int h = blockIdx.x % a.H;
+  int piece, block, b, first_result, results;
+  TokenRange range = {};
+  if constexpr (TREE) {                                    // blockIdx: (piece of all sequences and kv head, block of rows)
+    const int item = blockIdx.x / a.H;
+    const Share share = share_of<kTokens>(a, lane, item);
+    if (share.b < 0) return;
+    b = share.b; piece = share.piece; block = blockIdx.y;
+    first_result = item - piece; results = share.pieces;
+    range = {share.tiles, 0};
+  } else {                                                 // (piece, block of rows: the last ones, which see most tokens, first; kv head), sequence
+    piece = (blockIdx.x / a.H) % a.slots; block = a.row_blocks - 1 - blockIdx.x / a.H / a.slots; b = blockIdx.y;
+    first_result = b * a.slots; results = a.slots;
+  }
   const PagedQueries w = paged_queries(a, b);
   const int rep = a.q_heads / a.H, n_rows = w.n * rep, row0 = block * kTileRows;
   if (row0 >= n_rows) return;
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
   const int limit = row_there ? past + qi : -1;
   const int wave_first = TREE ? past - 1 : uniform(past + min(row0 + 32 * wave, n_rows - 1) / rep);      // smallest limit of the wave's rows
   const int last_limit = TREE ? w.len - 1 : uniform(past + min(row0 + kTileRows - 1, n_rows - 1) / rep);
-  const TokenRange range = piece_range(piece, (tiles_of_tokens(last_limit + 1, kTokens) + a.slots - 1) / a.slots, kTokens, last_limit + 1);
+  range = piece_range(piece, TREE ? range.begin : (tiles_of_tokens(last_limit + 1, kTokens) + a.slots - 1) / a.slots, kTokens, last_limit + 1);
   const int t_begin = range.begin, t_end = range.end;
 
   Tile codes;
@@ -384,10 +396,11 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 
   // ---- results: register n of product R is coordinate 16 (2 R + n / 8) + 8 hf + n % 8
   sum = far_sum<32>(sum);
-  if (a.slots > 1) {
-    if (block == 0 && h == 0 && piece == 0 && threadIdx.x == 0) a.heads[b] = int2{b * a.slots, a.slots};
+  if (TREE && a.heads != nullptr && block == 0 && h == 0 && piece == 0 && threadIdx.x == 0) a.heads[b] = int2{first_result, results};
+  if (results > 1) {
+    if (!TREE && block == 0 && h == 0 && piece == 0 && threadIdx.x == 0) a.heads[b] = int2{first_result, results};
     if (!row_there) return;
-    const int64_t at = ((int64_t)(b * a.slots + piece) * a.max_queries + qi) * a.q_heads + qh;
+    const int64_t at = ((int64_t)(first_result + piece) * a.max_queries + qi) * a.q_heads + qh;
     float* const part = a.part + at * kGroup + 8 * hf;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -435,7 +448,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 }
 
 template <bool TREE> hipError_t launch_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.H * a.slots * a.row_blocks), (unsigned)a.batch);
+  const dim3 grid = TREE ? dim3((unsigned)(a.H * a.items), (unsigned)a.row_blocks) : dim3((unsigned)(a.H * a.slots * a.row_blocks), (unsigned)a.batch);
 #define AQUAKV_TILES(NCW) paged_tiles_kernel<NCW, TREE><<<grid, 64 * kTileWaves, 0, stream>>>(a)
   switch (n_codewords) {
     case kRtn2: AQUAKV_TILES(kRtn2); break;

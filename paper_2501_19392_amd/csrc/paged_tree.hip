@@ -4,8 +4,8 @@
 
 namespace aquakv {
 
-hipError_t launch_paged_tree_rows(int dtype, int n_codewords, bool two, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream) {
-  return paged::launch_rows<true>(dtype, n_codewords, two, blocks, a, stream);
+hipError_t launch_paged_tree_rows(int dtype, int n_codewords, int cols, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream) {
+  return paged::launch_rows<true>(dtype, n_codewords, cols, blocks, a, stream);
 }
 hipError_t launch_paged_tree_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream) { return paged::launch_tiles<true>(n_codewords, a, stream); }
 

@@ -52,6 +52,35 @@ def test_drafts_see_their_ancestors(dtype, fmt, H, QH, lengths, page, counts):
     P.check(got, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, dtype), "tree")
 
 
+@pytest.mark.parametrize("fmt,H,QH,counts,room", [
+    ("grid256", 8, 32, [12, 9], 40000), ("grid64", 8, 64, [17, 18], 40000), ("grid16", 4, 24, [8, 1], 70000),      # three columns of rows: 1 and 3 tiles of 48, 1
+    ("grid256", 8, 32, [20, 3], 2000), ("rtn4", 8, 24, [27, 30], 2000), ("grid64", 8, 64, [23, 9], 300), ("grid16", 1, 8, [50], 1000),      # 3, 3, 6, 13 tiles of 32
+    ("grid256", 8, 32, [64, 50], 40000), ("rtn2", 8, 32, [40, 33], 40000), ("grid16", 2, 32, [40], 600), ("grid256", 1, 16, [130], 500)])      # blocks of 256 rows
+def test_row_tiles(fmt, H, QH, counts, room):
+    """The ways that rows are shared out go by the sizes a call has room for: wide page tables, of which little is used."""
+    page, lengths = 16, [390, 77][:len(counts)]
+    lengths[0] = max(lengths[0], counts[0])
+    print(f"case row tiles {fmt} H={H} QH={QH} {counts} room={room}", flush=True)
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, H, lengths, page, seed=7)
+    table = torch.cat([table, torch.full((len(counts), max(room // page - table.shape[1], 0)), -1, dtype=torch.int32)], 1).contiguous()
+    trees = [T.random_tree(n, gen) for n in counts]
+    q = queries(gen, sum(counts), QH, "bf16")
+    got = attend(lg, pages, table, lens, q, counts, trees)
+    torch.cuda.synchronize()
+    P.check(got, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, "bf16"), "row tiles")
+
+
+@pytest.mark.parametrize("fmt,n,QH", [("grid256", 12, 32), ("grid64", 20, 32), ("rtn4", 26, 32)])
+def test_long_sequences_in_many_pieces(fmt, n, QH):
+    """Several pieces of each row tile, joined."""
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, 8, [9000, 5001, n], 64, seed=8)
+    trees = [T.random_tree(n, gen) for _ in range(3)]
+    q = queries(gen, 3 * n, QH, "bf16")
+    got = attend(lg, pages, table, lens, q, [n] * 3, trees, ragged=False)
+    torch.cuda.synchronize()
+    P.check(got, *T.reference(lo, pages, table, lens, q, [n] * 3, trees, SCALE, "bf16"), "pieces")
+
+
 @pytest.mark.parametrize("fmt,QH,n", [("grid256", 4, 6), ("grid256", 16, 40), ("rtn4", 4, 6), ("rtn4", 16, 40), ("grid64", 1, 3)])
 def test_any_mask_of_the_last_tokens(fmt, QH, n):
     """Bits as they come: rows that see nothing, not even themselves; the future; words behind those that are needed."""
