@@ -1871,10 +1871,10 @@ int aquakv_paged_select(const aquakv_layer* L, const aquakv_pages* pages, int32_
                        {mass, tokens * L->kv_heads * sizeof(float), "mass"}};
   CHECK(check_no_alias(outs, 3, ins, 3));
   aquakv::PagedSelectArgs a = {};
-  a.page_table = page_table; a.seq_lens = seq_lens; a.mass = mass; a.kept = kept; a.n_kept = n_kept; a.keys = static_cast<uint32_t*>(workspace);
+  a.page_table = page_table; a.seq_lens = seq_lens; a.mass = mass; a.kept = kept; a.n_kept = n_kept;
   a.table_pages = table_pages; a.batch = batch; a.H = L->kv_heads; a.n_pages = pages->n_pages; a.page_tokens = pages->page_tokens;
   a.budget = budget; a.n_first = n_first; a.n_last = n_last;
-  HIP_TRY(aquakv::launch_paged_select(a, static_cast<hipStream_t>(stream)));
+  HIP_TRY(aquakv::launch_paged_select(a, workspace, static_cast<hipStream_t>(stream)));
   return AQUAKV_OK;
 }
 
@@ -1883,9 +1883,7 @@ int check_keep_shape(const aquakv_layer* L, const aquakv_pages* pages, int32_t b
   CHECK(check_pages(L, pages));
   if (batch < 0 || max_kept < 0) return fail(AQUAKV_EINVAL, "batch=%d max_kept=%d", batch, max_kept);
   if (batch > 65535) return fail(AQUAKV_EUNSUPPORTED, "batch=%d: at most 65535 sequences", batch);
-  // (threads of a launch: below 2^32, one per 16 bytes of a row, or per head)
-  if ((int64_t)max_kept * std::max<int64_t>(make_plan(L, 1).code_row, L->kv_heads) >= ((int64_t)1 << 31) * 8)
-    return fail(AQUAKV_EUNSUPPORTED, "max_kept=%d rows of %d heads", max_kept, L->kv_heads);
+  if (max_kept >= (1 << 29)) return fail(AQUAKV_EUNSUPPORTED, "max_kept=%d", max_kept);      // (threads of a launch: below 2^32)
   return AQUAKV_OK;
 }
 }  // namespace

@@ -289,11 +289,11 @@ struct PagedSelectArgs {
   const int32_t *page_table, *seq_lens;           // [batch, table_pages], [batch]
   const float* mass;                              // [n_pages, H, page_tokens]
   int32_t *kept, *n_kept;
-  uint32_t* keys;                                 // [batch, table_pages * page_tokens]
+  uint32_t* keys;                                 // (set by the launcher)
   int table_pages, batch, H, n_pages, page_tokens, budget, n_first, n_last;
 };
 size_t paged_select_workspace_bytes(int64_t batch, int64_t table_pages, int64_t page_tokens);
-hipError_t launch_paged_select(const PagedSelectArgs& a, hipStream_t stream);
+hipError_t launch_paged_select(const PagedSelectArgs& a, void* workspace, hipStream_t stream);
 // Token kept[b][i] of a sequence becomes its token first[b] + i, in pages of the same table or (to_table) of another one.
 struct PagedKeepArgs {
   PagedPool pool;

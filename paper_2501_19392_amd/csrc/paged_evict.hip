@@ -6,15 +6,16 @@
 namespace aquakv {
 namespace {
 
-// Token -> row of the pool (page * page_tokens + place), -1: its page is not in the pool.
+// Token -> its page in the pool, -1: not there; its place in the page.
 struct PageDivider { uint32_t tokens, magic; };
-__device__ __forceinline__ int64_t row_of_token(const int32_t* table, int table_pages, const PageDivider& d, int n_pages, int64_t token) {
-  if (token < 0 || token >= (int64_t)table_pages * d.tokens) return -1;
+struct Place { int page; uint32_t in; };
+__device__ __forceinline__ Place place_of_token(const int32_t* table, int table_pages, const PageDivider& d, int n_pages, int64_t token) {
+  if (token < 0 || token >= (int64_t)table_pages * d.tokens) return {-1, 0u};
   const uint32_t t = (uint32_t)token;
   uint32_t page = (uint32_t)(((uint64_t)t * d.magic) >> 32);                 // (one short at most)
   if (t - page * d.tokens >= d.tokens) ++page;
   const int at = table[page];
-  return (uint32_t)at < (uint32_t)n_pages ? (int64_t)at * d.tokens + (t - page * d.tokens) : -1;
+  return {(uint32_t)at < (uint32_t)n_pages ? at : -1, t - page * d.tokens};
 }
 PageDivider divider(int page_tokens) { return {(uint32_t)page_tokens, (uint32_t)((uint64_t(1) << 32) / (uint32_t)page_tokens)}; }
 
@@ -27,115 +28,236 @@ __device__ __forceinline__ uint32_t key_of(float mass) {
   return (x >> 31) ? ~x : x | 0x80000000u;
 }
 constexpr uint32_t kAlways = 0xffffffffu;
-__global__ __launch_bounds__(256) void mass_keys_kernel(const PagedSelectArgs a, PageDivider d) {
-  const int b = blockIdx.y;
-  const int64_t room = (int64_t)a.table_pages * a.page_tokens;
-  const int64_t len = min((int64_t)max(a.seq_lens[b], 0), room), t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= len) return;
-  const int64_t row = row_of_token(a.page_table + (int64_t)b * a.table_pages, a.table_pages, d, a.n_pages, t);
-  uint32_t key = 0u;
-  if (row >= 0) {
-    if (t < a.n_first || t >= len - a.n_last) {
-      key = kAlways;
-    } else {
-      const int64_t page = row / a.page_tokens;
-      const float* const at = a.mass + page * a.H * a.page_tokens + (row - page * a.page_tokens);
-      float sum = at[0];
-      for (int h = 1; h < a.H; ++h) sum += at[(int64_t)h * a.page_tokens];
-      key = key_of(sum);
-    }
+__device__ __forceinline__ int cached(const PagedSelectArgs& a, int b) { return (int)min((int64_t)max(a.seq_lens[b], 0), (int64_t)a.table_pages * a.page_tokens); }
+__device__ __forceinline__ uint32_t token_key(const PagedSelectArgs& a, const PageDivider& d, int b, int len, int t) {
+  const Place at = place_of_token(a.page_table + (int64_t)b * a.table_pages, a.table_pages, d, a.n_pages, t);
+  if (at.page < 0) return 0u;
+  if (t < a.n_first || t >= len - a.n_last) return kAlways;
+  const float* const mass = a.mass + (int64_t)at.page * a.H * a.page_tokens + at.in;
+  float sum = mass[0];
+  int h = 1;
+  for (; h + 7 <= a.H; h += 7) {                           // (requested together, added in order)
+    float x[7];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) x[i] = mass[(int64_t)(h + i) * a.page_tokens];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) sum += x[i];
   }
-  a.keys[b * room + t] = key;
+  for (; h < a.H; ++h) sum += mass[(int64_t)h * a.page_tokens];
+  return key_of(sum);
 }
 
-// One workgroup a sequence: the budget-th largest key by its digits (11, 11, 10 bits), then the tokens above it and the first of those that have it, in order:
-// every wave has a run of the tokens and counts its own first.
+// The budget-th largest key digit by digit: 11, 11 and 10 bits.  What is known of it ahead of a digit: the ones before it, and how many tokens are still to be taken
+// among the keys that have those.
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(const PagedSelectArgs a) {
-  __shared__ uint32_t bins[kBins];
-  __shared__ uint32_t sums[kSelectWaves], above[kSelectWaves], equal[kSelectWaves];
-  __shared__ uint32_t chosen[2];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t room = (int64_t)a.table_pages * a.page_tokens;
-  const int len = (int)min((int64_t)max(a.seq_lens[b], 0), room), n = min(len, a.budget);
-  const uint32_t* const keys = a.keys + b * room;
-  int32_t* const kept = a.kept + (int64_t)b * a.budget;
-  for (int i = n + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
-  if (tid == 0) a.n_kept[b] = n;
-  if (n == 0) return;
-  if (len <= a.budget) {
-    for (int i = tid; i < n; i += kSelectThreads) kept[i] = i;
-    return;
-  }
-  uint32_t prefix = 0, need = (uint32_t)n;                 // digits found so far; so many are still to be taken among the keys that have them
-#pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11, above_shift = shift + width;
-    for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < len; i += kSelectThreads) {
-      const uint32_t k = keys[i];
-      if (pass == 0 || (k >> above_shift) == prefix) atomicAdd(&bins[(k >> shift) & ((1u << width) - 1u)], 1u);
-    }
-    __syncthreads();
-    // sums from the largest digit down: thread i has digits 2047 - 2 i and the one below it
-    const uint32_t x = bins[kBins - 1 - 2 * tid], y = bins[kBins - 2 - 2 * tid];
-    uint32_t run = x + y;
+__device__ __forceinline__ int shift_of(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+__device__ __forceinline__ int width_of(int digit) { return digit == 2 ? 10 : 11; }
+struct Known { uint32_t prefix, need; };
+struct Scan { uint32_t sums[kSelectWaves], chosen[2]; };
+// Thread i has the counts of digits 2047 - 2 i (x) and the one below it (y).
+__device__ __forceinline__ Known next_digit(Known k, int digit, uint32_t x, uint32_t y, Scan& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t run = x + y;
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const uint32_t o = __shfl_up(run, s);
-      if (lane >= s) run += o;
-    }
-    if (lane == 63) sums[wave] = run;
-    __syncthreads();
-    uint32_t before = run - x - y;
-    for (int w = 0; w < wave; ++w) before += sums[w];
-    if (before < need && before + x >= need) { chosen[0] = kBins - 1 - 2 * tid; chosen[1] = need - before; }
-    else if (before + x < need && before + x + y >= need) { chosen[0] = kBins - 2 - 2 * tid; chosen[1] = need - before - x; }
-    __syncthreads();
-    prefix = prefix << width | chosen[0];
-    need = chosen[1];
-    __syncthreads();
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(run, d);
+    if (lane >= d) run += o;
   }
-  // prefix is the last key that is taken, of which the first `need` tokens are
-  const int each = ((len + kSelectWaves - 1) / kSelectWaves + 63) & ~63, from = wave * each, to = from + max(min(each, len - from), 0);
-  uint32_t more = 0, same = 0;
-  for (int i = from + lane; i < to; i += 64) {
-    const uint32_t k = keys[i];
-    more += k > prefix;
-    same += k == prefix;
-  }
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    more += __shfl_xor(more, s);
-    same += __shfl_xor(same, s);
-  }
-  if (lane == 0) { above[wave] = more; equal[wave] = same; }
+  if (lane == 63) s.sums[wave] = run;
   __syncthreads();
-  uint32_t tie = 0, at = 0;                                // of the tokens before this wave's: those that have the last key, those that are kept
-  for (int w = 0; w < wave; ++w) { at += above[w]; tie += equal[w]; }
-  at += min(tie, need);
+  uint32_t before = run - x - y;
+  for (int w = 0; w < wave; ++w) before += s.sums[w];
+  if (before < k.need && before + x >= k.need) { s.chosen[0] = kBins - 1 - 2 * tid; s.chosen[1] = k.need - before; }
+  else if (before + x < k.need && before + x + y >= k.need) { s.chosen[0] = kBins - 2 - 2 * tid; s.chosen[1] = k.need - before - x; }
+  __syncthreads();
+  k = {k.prefix << width_of(digit) | s.chosen[0], s.chosen[1]};
+  __syncthreads();
+  return k;
+}
+// Whether a key counts for a digit, and for which value of it.
+__device__ __forceinline__ bool counts(uint32_t key, const Known& k, int digit) { return digit == 0 || key >> (shift_of(digit) + width_of(digit)) == k.prefix; }
+__device__ __forceinline__ uint32_t digit_of(uint32_t key, int digit) { return (key >> shift_of(digit)) & ((1u << width_of(digit)) - 1u); }
+
+// The tokens of a run that are kept, in order: `at` of this sequence's, and `tie` that have the last key, lie before it.  64 at a time, one wave.
+template <typename Key> __device__ __forceinline__ void emit(int32_t* kept, const Known& k, uint32_t at, uint32_t tie, int from, int to, const Key& key) {
+  const int lane = threadIdx.x & 63;
   const uint64_t below = (1ull << lane) - 1;
   for (int i0 = from; i0 < to; i0 += 64) {
     const int i = i0 + lane;
-    const uint32_t k = i < to ? keys[i] : 0u;
-    const uint64_t ties = __builtin_amdgcn_ballot_w64(i < to && k == prefix);
-    const bool keep = i < to && (k > prefix || (k == prefix && tie + __builtin_popcountll(ties & below) < need));
+    const uint32_t x = i < to ? key(i) : 0u;
+    const uint64_t ties = __builtin_amdgcn_ballot_w64(i < to && x == k.prefix);
+    const bool keep = i < to && (x > k.prefix || (x == k.prefix && tie + __builtin_popcountll(ties & below) < k.need));
     const uint64_t all = __builtin_amdgcn_ballot_w64(keep);
     if (keep) kept[at + __builtin_popcountll(all & below)] = i;
     at += __builtin_popcountll(all);
     tie += __builtin_popcountll(ties);
   }
 }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+// Everything but the choice: what is behind the tokens that are kept, and sequences that keep all of theirs.  -> whether that was all
+__device__ __forceinline__ bool keeps_all(const PagedSelectArgs& a, int b, int len, int tid, int threads) {
+  const int n = min(len, a.budget);
+  int32_t* const kept = a.kept + (int64_t)b * a.budget;
+  for (int i = n + tid; i < a.budget; i += threads) kept[i] = -1;
+  if (tid == 0) a.n_kept[b] = n;
+  if (n != 0 && len <= a.budget)
+    for (int i = tid; i < n; i += threads) kept[i] = i;
+  return n == 0 || len <= a.budget;
+}
+
+// One workgroup a sequence, keys in LDS.
+constexpr int kHeldKeys = 32768;
+template <int KEYS> __global__ __launch_bounds__(kSelectThreads) void select_held_kernel(const PagedSelectArgs a, const PageDivider d) {
+  __shared__ uint32_t keys[KEYS];
+  __shared__ uint32_t bins[kBins];
+  __shared__ uint32_t above[kSelectWaves], equal[kSelectWaves];
+  __shared__ Scan scan;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, len = cached(a, b);
+  if (keeps_all(a, b, len, tid, kSelectThreads)) return;
+  for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
+  __syncthreads();
+  for (int i = tid; i < len; i += kSelectThreads) {
+    const uint32_t x = token_key(a, d, b, len, i);
+    keys[i] = x;
+    atomicAdd(&bins[digit_of(x, 0)], 1u);
+  }
+  __syncthreads();
+  Known k = {0u, (uint32_t)a.budget};
+  for (int digit = 0;;) {
+    k = next_digit(k, digit, bins[kBins - 1 - 2 * tid], bins[kBins - 2 - 2 * tid], scan);
+    if (++digit == 3) break;
+    for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < len; i += kSelectThreads)
+      if (counts(keys[i], k, digit)) atomicAdd(&bins[digit_of(keys[i], digit)], 1u);
+    __syncthreads();
+  }
+  // a run of the tokens for each wave, which counts what it keeps first
+  const int each = ((len + kSelectWaves - 1) / kSelectWaves + 63) & ~63, from = min(wave * each, len), to = from + min(each, len - from);
+  uint32_t more = 0, same = 0;
+  for (int i = from + lane; i < to; i += 64) {
+    more += keys[i] > k.prefix;
+    same += keys[i] == k.prefix;
+  }
+  more = wave_sum(more);
+  same = wave_sum(same);
+  if (lane == 0) { above[wave] = more; equal[wave] = same; }
+  __syncthreads();
+  uint32_t at = 0, tie = 0;
+  for (int w = 0; w < wave; ++w) { at += above[w]; tie += equal[w]; }
+  emit(a.kept + (int64_t)b * a.budget, k, at + min(tie, k.need), tie, from, to, [&](int i) { return keys[i]; });
+}
+
+// Long sequences: a workgroup a slab of at least kSlab tokens, of which there are at most kMostSlabs, a launch a digit.  Each counts its slab's keys by the digit; the
+// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.
+constexpr int kSlab = 4096, kMostSlabs = 256;
+struct Slabs {
+  uint32_t* counts;                                        // [batch, 3, n, kBins]
+  uint32_t* above;                                         // [batch, 2, n]: keys of a slab above the last one by their first, second digit
+  Known* known;                                            // [batch, 2]: behind the first, second digit
+  int n, tokens;                                           // slabs that there is room for; tokens of each, a multiple of kSlab
+};
+// The next digit, and of the counts that it goes by: keys above it and at it, of slab `slab` (own) or of all before it.  (The thread's share: to be added up.)
+struct Found { Known k; uint32_t above, at; };
+__device__ __forceinline__ Found found(const Slabs& s, Known k, int b, int digit, int slabs, int slab, bool own, Scan& scan) {
+  uint32_t x = 0, y = 0, px = 0, py = 0;
+  const uint32_t* const from = s.counts + ((int64_t)b * 3 + digit) * s.n * kBins + kBins - 2 - 2 * threadIdx.x;
+#pragma unroll 8
+  for (int i = 0; i < slabs; ++i) {
+    const u32x2 c = *reinterpret_cast<const u32x2*>(from + (int64_t)i * kBins);
+    x += c.y;
+    y += c.x;
+    if (own ? i == slab : i < slab) { px += c.y; py += c.x; }
+  }
+  Found f;
+  f.k = next_digit(k, digit, x, y, scan);
+  const uint32_t last = digit_of(f.k.prefix << shift_of(digit), digit), bx = kBins - 1 - 2 * threadIdx.x, by = bx - 1;
+  f.above = (bx > last ? px : 0u) + (by > last ? py : 0u);
+  f.at = (bx == last ? px : 0u) + (by == last ? py : 0u);
+  return f;
+}
+template <int DIGIT> __global__ __launch_bounds__(kSelectThreads) void slab_counts_kernel(const PagedSelectArgs a, const PageDivider d, const Slabs s) {
+  __shared__ uint32_t bins[kBins];
+  __shared__ uint32_t above;
+  __shared__ Scan scan;
+  const int b = blockIdx.y, slab = blockIdx.x, tid = threadIdx.x, len = cached(a, b), slabs = (len + s.tokens - 1) / s.tokens;
+  if (slab >= slabs || len <= a.budget || a.budget == 0) return;
+  for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
+  if (tid == 0) above = 0;
+  Known k = {0u, (uint32_t)a.budget};
+  if constexpr (DIGIT > 0) {
+    if (DIGIT == 2) k = s.known[2 * b];
+    const Found f = found(s, k, b, DIGIT - 1, slabs, slab, true, scan);
+    k = f.k;
+    const uint32_t more = wave_sum(f.above);
+    if ((tid & 63) == 0) atomicAdd(&above, more);
+    if (slab == 0 && tid == 0) s.known[2 * b + DIGIT - 1] = k;
+  }
+  __syncthreads();
+  if (DIGIT > 0 && tid == 0) s.above[((int64_t)b * 2 + DIGIT - 1) * s.n + slab] = above;
+  uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
+  const int from = slab * s.tokens, to = from + min(s.tokens, len - from);
+#pragma unroll 4
+  for (int t = from + tid; t < to; t += kSelectThreads) {
+    const uint32_t x = DIGIT == 0 ? token_key(a, d, b, len, t) : keys[t];
+    if (DIGIT == 0) keys[t] = x;
+    if (counts(x, k, DIGIT)) atomicAdd(&bins[digit_of(x, DIGIT)], 1u);
+  }
+  __syncthreads();
+  uint32_t* const out = s.counts + (((int64_t)b * 3 + DIGIT) * s.n + slab) * kBins;
+  for (int i = tid; i < kBins; i += kSelectThreads) out[i] = bins[i];
+}
+__global__ __launch_bounds__(kSelectThreads) void slab_emit_kernel(const PagedSelectArgs a, const Slabs s) {
+  __shared__ Scan scan;
+  __shared__ uint32_t above[kSelectWaves], equal[kSelectWaves], before[2];
+  const int b = blockIdx.y, slab = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, len = cached(a, b), slabs = (len + s.tokens - 1) / s.tokens;
+  if (len <= a.budget || a.budget == 0) {
+    keeps_all(a, b, len, slab * kSelectThreads + tid, s.n * kSelectThreads);
+    return;
+  }
+  if (slab >= slabs) return;
+  if (slab == 0 && tid == 0) a.n_kept[b] = a.budget;
+  if (tid < 2) before[tid] = 0;
+  const Found f = found(s, s.known[2 * b + 1], b, 2, slabs, slab, false, scan);
+  const Known k = f.k;
+  __syncthreads();
+  // of the slabs before this one: keys above the last one, and those that have it
+  uint32_t more = f.above, same = f.at;
+  for (int i = tid; i < 2 * slab; i += kSelectThreads) more += s.above[((int64_t)b * 2 + (i >= slab)) * s.n + (i >= slab ? i - slab : i)];
+  more = wave_sum(more);
+  same = wave_sum(same);
+  if (lane == 0) {
+    atomicAdd(&before[0], more);
+    atomicAdd(&before[1], same);
+  }
+  const uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
+  const int each = s.tokens / kSelectWaves, from = min(slab * s.tokens + wave * each, len), to = from + min(each, len - from);
+  more = same = 0;
+  for (int i = from + lane; i < to; i += 64) {
+    const uint32_t x = keys[i];
+    more += x > k.prefix;
+    same += x == k.prefix;
+  }
+  more = wave_sum(more);
+  same = wave_sum(same);
+  if (lane == 0) { above[wave] = more; equal[wave] = same; }
+  __syncthreads();
+  uint32_t at = before[0], tie = before[1];
+  for (int w = 0; w < wave; ++w) { at += above[w]; tie += equal[w]; }
+  emit(a.kept + (int64_t)b * a.budget, k, at + min(tie, k.need), tie, from, to, [&](int i) { return keys[i]; });
+}
 
 // ---------------------------------------------------------------- keep
-// The arrays of a pool as units of 16, 8, 4 or 2 bytes: unit u of a row at row * row_bytes + u * unit, or (mass: [page][head][token]) by page, head and place.
+// The arrays of a pool as units of 16, 8, 4 or 2 bytes: a row's lie side by side, those of mass ([page][head][token]) page_tokens apart.
 struct KeepArray { uint8_t* p; int units, unit; };
-struct KeepLaunch { KeepArray arrays[5]; int n_arrays; PageDivider d; uint8_t* staged; int64_t staged_at[5]; };
-__device__ __forceinline__ uint8_t* unit_at(const KeepArray& x, bool mass, const PageDivider& d, int64_t row, int u) {
-  if (!mass) return x.p + (row * x.units + u) * x.unit;
-  const int64_t page = row / d.tokens;
-  return x.p + ((page * x.units + u) * d.tokens + (row - page * d.tokens)) * 4;
+struct KeepLaunch { KeepArray arrays[5]; int n_arrays, row_lanes; PageDivider d; uint8_t* staged; int64_t staged_at[5]; };
+__device__ __forceinline__ uint8_t* unit_at(const KeepArray& x, bool mass, const PageDivider& d, const Place& at, int u) {
+  if (!mass) return x.p + (((int64_t)at.page * d.tokens + at.in) * x.units + u) * x.unit;
+  return x.p + (((int64_t)at.page * x.units + u) * d.tokens + at.in) * 4;
 }
 __device__ __forceinline__ u32x4 load_unit(const uint8_t* p, int unit) {
   u32x4 x = {0, 0, 0, 0};
@@ -151,17 +273,18 @@ __device__ __forceinline__ void store_unit(uint8_t* p, int unit, const u32x4& x)
   else if (unit == 4) *reinterpret_cast<uint32_t*>(p) = x.x;
   else *reinterpret_cast<uint16_t*>(p) = (uint16_t)x.x;
 }
-// Rows that entry i of sequence b goes from and to, -1: nothing to move.
-struct Move { int64_t from, to; };
+// Places that entry i of sequence b goes from and to, page -1: nothing to move.
+struct Move { Place from, to; };
 __device__ __forceinline__ Move move_of(const PagedKeepArgs& a, const PageDivider& d, int b, int i) {
-  if (i >= min(a.n_kept[b], a.max_kept)) return {-1, -1};
+  const Place none = {-1, 0u};
+  if (i >= min(a.n_kept[b], a.max_kept)) return {none, none};
   const int64_t first = a.first != nullptr ? a.first[b] : 0;
-  Move m;
-  m.from = row_of_token(a.page_table + (int64_t)b * a.table_pages, a.table_pages, d, a.pool.n_pages, a.kept[(int64_t)b * a.max_kept + i]);
-  m.to = a.to_table != nullptr ? row_of_token(a.to_table + (int64_t)b * a.to_pages, a.to_pages, d, a.pool.n_pages, first + i)
-                               : row_of_token(a.page_table + (int64_t)b * a.table_pages, a.table_pages, d, a.pool.n_pages, first + i);
-  if (first < 0 || m.from == m.to) m.from = -1;
-  return m;
+  const int32_t* const table = a.page_table + (int64_t)b * a.table_pages;
+  const Place from = place_of_token(table, a.table_pages, d, a.pool.n_pages, a.kept[(int64_t)b * a.max_kept + i]);
+  const Place to = a.to_table != nullptr ? place_of_token(a.to_table + (int64_t)b * a.to_pages, a.to_pages, d, a.pool.n_pages, first + i)
+                                         : place_of_token(table, a.table_pages, d, a.pool.n_pages, first + i);
+  if (first < 0 || from.page < 0 || to.page < 0 || (from.page == to.page && from.in == to.in)) return {none, none};
+  return {from, to};
 }
 
 // A workgroup has a column of units of one array and takes it through all entries of a sequence: all reads, then all writes, so that the rows may be
@@ -179,36 +302,60 @@ __global__ __launch_bounds__(kMoveThreads) void keep_columns_kernel(const PagedK
   const int per_pass = blockDim.x / lanes, row = threadIdx.x / lanes, u = column * lanes + threadIdx.x % lanes;
   const bool there = row < per_pass && u < x.units;
   u32x4 v[UNITS];
-  int64_t to[UNITS];
+  Place to[UNITS];
 #pragma unroll
   for (int k = 0; k < UNITS; ++k) {
-    const Move m = there ? move_of(a, l.d, b, k * per_pass + row) : Move{-1, -1};
-    to[k] = m.from < 0 ? -1 : m.to;
-    if (to[k] >= 0) v[k] = load_unit(unit_at(x, mass, l.d, m.from, u), x.unit);
+    Move m = {{-1, 0u}, {-1, 0u}};
+    if (there) m = move_of(a, l.d, b, k * per_pass + row);
+    to[k] = m.to;
+    if (m.from.page >= 0) v[k] = load_unit(unit_at(x, mass, l.d, m.from, u), x.unit);
   }
   __builtin_amdgcn_s_waitcnt(0);                           // (every read has come back)
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < UNITS; ++k)
-    if (to[k] >= 0) store_unit(unit_at(x, mass, l.d, to[k], u), x.unit, v[k]);
+    if (to[k].page >= 0) store_unit(unit_at(x, mass, l.d, to[k], u), x.unit, v[k]);
 }
 
-// A thread takes a unit of an entry's row: from pages to other pages, to the workspace, or back from it.  blockIdx = (block of units, array, sequence).
+// 64 entries a workgroup, whose places are worked out first: from pages to other pages, to the workspace, or back from it.  blockIdx = (entries, sequence).
 enum KeepWay : int { kAcross = 0, kOut = 1, kBack = 2 };
-template <int WAY>
-__global__ __launch_bounds__(256) void keep_rows_kernel(const PagedKeepArgs a, const KeepLaunch l) {
-  const int b = blockIdx.z, n = blockIdx.y;
-  const bool mass = n == 4;
-  const KeepArray x = l.arrays[n];
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int i = (int)(mass ? id % a.max_kept : id / x.units), u = (int)(mass ? id / a.max_kept : id - (int64_t)i * x.units);
-  if (i >= a.max_kept || u >= x.units) return;
-  const Move m = move_of(a, l.d, b, i);
-  if (m.from < 0 || m.to < 0) return;
-  uint8_t* const staged = l.staged + l.staged_at[n] + ((int64_t)b * a.max_kept * x.units + id) * x.unit;
-  const uint8_t* const from = WAY == kBack ? staged : unit_at(x, mass, l.d, m.from, u);
-  uint8_t* const to = WAY == kOut ? staged : unit_at(x, mass, l.d, m.to, u);
-  store_unit(to, x.unit, load_unit(from, x.unit));
+constexpr int kRowsEach = 64, kAhead = 8;
+template <int WAY> __global__ __launch_bounds__(256) void keep_rows_kernel(const PagedKeepArgs a, const KeepLaunch l) {
+  __shared__ Move moves[kRowsEach];
+  const int b = blockIdx.y, e0 = blockIdx.x * kRowsEach, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (threadIdx.x < kRowsEach) moves[threadIdx.x] = move_of(a, l.d, b, e0 + threadIdx.x);
+  __syncthreads();
+  const auto staged = [&](int n, int e, int u) { return l.staged + l.staged_at[n] + (((int64_t)b * a.max_kept + e0 + e) * l.arrays[n].units + u) * l.arrays[n].unit; };
+  // codes, units of 16 bytes: l.row_lanes lanes a row (keys, then values), kAhead rows of each in flight
+  const int rows = 64 / l.row_lanes, each = l.arrays[0].units;
+  for (int u = lane & (l.row_lanes - 1); u < 2 * each; u += l.row_lanes) {
+    const bool values = u >= each;
+    const KeepArray x = {values ? l.arrays[2].p : l.arrays[0].p, each, 16};
+    const int at = values ? u - each : u, n = values ? 2 : 0;
+    for (int base = wave * rows + lane / l.row_lanes; base < kRowsEach; base += 4 * rows * kAhead) {
+      u32x4 v[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int e = base + 4 * rows * k;
+        if (e < kRowsEach && moves[e].from.page >= 0) v[k] = *reinterpret_cast<const u32x4*>(WAY == kBack ? staged(n, e, at) : unit_at(x, false, l.d, moves[e].from, at));
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int e = base + 4 * rows * k;
+        if (e < kRowsEach && moves[e].from.page >= 0) *reinterpret_cast<u32x4*>(WAY == kOut ? staged(n, e, at) : unit_at(x, false, l.d, moves[e].to, at)) = v[k];
+      }
+    }
+  }
+  for (int n = 1; n < l.n_arrays; n += n == 3 ? 1 : 2) {   // scales, mass
+    const bool mass = n == 4;
+    const KeepArray x = l.arrays[n];
+    for (int i = threadIdx.x; i < kRowsEach * x.units; i += 256) {
+      const int e = i % kRowsEach, u = i / kRowsEach;
+      if (moves[e].from.page < 0) continue;
+      store_unit(WAY == kOut ? staged(n, e, u) : unit_at(x, mass, l.d, moves[e].to, u), x.unit,
+                 load_unit(WAY == kBack ? staged(n, e, u) : unit_at(x, mass, l.d, moves[e].from, u), x.unit));
+    }
+  }
 }
 
 int unit_of(int64_t bytes) { return bytes % 16 == 0 ? 16 : bytes % 8 == 0 ? 8 : bytes % 4 == 0 ? 4 : 2; }
@@ -219,6 +366,7 @@ KeepLaunch keep_launch(const PagedKeepArgs& a) {
   for (int i = 0; i < 4; ++i) l.arrays[i] = {p[i], (int)(bytes[i] / unit_of(bytes[i])), unit_of(bytes[i])};
   l.arrays[4] = {reinterpret_cast<uint8_t*>(a.mass), a.H, 4};
   l.n_arrays = a.mass != nullptr ? 5 : 4;
+  for (l.row_lanes = 1; l.row_lanes < 64 && l.row_lanes < 2 * l.arrays[0].units; l.row_lanes *= 2) {}
   l.d = divider(a.pool.page_tokens);
   return l;
 }
@@ -227,13 +375,40 @@ constexpr int kMostHeld = kMoveThreads * kMoveUnits;
 
 }  // namespace
 
-size_t paged_select_workspace_bytes(int64_t batch, int64_t table_pages, int64_t page_tokens) { return (size_t)(batch * table_pages * page_tokens) * sizeof(uint32_t); }
+namespace {
+// One workgroup a sequence where its keys fit into LDS, otherwise slabs.
+bool keys_held(int64_t room) { return room <= kHeldKeys; }
+int64_t slab_tokens(int64_t room) { return ((room + kMostSlabs - 1) / kMostSlabs + kSlab - 1) / kSlab * kSlab; }
+int64_t slabs_of(int64_t room) { return (room + slab_tokens(room) - 1) / slab_tokens(room); }
+}  // namespace
 
-hipError_t launch_paged_select(const PagedSelectArgs& a, hipStream_t stream) {
+size_t paged_select_workspace_bytes(int64_t batch, int64_t table_pages, int64_t page_tokens) {
+  const int64_t room = table_pages * page_tokens;
+  return keys_held(room) ? 0 : (size_t)(batch * slabs_of(room)) * (slab_tokens(room) + 3 * kBins + 2) * sizeof(uint32_t) + (size_t)batch * 2 * sizeof(Known);
+}
+
+hipError_t launch_paged_select(const PagedSelectArgs& a, void* workspace, hipStream_t stream) {
+  PagedSelectArgs args = a;
   const int64_t room = (int64_t)a.table_pages * a.page_tokens;
-  mass_keys_kernel<<<dim3((unsigned)((room + 255) / 256), (unsigned)a.batch), 256, 0, stream>>>(a, divider(a.page_tokens));
-  if (const hipError_t e = hipGetLastError()) return e;
-  select_kernel<<<(unsigned)a.batch, kSelectThreads, 0, stream>>>(a);
+  const PageDivider d = divider(a.page_tokens);
+  if (keys_held(room)) {
+    if (room <= 8192) select_held_kernel<8192><<<(unsigned)a.batch, kSelectThreads, 0, stream>>>(args, d);
+    else select_held_kernel<kHeldKeys><<<(unsigned)a.batch, kSelectThreads, 0, stream>>>(args, d);
+    return hipGetLastError();
+  }
+  const int64_t n = slabs_of(room);
+  args.keys = static_cast<uint32_t*>(workspace);
+  Slabs s = {};
+  s.n = (int)n;
+  s.tokens = (int)slab_tokens(room);
+  s.counts = args.keys + a.batch * n * s.tokens;
+  s.known = reinterpret_cast<Known*>(s.counts + a.batch * 3 * n * kBins);
+  s.above = reinterpret_cast<uint32_t*>(s.known + 2 * a.batch);
+  const dim3 grid((unsigned)n, (unsigned)a.batch);
+  slab_counts_kernel<0><<<grid, kSelectThreads, 0, stream>>>(args, d, s);
+  slab_counts_kernel<1><<<grid, kSelectThreads, 0, stream>>>(args, d, s);
+  slab_counts_kernel<2><<<grid, kSelectThreads, 0, stream>>>(args, d, s);
+  slab_emit_kernel<<<grid, kSelectThreads, 0, stream>>>(args, s);
   return hipGetLastError();
 }
 
@@ -269,14 +444,13 @@ hipError_t launch_paged_keep(const PagedKeepArgs& a, void* workspace, hipStream_
     else keep_columns_kernel<8><<<grid, threads, 0, stream>>>(a, l, cols);
     return hipGetLastError();
   }
-  int64_t most = 0, at = 0;
+  int64_t at = 0;
   l.staged = static_cast<uint8_t*>(workspace);
   for (int i = 0; i < l.n_arrays; ++i) {
-    most = std::max<int64_t>(most, (int64_t)a.max_kept * l.arrays[i].units);
     l.staged_at[i] = at;
     at += ((int64_t)a.batch * a.max_kept * l.arrays[i].units * l.arrays[i].unit + 255) & ~(int64_t)255;
   }
-  const dim3 grid((unsigned)((most + 255) / 256), (unsigned)l.n_arrays, (unsigned)a.batch);
+  const dim3 grid((unsigned)((a.max_kept + kRowsEach - 1) / kRowsEach), (unsigned)a.batch);
   if (a.to_table != nullptr) {
     keep_rows_kernel<kAcross><<<grid, 256, 0, stream>>>(a, l);
     return hipGetLastError();
