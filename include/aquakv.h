@@ -563,10 +563,10 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  * aquakv_paged_keep -- token kept[b, i] of sequence b becomes its token first[b] + i (first NULL: i), i < n_kept[b] (at most max_kept): codes, scales and, if
  *   given, mass.  kept [batch, max_kept], n_kept, first [batch]: device int32, aligned to 4 bytes.  So an eviction is select and keep, and drafts that were
  *   accepted are kept with first = the tokens ahead of the drafts; the caller's sequence then has first[b] + n_kept[b] tokens.  to_table NULL: in the
- *   pages that page_table names; all rows of a sequence are read before any is written, so entries may be in any order and may repeat.  Else to
- *   pages that to_table [batch, to_pages] names, which may not be ones that the call reads.  What goes from or to a token outside its table
- *   or a page that is not in the pool is left out.  Two entries, or two sequences, that name the same row to write to leave anything there; no sequence may read
- *   rows that the call writes for another one.  Keys keep the rotation that they have.
+ *   pages that page_table names, entries of a sequence ascending and from first[b] on (a sequence moves together; its table names no page twice).  Else to
+ *   pages that to_table [batch, to_pages] names, which may not be ones that the call reads; entries in any order, some more than once.  What goes from or to a
+ *   token outside its table or a page that is not in the pool is left out.  Rows that are written against this, or for two entries or sequences, hold
+ *   anything afterwards, and so does what is read from such rows.  Keys keep the rotation that they have.
  *   workspace: aquakv_paged_keep_workspace_bytes() bytes for the same layer, pages and sizes (with_mass: 0, or 1 where mass is given).
  *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens

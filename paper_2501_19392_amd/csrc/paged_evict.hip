@@ -268,10 +268,15 @@ __device__ __forceinline__ u32x4 load_unit(const uint8_t* p, int unit) {
   return x;
 }
 __device__ __forceinline__ void store_unit(uint8_t* p, int unit, const u32x4& x) {
-  if (unit == 16) *reinterpret_cast<u32x4*>(p) = x;
+  if (unit == 16) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
   else if (unit == 8) *reinterpret_cast<u32x2*>(p) = u32x2{x.x, x.y};
   else if (unit == 4) *reinterpret_cast<uint32_t*>(p) = x.x;
   else *reinterpret_cast<uint16_t*>(p) = (uint16_t)x.x;
+}
+__device__ __forceinline__ Place place_of_row(const PageDivider& d, int row) {
+  uint32_t page = (uint32_t)(((uint64_t)(uint32_t)row * d.magic) >> 32);
+  if (row - page * d.tokens >= d.tokens) ++page;
+  return {(int)page, row - page * d.tokens};
 }
 // Places that entry i of sequence b goes from and to, page -1: nothing to move.
 struct Move { Place from, to; };
@@ -287,39 +292,67 @@ __device__ __forceinline__ Move move_of(const PagedKeepArgs& a, const PageDivide
   return {from, to};
 }
 
-// A workgroup has a column of units of one array and takes it through all entries of a sequence: all reads, then all writes, so that the rows may be
-// the same ones in any order.  blockIdx = (array and column, sequence); LANES threads a row.
-constexpr int kMoveThreads = 1024, kMoveUnits = 8;
-struct Columns { int first[6], lanes; };                   // blockIdx.x from which an array's columns go
-template <int UNITS>
-__global__ __launch_bounds__(kMoveThreads) void keep_columns_kernel(const PagedKeepArgs a, const KeepLaunch l, const Columns cols) {
+// In place: a workgroup takes a column of up to 128 bytes of one array's rows through the entries of a sequence, a round of them after the other.  As entries ascend, none
+// of the rows that a round writes is read later, so that two rounds more are on their way meanwhile; within a round all reads come back before anything is
+// written.  blockIdx = (array and column, sequence).
+constexpr int kMoveThreads = 1024, kMoveUnits = 4, kMoveLanes = 8, kMoveChunk = 4096;
+struct Columns { int first[6]; };                          // blockIdx.x from which an array's columns go
+template <int UNITS, int CHUNK>
+__global__ __launch_bounds__(kMoveThreads) void keep_in_place_kernel(const PagedKeepArgs a, const KeepLaunch l, const Columns cols) {
+  __shared__ int2 rows[CHUNK];                             // that a chunk's entries go from and to, -1: nothing to move
   const int b = blockIdx.y;
   int n = 0;
   while (n + 1 < l.n_arrays && (int)blockIdx.x >= cols.first[n + 1]) ++n;
   const bool mass = n == 4;
   const KeepArray x = l.arrays[n];
-  const int lanes = mass ? 1 : min(cols.lanes, x.units), column = blockIdx.x - cols.first[n];
-  const int per_pass = blockDim.x / lanes, row = threadIdx.x / lanes, u = column * lanes + threadIdx.x % lanes;
+  const int lanes = mass ? 1 : min(kMoveLanes, x.units), column = blockIdx.x - cols.first[n];
+  const int per_pass = blockDim.x / lanes, row = threadIdx.x / lanes, u = column * lanes + threadIdx.x % lanes, round = per_pass * UNITS;
   const bool there = row < per_pass && u < x.units;
-  u32x4 v[UNITS];
-  Place to[UNITS];
+  const int count = min(a.n_kept[b], a.max_kept);
+  const auto at = [&](int row) { return mass ? unit_at(x, true, l.d, place_of_row(l.d, row), u) : x.p + ((int64_t)row * x.units + u) * x.unit; };
+  struct Set { u32x4 v[UNITS]; };
+  for (int c0 = 0; c0 < count; c0 += CHUNK) {
+    const int entries = min(CHUNK, count - c0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) {
+      const Move m = move_of(a, l.d, b, c0 + i);
+      rows[i] = m.from.page < 0 ? int2{-1, -1} : int2{(int)(m.from.page * l.d.tokens + m.from.in), (int)(m.to.page * l.d.tokens + m.to.in)};
+    }
+    __syncthreads();
+    const auto request = [&](Set& set, int i0) {
 #pragma unroll
-  for (int k = 0; k < UNITS; ++k) {
-    Move m = {{-1, 0u}, {-1, 0u}};
-    if (there) m = move_of(a, l.d, b, k * per_pass + row);
-    to[k] = m.to;
-    if (m.from.page >= 0) v[k] = load_unit(unit_at(x, mass, l.d, m.from, u), x.unit);
+      for (int k = 0; k < UNITS; ++k) {
+        const int i = i0 + k * per_pass + row;
+        const int from = there && i < entries ? rows[i].x : -1;
+        if (from >= 0) set.v[k] = load_unit(at(from), x.unit);
+      }
+    };
+    const auto finish = [&](Set& set, int i0, Set& next) { // a round is written, the one two behind it requested
+#pragma unroll
+      for (int k = 0; k < UNITS; ++k) asm volatile("" : "+v"(set.v[k].x), "+v"(set.v[k].y), "+v"(set.v[k].z), "+v"(set.v[k].w));      // (its reads have come back)
+      __syncthreads();
+      request(next, i0 + 2 * round);
+#pragma unroll
+      for (int k = 0; k < UNITS; ++k) {
+        const int i = i0 + k * per_pass + row;
+        const int to = there && i < entries ? rows[i].y : -1;
+        if (to >= 0) store_unit(at(to), x.unit, set.v[k]);
+      }
+    };
+    Set s0 = {}, s1 = {}, s2 = {};
+    request(s0, 0);
+    request(s1, round);
+    for (int i0 = 0; i0 < entries; i0 += 3 * round) {
+      finish(s0, i0, s2);
+      finish(s1, i0 + round, s0);
+      finish(s2, i0 + 2 * round, s1);
+    }
   }
-  __builtin_amdgcn_s_waitcnt(0);                           // (every read has come back)
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < UNITS; ++k)
-    if (to[k].page >= 0) store_unit(unit_at(x, mass, l.d, to[k], u), x.unit, v[k]);
 }
 
 // 64 entries a workgroup, whose places are worked out first: from pages to other pages, to the workspace, or back from it.  blockIdx = (entries, sequence).
 enum KeepWay : int { kAcross = 0, kOut = 1, kBack = 2 };
-constexpr int kRowsEach = 64, kAhead = 8;
+constexpr int kRowsEach = 32, kAhead = 8;
 template <int WAY> __global__ __launch_bounds__(256) void keep_rows_kernel(const PagedKeepArgs a, const KeepLaunch l) {
   __shared__ Move moves[kRowsEach];
   const int b = blockIdx.y, e0 = blockIdx.x * kRowsEach, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -342,7 +375,10 @@ template <int WAY> __global__ __launch_bounds__(256) void keep_rows_kernel(const
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const int e = base + 4 * rows * k;
-        if (e < kRowsEach && moves[e].from.page >= 0) *reinterpret_cast<u32x4*>(WAY == kOut ? staged(n, e, at) : unit_at(x, false, l.d, moves[e].to, at)) = v[k];
+        if (e < kRowsEach && moves[e].from.page >= 0) {
+          if (WAY == kOut) *reinterpret_cast<u32x4*>(staged(n, e, at)) = v[k];
+          else store_unit(unit_at(x, false, l.d, moves[e].to, at), 16, v[k]);
+        }
       }
     }
   }
@@ -370,8 +406,9 @@ KeepLaunch keep_launch(const PagedKeepArgs& a) {
   l.d = divider(a.pool.page_tokens);
   return l;
 }
-// Rows in place whose column a workgroup can hold.
-constexpr int kMostHeld = kMoveThreads * kMoveUnits;
+// In place through the workspace, in two launches: few sequences of many entries, whose columns are too few workgroups (1 x 3800 entries: 17.4 us, by columns 26; 1 x 20 000:
+// 26.6, 147; 8 x 7900, 64 columns: 62, 65; 32 x 3800: 113, 81; 1 x 900: 16.0, 10.5).
+bool through_workspace(int64_t batch, int64_t max_kept, int64_t code_row) { return max_kept > 1024 && batch * 2 * ((code_row + 127) / 128) < 64; }
 
 }  // namespace
 
@@ -413,7 +450,7 @@ hipError_t launch_paged_select(const PagedSelectArgs& a, void* workspace, hipStr
 }
 
 size_t paged_keep_workspace_bytes(int64_t batch, int64_t max_kept, int64_t code_row, int64_t scale_row, int64_t H, bool mass) {
-  if (max_kept <= kMostHeld) return 0;
+  if (!through_workspace(batch, max_kept, code_row)) return 0;
   size_t n = 0;
   const int64_t bytes[5] = {code_row, scale_row, code_row, scale_row, mass ? 4 * H : 0};
   for (const int64_t x : bytes) n += ((size_t)(batch * max_kept * x) + 255) & ~(size_t)255;
@@ -422,26 +459,21 @@ size_t paged_keep_workspace_bytes(int64_t batch, int64_t max_kept, int64_t code_
 
 hipError_t launch_paged_keep(const PagedKeepArgs& a, void* workspace, hipStream_t stream) {
   KeepLaunch l = keep_launch(a);
-  if (a.to_table == nullptr && a.max_kept <= kMostHeld) {
+  if (a.to_table == nullptr && !through_workspace(a.batch, a.max_kept, a.code_row)) {
     Columns cols = {};
-    cols.lanes = std::min(8, kMostHeld / a.max_kept);
-    cols.lanes = cols.lanes >= 8 ? 8 : cols.lanes >= 4 ? 4 : cols.lanes >= 2 ? 2 : 1;
     int most = 1, at = 0;
     for (int i = 0; i < l.n_arrays; ++i) {
-      const int lanes = i == 4 ? 1 : std::min(cols.lanes, l.arrays[i].units);
+      const int lanes = i == 4 ? 1 : std::min(kMoveLanes, l.arrays[i].units);
       cols.first[i] = at;
       at += (l.arrays[i].units + lanes - 1) / lanes;
       most = std::max(most, lanes);
     }
     cols.first[l.n_arrays] = at;
-    // threads for all entries at once, up to a workgroup's; what is more goes into registers
-    const int threads = std::min<int64_t>(((int64_t)a.max_kept * most + 63) / 64 * 64, kMoveThreads);
-    const int units = (a.max_kept + threads / most - 1) / (threads / most);
+    // threads for all entries at once, up to a workgroup's
+    const int threads = (int)std::min<int64_t>(((int64_t)a.max_kept * most + 63) / 64 * 64, kMoveThreads);
     const dim3 grid((unsigned)at, (unsigned)a.batch);
-    if (units <= 1) keep_columns_kernel<1><<<grid, threads, 0, stream>>>(a, l, cols);
-    else if (units <= 2) keep_columns_kernel<2><<<grid, threads, 0, stream>>>(a, l, cols);
-    else if (units <= 4) keep_columns_kernel<4><<<grid, threads, 0, stream>>>(a, l, cols);
-    else keep_columns_kernel<8><<<grid, threads, 0, stream>>>(a, l, cols);
+    if (threads < kMoveThreads) keep_in_place_kernel<1, kMoveThreads><<<grid, threads, 0, stream>>>(a, l, cols);
+    else keep_in_place_kernel<kMoveUnits, kMoveChunk><<<grid, threads, 0, stream>>>(a, l, cols);
     return hipGetLastError();
   }
   int64_t at = 0;

@@ -119,12 +119,15 @@ def kept_by_hand(pool, mass, page, n_pages, table, kept, n_kept, first, to_table
 
 
 @pytest.mark.parametrize("fmt,H,page,lengths,most,way,with_first,with_mass", [
-    ("grid256", 8, 64, [300, 77], 60, "ascending", False, True), ("grid64", 3, 24, [500, 40, 9], 33, "any", True, False),
-    ("grid16", 1, 8, [1500], 1024, "ascending", False, True), ("grid256", 1, 16, [1500, 3], 1025, "any", False, True),
-    ("rtn4", 8, 32, [2600], 2500, "any", True, True), ("rtn2", 5, 16, [5100, 900], 5000, "ascending", False, False),
-    ("grid256", 2, 128, [8300], 8192, "any", False, True), ("grid64", 1, 40, [9100, 50], 9000, "ascending", False, True),
-    ("rtn4", 3, 8, [9500], 9001, "any", True, True), ("grid16", 7, 16, [64], 1, "any", True, True), ("grid256", 12, 8, [200, 100], 90, "across", False, True),
-    ("rtn2", 2, 24, [700, 60], 600, "across", True, False), ("grid64", 8, 16, [400], 128, "across", True, True)])
+    ("grid256", 8, 64, [300, 77], 60, "ascending", False, True), ("grid64", 3, 24, [500, 40, 9], 33, "gaps", True, False),
+    ("grid16", 1, 8, [1500], 1024, "ascending", False, True), ("grid256", 1, 16, [1500, 3], 1025, "gaps", False, True),
+    ("rtn4", 8, 32, [2600], 2500, "gaps", True, True), ("rtn2", 5, 16, [5100, 900], 5000, "ascending", False, False),
+    ("grid256", 2, 128, [8300], 8192, "gaps", False, True), ("grid64", 1, 40, [9100, 50], 9000, "ascending", False, True),
+    ("rtn4", 3, 8, [9500], 9001, "gaps", True, True), ("grid16", 7, 16, [64], 1, "gaps", True, True),
+    ("grid256", 33, 8, [1400, 900], 1200, "ascending", True, True), ("rtn4", 33, 16, [4500], 4300, "gaps", False, True),      # columns of more entries than a round
+    ("grid64", 32, 8, [9000], 8700, "ascending", False, True), ("grid16", 64, 24, [1300], 1025, "gaps", False, False),         # ... than a chunk
+    ("grid256", 12, 8, [200, 100], 90, "across", False, True), ("rtn2", 2, 24, [700, 60], 600, "across", True, False), ("grid64", 8, 16, [400], 128, "across", True, True),
+    ("grid16", 1, 16, [400, 7], 300, "across", False, True), ("rtn4", 5, 32, [90], 33, "across", True, True)])
 def test_rows_that_are_kept(fmt, H, page, lengths, most, way, with_first, with_mass):
     from paper_2501_19392_amd import binding as B
     print(f"case keep {fmt} H={H} page={page} {lengths} most={most} {way}", flush=True)
@@ -136,15 +139,15 @@ def test_rows_that_are_kept(fmt, H, page, lengths, most, way, with_first, with_m
     n_kept, first = torch.zeros(b, dtype=torch.int32), torch.zeros(b, dtype=torch.int32)
     for i, n in enumerate(lengths):
         m = min(most, n)
-        if way == "any":                                                    # any order, some twice, some that are not there
+        first[i] = 5 if with_first and n > 64 and m + 5 <= n else 0
+        if way == "across":                                                 # any order, some twice
             kept[i, :m] = torch.randint(0, n, (m,), generator=gen).to(torch.int32)
-            if m > 4:
-                kept[i, 2], kept[i, 3], kept[i, 4] = -1, 1 << 30, -(1 << 31)
         else:
-            kept[i, :m] = torch.randperm(n, generator=gen)[:m].sort().values.to(torch.int32)
+            kept[i, :m] = int(first[i]) + torch.randperm(n - int(first[i]), generator=gen)[:m].sort().values.to(torch.int32)
+        if way != "ascending" and m > 4:                                    # some that are not there
+            kept[i, 2], kept[i, 3], kept[i, 4] = -1, 1 << 30, -(1 << 31)
         n_kept[i] = m if i == 0 else m - m // 3
-        first[i] = 5 if i == 0 and n > 64 else 0
-    if way == "any" and table.shape[1] > 4:
+    if way == "gaps" and table.shape[1] > 4:
         table[0, 3] = -1
     to = None
     if way == "across":
@@ -200,7 +203,7 @@ def test_rows_behind_4_gib(way):
         part = torch.randint(0, 256, (len(rows), *x.shape[1:], x.element_size()), generator=gen, dtype=torch.int32).to(torch.uint8).contiguous().view(x.dtype)
         src[k] = part.view(len(rows), *x.shape[1:])
         x[rows.cuda()] = src[k].cuda()
-    m = 9000 if way == "staged" else 4000
+    m = 4000 if way == "staged" else 1000 if way == "in place" else 4000
     kept = torch.randperm(len(rows), generator=gen)[:m].sort().values.to(torch.int32)[None]
     ws = torch.empty(B.aquakv_paged_keep_workspace_bytes(lg, pages, 1, m, False), dtype=torch.uint8, device="cuda")
     B.aquakv_paged_keep(lg, pages, 1, table.cuda(), kept.cuda(), torch.tensor([m], dtype=torch.int32).cuda(), None, None if to is None else to.cuda(), None, ws)
