@@ -1802,7 +1802,7 @@ size_t aquakv_paged_weights_workspace_bytes(const aquakv_layer* L, const aquakv_
   aquakv::PagedAttendArgs a = {};
   a.pool = pool_of(pages);
   a.batch = batch; a.table_pages = table_pages; a.max_queries = max_queries; a.q_heads = q_heads; a.H = L->kv_heads;
-  return aquakv::paged_weights_workspace_bytes(L->dtype, quantizer_id(L), a) + 256;
+  return aquakv::paged_weights_workspace_bytes(quantizer_id(L), a) + 256;
 }
 
 int aquakv_paged_weights(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,

@@ -259,10 +259,8 @@ template <int NCW, int TERMS> struct Codes {
     if constexpr (!kRtn) __builtin_memcpy(&p, codebook + 2 * kPoints * (lane & (NCW / kPoints - 1)), sizeof(p));
     return p;
   }
-  // -> exponent e of the grid: it is held times 2^-e.  Wave `wave` of WAVES writes its share of every point's row; lanes start at different
-  // places of their rows, so that their banks differ.
-  template <int WAVES> static __device__ __forceinline__ int stage(const Points& p, unsigned char* lds, int lane, int wave) {
-    if constexpr (kRtn) return 0;
+  // The grid's exponent e, so that it is held times 2^-e.
+  static __device__ __forceinline__ int exponent(const Points& p) {
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < 2 * kPoints; ++i) top = fmaxf(top, fabsf(p.x[i]));
@@ -271,7 +269,13 @@ template <int NCW, int TERMS> struct Codes {
     top = fmaxf(top, octet_mirror(top));
     top = fmaxf(top, quad_xor<1>(top));
     top = fmaxf(top, quad_xor<2>(top));
-    const int e = max(uniform(__builtin_amdgcn_frexp_expf(top)), -100);
+    return max(uniform(__builtin_amdgcn_frexp_expf(top)), -100);
+  }
+  // -> exponent e of the grid.  Wave `wave` of WAVES writes its share of every point's row; lanes start at different
+  // places of their rows, so that their banks differ.
+  template <int WAVES> static __device__ __forceinline__ int stage(const Points& p, unsigned char* lds, int lane, int wave) {
+    if constexpr (kRtn) return 0;
+    const int e = exponent(p);
     constexpr int kLanes = NCW / kPoints;                  // lanes that hold different points
     constexpr int kChunks = 16 * kLanes / 64;              // 16-byte pieces of its points' rows that a lane of the workgroup writes, over the waves
 #pragma unroll

@@ -295,7 +295,7 @@ __device__ __forceinline__ Move move_of(const PagedKeepArgs& a, const PageDivide
 // In place: a workgroup takes a column of up to 128 bytes of one array's rows through the entries of a sequence, a round of them after the other.  As entries ascend, none
 // of the rows that a round writes is read later, so that two rounds more are on their way meanwhile; within a round all reads come back before anything is
 // written.  blockIdx = (array and column, sequence).
-constexpr int kMoveThreads = 1024, kMoveUnits = 4, kMoveLanes = 8, kMoveChunk = 4096;
+constexpr int kMoveThreads = 1024, kMoveUnits = 2, kMoveLanes = 8, kMoveChunk = 4096;
 struct Columns { int first[6]; };                          // blockIdx.x from which an array's columns go
 template <int UNITS, int CHUNK>
 __global__ __launch_bounds__(kMoveThreads) void keep_in_place_kernel(const PagedKeepArgs a, const KeepLaunch l, const Columns cols) {

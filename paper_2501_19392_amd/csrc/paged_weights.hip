@@ -11,28 +11,60 @@ namespace {
 using namespace paged;
 
 constexpr int kFewRows = 8;                                // of a kv head, whose scores are kept (else they are taken again)
-constexpr int kMassWaves = 4, kMassTokens = kTile * kMassWaves;      // of a workgroup that takes many rows
+constexpr int kMassWaves = 4, kStaged = 2, kMassTokens = kTile * kMassWaves;      // of a workgroup that takes many rows
 
 struct WeightsArgs {
   float* scores;                                           // few rows: [batch, H, rows, room], powers of two
-  f32x2* stats;                                            // [items, H, rows]: reference, sum
-  int2* heads;                                             // [batch]: first item, items
-  u32x4* packed;                                           // many rows: [batch, H, row tiles, term, piece, lane] operands of 16 rows
-  struct Row { float f, qsum0, qsum1, ref, inv, pad[3]; }* rows;      // [batch, H, row tiles, 16]
+  f32x2* stats;                                            // few rows: [items, H, rows], many: [batch, H, row tiles, token tiles, 16]: reference, sum
+  int2* heads;                                             // few rows: [batch]: first item, items
+  struct Row { float f, qsum0, qsum1, none; float ref, inv, pad[2]; };
+  struct Packed { u32x4 q[2][4][64]; Row rows[16]; };      // operands of 16 rows [term][piece][lane], and the rows' numbers
+  Packed* packed;                                          // many rows: [batch, H, row tiles]
   float* mass;
   float keep;
   int row_cap, tiles, room;                                // max_queries * (q_heads / H); row tiles; table_pages * page_tokens
 };
 
-// Scores and statistics of COLS columns of 16 rows: one wave a piece of one kv head, as in paged_rows.h.
-template <typename T, int NCW, int COLS> struct ScoreShape {
-  static constexpr int kWaves = is_rtn(NCW) ? 4 : 8, kPerSimd = COLS == 2 ? 3 : 4;
+// A row's query as operands: rotated, a power of two that brings it to fp16's range taken off.  f: what a product times the token's scale is to be multiplied by.
+template <typename T, int NCW> __device__ __forceinline__ void query_operands(const PagedAttendArgs& a, const typename Codes<NCW, 2>::template Query<T>& asked, int c_exp,
+                                                                              int lane, f16x8 (&q)[2][4], float (&qsum)[2], float& f) {
+  typedef Codes<NCW, 2> C;
+  constexpr bool kRtn = is_rtn(NCW);
+  float v[32];
+  C::template rotate_query<T>(asked, lane, v);
+  const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
+  float top = 0.f;
+#pragma unroll
+  for (int r = 0; r < 32; ++r) top = fmaxf(top, fabsf(v[r]));
+  const int e = max(__builtin_amdgcn_frexp_expf(column_max(top) * fabsf(by)), -100);
+  f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? C::kFieldExp : c_exp), 126));
+  const float scaled = __builtin_ldexpf(by, kQueryExp - e);
+#pragma unroll
+  for (int r = 0; r < 32; ++r) v[r] *= scaled;
+  C::pack_query(v, q, qsum);
+}
+
+// Uniform codes of piece j of the coordinates as an operand (as in Codes::scores).
+template <typename C> __device__ __forceinline__ f16x8 code_operand(const uint32_t (&x)[4], int j) {
+  const uint32_t d = C::kFields == 2 ? x[j] : (j & 1) ? x[j >> 1] >> 8 : x[j >> 1];
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = C::kFields == 2 ? C::field((i & 2) ? d >> 8 : d, i & 1) : C::field(d, i);
+  return operand(y[0], y[1], y[2], y[3]);
+}
+
+// Few rows: scores and statistics, one wave a piece of one kv head, as in paged_rows.h, but that a row has two columns: m its query's first terms, m + 8 the second
+// ones.  A product with a key's operands then gives what both are to be added up from, and the two lanes share the eight tokens of their columns: 16 products a tile for 32.
+// A look-up in a grid reads both terms of a point with one instruction (8 bytes a lane, all banks) and leaves them side by side in the operand, {point 0, its rest, point 1,
+// its rest}: the query's pairs of coordinates are there twice instead.
+template <int NCW> struct ScoreShape {
+  static constexpr int kWaves = is_rtn(NCW) ? 4 : 8, kPerSimd = 4;
   static constexpr int kThreads = 64 * kWaves, kSlots = 256 * 4 * kPerSimd;
 };
-template <typename T, int NCW, int COLS, bool FAR>
-__global__ __launch_bounds__((ScoreShape<T, NCW, COLS>::kThreads)) __attribute__((amdgpu_waves_per_eu((ScoreShape<T, NCW, COLS>::kPerSimd)))) void
+template <typename T, int NCW, bool FAR>
+__global__ __launch_bounds__((ScoreShape<NCW>::kThreads)) __attribute__((amdgpu_waves_per_eu((ScoreShape<NCW>::kPerSimd)))) void
 weights_scores_kernel(const PagedAttendArgs a, const WeightsArgs x) {
-  constexpr int kWaves = ScoreShape<T, NCW, COLS>::kWaves, kRows = 16 * COLS;
+  constexpr int kWaves = ScoreShape<NCW>::kWaves;
   constexpr bool kRtn = is_rtn(NCW);
   typedef Codes<NCW, 2> C;
   __shared__ __align__(256) unsigned char lds[(kRtn ? 16 : C::kTableBytes) + kWaves * C::kScaleBytes];
@@ -46,105 +78,127 @@ weights_scores_kernel(const PagedAttendArgs a, const WeightsArgs x) {
   if ((int)(blockIdx.x * kWaves / a.H) >= share.items) return;
   const int b = max(share.b, 0), rep = a.q_heads / a.H;
   const PagedQueries w = paged_queries(a, b);
-  const int n_rows = w.n * rep, row0 = blockIdx.y * kRows, past = w.len - w.count;
-  const bool idle = share.b < 0 || row0 >= n_rows;
-  const int first_limit = uniform(past + row0 / rep), last_limit = uniform(past + min(row0 + kRows - 1, n_rows - 1) / rep);
+  const int n_rows = w.n * rep, past = w.len - w.count;
+  const bool idle = share.b < 0 || n_rows == 0;
+  const int first_limit = past, last_limit = uniform(past + (n_rows - 1) / rep);
   const TokenRange range = piece_range(share.piece, share.tiles, kTile, idle ? 0 : last_limit + 1);
   const int t_begin = range.begin, t_end = range.end;
-  const bool any = t_begin < t_end;
-  struct { f16x8 q[2][4]; float qsum[2], f, ref, sum; int limit; } col[COLS];
-  typename C::template Query<T> asked[COLS] = {};
-  if (!idle) {
-#pragma unroll
-    for (int i = 0; i < COLS; ++i) {
-      const int row = row0 + 16 * i + m, there = min(row, n_rows - 1), qi = there / rep, qh = h * rep + there % rep;
-      col[i].limit = row < n_rows ? past + qi : -1;
-      asked[i] = C::template request_query<T>(static_cast<const T*>(a.q) + (w.first + qi) * a.q_stride + qh * kGroup, a.signs_k, h, g);
-    }
+  int limit = -1;
+  typename C::template Query<T> asked = {};
+  if (!idle) {                                             // (rows that are not there: the last one again)
+    const int there = min(m & 7, n_rows - 1), qi = there / rep, qh = h * rep + there % rep;
+    limit = past + qi;
+    asked = C::template request_query<T>(static_cast<const T*>(a.q) + (w.first + qi) * a.q_stride + qh * kGroup, a.signs_k, h, g);
   }
-  Rows r0 = {}, r1 = {};
-  typename C::Keys k = {}, next = {};
-  if (any) {
-    r0 = rows_of(a, b, t_begin);
-    r1 = rows_of(a, b, t_begin + kTile);
-    k = C::template request_keys<FAR, false>(a, r0, h, lane);
+  // Keys are requested two tiles ahead, the rows that they are in three ahead.
+  struct Tile { typename C::Keys k; unsigned there; };
+  Tile s0 = {}, s1 = {}, s2 = {};
+  Rows ahead = {};
+  const auto request = [&](Tile& tile, const Rows& r, int t) {
+    tile.there = there_of(r);
+    if (t < t_end) tile.k = C::template request_keys<FAR, false>(a, r, h, lane);
+  };
+  if (t_begin < t_end) {
+    request(s0, rows_of(a, b, t_begin), t_begin);
+    request(s1, rows_of(a, b, t_begin + kTile), t_begin + kTile);
+    ahead = rows_of(a, b, t_begin + 2 * kTile);
   }
   const int c_exp = C::template stage<kWaves>(points, lds, lane, wave);
   __syncthreads();
   if (idle) return;
+  constexpr int kParts = kRtn ? 1 : 2;                     // operands that a piece of the coordinates takes
+  f16x8 q[4][kParts];
+  float qsum[2], f;
+  {
+    f16x8 both[2][4];
+    query_operands<T, NCW>(a, asked, c_exp, lane, both, qsum, f);
 #pragma unroll
-  for (int i = 0; i < COLS; ++i) {
-    float v[32];
-    C::template rotate_query<T>(asked[i], lane, v);
-    const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
-    float top = 0.f;
+    for (int j = 0; j < 4; ++j) {
+      const u32x4 hi = __builtin_bit_cast(u32x4, both[0][j]), lo = __builtin_bit_cast(u32x4, both[1][j]);
+      u32x4 y;
 #pragma unroll
-    for (int r = 0; r < 32; ++r) top = fmaxf(top, fabsf(v[r]));
-    const int e = max(__builtin_amdgcn_frexp_expf(column_max(top) * fabsf(by)), -100);
-    col[i].f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? C::kFieldExp : c_exp), 126));
-    const float scaled = __builtin_ldexpf(by, kQueryExp - e);
-#pragma unroll
-    for (int r = 0; r < 32; ++r) v[r] *= scaled;
-    C::pack_query(v, col[i].q, col[i].qsum);
-    col[i].ref = -3.0e38f;
-    col[i].sum = 0.f;
-  }
-#pragma unroll 1
-  for (int t = t_begin; t < t_end; t += kTile) {
-    const bool more = t + kTile < t_end;
-    if (more) next = C::template request_keys<FAR, false>(a, r1, h, lane);
-    const unsigned there = there_of(r0);
-    const Rows r2 = rows_of(a, b, t + 2 * kTile);
-    asm volatile("" ::: "memory");                         // (a wave's LDS accesses stay in order)
-    C::put_scales(k, scale_lds, lane);
-    asm volatile("" ::: "memory");
-    f32x4 s[COLS][C::kHalves][2] = {};
-#pragma unroll
-    for (int p = 0; p < 2; ++p) C::scores(k, p, lds, lane, col, s);
-    const int held = (there >> g) & 1 ? w.len - (t + 8 * g) : 0;
-    const bool masked = t + kTile - 1 > first_limit || t + kTile > t_end || there != 15u;
-#pragma unroll
-    for (int i = 0; i < COLS; ++i) {
-      float y[8];
-      C::scaled(s[i], scale_lds, g, col[i].qsum, y);
-      if (masked) {
-        asm volatile("");
-        const int seen = min(col[i].limit + 1 - (t + 8 * g), held);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = e < seen ? y[e] : -INFINITY;
-      }
-      float top = y[0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, y[e]);
-      if (__builtin_amdgcn_ballot_w64(__fmaf_rn(top, col[i].f, -col[i].ref) > kTopExp) != 0) {
-        const float moved = fmaxf(col[i].ref, column_max(top * col[i].f) - kStartExp);
-        col[i].sum *= __builtin_amdgcn_exp2f(col[i].ref - moved);
-        col[i].ref = moved;
-      }
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], col[i].f, -col[i].ref));
-      col[i].sum += sum_of(p);
-      if constexpr (COLS == 1) {                           // (times a power of two: exact)
-        const int at = t + 8 * g;
-        if (m < n_rows && at < x.room) {
-          float* const to = x.scores + (((int64_t)b * a.H + h) * x.row_cap + m) * x.room + at;
-          *reinterpret_cast<f32x4*>(to) = f32x4{y[0], y[1], y[2], y[3]} * col[i].f;
-          *reinterpret_cast<f32x4*>(to + 4) = f32x4{y[4], y[5], y[6], y[7]} * col[i].f;
-        }
+      for (int i = 0; i < 4; ++i) y[i] = m < 8 ? hi[i] : lo[i];
+      if constexpr (kRtn) {
+        q[j][0] = __builtin_bit_cast(f16x8, y);
+      } else {
+        q[j][0] = operand(y.x, y.x, y.y, y.y);
+        q[j][1] = operand(y.z, y.z, y.w, y.w);
       }
     }
-    k = next;
-    r0 = r1;
-    r1 = r2;
   }
-  if (share.piece == 0 && h == 0 && blockIdx.y == 0 && lane == 0) x.heads[b] = int2{item, share.pieces};
+  float ref = -3.0e38f, sum = 0.f;
+  const int first = 8 * g + 4 * (m >> 3);                  // the lane's four tokens of a tile
+  float* const to = x.scores + (((int64_t)b * a.H + h) * x.row_cap + (m & 7)) * x.room + first;
+  const auto step = [&](const Tile& tile, int t, Tile& next) {
+    if (t >= t_end) return;
+    request(next, ahead, t + 2 * kTile);
+    ahead = rows_of(a, b, t + 3 * kTile);
+    asm volatile("" ::: "memory");                         // (a wave's LDS accesses stay in order)
+    C::put_scales(tile.k, scale_lds, lane);
+    asm volatile("" ::: "memory");
+    f32x4 s[C::kHalves][2] = {};
 #pragma unroll
-  for (int i = 0; i < COLS; ++i) {
-    const float sum = column_sum(col[i].sum);
-    const int row = row0 + 16 * i + m;
-    if (g == 0 && row < n_rows) x.stats[((int64_t)item * a.H + h) * x.row_cap + row] = f32x2{col[i].ref, sum};
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const uint32_t w4[4] = {tile.k.k[p].x, tile.k.k[p].y, tile.k.k[p].z, tile.k.k[p].w};
+        if constexpr (kRtn) {
+          s[j >> 1][p] = mfma(code_operand<C>(w4, j), q[j][0], s[j >> 1][p]);
+        } else {
+          u32x2 y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const u32x2*>(lds + C::offset(w4, 4 * j + i, C::lane_copy(lane)));
+          s[0][p] = mfma(operand(y[0].x, y[0].y, y[1].x, y[1].y), q[j][0], s[0][p]);
+          s[0][p] = mfma(operand(y[2].x, y[2].y, y[3].x, y[3].y), q[j][kParts - 1], s[0][p]);
+        }
+      }
+    // product p has the tokens 8 g + 4 p ...: the lane's own p is m / 8, the other one's goes to the lane of the row's other column
+    float y[4];
+    const auto four = [&](int row) { return *reinterpret_cast<const u32x2*>(scale_lds + 64 * row + 2 * first); };
+    const auto half_of = [](const u32x2& w, int e) { return (float)__builtin_bit_cast(f16x2, e < 2 ? w.x : w.y)[e & 1]; };
+    const auto int_of = [](const u32x2& w, int e) { return (float)(((e < 2 ? w.x : w.y) >> (16 * (e & 1))) & 0xffffu); };
+#pragma unroll
+    for (int k = 0; k < C::kHalves; ++k) {
+      const u32x2 step = four(C::kKeys + 2 * k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float own = m < 8 ? s[k][0][e] : s[k][1][e], other = m < 8 ? s[k][1][e] : s[k][0][e];
+        float z = own + row_xor8(other);
+        if constexpr (kRtn) z = __fmaf_rn(-int_of(four(C::kKeys + 2 * k + 1), e), qsum[k], z);
+        y[e] = k == 0 ? z * half_of(step, e) : __fmaf_rn(z, half_of(step, e), y[e]);
+      }
+    }
+    if (t + kTile - 1 > first_limit || tile.there != 15u) {
+      asm volatile("");
+      const int seen = min(limit + 1 - (t + first), (tile.there >> g) & 1 ? w.len - (t + first) : 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = e < seen ? y[e] : -INFINITY;
+    }
+    const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+    if (__builtin_amdgcn_ballot_w64(__fmaf_rn(top, f, -ref) > kTopExp) != 0) {
+      const float most = column_max(top * f), moved = fmaxf(ref, fmaxf(most, row_xor8(most)) - kStartExp);
+      sum *= __builtin_amdgcn_exp2f(ref - moved);
+      ref = moved;
+    }
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[e] *= f;                                           // (a power of two: exact)
+      p[e] = __builtin_amdgcn_exp2f(y[e] - ref);
+    }
+    sum += sum_of(p);
+    if ((m & 7) < n_rows && t + first < x.room) *reinterpret_cast<f32x4*>(to + t) = f32x4{y[0], y[1], y[2], y[3]};
+  };
+#pragma unroll 1
+  for (int t = t_begin; t < t_end; t += 3 * kTile) {
+    step(s0, t, s2);
+    step(s1, t + kTile, s0);
+    step(s2, t + 2 * kTile, s1);
   }
+  if (share.piece == 0 && h == 0 && lane == 0) x.heads[b] = int2{item, share.pieces};
+  sum = column_sum(sum);
+  sum += row_xor8(sum);
+  if (g == 0 && m < n_rows) x.stats[((int64_t)item * a.H + h) * x.row_cap + m] = f32x2{ref, sum};
 }
 
 // Reference and 1 / sum (0: the row sees nothing) of one row from its pieces, by `lanes` neighbouring lanes: every one gets it.
@@ -217,202 +271,283 @@ __global__ __launch_bounds__(256) void weights_from_scores_kernel(const PagedAtt
   }
 }
 
-// Many rows: their statistics joined, their queries as operands.  One wave for 16 rows of a kv head: blockIdx = (row tile and kv head, sequence).
+// Many rows: their queries as operands.  One wave for 16 rows of a kv head: blockIdx = (row tile and kv head, sequence).
 template <typename T, int NCW>
 __global__ __launch_bounds__(64) void weights_rows_kernel(const PagedAttendArgs a, const WeightsArgs x) {
   typedef Codes<NCW, 2> C;
-  constexpr bool kRtn = is_rtn(NCW);
   const int lane = threadIdx.x, m = lane & 15, g = lane >> 4, b = blockIdx.y, h = blockIdx.x % a.H, tile = blockIdx.x / a.H;
   const PagedQueries w = paged_queries(a, b);
-  const int rep = a.q_heads / a.H, n_rows = w.n * rep, row = 16 * tile + m, there = min(row, n_rows - 1), qi = there / rep, qh = h * rep + there % rep;
+  const int rep = a.q_heads / a.H, n_rows = w.n * rep, there = min(16 * tile + m, n_rows - 1), qi = there / rep, qh = h * rep + there % rep;
   if (16 * tile >= n_rows) return;
   const typename C::template Query<T> asked = C::template request_query<T>(static_cast<const T*>(a.q) + (w.first + qi) * a.q_stride + qh * kGroup, a.signs_k, h, g);
   int c_exp = 0;
-  if constexpr (!kRtn) {                                   // the grid's exponent, as stage() takes it
+  if constexpr (!is_rtn(NCW)) {                            // the grid's exponent, as stage() takes it
     float top = 0.f;
-    for (int i = lane; i < 2 * NCW; i += 64) top = fmaxf(top, fabsf(a.codebook[i]));
+#pragma unroll
+    for (int i = 0; i < (2 * NCW + 63) / 64; ++i) top = fmaxf(top, fabsf(a.codebook[min(64 * i + lane, 2 * NCW - 1)]));
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
     c_exp = max(__builtin_amdgcn_frexp_expf(top), -100);
   }
-  const int2 head = x.heads[b];
-  // lanes of a row are 16 apart here
-  const f32x2* const at = x.stats + ((int64_t)head.x * a.H + h) * x.row_cap + there;
-  float ref = -3.0e38f, sum = 0.f;
-  for (int i = g; i < head.y; i += 4) {
-    const f32x2 s = at[(int64_t)i * a.H * x.row_cap];
-    const float top = fmaxf(ref, s.x);
-    sum = __fmaf_rn(sum, __builtin_amdgcn_exp2f(ref - top), s.y * __builtin_amdgcn_exp2f(s.x - top));
-    ref = top;
-  }
-  const float all = column_max(ref);
-  sum = column_sum(sum * __builtin_amdgcn_exp2f(ref - all));
-  float v[32];
-  C::template rotate_query<T>(asked, lane, v);
-  const float by = a.scale * 1.4426950408889634f * (kRtn ? 1.0f : kRsqrtG);
-  float top = 0.f;
-#pragma unroll
-  for (int r = 0; r < 32; ++r) top = fmaxf(top, fabsf(v[r]));
-  const int e = max(__builtin_amdgcn_frexp_expf(column_max(top) * fabsf(by)), -100);
-  const float scaled = __builtin_ldexpf(by, kQueryExp - e);
-#pragma unroll
-  for (int r = 0; r < 32; ++r) v[r] *= scaled;
   f16x8 q[2][4];
-  float qsum[2];
-  C::pack_query(v, q, qsum);
+  float qsum[2], f;
+  query_operands<T, NCW>(a, asked, c_exp, lane, q, qsum, f);
   const int64_t to = ((int64_t)b * a.H + h) * x.tiles + tile;
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x.packed[(to * 8 + 4 * n + j) * 64 + lane] = __builtin_bit_cast(u32x4, q[n][j]);
+    for (int j = 0; j < 4; ++j) x.packed[to].q[n][j][lane] = __builtin_bit_cast(u32x4, q[n][j]);
   if (g == 0) {
     WeightsArgs::Row r = {};
-    r.f = __builtin_ldexpf(1.0f, min(e - kQueryExp + (kRtn ? C::kFieldExp : c_exp), 126));
-    r.qsum0 = qsum[0]; r.qsum1 = qsum[1]; r.ref = all; r.inv = sum == 0.f || row >= n_rows ? 0.f : 1.0f / sum;      // (rows that are not there: the last one again, which adds nothing)
-    x.rows[to * 16 + m] = r;
+    r.f = f; r.qsum0 = qsum[0]; r.qsum1 = qsum[1];
+    x.packed[to].rows[m] = r;
   }
 }
 
-// Many rows: a wave has 32 tokens of a kv head as operands and takes the row tiles in turn.  blockIdx = (128 tokens and kv head, sequence).
-template <int NCW>
-__global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu(2))) void weights_mass_kernel(const PagedAttendArgs a, const WeightsArgs x) {
+// Row tiles that see something of the 32 tokens from t on: from this one.
+__device__ __forceinline__ int first_tile(int t, int past, int rep) { return max(t - past, 0) * rep / 16; }
+__device__ __forceinline__ int64_t token_tiles(const WeightsArgs& x) { return (x.room + kTile - 1) / kTile; }
+
+// Many rows: a wave has 32 tokens of a kv head as operands, which take their conversion once, and goes through the row tiles, whose operands its workgroup brings to LDS,
+// kStaged of them while the ones before are multiplied.  First for the statistics of the rows over its tokens, then, when those are joined, for the weights.
+// The grid is there once (look-ups are few, and meet in banks as they will): LDS has room for four workgroups.  blockIdx = (128 tokens and kv head, sequence).
+template <int NCW, bool MASS>
+__global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu(3))) void weights_tokens_kernel(const PagedAttendArgs a, const WeightsArgs x) {
   typedef Codes<NCW, 2> C;
   constexpr bool kRtn = is_rtn(NCW);
-  constexpr int kTable = kRtn ? 16 : C::kTableBytes, kTerms = kRtn ? 1 : 2;
-  __shared__ __align__(256) unsigned char lds[kTable + kMassWaves * C::kScaleBytes];
+  constexpr int kTable = kRtn ? 16 : NCW * 8, kTerms = kRtn ? 1 : 2, kThreads = 64 * kMassWaves;
+  constexpr int kUnits = sizeof(WeightsArgs::Packed) / 16 * kStaged, kEach = (kUnits + kThreads - 1) / kThreads;
+  __shared__ __align__(256) unsigned char table[kTable];
+  __shared__ __align__(256) unsigned char scale_space[kMassWaves * C::kScaleBytes];
+  __shared__ WeightsArgs::Packed staged[2][kStaged];
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  unsigned char* const scale_lds = lds + kTable + wave * C::kScaleBytes;
+  unsigned char* const scale_lds = scale_space + wave * C::kScaleBytes;
   const int b = blockIdx.y, h = blockIdx.x % a.H, t0 = (blockIdx.x / a.H) * kMassTokens, t = t0 + wave * kTile;
   const PagedQueries w = paged_queries(a, b);
   if (t0 >= w.len || w.n == 0) return;
+  const int rep = a.q_heads / a.H, n_rows = w.n * rep, past = w.len - w.count, tiles = (n_rows + 15) / 16;
+  const int first = first_tile(t0, past, rep);             // (later tokens' first row tiles are no earlier)
+  const int64_t head = ((int64_t)b * a.H + h) * x.tiles;
+  u32x4 coming[kEach];
+  const auto request = [&](int tile) {
+    const u32x4* const from = reinterpret_cast<const u32x4*>(x.packed + head + tile);
+    const int there = min(tiles - tile, kStaged) * (int)(sizeof(WeightsArgs::Packed) / 16);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (i * kThreads + (int)threadIdx.x < there) coming[i] = from[i * kThreads + threadIdx.x];
+  };
+  const auto put = [&](int buffer) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (i * kThreads + (int)threadIdx.x < kUnits) reinterpret_cast<u32x4*>(staged[buffer])[i * kThreads + threadIdx.x] = coming[i];
+  };
+  request(first);
   const typename C::Points points = C::request_points(a.codebook, lane);
-  const Rows r = rows_of(a, b, t);
+  const Rows r = rows_of(a, b, t);                         // (a wave behind the sequence: its pages, if any, are read and not used)
   const typename C::Keys keys = C::template request_keys<true, false>(a, r, h, lane);
-  C::template stage<kMassWaves>(points, lds, lane, wave);
-  __syncthreads();
-  if (t >= w.len) return;
+  if constexpr (!kRtn) {
+    const int e = C::exponent(points);
+    if (wave == 0) {
+#pragma unroll
+      for (int i = 0; i < C::kPoints; ++i) {
+        if (lane >= NCW / C::kPoints) break;
+        const float px = __builtin_ldexpf(points.x[2 * i], -e), py = __builtin_ldexpf(points.x[2 * i + 1], -e);
+        uint32_t hi = f16_pair(px, py);
+        asm("" : "+v"(hi));                                // (as in split_f16)
+        const f16x2 top = __builtin_bit_cast(f16x2, hi);
+        *reinterpret_cast<u32x2*>(table + 8 * (C::kPoints * lane + i)) = u32x2{hi, f16_pair(px - (float)top[0], py - (float)top[1])};
+      }
+    }
+  }
   C::put_scales(keys, scale_lds, lane);
-  asm volatile("" ::: "memory");
+  put(0);
+  __syncthreads();
   f16x8 k[2][4][kTerms];                                   // [product][piece of the coordinates][term]
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     const uint32_t y[4] = {keys.k[p].x, keys.k[p].y, keys.k[p].z, keys.k[p].w};
     if constexpr (kRtn) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t z[4];
-        const uint32_t d = NCW == kRtn4 ? y[j] : (j & 1) ? y[j >> 1] >> 8 : y[j >> 1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = NCW == kRtn4 ? C::field((i & 2) ? d >> 8 : d, i & 1) : C::field(d, i);
-        k[p][j][0] = operand(z[0], z[1], z[2], z[3]);
-      }
+      for (int j = 0; j < 4; ++j) k[p][j][0] = code_operand<C>(y, j);
     } else {
-      const uint32_t at = C::lane_copy(lane);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        uint32_t o[4];
+        u32x2 o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = C::offset(y, 4 * j + i, at);
-        k[p][j][0] = operand(C::point(lds, o[0]), C::point(lds, o[1]), C::point(lds, o[2]), C::point(lds, o[3]));
-        k[p][j][kTerms - 1] = operand(C::template point<1>(lds, o[0]), C::template point<1>(lds, o[1]), C::template point<1>(lds, o[2]), C::template point<1>(lds, o[3]));
+        for (int i = 0; i < 4; ++i) o[i] = *reinterpret_cast<const u32x2*>(table + (C::offset(y, 4 * j + i, 0u) >> 5));
+        k[p][j][0] = operand(o[0].x, o[1].x, o[2].x, o[3].x);
+        k[p][j][kTerms - 1] = operand(o[0].y, o[1].y, o[2].y, o[3].y);
       }
     }
   }
-  const int rep = a.q_heads / a.H, n_rows = w.n * rep, past = w.len - w.count;
   const unsigned there = there_of(r);
   const int held = (there >> g) & 1 ? w.len - (t + 8 * g) : 0;
   float gained[8] = {};
-  const int from = max(t - past, 0) * rep / 16, tiles = (n_rows + 15) / 16;      // (rows ahead of it see none of these tokens)
-  const int64_t head = ((int64_t)b * a.H + h) * x.tiles;
-  const u32x4* const packed = x.packed + head * 8 * 64 + lane;
-  const WeightsArgs::Row* const rows = x.rows + head * 16 + m;
-#pragma unroll 1
-  for (int tile = from; tile < tiles; ++tile) {
-    f16x8 q[2][4];
+  f32x2* const stats = x.stats + (head * token_tiles(x) + t / kTile) * 16 + m;
+  float sigma[8];                                          // grids: the scales of the lane's tokens
+  if constexpr (!kRtn) {
+    const u32x4 ks = C::eight(scale_lds, C::kKeys, g);
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[n][j] = __builtin_bit_cast(f16x8, packed[((int64_t)tile * 8 + 4 * n + j) * 64]);
-    const WeightsArgs::Row row = rows[(int64_t)tile * 16];
-    f32x4 s[C::kHalves][2] = {};
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f32x4& y = s[kRtn ? j >> 1 : 0][p];
-        y = mfma(k[p][j][0], q[0][j], y);
-        y = mfma(k[p][j][0], q[1][j], y);
-        if constexpr (!kRtn) y = mfma(k[p][j][1], q[0][j], y);
-      }
+    for (int e = 0; e < 8; ++e) sigma[e] = C::half_at(ks, e);
+  }
+  const auto finish = [&](const f32x4 (&s)[C::kHalves][2], const WeightsArgs::Row& row, int tile) {
+    const float f = row.f, qsum[2] = {row.qsum0, row.qsum1};
     float y[8];
-    const float qsum[2] = {row.qsum0, row.qsum1};
-    C::scaled(s, scale_lds, g, qsum, y);
+    if constexpr (kRtn) {
+      C::scaled(s, scale_lds, g, qsum, y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = s[0][e >> 2][e & 3] * sigma[e];
+    }
     if (t + kTile - 1 > past + 16 * tile / rep || there != 15u) {
       asm volatile("");
       const int mine = 16 * tile + m, seen = mine < n_rows ? min(past + mine / rep + 1 - (t + 8 * g), held) : 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = e < seen ? y[e] : -INFINITY;
     }
+    if constexpr (MASS) {
+      const float ref = row.ref, inv = row.inv;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) gained[e] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(y[e], row.f, -row.ref)), row.inv, gained[e]);
-  }
-  // sums over the 16 rows of a lane group; lane m < 8 has token 8 g + m
-  float mine = 0.f;
+      for (int e = 0; e < 8; ++e) gained[e] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref)), inv, gained[e]);
+    } else {
+      float top = y[0];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float y = gained[e];
-    y += quad_xor<1>(y);
-    y += quad_xor<2>(y);
-    y += octet_mirror(y);
-    y += row_xor8(y);
-    mine = m == e ? y : mine;
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, y[e]);
+      const float ref = fmaxf(column_max(top) * f, -3.0e38f);
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref));
+      const float sum = column_sum(sum_of(p));
+      if (g == 0) stats[(int64_t)tile * token_tiles(x) * 16] = f32x2{ref, sum};
+    }
+  };
+  const int from = first_tile(t, past, rep);
+  int buffer = 0;
+#pragma unroll 1
+  for (int tile = first; tile < tiles; tile += kStaged, buffer ^= 1) {
+    const bool more = tile + kStaged < tiles;
+    if (more) request(tile + kStaged);
+    if (t < w.len) {
+      // products of kStaged row tiles and two halves of the tokens in turn (a product waits for the last one of its own); of a row tile that is not there, anything
+      f32x4 s[kStaged][C::kHalves][2] = {};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          f16x8 q[kStaged];
+#pragma unroll
+          for (int i = 0; i < kStaged; ++i) q[i] = __builtin_bit_cast(f16x8, staged[buffer][i].q[n][j][lane]);
+#pragma unroll
+          for (int term = 0; term < (n == 0 ? kTerms : 1); ++term)
+#pragma unroll
+            for (int i = 0; i < kStaged; ++i)
+#pragma unroll
+              for (int p = 0; p < 2; ++p) {
+                f32x4& y = s[i][kRtn ? j >> 1 : 0][p];
+                y = mfma(k[p][j][term], q[i], y);
+              }
+        }
+#pragma unroll
+      for (int i = 0; i < kStaged; ++i)
+        if (tile + i >= from && tile + i < tiles) finish(s[i], staged[buffer][i].rows[m], tile + i);
+    }
+    if (more) put(buffer ^ 1);
+    __syncthreads();
   }
-  const int token = t + 8 * g + m;
-  if (m >= 8 || m >= held) return;
-  const int64_t place = mass_place(a, b, h, (uint32_t)(t / 8 + g));
-  float* const to = x.mass + place + m;
-  if (x.keep != 0.f && token < past) mine = __fmaf_rn(x.keep, *to, mine);
-  *to = mine;
+  if (t >= w.len) return;
+  if constexpr (MASS) {
+    // sums over the 16 rows of a lane group; lane m < 8 has token 8 g + m
+    float mine = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float y = gained[e];
+      y += quad_xor<1>(y);
+      y += quad_xor<2>(y);
+      y += octet_mirror(y);
+      y += row_xor8(y);
+      mine = m == e ? y : mine;
+    }
+    const int token = t + 8 * g + m;
+    if (m >= 8 || m >= held) return;
+    const int64_t place = mass_place(a, b, h, (uint32_t)(t / 8 + g));
+    float* const to = x.mass + place + m;
+    if (x.keep != 0.f && token < past) mine = __fmaf_rn(x.keep, *to, mine);
+    *to = mine;
+  }
 }
 
-struct WeightsPlan { bool few; unsigned blocks, row_tiles; int slots, rows; int64_t items, room; size_t scores, stats, heads, packed, row_bytes; };
-template <typename T, int NCW> WeightsPlan weights_plan(const PagedAttendArgs& a) {
+// Many rows: the statistics of a row tile over all token tiles.  blockIdx = (row tile and kv head, sequence); wave w takes token tiles 4 w + g, 4 w + g + 16, ...
+__global__ __launch_bounds__(256) void weights_join_kernel(const PagedAttendArgs a, const WeightsArgs x) {
+  __shared__ f32x2 part[4][16];
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6, b = blockIdx.y, h = blockIdx.x % a.H, tile = blockIdx.x / a.H;
+  const PagedQueries w = paged_queries(a, b);
+  const int rep = a.q_heads / a.H, n_rows = w.n * rep, past = w.len - w.count, n = tiles_of_tokens(w.len, kTile);
+  if (16 * tile >= n_rows) return;
+  const int64_t at = ((int64_t)b * a.H + h) * x.tiles + tile;
+  const f32x2* const from = x.stats + at * token_tiles(x) * 16 + m;
+  float ref = -3.0e38f, sum = 0.f;
+#pragma unroll 8
+  for (int i = 4 * wave + g; i < n; i += 16) {             // (tiles that this row tile was left out of are the last ones)
+    f32x2 s = {-3.0e38f, 0.f};
+    if (tile >= first_tile(i * kTile, past, rep)) s = from[(int64_t)i * 16];
+    const float top = fmaxf(ref, s.x);
+    sum = __fmaf_rn(sum, __builtin_amdgcn_exp2f(ref - top), s.y * __builtin_amdgcn_exp2f(s.x - top));
+    ref = top;
+  }
+  const float all = column_max(ref);
+  sum = column_sum(sum * __builtin_amdgcn_exp2f(ref - all));
+  if (g == 0) part[wave][m] = f32x2{all, sum};
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  float top = part[0][m].x, total = 0.f;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) top = fmaxf(top, part[i][m].x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) total = __fmaf_rn(part[i][m].y, __builtin_amdgcn_exp2f(part[i][m].x - top), total);
+  WeightsArgs::Row& row = x.packed[at].rows[m];
+  row.ref = top;
+  row.inv = total == 0.f || 16 * tile + m >= n_rows ? 0.f : 1.0f / total;      // (rows that are not there: the last one again, which adds nothing)
+}
+
+struct WeightsPlan { bool few; unsigned blocks; int slots, rows; int64_t room; size_t scores, stats, heads, packed; };
+template <int NCW> WeightsPlan weights_plan(const PagedAttendArgs& a) {
   WeightsPlan p = {};
   const int64_t rows = std::max<int64_t>(a.max_queries, 1) * (a.q_heads / a.H), room = (int64_t)a.table_pages * a.pool.page_tokens, most = (room + kTile - 1) / kTile;
+  const auto padded = [](int64_t n) { return ((size_t)n + 255) & ~(size_t)255; };
+  const int64_t heads = (int64_t)a.batch * a.H, tiles = (rows + 15) / 16;
   p.few = rows <= kFewRows;
   p.rows = (int)rows;
   p.room = room;
-  p.row_tiles = p.few ? 1 : (unsigned)((rows + 31) / 32);
-  p.slots = (int)std::max<int64_t>((p.few ? ScoreShape<T, NCW, 1>::kSlots : ScoreShape<T, NCW, 2>::kSlots) / (a.H * (int64_t)p.row_tiles), 1);
-  p.items = std::min(a.batch * std::max<int64_t>(most, 1), std::max<int64_t>(p.slots - a.batch, std::max(p.slots / 2, 1)) + a.batch);
-  constexpr int kWaves = ScoreShape<T, NCW, 1>::kWaves;
-  p.blocks = (unsigned)((p.items * a.H + kWaves - 1) / kWaves);
-  const auto padded = [](int64_t n) { return ((size_t)n + 255) & ~(size_t)255; };
-  const int64_t heads = (int64_t)a.batch * a.H, tiles = (rows + 15) / 16;
-  p.scores = p.few ? padded(heads * rows * room * sizeof(float)) : 0;
-  p.stats = padded(p.items * a.H * rows * sizeof(f32x2));
-  p.heads = padded(a.batch * (int64_t)sizeof(int2));
-  p.packed = p.few ? 0 : padded(heads * tiles * 8 * 64 * sizeof(u32x4));
-  p.row_bytes = p.few ? 0 : padded(heads * tiles * 16 * sizeof(WeightsArgs::Row));
+  if (p.few) {
+    p.slots = std::max(ScoreShape<NCW>::kSlots / a.H, 1);
+    const int64_t items = std::min(a.batch * std::max<int64_t>(most, 1), std::max<int64_t>(p.slots - a.batch, std::max(p.slots / 2, 1)) + a.batch);
+    p.blocks = (unsigned)((items * a.H + ScoreShape<NCW>::kWaves - 1) / ScoreShape<NCW>::kWaves);
+    p.scores = padded(heads * rows * room * sizeof(float));
+    p.stats = padded(items * a.H * rows * sizeof(f32x2));
+    p.heads = padded(a.batch * (int64_t)sizeof(int2));
+  } else {
+    p.stats = padded(heads * tiles * most * 16 * sizeof(f32x2));
+    p.packed = padded(heads * tiles * sizeof(WeightsArgs::Packed));
+  }
   return p;
 }
-WeightsPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a) {
+WeightsPlan plan_of(int n_codewords, const PagedAttendArgs& a) {
   WeightsPlan p = {};
-  AQUAKV_PAGED(dtype, n_codewords, (p = weights_plan<T, N>(a)));
+  AQUAKV_PAGED_N(n_codewords, (p = weights_plan<N>(a)));
   return p;
 }
 
 }  // namespace
 
-size_t paged_weights_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a) {
-  const WeightsPlan p = plan_of(dtype, n_codewords, a);
-  return p.scores + p.stats + p.heads + p.packed + p.row_bytes;
+size_t paged_weights_workspace_bytes(int n_codewords, const PagedAttendArgs& a) {
+  const WeightsPlan p = plan_of(n_codewords, a);
+  return p.scores + p.stats + p.heads + p.packed;
 }
 
 hipError_t launch_paged_weights(int dtype, int n_codewords, const PagedAttendArgs& args, float keep, float* mass, void* workspace, hipStream_t stream) {
   PagedAttendArgs a = args;
-  const WeightsPlan plan = plan_of(dtype, n_codewords, a);
+  const WeightsPlan plan = plan_of(n_codewords, a);
   a.slots = plan.slots;
   a.page_groups = a.pool.page_tokens / 8;
   a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
@@ -422,31 +557,25 @@ hipError_t launch_paged_weights(int dtype, int n_codewords, const PagedAttendArg
   x.scores = reinterpret_cast<float*>(take(plan.scores));
   x.stats = reinterpret_cast<f32x2*>(take(plan.stats));
   x.heads = reinterpret_cast<int2*>(take(plan.heads));
-  x.packed = reinterpret_cast<u32x4*>(take(plan.packed));
-  x.rows = reinterpret_cast<WeightsArgs::Row*>(take(plan.row_bytes));
+  x.packed = reinterpret_cast<WeightsArgs::Packed*>(take(plan.packed));
   x.mass = mass; x.keep = keep;
   x.row_cap = plan.rows; x.tiles = (plan.rows + 15) / 16; x.room = (int)plan.room;
-  const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;
-  const dim3 grid(plan.blocks, plan.row_tiles);
-#define AQUAKV_SCORES(T, N, COLS)                                                                                                    \
-  (far ? weights_scores_kernel<T, N, COLS, true><<<grid, ScoreShape<T, N, COLS>::kThreads, 0, stream>>>(a, x)                         \
-       : weights_scores_kernel<T, N, COLS, false><<<grid, ScoreShape<T, N, COLS>::kThreads, 0, stream>>>(a, x))
   if (plan.few) {
-    AQUAKV_PAGED(dtype, n_codewords, (AQUAKV_SCORES(T, N, 1)));
-  } else {
-    AQUAKV_PAGED(dtype, n_codewords, (AQUAKV_SCORES(T, N, 2)));
-  }
-#undef AQUAKV_SCORES
-  if (const hipError_t e = hipGetLastError()) return e;
-  if (plan.few) {
+    const bool far = (uint64_t)a.pool.rows * a.H * (kGroup / 2) > 0xffffffffull;
+    AQUAKV_PAGED(dtype, n_codewords, (far ? weights_scores_kernel<T, N, true><<<plan.blocks, ScoreShape<N>::kThreads, 0, stream>>>(a, x)
+                                          : weights_scores_kernel<T, N, false><<<plan.blocks, ScoreShape<N>::kThreads, 0, stream>>>(a, x)));
+    if (const hipError_t e = hipGetLastError()) return e;
     weights_from_scores_kernel<<<dim3((unsigned)((plan.room + kChunk - 1) / kChunk * a.H), (unsigned)a.batch), 256, 0, stream>>>(a, x);
     return hipGetLastError();
   }
-  const dim3 tiles((unsigned)(x.tiles * a.H), (unsigned)a.batch);
+  const dim3 tiles((unsigned)(x.tiles * a.H), (unsigned)a.batch), tokens((unsigned)((plan.room + kMassTokens - 1) / kMassTokens * a.H), (unsigned)a.batch);
   AQUAKV_PAGED(dtype, n_codewords, (weights_rows_kernel<T, N><<<tiles, 64, 0, stream>>>(a, x)));
   if (const hipError_t e = hipGetLastError()) return e;
-  const dim3 tokens((unsigned)((plan.room + kMassTokens - 1) / kMassTokens * a.H), (unsigned)a.batch);
-  AQUAKV_PAGED_N(n_codewords, (weights_mass_kernel<N><<<tokens, 64 * kMassWaves, 0, stream>>>(a, x)));
+  AQUAKV_PAGED_N(n_codewords, (weights_tokens_kernel<N, false><<<tokens, 64 * kMassWaves, 0, stream>>>(a, x)));
+  if (const hipError_t e = hipGetLastError()) return e;
+  weights_join_kernel<<<tiles, 256, 0, stream>>>(a, x);
+  if (const hipError_t e = hipGetLastError()) return e;
+  AQUAKV_PAGED_N(n_codewords, (weights_tokens_kernel<N, true><<<tokens, 64 * kMassWaves, 0, stream>>>(a, x)));
   return hipGetLastError();
 }
 
