@@ -556,8 +556,30 @@ def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_p
     return _lib.aquakv_paged_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table_pages, q_rows, max_queries)
 
 
+def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
+                        workspace, stream=None) -> None:
+    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence].  Tensors have to be on the current
+    device (ValueError otherwise), whose current stream is taken unless one is given."""
+    row, dtype, here = q_heads * layer.head_dim, layer.dtype, _here()
+    _pool_here(layer, pages, here)
+    at, stride, q_rows = _rows(q, dtype, row, "q", here)
+    if q_rows is None or page_table is None or page_table.__class__ is int:
+        raise ValueError("q and page_table must be tensors: their shapes say how many rows and pages there are")
+    if page_table.dim() != 2 or page_table.shape[0] != batch:
+        raise ValueError("page_table must be [batch, pages]")
+    pages_each = page_table.shape[1]
+    if workspace.__class__ is torch.Tensor and workspace.get_device() != here:
+        raise ValueError("workspace is not on the current device")
+    ws, nbytes = _ws(workspace)
+    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads,
+                                    _typed(page_table, torch.int32, batch * pages_each, "page_table", here), pages_each,
+                                    _typed(seq_lens, torch.int32, batch, "seq_lens", here), q_rows, max_queries,
+                                    _typed(q_start, torch.int32, batch + 1, "q_start", here), at, stride, score_scale,
+                                    _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
+
+
 def _asked(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, q_start, workspace):
-    """What the calls that attend over pages have in common -> (the current device, arguments as the C calls take them, by name)"""
+    """What the other calls that attend over pages have in common -> (the current device, row length, dtype, arguments as the C calls take them)"""
     row, dtype, here = q_heads * layer.head_dim, layer.dtype, _here()
     _pool_here(layer, pages, here)
     at, stride, q_rows = _rows(q, dtype, row, "q", here)
@@ -570,16 +592,6 @@ def _asked(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, q_st
         raise ValueError("workspace is not on the current device")
     return (here, row, dtype, _typed(page_table, torch.int32, batch * pages_each, "page_table", here), pages_each,
             _typed(seq_lens, torch.int32, batch, "seq_lens", here), q_rows, _typed(q_start, torch.int32, batch + 1, "q_start", here), at, stride)
-
-
-def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,
-                        workspace, stream=None) -> None:
-    """q: [q_rows, q_heads, 128], rows may lie apart; page_table: [batch, pages of the longest sequence].  Tensors have to be on the current
-    device (ValueError otherwise), whose current stream is taken unless one is given."""
-    here, row, dtype, table, pages_each, lens, q_rows, start, at, stride = _asked(layer, pages, batch, q_heads, page_table, seq_lens, q, q_start, workspace)
-    ws, nbytes = _ws(workspace)
-    _check(_lib.aquakv_paged_attend(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table, pages_each, lens, q_rows, max_queries, start, at, stride,
-                                    score_scale, _typed(out, dtype, q_rows * row, "out", here), ws, nbytes, _stream(stream)))
 
 
 def aquakv_paged_attend_tree(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, tree, score_scale: float,
@@ -606,6 +618,8 @@ def _table(x, batch: int, name: str, device: int):
 
 def _mass(x, layer, pages, device: int):
     """[n_pages, kv_heads, page_tokens]"""
+    if x is None:
+        return None
     c = pages.c if isinstance(pages, Pages) else pages
     return _typed(x, torch.float32, c.n_pages * c.page_tokens * layer.kv_heads, "mass", device)
 
@@ -667,38 +681,44 @@ def aquakv_paged_keep(layer, pages, batch: int, page_table, kept, n_kept, first,
 ROTARY_LAYOUTS = {"half": 0, "pairs": 1}
 
 
+def _tables(cos, sin, device: int):
+    """rope_cos, rope_sin [rows, rotary_dim / 2] -> (addresses, rows, rotary_dim / 2)"""
+    shape = cos.shape
+    if len(shape) != 2 or sin.shape != shape:
+        raise ValueError("rope_cos and rope_sin must be tensors [rows, rotary_dim / 2]")
+    if not (cos.dtype is sin.dtype is torch.float32 and cos.get_device() == sin.get_device() == device and cos.is_contiguous() and sin.is_contiguous()):
+        raise ValueError("rope_cos and rope_sin must be contiguous, torch.float32, on the current device")
+    return cos.data_ptr(), sin.data_ptr(), shape[0], shape[1]
+
+
 def aquakv_rotary(x, positions, rope_cos, rope_sin, rotary_dim: int, layout: str, out, transposed: bool = False, stream=None) -> None:
     """x, out: [tokens, heads, 128], rows may lie apart (out = x: in place); positions: int32 [tokens]; rope_cos, rope_sin: fp32
     [rows, rotary_dim / 2]; layout: "half" or "pairs".  Tensors have to be on the current device (ValueError otherwise), whose current stream is
     taken unless one is given."""
-    here = _here()
-    if x.dim() != 3 or out.shape != x.shape:
+    here, dtype, shape = _here(), x.dtype, x.shape
+    if len(shape) != 3 or shape[2] != 128 or out.shape != shape:
         raise ValueError("x and out must be tensors [tokens, heads, 128] of one shape")
-    if layout not in ROTARY_LAYOUTS:
-        raise ValueError(f"layout {layout!r}: one of {sorted(ROTARY_LAYOUTS)}")
-    tokens, heads, g = x.shape
-    if g != 128:
-        raise ValueError("x and out must be tensors [tokens, heads, 128] of one shape")
-    at, stride, _ = _rows(x, x.dtype, heads * 128, "x", here)
-    to, to_stride, _ = _rows(out, x.dtype, heads * 128, "out", here)
-    if rope_cos.dim() != 2 or rope_cos.shape[1] * 2 != rotary_dim or rope_sin.shape != rope_cos.shape:
+    tokens, heads = shape[0], shape[1]
+    at, stride, _ = _rows(x, dtype, heads * 128, "x", here)
+    to, to_stride, _ = (at, stride, tokens) if out is x else _rows(out, dtype, heads * 128, "out", here)
+    cos, sin, rows, pairs = _tables(rope_cos, rope_sin, here)
+    if 2 * pairs != rotary_dim:
         raise ValueError("rope_cos and rope_sin must be tensors [rows, rotary_dim / 2]")
-    rows, n = rope_cos.shape[0], rope_cos.numel()
-    _check(_lib.aquakv_rotary(_dtype_code(x.dtype), tokens, heads, at, stride, _typed(positions, torch.int32, tokens, "positions", here),
-                              _typed(rope_cos, torch.float32, n, "rope_cos", here), _typed(rope_sin, torch.float32, n, "rope_sin", here), rows,
-                              rotary_dim, ROTARY_LAYOUTS[layout], int(transposed), to, to_stride, _stream(stream)))
+    order = ROTARY_LAYOUTS.get(layout)
+    if order is None:
+        raise ValueError(f"layout {layout!r}: one of {sorted(ROTARY_LAYOUTS)}")
+    status = _lib.aquakv_rotary(0 if dtype is torch.bfloat16 else _dtype_code(dtype), tokens, heads, at, stride,
+                                _typed(positions, torch.int32, tokens, "positions", here), cos, sin, rows, rotary_dim, order, 1 if transposed else 0,
+                                to, to_stride, _stream(stream))
+    if status != AQUAKV_OK:
+        raise AquaKVError(status)
 
 
 def aquakv_rotary_tables(rope_cos, rope_sin, base: float, first: int = 0, factor: float = 1.0, original_len: float = 0.0, low_turns: float = 0.0,
                          high_turns: float = 0.0, magnitude: float = 1.0, stream=None) -> None:
     """rope_cos, rope_sin: fp32 [rows, rotary_dim / 2], written for positions first ... first + rows - 1."""
-    here = _here()
-    if rope_cos.dim() != 2 or rope_sin.shape != rope_cos.shape:
-        raise ValueError("rope_cos and rope_sin must be tensors [rows, rotary_dim / 2]")
-    (rows, pairs), n = rope_cos.shape, rope_cos.numel()
-    _check(_lib.aquakv_rotary_tables(rows, first, 2 * pairs, base, factor, original_len, low_turns, high_turns, magnitude,
-                                     _typed(rope_cos, torch.float32, n, "rope_cos", here), _typed(rope_sin, torch.float32, n, "rope_sin", here),
-                                     _stream(stream)))
+    cos, sin, rows, pairs = _tables(rope_cos, rope_sin, _here())
+    _check(_lib.aquakv_rotary_tables(rows, first, 2 * pairs, base, factor, original_len, low_turns, high_turns, magnitude, cos, sin, _stream(stream)))
 
 
 def aquakv_fit_workspace_bytes(d_in: int, d_out: int) -> int:

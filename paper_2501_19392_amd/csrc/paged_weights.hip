@@ -319,7 +319,7 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
   constexpr int kUnits = sizeof(WeightsArgs::Packed) / 16 * kStaged, kEach = (kUnits + kThreads - 1) / kThreads;
   __shared__ __align__(256) unsigned char table[kTable];
   __shared__ __align__(256) unsigned char scale_space[kMassWaves * C::kScaleBytes];
-  __shared__ WeightsArgs::Packed staged[2][kStaged];
+  __shared__ union { WeightsArgs::Packed tiles[kStaged]; u32x4 units[kEach * kThreads]; } staged[2];
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned char* const scale_lds = scale_space + wave * C::kScaleBytes;
@@ -329,20 +329,21 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
   const int rep = a.q_heads / a.H, n_rows = w.n * rep, past = w.len - w.count, tiles = (n_rows + 15) / 16;
   const int first = first_tile(t0, past, rep);             // (later tokens' first row tiles are no earlier)
   const int64_t head = ((int64_t)b * a.H + h) * x.tiles;
-  u32x4 coming[kEach];
-  const auto request = [&](int tile) {
-    const u32x4* const from = reinterpret_cast<const u32x4*>(x.packed + head + tile);
-    const int there = min(tiles - tile, kStaged) * (int)(sizeof(WeightsArgs::Packed) / 16);
+  struct Coming { u32x4 x[kEach]; };
+  Coming even, odd;
+  // (Neither has a branch: loads wait for each other across them.  Behind the last row tile its end again, and behind a stage what no one reads.)
+  const auto request = [&](Coming& coming, int tile) {
+    const int from = min(tile, tiles - 1), last = min(tiles - from, kStaged) * (int)(sizeof(WeightsArgs::Packed) / 16) - 1;
+    const u32x4* const at = reinterpret_cast<const u32x4*>(x.packed + head + from);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (i * kThreads + (int)threadIdx.x < there) coming[i] = from[i * kThreads + threadIdx.x];
+    for (int i = 0; i < kEach; ++i) coming.x[i] = at[min(i * kThreads + (int)threadIdx.x, last)];
   };
-  const auto put = [&](int buffer) {
+  const auto put = [&](const Coming& coming, int buffer) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (i * kThreads + (int)threadIdx.x < kUnits) reinterpret_cast<u32x4*>(staged[buffer])[i * kThreads + threadIdx.x] = coming[i];
+    for (int i = 0; i < kEach; ++i) staged[buffer].units[i * kThreads + threadIdx.x] = coming.x[i];
   };
-  request(first);
+  request(even, first);
+  request(odd, first + kStaged);
   const typename C::Points points = C::request_points(a.codebook, lane);
   const Rows r = rows_of(a, b, t);                         // (a wave behind the sequence: its pages, if any, are read and not used)
   const typename C::Keys keys = C::template request_keys<true, false>(a, r, h, lane);
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
     }
   }
   C::put_scales(keys, scale_lds, lane);
-  put(0);
+  put(even, 0);
   __syncthreads();
   f16x8 k[2][4][kTerms];                                   // [product][piece of the coordinates][term]
 #pragma unroll
@@ -423,11 +424,9 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
     }
   };
   const int from = first_tile(t, past, rep);
-  int buffer = 0;
-#pragma unroll 1
-  for (int tile = first; tile < tiles; tile += kStaged, buffer ^= 1) {
-    const bool more = tile + kStaged < tiles;
-    if (more) request(tile + kStaged);
+  // A stage is requested two stages ahead: what another chiplet wrote takes longer than one.
+  const auto stage_of = [&](int tile, int buffer, Coming& next, const Coming& behind) {
+    request(next, tile + 2 * kStaged);
     if (t < w.len) {
       // products of kStaged row tiles and two halves of the tokens in turn (a product waits for the last one of its own); of a row tile that is not there, anything
       f32x4 s[kStaged][C::kHalves][2] = {};
@@ -437,7 +436,7 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
         for (int n = 0; n < 2; ++n) {
           f16x8 q[kStaged];
 #pragma unroll
-          for (int i = 0; i < kStaged; ++i) q[i] = __builtin_bit_cast(f16x8, staged[buffer][i].q[n][j][lane]);
+          for (int i = 0; i < kStaged; ++i) q[i] = __builtin_bit_cast(f16x8, staged[buffer].tiles[i].q[n][j][lane]);
 #pragma unroll
           for (int term = 0; term < (n == 0 ? kTerms : 1); ++term)
 #pragma unroll
@@ -448,12 +447,26 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
                 y = mfma(k[p][j][term], q[i], y);
               }
         }
+      // operands are read two steps ahead of their products
+      constexpr int kFirst = 2 * kTerms * kStaged, kSecond = 2 * kStaged;
+#define AQUAKV_STEP(MFMAS, READS) __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0); __builtin_amdgcn_sched_group_barrier(0x100, READS, 0)
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * kStaged, 0);
+      AQUAKV_STEP(kFirst, kStaged); AQUAKV_STEP(kSecond, kStaged); AQUAKV_STEP(kFirst, kStaged);
+      AQUAKV_STEP(kSecond, kStaged); AQUAKV_STEP(kFirst, kStaged); AQUAKV_STEP(kSecond, kStaged);
+#undef AQUAKV_STEP
+      __builtin_amdgcn_sched_group_barrier(0x008, kFirst + kSecond, 0);
 #pragma unroll
       for (int i = 0; i < kStaged; ++i)
-        if (tile + i >= from && tile + i < tiles) finish(s[i], staged[buffer][i].rows[m], tile + i);
+        if (tile + i >= from && tile + i < tiles) finish(s[i], staged[buffer].tiles[i].rows[m], tile + i);
     }
-    if (more) put(buffer ^ 1);
+    put(behind, buffer ^ 1);
     __syncthreads();
+  };
+#pragma unroll 1
+  for (int tile = first; tile < tiles; tile += 2 * kStaged) {
+    stage_of(tile, 0, even, odd);
+    if (tile + kStaged >= tiles) break;
+    stage_of(tile + kStaged, 1, odd, even);
   }
   if (t >= w.len) return;
   if constexpr (MASS) {
