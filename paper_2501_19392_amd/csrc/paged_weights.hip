@@ -11,7 +11,7 @@ namespace {
 using namespace paged;
 
 constexpr int kFewRows = 8;                                // of a kv head, whose scores are kept (else they are taken again)
-constexpr int kMassWaves = 4, kStaged = 2, kMassTokens = kTile * kMassWaves;      // of a workgroup that takes many rows
+constexpr int kMassWaves = 4, kStaged = 2, kBehind = 4 * kStaged, kMassTokens = kTile * kMassWaves;      // of a workgroup that takes many rows
 
 struct WeightsArgs {
   float* scores;                                           // few rows: [batch, H, rows, room], powers of two
@@ -327,16 +327,15 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
   const PagedQueries w = paged_queries(a, b);
   if (t0 >= w.len || w.n == 0) return;
   const int rep = a.q_heads / a.H, n_rows = w.n * rep, past = w.len - w.count, tiles = (n_rows + 15) / 16;
-  const int first = first_tile(t0, past, rep);             // (later tokens' first row tiles are no earlier)
+  const int first = min(first_tile(t0, past, rep), tiles); // (later tokens' first row tiles are no earlier; the sequence may have more rows than are answered)
   const int64_t head = ((int64_t)b * a.H + h) * x.tiles;
   struct Coming { u32x4 x[kEach]; };
   Coming even, odd;
-  // (Neither has a branch: loads wait for each other across them.  Behind the last row tile its end again, and behind a stage what no one reads.)
+  // (Neither has a branch or a bound: loads wait for each other across the one, and the other is work.  There is room for kBehind row tiles behind the last one.)
   const auto request = [&](Coming& coming, int tile) {
-    const int from = min(tile, tiles - 1), last = min(tiles - from, kStaged) * (int)(sizeof(WeightsArgs::Packed) / 16) - 1;
-    const u32x4* const at = reinterpret_cast<const u32x4*>(x.packed + head + from);
+    const u32x4* const at = reinterpret_cast<const u32x4*>(x.packed + head + tile);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) coming.x[i] = at[min(i * kThreads + (int)threadIdx.x, last)];
+    for (int i = 0; i < kEach; ++i) coming.x[i] = at[(unsigned)(i * kThreads) + threadIdx.x];
   };
   const auto put = [&](const Coming& coming, int buffer) {
 #pragma unroll
@@ -541,7 +540,7 @@ template <int NCW> WeightsPlan weights_plan(const PagedAttendArgs& a) {
     p.heads = padded(a.batch * (int64_t)sizeof(int2));
   } else {
     p.stats = padded(heads * tiles * most * 16 * sizeof(f32x2));
-    p.packed = padded(heads * tiles * sizeof(WeightsArgs::Packed));
+    p.packed = padded((heads * tiles + kBehind) * sizeof(WeightsArgs::Packed));
   }
   return p;
 }

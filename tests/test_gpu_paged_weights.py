@@ -112,7 +112,7 @@ def test_weights_are_added_up(dtype, fmt, H, QH, lengths, page, counts, keep):
     assert torch.equal(weights(lg, pages, table, lens, q, counts, keep, mass).view(torch.int32), got.view(torch.int32))      # the same bits each time
 
 
-@pytest.mark.parametrize("QH,counts,max_queries", [(4, [2, 0, 1, 3], 2), (16, [12, 0, 3, 30], 11)])
+@pytest.mark.parametrize("QH,counts,max_queries", [(4, [2, 0, 1, 3], 2), (16, [12, 0, 3, 30], 11), (16, [90, 0, 1, 240], 3)])
 def test_ragged_and_empty_sequences(QH, counts, max_queries):
     """No queries: left as it was; more rows than are answered; no tokens; pages that are not in the pool."""
     H, page, lengths = 2, 16, [100, 50, 0, 240]
