@@ -551,7 +551,7 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   as they were; where a sequence has more than max_queries rows, those that are not answered add nothing.  A page that two sequences name has
  *   anything in its mass afterwards.  After drafts were accepted (aquakv_paged_keep) the accepted ones are the last tokens, and their queries are taken here.
  *   Both dtypes: products of two fp16 numbers for each factor (22 bits), fp32 sums in a fixed order: the same bits each time.  Beyond the limits of
- *   aquakv_paged_attend: table_pages * page_tokens * kv_heads < 2^32.  workspace: aquakv_paged_weights_workspace_bytes() bytes, which hold the scores of all
+ *   aquakv_paged_attend: table_pages * page_tokens * kv_heads < 2^31.  workspace: aquakv_paged_weights_workspace_bytes() bytes, which hold the scores of all
  *   tokens there is room for where a kv head has at most 8 rows (queries x query heads).
  *
  * aquakv_paged_select -- which tokens of a cache are kept: of each sequence the `budget` tokens with the largest mass, its first n_first and last
@@ -614,13 +614,14 @@ int aquakv_paged_keep(const aquakv_layer* layer, const aquakv_pages* pages, int3
  *   the way back for tables of magnitude 1, and the gradient for any.  fp32 arithmetic, one rounding to dtype.
  *   Token t is at x + t * x_stride elements and goes to out + t * out_stride (rows contiguous, 16-byte aligned).  out = x with the same stride: in place;
  *   otherwise they may not overlap.  A token whose position is outside the tables is left out: its row of `out` stays as it was.  positions: int32 [tokens].
- *   tokens * heads < 2^30.
+ *   tokens * (heads / 4, rounded up) < 2^27.
  *
  * aquakv_rotary_tables -- rope_cos, rope_sin [rows, rotary_dim / 2] for positions first ... first + rows - 1 (below 2^31):
  *   magnitude * cos, sin(position * w_i),  w_i = base^(-2 i / rotary_dim) (k_i + (1 - k_i) / factor):
  *   factor 1: plain frequencies.  Otherwise, for contexts `factor` times as long, original_len 0: k_i = 0, all frequencies alike; original_len > 0:
  *   k_i = (r_i - low_turns) / (high_turns - low_turns) cut to 0 ... 1, r_i = the turns that frequency i makes over original_len positions, so that fast
  *   frequencies stay and slow ones are stretched.  magnitude: 1, or what scores are scaled by (both of query and key).  Angles in 64 bits.
+ *   rows * rotary_dim / 2 < 2^35.
  */
 typedef enum { AQUAKV_ROTARY_HALVES = 0, AQUAKV_ROTARY_PAIRS = 1 } aquakv_rotary_layout;
 int aquakv_rotary(int32_t dtype, int64_t tokens, int32_t heads, const void* x, int64_t x_stride, const int32_t* positions, const float* rope_cos,

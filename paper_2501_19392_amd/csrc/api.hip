@@ -1812,8 +1812,8 @@ int aquakv_paged_weights(const aquakv_layer* L, const aquakv_pages* pages, int32
   if (q_start == nullptr && q_rows != (int64_t)batch * max_queries)
     return fail(AQUAKV_EINVAL, "q_rows=%lld: without q_start every one of %d sequences has %d", (long long)q_rows, batch, max_queries);
   if (!std::isfinite(keep)) return fail(AQUAKV_EINVAL, "keep=%g", (double)keep);
-  // (threads of a launch: below 2^32, a fourth of the tokens of each kv head)
-  if ((int64_t)table_pages * pages->page_tokens * L->kv_heads >= ((int64_t)1 << 32))
+  // (threads of a launch: below 2^32, two a token and kv head)
+  if ((int64_t)table_pages * pages->page_tokens * L->kv_heads >= ((int64_t)1 << 31))
     return fail(AQUAKV_EUNSUPPORTED, "%d pages of %d tokens of %d heads", table_pages, pages->page_tokens, L->kv_heads);
   if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;
   const int64_t row = (int64_t)q_heads * 128;
@@ -1934,7 +1934,8 @@ int aquakv_rotary(int32_t dtype, int64_t tokens, int32_t heads, const void* x, i
   if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return fail(AQUAKV_EINVAL, "rotary_dim=%d of heads of 128", rotary_dim);
   if (rotary_dim % 16) return fail(AQUAKV_EUNSUPPORTED, "rotary_dim=%d: multiples of 16 are built", rotary_dim);
   if (layout != AQUAKV_ROTARY_HALVES && layout != AQUAKV_ROTARY_PAIRS) return fail(AQUAKV_EINVAL, "layout=%d", layout);
-  if (tokens > (1LL << 31) || tokens * heads >= (1LL << 30)) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, heads);
+  // (threads of a launch: below 2^32, up to 32 for four heads of a token)
+  if (tokens >= (1LL << 27) || tokens * ((heads + 3LL) / 4) >= (1LL << 27)) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, heads);
   if (tokens == 0) return AQUAKV_OK;
   const int64_t row = (int64_t)heads * 128;
   const size_t eb = elem_bytes(dtype), angles = (size_t)rope_rows * (rotary_dim / 2) * sizeof(float);
@@ -1963,6 +1964,7 @@ int aquakv_rotary_tables(int64_t rows, int64_t first, int32_t rotary_dim, double
   if (rotary_dim % 16) return fail(AQUAKV_EUNSUPPORTED, "rotary_dim=%d: multiples of 16 are built", rotary_dim);
   if (rows < 0 || first < 0 || rows > 0x7fffffffLL || first > 0x7fffffffLL - rows)
     return fail(AQUAKV_EINVAL, "positions %lld ... of %lld rows", (long long)first, (long long)rows);
+  if (rows * (rotary_dim / 2) >= (1LL << 35)) return fail(AQUAKV_EUNSUPPORTED, "rows=%lld of %d angles", (long long)rows, rotary_dim / 2);
   if (!(base > 0) || !std::isfinite(base) || !(factor > 0) || !std::isfinite(factor) || !std::isfinite(magnitude))
     return fail(AQUAKV_EINVAL, "base=%g factor=%g magnitude=%g", base, factor, (double)magnitude);
   if (!(original_len >= 0) || !std::isfinite(original_len)) return fail(AQUAKV_EINVAL, "original_len=%g", original_len);
@@ -1980,6 +1982,7 @@ int aquakv_rotary_tables(int64_t rows, int64_t first, int32_t rotary_dim, double
     const double turns = std::pow(base, -2.0 * i / rotary_dim) / 6.283185307179586476925;
     const double kept = original_len > 0 ? std::min(std::max((original_len * turns - low_turns) / (high_turns - low_turns), 0.0), 1.0) : 0.0;
     a.turns[i] = turns * (kept + (1.0 - kept) / factor);
+    if (!(a.turns[i] < 0x1p62)) return fail(AQUAKV_EINVAL, "base=%g factor=%g: no finite frequency %d", base, factor, i);      // (positions below 2^31: their angles are finite)
   }
   HIP_TRY(aquakv::launch_rotary_tables(a, static_cast<hipStream_t>(stream)));
   return AQUAKV_OK;

@@ -84,7 +84,7 @@ def test_sizes_that_all_refuse(call, kw, want):
     ("tree", dict(words=(1 << 17) + 1), B.AQUAKV_EUNSUPPORTED), ("tree", dict(q_heads=12), B.AQUAKV_EINVAL), ("tree", dict(table_pages=0), B.AQUAKV_EINVAL),
     ("tree", dict(max_queries=1 << 27, words=1 << 22), B.AQUAKV_EUNSUPPORTED),
     ("weights", dict(keep=float("nan")), B.AQUAKV_EINVAL), ("weights", dict(keep=float("inf")), B.AQUAKV_EINVAL), ("weights", dict(q_heads=12), B.AQUAKV_EINVAL),
-    ("weights", dict(table_pages=(1 << 25) - 1000, page_tokens=64), B.AQUAKV_EUNSUPPORTED), ("weights", dict(max_queries=-1), B.AQUAKV_EINVAL),
+    ("weights", dict(table_pages=(1 << 25) - 1000, page_tokens=64), B.AQUAKV_EUNSUPPORTED), ("weights", dict(table_pages=1 << 24, page_tokens=16), B.AQUAKV_EUNSUPPORTED), ("weights", dict(max_queries=-1), B.AQUAKV_EINVAL),
     ("select", dict(budget=-1), B.AQUAKV_EINVAL), ("select", dict(n_first=-1), B.AQUAKV_EINVAL), ("select", dict(n_last=-2), B.AQUAKV_EINVAL),
     ("select", dict(budget=4), B.AQUAKV_EINVAL), ("select", dict(n_first=1 << 30, n_last=1 << 30, budget=2147483647), B.AQUAKV_EINVAL),
     ("select", dict(table_pages=0), B.AQUAKV_EINVAL),
@@ -93,7 +93,7 @@ def test_sizes_that_all_refuse(call, kw, want):
     ("rotary", dict(dtype=3), B.AQUAKV_EINVAL), ("rotary", dict(tokens=-1), B.AQUAKV_EINVAL), ("rotary", dict(heads=0), B.AQUAKV_EINVAL),
     ("rotary", dict(rows=0), B.AQUAKV_EINVAL), ("rotary", dict(dim=0), B.AQUAKV_EINVAL), ("rotary", dict(dim=130), B.AQUAKV_EINVAL), ("rotary", dict(dim=33), B.AQUAKV_EINVAL),
     ("rotary", dict(dim=40), B.AQUAKV_EUNSUPPORTED), ("rotary", dict(layout=2), B.AQUAKV_EINVAL), ("rotary", dict(tokens=1 << 25), B.AQUAKV_EUNSUPPORTED),
-    ("rotary", dict(tokens=1 << 62), B.AQUAKV_EUNSUPPORTED), ("rotary", dict(x_stride=QH * 128 - 8), B.AQUAKV_EINVAL), ("rotary", dict(out_stride=QH * 128 + 4), B.AQUAKV_EALIGN)])
+    ("rotary", dict(tokens=1 << 62), B.AQUAKV_EUNSUPPORTED), ("rotary", dict(tokens=1 << 27, heads=1, x_stride=128, out_stride=128), B.AQUAKV_EUNSUPPORTED), ("rotary", dict(x_stride=QH * 128 - 8), B.AQUAKV_EINVAL), ("rotary", dict(out_stride=QH * 128 + 4), B.AQUAKV_EALIGN)])
 def test_sizes_of_each(call, kw, want):
     c = Buffers()
     c.n.update(kw)
@@ -186,6 +186,7 @@ def tables(rows=10, first=0, dim=64, base=1e4, factor=1.0, original=0.0, low=0.0
     (dict(original=8192.0, low=4.0, high=1.0), B.AQUAKV_EINVAL), (dict(original=8192.0, low=-1.0, high=1.0), B.AQUAKV_EINVAL),
     (dict(original=8192.0, low=1.0, high=float("inf")), B.AQUAKV_EINVAL), (dict(magnitude=float("nan")), B.AQUAKV_EINVAL), (dict(cos=None), B.AQUAKV_ENULL),
     (dict(sin=None), B.AQUAKV_ENULL), (dict(sin=(2 << 32) + 4), B.AQUAKV_EALIGN), (dict(sin=1 << 32), B.AQUAKV_EINVAL), (dict(sin=(1 << 32) + 1264), B.AQUAKV_EINVAL),
+    (dict(rows=1 << 29, dim=128), B.AQUAKV_EUNSUPPORTED), (dict(factor=1e-300), B.AQUAKV_EINVAL), (dict(base=1e-300), B.AQUAKV_EINVAL),
     (dict(rows=0, cos=None, sin=None), B.AQUAKV_OK)])
 def test_tables(kw, want):
     assert tables(**kw) == want, B.aquakv_last_error()
