@@ -153,9 +153,9 @@ template <int KEYS> __global__ __launch_bounds__(kSelectThreads) void select_hel
 }
 
 // Long sequences: a workgroup a slab of at least kSlab tokens, of which there are at most kMostSlabs, a launch a digit.  Each counts its slab's keys by the digit; the
-// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.  131 072 tokens: 6.6, 8.9, 8.3 and 10.4 us, of which
+// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.  131 072 tokens: 6.7, 8.0, 7.7 and 10.3 us, of which
 // a launch that reads 256 KB of counts from the caches is most (one workgroup for all of it: 140 us).
-constexpr int kSlab = 4096, kMostSlabs = 256;
+constexpr int kSlab = 4096, kMostSlabs = 256, kHeld = kSlab / kSelectThreads;
 struct Slabs {
   uint32_t* counts;                                        // [batch, 3, n, kBins]
   uint32_t* above;                                         // [batch, 2, n]: keys of a slab above the last one by their first, second digit
@@ -191,7 +191,12 @@ template <int DIGIT> __global__ __launch_bounds__(kSelectThreads) void slab_coun
   for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
   if (tid == 0) above = 0;
   Known k = {0u, (uint32_t)a.budget};
+  uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
+  const int from = slab * s.tokens, to = from + min(s.tokens, len - from);
+  uint32_t held[kHeld];                                    // the first ones, on their way while the digit before is found
   if constexpr (DIGIT > 0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = keys[min(from + i * kSelectThreads + tid, to - 1)];
     if (DIGIT == 2) k = s.known[2 * b];
     const Found f = found(s, k, b, DIGIT - 1, slabs, slab, true, scan);
     k = f.k;
@@ -201,10 +206,13 @@ template <int DIGIT> __global__ __launch_bounds__(kSelectThreads) void slab_coun
   }
   __syncthreads();
   if (DIGIT > 0 && tid == 0) s.above[((int64_t)b * 2 + DIGIT - 1) * s.n + slab] = above;
-  uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
-  const int from = slab * s.tokens, to = from + min(s.tokens, len - from);
+  if constexpr (DIGIT > 0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (from + i * kSelectThreads + tid < to && counts(held[i], k, DIGIT)) atomicAdd(&bins[digit_of(held[i], DIGIT)], 1u);
+  }
 #pragma unroll 4
-  for (int t = from + tid; t < to; t += kSelectThreads) {
+  for (int t = from + (DIGIT > 0 ? kHeld * kSelectThreads : 0) + tid; t < to; t += kSelectThreads) {
     const uint32_t x = DIGIT == 0 ? token_key(a, d, b, len, t) : keys[t];
     if (DIGIT == 0) keys[t] = x;
     if (counts(x, k, DIGIT)) atomicAdd(&bins[digit_of(x, DIGIT)], 1u);
@@ -224,6 +232,11 @@ __global__ __launch_bounds__(kSelectThreads) void slab_emit_kernel(const PagedSe
   if (slab >= slabs) return;
   if (slab == 0 && tid == 0) a.n_kept[b] = a.budget;
   if (tid < 2) before[tid] = 0;
+  const uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
+  const int each = s.tokens / kSelectWaves, from = (int)min((int64_t)slab * s.tokens + wave * each, (int64_t)len), to = from + min(each, len - from);
+  uint32_t held[kHeld];                                    // the first ones, on their way while the last digit is found
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = keys[min(from + 64 * i + lane, len - 1)];
   const Found f = found(s, s.known[2 * b + 1], b, 2, slabs, slab, false, scan);
   const Known k = f.k;
   __syncthreads();
@@ -236,10 +249,13 @@ __global__ __launch_bounds__(kSelectThreads) void slab_emit_kernel(const PagedSe
     atomicAdd(&before[0], more);
     atomicAdd(&before[1], same);
   }
-  const uint32_t* const keys = a.keys + (int64_t)b * s.n * s.tokens;
-  const int each = s.tokens / kSelectWaves, from = (int)min((int64_t)slab * s.tokens + wave * each, (int64_t)len), to = from + min(each, len - from);
   more = same = 0;
-  for (int i = from + lane; i < to; i += 64) {
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    more += from + 64 * i + lane < to && held[i] > k.prefix;
+    same += from + 64 * i + lane < to && held[i] == k.prefix;
+  }
+  for (int i = from + 64 * kHeld + lane; i < to; i += 64) {
     const uint32_t x = keys[i];
     more += x > k.prefix;
     same += x == k.prefix;
@@ -354,7 +370,7 @@ __global__ __launch_bounds__(kMoveThreads) void keep_in_place_kernel(const Paged
 }
 
 // kRowsEach entries a workgroup, whose places are worked out first: from pages to other pages, to the workspace, or back from it.  Bound by memory: 94 000 rows of 1 KB to other
-// pages 46 us, 4.5 TB/s; stores that went by the L2s' lines took 60 (as they are what is written and not read again).  blockIdx = (entries, sequence).
+// pages 48 us, 4.3 TB/s; stores that went by the L2s' lines took 60 (as they are what is written and not read again).  blockIdx = (entries, sequence).
 enum KeepWay : int { kAcross = 0, kOut = 1, kBack = 2 };
 constexpr int kRowsEach = 32, kAhead = 8;
 template <int WAY> __global__ __launch_bounds__(256) void keep_rows_kernel(const PagedKeepArgs a, const KeepLaunch l) {
