@@ -552,7 +552,8 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   anything in its mass afterwards.  After drafts were accepted (aquakv_paged_keep) the accepted ones are the last tokens, and their queries are taken here.
  *   Both dtypes: products of two fp16 numbers for each factor (22 bits), fp32 sums in a fixed order: the same bits each time.  Beyond the limits of
  *   aquakv_paged_attend: table_pages * page_tokens * kv_heads < 2^31.  workspace: aquakv_paged_weights_workspace_bytes() bytes, which hold the scores of all
- *   tokens there is room for where a kv head has at most 8 rows (queries x query heads).
+ *   tokens there is room for where a kv head has at most 8 rows (queries x query heads), else 8 bytes for each row and 32 tokens and 544 for each row.  A query
+ *   without numbers reaches the tokens that it sees, no others.
  *
  * aquakv_paged_select -- which tokens of a cache are kept: of each sequence the `budget` tokens with the largest mass, its first n_first and last
  *   n_last ones (n_first + n_last <= budget) whatever theirs is.  mass: fp32 [n_pages, kv_heads, page_tokens] as aquakv_paged_weights accumulates

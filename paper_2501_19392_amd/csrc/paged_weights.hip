@@ -259,7 +259,7 @@ __global__ __launch_bounds__(256) void weights_from_scores_kernel(const PagedAtt
     const f32x4 s = *reinterpret_cast<const f32x4*>(from);
     const f32x2 st = stat[r];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) gained[e] = __fmaf_rn(e < seen ? __builtin_amdgcn_exp2f(s[e] - st.x) : 0.f, st.y, gained[e]);
+    for (int e = 0; e < 4; ++e) gained[e] = e < seen ? __fmaf_rn(__builtin_amdgcn_exp2f(s[e] - st.x), st.y, gained[e]) : gained[e];
   }
   if (x.keep != 0.f && t < past) {
     const f32x4 old = *reinterpret_cast<const f32x4*>(to);
@@ -313,7 +313,7 @@ __device__ __forceinline__ int64_t token_tiles(const WeightsArgs& x) { return (x
 
 // Many rows: a wave has 32 tokens of a kv head as operands, which take their conversion once, and goes through the row tiles, whose operands its workgroup brings to LDS,
 // kStaged of them while the ones before are multiplied.  First for the statistics of the rows over its tokens, then, when those are joined, for the weights.
-// 64 queries of 4 heads a kv head over 12 288 tokens: 25.8 and 24.0 us, of which 6 are the way in; matrix cores busy in 45 % of a wave's time, vector pipes in as much, the rest
+// 64 queries of 4 heads a kv head over 12 288 tokens: 25.4 and 23.9 us, of which 6 are the way in; matrix cores busy in 45 % of a wave's time, vector pipes in as much, the rest
 // waits for operands from LDS, which is as busy.  (Row tiles requested behind a bound or a branch: 28 and 25; operands straight from the caches: 31 and 30.)
 // The grid is there once (look-ups are few, and meet in banks as they will): LDS has room for four workgroups.  blockIdx = (128 tokens and kv head, sequence).
 template <int NCW, bool MASS>
@@ -410,6 +410,12 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
       const int mine = 16 * tile + m, seen = mine < n_rows ? min(past + mine / rep + 1 - (t + 8 * g), held) : 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = e < seen ? y[e] : -INFINITY;
+      if constexpr (MASS) {                                // (a row without numbers reaches no token that it does not see)
+        const float ref = row.ref, inv = row.inv;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) gained[e] = e < seen ? __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref)), inv, gained[e]) : gained[e];
+        return;
+      }
     }
     if constexpr (MASS) {
       const float ref = row.ref, inv = row.inv;
@@ -419,12 +425,12 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
       float top = y[0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, y[e]);
-      const float ref = fmaxf(column_max(top) * f, -3.0e38f);
+      const float most = fmaxf(column_max(top) * f, -3.0e38f);
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -ref));
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__fmaf_rn(y[e], f, -most));
       const float sum = column_sum(sum_of(p));
-      if (g == 0) stats[(int64_t)tile * token_tiles(x) * 16] = f32x2{ref, sum};
+      if (g == 0) stats[(int64_t)tile * token_tiles(x) * 16] = f32x2{most, sum};
     }
   };
   const int from = first_tile(t, past, rep);

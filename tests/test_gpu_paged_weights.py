@@ -204,3 +204,24 @@ def test_a_pool_of_more_than_4_gib(n):
     torch.cuda.synchronize()
     at = torch.arange(6, dtype=torch.int32).view(2, 3)
     check(big[table.view(-1).long().cuda()].cpu(), mass, *wanted(lo, small, at, lens, q, [n, n], n, 1.0, mass))
+
+
+@pytest.mark.parametrize("backbone", ["grid256", "rtn4"])
+@pytest.mark.parametrize("n,bad", [(2, 0), (20, 3), (20, 18)])
+def test_query_without_numbers(backbone, n, bad):
+    """It reaches the tokens that it sees and no others: those get what they get from the later queries."""
+    QH, page, length = 4, 16, 150
+    lo, lg, pages = P.make(1, "bf16", backbone, 12, page)
+    gen = torch.Generator().manual_seed(n + bad)
+    P.fill(lo, pages, gen)
+    table, lens = torch.arange(12, dtype=torch.int32)[None], torch.tensor([length], dtype=torch.int32)
+    q = torch.randn(n, QH, 128, generator=gen).bfloat16().cuda()
+    mass = some_mass(pages, 1, gen)
+    seen = length - n + bad + 1                             # tokens that the bad query sees
+    want, bound, written = wanted(lo, pages, table, lens, q, [n], n, 1.0, mass)
+    q[bad, 1, 5] = torch.nan
+    got = weights(lg, pages, table, lens, q, [n], 1.0, mass).flatten()
+    assert got[:seen].isnan().all()
+    off = (got.double() - want.flatten())[seen:length].abs()
+    assert (off <= bound.flatten()[seen:length]).all()
+    assert torch.equal(got[length:], mass.flatten()[length:])
