@@ -118,3 +118,47 @@ def test_drafts_behind_almost_2_31_tokens():
     bound = (p * V.norm(dim=-1)[None] * (2 * d + 2 * top + 2 * u + 2 * (2 ** 15) * s)).sum(-1) + 2.0 ** -8 * want.norm(dim=-1)
     assert torch.isfinite(out).all()
     assert ((out[:, 0].double().cpu() - want).norm(dim=-1) <= bound).all()
+
+
+@pytest.mark.parametrize("backbone,n", [("grid256", 1), ("grid256", 6), ("rtn4", 5), ("grid256", 40)])
+def test_pages_beyond_2_32_bytes(backbone, n):
+    """The same rows at the start of a pool and beyond 2^32 bytes of codes: the same bits from all calls."""
+    from paper_2501_19392_amd import binding as B
+    from tests import tree_utils as T
+    H, QH, page, m = 8, 32, 256, 40                          # m pages of two sequences
+    n_pages = (1 << 32) // (H * 64) // page + m + 8
+    lo, lg, pages = P.make(H, "bf16", backbone, n_pages, page)
+    assert pages.k_codes.numel() > 1 << 32
+    gen = torch.Generator().manual_seed(n)
+    few = B.Pages(lg, m, page)
+    P.fill(lo, few, gen)
+    near, far = torch.arange(m, dtype=torch.int32).view(2, m // 2), n_pages - 1 - torch.arange(m, dtype=torch.int32).view(2, m // 2)
+    lens = torch.tensor([m // 2 * page - 3, 1111], dtype=torch.int32).cuda()
+    q = torch.randn(2 * n, QH, 128, generator=gen).bfloat16().cuda()
+    tree = torch.cat([T.words_of(T.random_tree(n, gen), 2) for _ in range(2)]).cuda()
+    first_mass = torch.rand(m, H, page, generator=gen).cuda()
+    results = []
+    for table in (near, far):
+        at = table.flatten().long()
+        rows = (at[:, None] * page + torch.arange(page)).flatten().cuda()
+        for k in ("k_codes", "k_scales", "v_codes", "v_scales"):
+            getattr(pages, k)[rows] = getattr(few, k)
+        mass = torch.zeros(n_pages, H, page, device="cuda")
+        mass[at.cuda()] = first_mass
+        table = table.cuda()
+        ws = torch.empty(B.aquakv_paged_workspace_bytes(lg, pages, 2, QH, m // 2, 2 * n, n), dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q)
+        B.aquakv_paged_attend_tree(lg, pages, 2, QH, table, lens, q, n, None, tree, SCALE, out, ws)
+        ws = torch.empty(B.aquakv_paged_weights_workspace_bytes(lg, pages, 2, QH, m // 2, 2 * n, n), dtype=torch.uint8, device="cuda")
+        B.aquakv_paged_weights(lg, pages, 2, QH, table, lens, q, n, None, SCALE, 0.5, mass, ws)
+        found = [out.clone(), mass[at.cuda()]]
+        kept, n_kept = torch.zeros(2, 700, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+        ws = torch.empty(B.aquakv_paged_select_workspace_bytes(lg, pages, 2, m // 2, 700) + 256, dtype=torch.uint8, device="cuda")
+        B.aquakv_paged_select(lg, pages, 2, table, lens, mass, 700, 3, 9, kept, n_kept, ws)
+        ws = torch.empty(B.aquakv_paged_keep_workspace_bytes(lg, pages, 2, 700, True) + 256, dtype=torch.uint8, device="cuda")
+        B.aquakv_paged_keep(lg, pages, 2, table, kept, n_kept, None, None, mass, ws)
+        found += [kept, n_kept, mass[at.cuda()]] + [getattr(pages, k)[rows] for k in ("k_codes", "k_scales", "v_codes", "v_scales")]
+        results.append([x.cpu() for x in found])
+    for i, (a, b) in enumerate(zip(*results)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+    assert torch.isfinite(results[0][0]).all()
