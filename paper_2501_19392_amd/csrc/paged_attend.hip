@@ -150,12 +150,15 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
   PagedPlan p = {};
   const int64_t rows = std::max<int64_t>(max_queries, 1) * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
   if (sizeof(T) == 2 && tree && tree_in_blocks(rows, is_rtn(NCW), batch * most * H)) {      // one workgroup a CU, pieces of equal size over all sequences
-    const int row_blocks = (int)((rows + kTileRows - 1) / kTileRows), slots = (int)std::max<int64_t>(256 / (H * row_blocks), 1);
+    const int row_blocks = (int)((rows + kTileRows - 1) / kTileRows), room = (int)std::max<int64_t>(256 / (H * row_blocks), 1);
+    // Whole sequences, with no results to keep and join, where they are several rounds of workgroups by themselves: 208 rows of 128 x 2000 tokens 312 us, in
+    // pieces 315, of 128 uneven ones 300, 305; 576 rows of 64 uneven ones of up to 4000 tokens 702, 714.
+    const int slots = batch >= 4 * room ? 1 : room;
     const int64_t tiles = std::max<int64_t>((table_pages * page_tokens + 63) / 64, 1);
-    const int64_t items = std::min(batch * tiles, std::max<int64_t>(slots - batch, std::max(slots / 2, 1)) + batch);
+    const int64_t items = slots == 1 ? batch : std::min(batch * tiles, std::max<int64_t>(slots - batch, std::max(slots / 2, 1)) + batch);
     if (items * H < (1 << 22)) {                           // (threads of a launch: below 2^32)
       p.row_blocks = row_blocks; p.slots = slots; p.items = items;
-      p.merge = tiles > 1;
+      p.merge = tiles > 1 && slots > 1;
       p.by_rows = items <= 16 * batch;
       p.many = items > kManyPieces * batch;
       return p;

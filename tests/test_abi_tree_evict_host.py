@@ -190,3 +190,11 @@ def tables(rows=10, first=0, dim=64, base=1e4, factor=1.0, original=0.0, low=0.0
     (dict(rows=0, cos=None, sin=None), B.AQUAKV_OK)])
 def test_tables(kw, want):
     assert tables(**kw) == want, B.aquakv_last_error()
+
+
+@pytest.mark.parametrize("batch,queries", [(32, 2048), (1, 2048), (64, 256), (1, 8192)])
+def test_chunks_need_no_results_of_pieces(batch, queries):
+    """Chunks of prompts, whose rows fill the chip by themselves: the one size for calls with and without a tree stays small."""
+    c = Buffers()
+    c.n.update(n_pages=100000, page_tokens=64, batch=batch, table_pages=256, q_rows=batch * queries, max_queries=queries)
+    assert 0 < c.size("tree") < 1 << 20

@@ -218,3 +218,17 @@ def test_a_pool_of_more_than_4_gib():
     at = torch.arange(6, dtype=torch.int32).view(2, 3)
     P.check(got, *T.reference(lo, small, at, lens, q, [n, n], trees, SCALE, "bf16"), "far")
     P.check(got_wide, *T.reference(lo, small, at, lens, wide, [40, 40], wide_trees, SCALE, "bf16"), "far, blocks of rows")
+
+
+@pytest.mark.parametrize("fmt", ["grid64", "rtn4"])
+def test_many_sequences_in_blocks_of_rows(fmt):
+    """So many that each is taken whole: uneven lengths, sequences without rows or tokens, rows that are not answered."""
+    H, QH, page, most = 8, 128, 16, 17
+    gen = torch.Generator().manual_seed(77)
+    lengths = [320, 0, 1, 17, 64, 65] + torch.randint(17, 320, (58,), generator=gen).tolist()
+    counts = [17, 0, 1, 17, 17, 0] + torch.randint(0, 18, (58,), generator=gen).tolist()
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, H, lengths, page, seed=8)
+    trees = [T.random_tree(n, gen) for n in counts]
+    q = queries(gen, sum(counts), QH, "bf16")
+    got = attend(lg, pages, table, lens, q, counts, trees, max_queries=most)
+    P.check(got, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, "bf16"), fmt)
