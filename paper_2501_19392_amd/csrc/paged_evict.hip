@@ -29,22 +29,44 @@ __device__ __forceinline__ uint32_t key_of(float mass) {
 }
 constexpr uint32_t kAlways = 0xffffffffu;
 __device__ __forceinline__ int cached(const PagedSelectArgs& a, int b) { return (int)min((int64_t)max(a.seq_lens[b], 0), (int64_t)a.table_pages * a.page_tokens); }
-__device__ __forceinline__ uint32_t token_key(const PagedSelectArgs& a, const PageDivider& d, int b, int len, int t) {
-  const Place at = place_of_token(a.page_table + (int64_t)b * a.table_pages, a.table_pages, d, a.n_pages, t);
-  if (at.page < 0) return 0u;
-  if (t < a.n_first || t >= len - a.n_last) return kAlways;
-  const float* const mass = a.mass + (int64_t)at.page * a.H * a.page_tokens + at.in;
-  float sum = mass[0];
-  int h = 1;
-  for (; h + 7 <= a.H; h += 7) {                           // (requested together, added in order)
-    float x[7];
+// The keys of N tokens, `step` apart from t on, for those below `to` (at least one token; the others: anything).  Without branches, so that the tokens' pages are
+// looked up together, then their masses, kHeads of each at once: one sequence of 131 072 tokens to 32 768 45.9 us with the moves, one token after the other 47.3.
+template <int N> __device__ __forceinline__ void token_keys(const PagedSelectArgs& a, const PageDivider& d, int b, int len, int t, int step, int to, uint32_t (&key)[N]) {
+  constexpr int kHeads = 4;
+  const int32_t* const table = a.page_table + (int64_t)b * a.table_pages;
+  uint32_t in[N];
+  int page[N];
 #pragma unroll
-    for (int i = 0; i < 7; ++i) x[i] = mass[(int64_t)(h + i) * a.page_tokens];
-#pragma unroll
-    for (int i = 0; i < 7; ++i) sum += x[i];
+  for (int k = 0; k < N; ++k) {
+    const uint32_t token = (uint32_t)min((int64_t)t + (int64_t)k * step, (int64_t)to - 1);
+    uint32_t p = (uint32_t)(((uint64_t)token * d.magic) >> 32);              // (one short at most)
+    if (token - p * d.tokens >= d.tokens) ++p;
+    in[k] = token - p * d.tokens;
+    page[k] = table[p];
+    key[k] = (int)token < a.n_first || (int)token >= len - a.n_last ? kAlways : 1u;
   }
-  for (; h < a.H; ++h) sum += mass[(int64_t)h * a.page_tokens];
-  return key_of(sum);
+  const float* at[N];
+  float sum[N] = {};
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const bool there = (uint32_t)page[k] < (uint32_t)a.n_pages;
+    at[k] = a.mass + (int64_t)(there ? page[k] : 0) * a.H * a.page_tokens + in[k];
+    if (!there) key[k] = 0u;
+  }
+  for (int h = 0; h < a.H; h += kHeads) {                  // (added in order)
+    float x[N][kHeads];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k][i] = at[k][(int64_t)min(h + i, a.H - 1) * a.page_tokens];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) sum[k] = h + i < a.H ? sum[k] + x[k][i] : sum[k];
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (key[k] == 1u) key[k] = key_of(sum[k]);
 }
 
 // The budget-th largest key digit by digit: 11, 11 and 10 bits.  What is known of it ahead of a digit: the ones before it, and how many tokens are still to be taken
@@ -77,7 +99,6 @@ __device__ __forceinline__ Known next_digit(Known k, int digit, uint32_t x, uint
 // Whether a key counts for a digit, and for which value of it.
 __device__ __forceinline__ bool counts(uint32_t key, const Known& k, int digit) { return digit == 0 || key >> (shift_of(digit) + width_of(digit)) == k.prefix; }
 __device__ __forceinline__ uint32_t digit_of(uint32_t key, int digit) { return (key >> shift_of(digit)) & ((1u << width_of(digit)) - 1u); }
-
 // The tokens of a run that are kept, in order: `at` of this sequence's, and `tie` that have the last key, lie before it.  64 at a time, one wave.
 template <typename Key> __device__ __forceinline__ void emit(int32_t* kept, const Known& k, uint32_t at, uint32_t tie, int from, int to, const Key& key) {
   const int lane = threadIdx.x & 63;
@@ -120,10 +141,17 @@ template <int KEYS> __global__ __launch_bounds__(kSelectThreads) void select_hel
   if (keeps_all(a, b, len, tid, kSelectThreads)) return;
   for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
   __syncthreads();
-  for (int i = tid; i < len; i += kSelectThreads) {
-    const uint32_t x = token_key(a, d, b, len, i);
-    keys[i] = x;
-    atomicAdd(&bins[digit_of(x, 0)], 1u);
+  constexpr int kAtOnce = 8;
+  for (int i0 = 0; i0 < len; i0 += kAtOnce * kSelectThreads) {
+    uint32_t x[kAtOnce];
+    token_keys(a, d, b, len, i0 + tid, kSelectThreads, len, x);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k * kSelectThreads + tid;
+      if (i >= len) break;
+      keys[i] = x[k];
+      atomicAdd(&bins[digit_of(x[k], 0)], 1u);                               // (adding up those of a wave first takes longer: 16.8 us)
+    }
   }
   __syncthreads();
   Known k = {0u, (uint32_t)a.budget};
@@ -153,7 +181,7 @@ template <int KEYS> __global__ __launch_bounds__(kSelectThreads) void select_hel
 }
 
 // Long sequences: a workgroup a slab of at least kSlab tokens, of which there are at most kMostSlabs, a launch a digit.  Each counts its slab's keys by the digit; the
-// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.  131 072 tokens: 6.7, 8.0, 7.7 and 10.3 us, of which
+// next launch adds the slabs up (every workgroup for itself) and counts the digit behind it; the last one writes the tokens.  131 072 tokens: 5.4, 7.8, 7.6 and 10.2 us, of which
 // a launch that reads 256 KB of counts from the caches is most (one workgroup for all of it: 140 us).
 constexpr int kSlab = 4096, kMostSlabs = 256, kHeld = kSlab / kSelectThreads;
 struct Slabs {
@@ -206,16 +234,25 @@ template <int DIGIT> __global__ __launch_bounds__(kSelectThreads) void slab_coun
   }
   __syncthreads();
   if (DIGIT > 0 && tid == 0) s.above[((int64_t)b * 2 + DIGIT - 1) * s.n + slab] = above;
-  if constexpr (DIGIT > 0) {
+  if constexpr (DIGIT == 0) {
+    for (int t = from; t < to; t += kHeld * kSelectThreads) {
+      token_keys(a, d, b, len, t + tid, kSelectThreads, to, held);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        if (t + tid >= to - i * kSelectThreads) break;
+        keys[t + tid + i * kSelectThreads] = held[i];
+        atomicAdd(&bins[digit_of(held[i], 0)], 1u);
+      }
+    }
+  } else {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
       if (from + i * kSelectThreads + tid < to && counts(held[i], k, DIGIT)) atomicAdd(&bins[digit_of(held[i], DIGIT)], 1u);
-  }
 #pragma unroll 4
-  for (int t = from + (DIGIT > 0 ? kHeld * kSelectThreads : 0) + tid; t < to; t += kSelectThreads) {
-    const uint32_t x = DIGIT == 0 ? token_key(a, d, b, len, t) : keys[t];
-    if (DIGIT == 0) keys[t] = x;
-    if (counts(x, k, DIGIT)) atomicAdd(&bins[digit_of(x, DIGIT)], 1u);
+    for (int t = from + kHeld * kSelectThreads + tid; t < to; t += kSelectThreads) {
+      const uint32_t x = keys[t];
+      if (counts(x, k, DIGIT)) atomicAdd(&bins[digit_of(x, DIGIT)], 1u);
+    }
   }
   __syncthreads();
   uint32_t* const out = s.counts + (((int64_t)b * 3 + DIGIT) * s.n + slab) * kBins;
