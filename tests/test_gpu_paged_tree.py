@@ -232,3 +232,19 @@ def test_many_sequences_in_blocks_of_rows(fmt):
     q = queries(gen, sum(counts), QH, "bf16")
     got = attend(lg, pages, table, lens, q, counts, trees, max_queries=most)
     P.check(got, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, "bf16"), fmt)
+
+
+@pytest.mark.parametrize("fmt,QH,n", [("grid256", 4, 3), ("grid256", 16, 12), ("rtn4", 16, 9), ("grid64", 64, 30), ("rtn2", 64, 20)])
+def test_query_without_numbers(fmt, QH, n):
+    """Rows of one that has none are NaN (whatever bits it has), all others what they are."""
+    H, page, lengths = 1, 16, [700, 90]
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, H, lengths, page, seed=9)
+    trees = [T.random_tree(n, gen) for _ in lengths]
+    q = queries(gen, 2 * n, QH, "bf16")
+    want, bound = T.reference(lo, pages, table, lens, q, [n, n], trees, SCALE, "bf16")
+    bad = torch.zeros(2 * n, QH, dtype=torch.bool)
+    bad[n // 2, QH - 1] = bad[n + 1, 0] = True
+    q[bad.cuda()] = float("nan")
+    got = attend(lg, pages, table, lens, q, [n, n], trees)
+    assert got.cpu()[bad].isnan().all()
+    P.check(got.cpu()[~bad], want[~bad], bound[~bad], fmt)
