@@ -29,12 +29,13 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
   const int pos = a.positions[t];
   const bool turn = piece < turned;
   const int at = turn ? piece * N : a.dim + (piece - turned) * N;
-  const T* const x = static_cast<const T*>(a.x) + t * a.x_stride + at;
-  T* const out = static_cast<T*>(a.out) + t * a.out_stride + at;
+  const int64_t first = (int64_t)h0 * kGroup + at;         // (a row may pass 2^31 coordinates)
+  const T* const x = static_cast<const T*>(a.x) + t * a.x_stride + first;
+  T* const out = static_cast<T*>(a.out) + t * a.out_stride + first;
   float v[kHeads][N], w[kHeads][N];
 #pragma unroll
   for (int k = 0; k < kHeads; ++k) {
-    const int h = min(h0 + k, a.heads - 1);
+    const int h = min(k, a.heads - 1 - h0);
     Storage<T>::load(x + h * kGroup, v[k]);
     if (!PAIRS && turn) Storage<T>::load(x + h * kGroup + half, w[k]);
   }
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
 #pragma unroll
   for (int k = 0; k < kHeads; ++k) {
     if (h0 + k >= a.heads) break;
-    Storage<T>::template store<false>(out + (h0 + k) * kGroup, 0, v[k]);
-    if (!PAIRS && turn) Storage<T>::template store<false>(out + (h0 + k) * kGroup + half, 0, w[k]);
+    Storage<T>::template store<false>(out + k * kGroup, 0, v[k]);
+    if (!PAIRS && turn) Storage<T>::template store<false>(out + k * kGroup + half, 0, w[k]);
   }
 }
 

@@ -122,3 +122,36 @@ def test_tables(rows, first, dim, base, scaling, magnitude):
     for got, want in ((cos, angle.cos()), (sin, angle.sin())):
         off = (got[:rows].cpu().double() - magnitude * want).abs()
         assert (off <= bound).all(), (off / bound).max()
+
+
+@pytest.mark.parametrize("dtype,layout,dim,in_place", [("bf16", "half", 64, False), ("fp32", "pairs", 128, True)])
+def test_a_row_of_more_than_2_31_coordinates(dtype, layout, dim, in_place):
+    """Heads from 2^24 on are found: every part of the row is, to the bit, what a call on that part alone gives, and what lies beside the rows is left."""
+    from paper_2501_19392_amd import binding as B
+    heads, beside, part = (1 << 24) + 5, 9, 1 << 21
+    print(f"case rotary {dtype} {layout} heads={heads} in_place={in_place}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    wide = torch.empty(1, beside + heads + beside, 128, dtype=TYPES[dtype], device="cuda")
+    for h in range(0, wide.shape[1], part):
+        wide[:, h:h + part] = torch.randn(wide[:, h:h + part].shape, generator=gen, device="cuda")
+    before = wide.clone()
+    x = wide[:, beside:beside + heads]
+    room = wide if in_place else torch.full_like(wide, 7.0)
+    out = room[:, beside:beside + heads]
+    angle = torch.rand(3, dim // 2, generator=gen, device="cuda") * 6.28
+    cos, sin, positions = angle.cos(), angle.sin(), torch.tensor([2], dtype=torch.int32, device="cuda")
+    B.aquakv_rotary(x, positions, cos, sin, dim, layout, out)
+    torch.cuda.synchronize()
+    for h in range(0, heads, part):
+        source = before[:, beside + h:beside + min(h + part, heads)]
+        want = torch.empty_like(source)
+        B.aquakv_rotary(source, positions, cos, sin, dim, layout, want)
+        assert torch.equal(out[:, h:h + part], want), h
+    for edge in (slice(None, beside), slice(beside + heads, None)):
+        assert torch.equal(room[:, edge], before[:, edge]) if in_place else (room[:, edge] == 7.0).all()
+    if not in_place:
+        assert torch.equal(wide, before)
+    last = before[:, beside + heads - 1:beside + heads].cpu().double()
+    want, size = rotated(last, cos[2:].cpu().double(), sin[2:].cpu().double(), dim, layout, False)
+    bound = HALF_STEP[dtype] * want.abs() + (1 + HALF_STEP[dtype]) * 2.0 ** -24 * (size + want.abs())
+    assert ((out[:, -1:].cpu().double() - want).abs() <= bound).all()
