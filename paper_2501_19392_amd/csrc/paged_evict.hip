@@ -120,13 +120,14 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
   return x;
 }
 // Everything but the choice: what is behind the tokens that are kept, and sequences that keep all of theirs.  -> whether that was all
+// (counted without a sign: a step past a budget or length near 2^31 stays above it)
 __device__ __forceinline__ bool keeps_all(const PagedSelectArgs& a, int b, int len, int tid, int threads) {
   const int n = min(len, a.budget);
   int32_t* const kept = a.kept + (int64_t)b * a.budget;
-  for (int i = n + tid; i < a.budget; i += threads) kept[i] = -1;
+  for (uint32_t i = n + tid; i < (uint32_t)a.budget; i += threads) kept[i] = -1;
   if (tid == 0) a.n_kept[b] = n;
   if (n != 0 && len <= a.budget)
-    for (int i = tid; i < n; i += threads) kept[i] = i;
+    for (uint32_t i = tid; i < (uint32_t)n; i += threads) kept[i] = (int32_t)i;
   return n == 0 || len <= a.budget;
 }
 

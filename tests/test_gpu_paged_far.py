@@ -162,3 +162,28 @@ def test_pages_beyond_2_32_bytes(backbone, n):
     for i, (a, b) in enumerate(zip(*results)):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
     assert torch.isfinite(results[0][0]).all()
+
+
+@pytest.mark.parametrize("room,length,batch", [(PAGE, 100, 1), (130 * PAGE, 17, 2), (PAGES * PAGE, PAGES * PAGE - 5, 1)])
+def test_a_budget_of_almost_2_31_tokens(room, length, batch):
+    """The list's end is reached and not passed: by one workgroup, by all slabs', and where almost as many tokens are kept."""
+    from paper_2501_19392_amd import binding as B
+    budget, beside = (1 << 31) - 1, 1 << 16
+    print(f"case budget room={room} length={length} batch={batch}", flush=True)
+    lo, lg, pages, table, gen = make(5)
+    table = table[:, :room // PAGE].repeat(batch, 1).contiguous()
+    mass = torch.rand(4, 1, PAGE, generator=gen).cuda()
+    lens = torch.full((batch,), length, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.aquakv_paged_select_workspace_bytes(lg, pages, batch, room // PAGE, budget), dtype=torch.uint8, device="cuda")
+    wide, n = torch.full((beside + batch * budget + beside,), 7, dtype=torch.int32, device="cuda"), torch.zeros(batch, dtype=torch.int32, device="cuda")
+    kept = wide[beside:beside + batch * budget].view(batch, budget)
+    B.aquakv_paged_select(lg, pages, batch, table, lens, mass, budget, 3, 4, kept, n, ws)
+    torch.cuda.synchronize()
+    assert n.tolist() == [length] * batch
+    part = 1 << 28
+    for row in kept:
+        for i in range(0, budget, part):
+            want = torch.arange(i, min(i + part, budget), device="cuda", dtype=torch.int32)
+            want[max(length - i, 0):] = -1
+            assert torch.equal(row[i:i + part], want), i
+    assert (wide[:beside] == 7).all() and (wide[beside + batch * budget:] == 7).all()
