@@ -531,8 +531,9 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   it (of 64 tokens), with all its bits down to 2^-22 of that.
  *   A call is laid out by max_queries: sequences of few queries beside one of more than 128 rows (queries x query heads of a kv head) take
  *   many times what they take in a call of their own.
- *   workspace: aquakv_paged_workspace_bytes() bytes (0 on invalid arguments) for the same layer, pages and sizes (other sizes may
- *   need more, smaller ones too); the call may write all of it, and nothing in it needs clearing.  Calls that may run at the same
+ *   workspace: aquakv_paged_attend_workspace_bytes() bytes (0 on invalid arguments) for the same layer, pages and sizes (other sizes may
+ *   need more, smaller ones too), with_tree 0, or 1 for aquakv_paged_attend_tree, whose pieces have results where a chunk of a prompt needs none;
+ *   aquakv_paged_workspace_bytes() are enough for either call.  The call may write all of it, and nothing in it needs clearing.  Calls that may run at the same
  *   time, captured ones included, need workspaces of their own.  At most 65535 sequences, max_queries * q_heads < 2^22, max_queries *
  *   (q_heads / kv_heads) <= 16 * 65535, q_rows < 2^31, batch * kv_heads < 2^25, table_pages * page_tokens < 2^31 - 4096 and 2^35 over
  *   the batch: AQUAKV_EUNSUPPORTED beyond.
@@ -585,6 +586,8 @@ int aquakv_paged_append(const aquakv_layer* layer, const aquakv_pages* pages, in
                         const float* rope_sin, int32_t rope_rows, void* Khat, void* Vhat, void* stream);
 size_t aquakv_paged_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads,
                                     int32_t table_pages, int64_t q_rows, int32_t max_queries);
+size_t aquakv_paged_attend_workspace_bytes(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads,
+                                           int32_t table_pages, int64_t q_rows, int32_t max_queries, int32_t with_tree);
 int aquakv_paged_attend(const aquakv_layer* layer, const aquakv_pages* pages, int32_t batch, int32_t q_heads, const int32_t* page_table,
                         int32_t table_pages, const int32_t* seq_lens, int64_t q_rows, int32_t max_queries, const int32_t* q_start,
                         const void* q, int64_t q_stride, float score_scale, void* out, void* workspace, size_t workspace_bytes,

@@ -42,7 +42,7 @@ EXPORTS = [
     "aquakv_fit_workspace_bytes", "aquakv_fit_predictor",
     "aquakv_softmax", "aquakv_weighted_workspace_bytes", "aquakv_decode_values_weighted", "aquakv_decode_values_attend",
     "aquakv_attend_raw", "aquakv_copy_ranges", "aquakv_encode_layers", "aquakv_attend_cache_workspace_bytes", "aquakv_attend_cache",
-    "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend", "aquakv_paged_attend_tree",
+    "aquakv_paged_append", "aquakv_paged_workspace_bytes", "aquakv_paged_attend_workspace_bytes", "aquakv_paged_attend", "aquakv_paged_attend_tree",
     "aquakv_paged_weights_workspace_bytes", "aquakv_paged_weights",
     "aquakv_paged_select_workspace_bytes", "aquakv_paged_select", "aquakv_paged_keep_workspace_bytes", "aquakv_paged_keep",
     "aquakv_rotary", "aquakv_rotary_tables",
@@ -128,6 +128,8 @@ _PP, _I32, _I64 = ctypes.POINTER(aquakv_pages), ctypes.c_int32, ctypes.c_int64
 _lib.aquakv_paged_append.argtypes = [_LP, _PP, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _I32, _P, _P, _P]
 _lib.aquakv_paged_workspace_bytes.restype = ctypes.c_size_t
 _lib.aquakv_paged_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, _I32]
+_lib.aquakv_paged_attend_workspace_bytes.restype = ctypes.c_size_t
+_lib.aquakv_paged_attend_workspace_bytes.argtypes = [_LP, _PP, _I32, _I32, _I32, _I64, _I32, _I32]
 _lib.aquakv_paged_attend.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
 _lib.aquakv_paged_attend_tree.argtypes = [_LP, _PP, _I32, _I32, _P, _I32, _P, _I64, _I32, _P, _P, _I32, _P, _I64, ctypes.c_float, _P, _P, ctypes.c_size_t, _P]
 _F32, _F64, _SZ = ctypes.c_float, ctypes.c_double, ctypes.c_size_t
@@ -554,6 +556,11 @@ def aquakv_paged_append(layer, pages, tokens: int, K, V, slots, positions, rope_
 
 def aquakv_paged_workspace_bytes(layer, pages, batch: int, q_heads: int, table_pages: int, q_rows: int, max_queries: int) -> int:
     return _lib.aquakv_paged_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table_pages, q_rows, max_queries)
+
+
+def aquakv_paged_attend_workspace_bytes(layer, pages, batch: int, q_heads: int, table_pages: int, q_rows: int, max_queries: int, with_tree: bool) -> int:
+    """What aquakv_paged_attend needs, or (with_tree) aquakv_paged_attend_tree; aquakv_paged_workspace_bytes: enough for either."""
+    return _lib.aquakv_paged_attend_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, q_heads, table_pages, q_rows, max_queries, int(with_tree))
 
 
 def aquakv_paged_attend(layer, pages, batch: int, q_heads: int, page_table, seq_lens, q, max_queries: int, q_start, score_scale: float, out,

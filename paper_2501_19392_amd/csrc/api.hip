@@ -1727,13 +1727,19 @@ int aquakv_paged_append(const aquakv_layer* L, const aquakv_pages* pages, int64_
   return AQUAKV_OK;
 }
 
-size_t aquakv_paged_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, int32_t table_pages,
-                                    int64_t q_rows, int32_t max_queries) {
+size_t aquakv_paged_attend_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, int32_t table_pages,
+                                           int64_t q_rows, int32_t max_queries, int32_t with_tree) {
   if (check_paged_shape(L, pages, batch, q_heads, table_pages, q_rows, max_queries) != AQUAKV_OK) return 0;
   aquakv::PagedAttendArgs a = {};
   a.pool = pool_of(pages);
   a.batch = batch; a.table_pages = table_pages; a.max_queries = max_queries; a.q_heads = q_heads; a.H = L->kv_heads;
-  return (aquakv::paged_attend_workspace_bytes(L->dtype, quantizer_id(L), a) + 255) / 256 * 256 + 256;
+  return (aquakv::paged_attend_workspace_bytes(L->dtype, quantizer_id(L), a, with_tree != 0) + 255) / 256 * 256 + 256;
+}
+
+size_t aquakv_paged_workspace_bytes(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch, int32_t q_heads, int32_t table_pages,
+                                    int64_t q_rows, int32_t max_queries) {
+  return std::max(aquakv_paged_attend_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries, 0),
+                  aquakv_paged_attend_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries, 1));
 }
 
 namespace {
@@ -1758,7 +1764,7 @@ int paged_attend(const aquakv_layer* L, const aquakv_pages* pages, int32_t batch
   CHECK(check_rows(q, "q", q_stride, row, eb));
   CHECK(check_ptr(out, "out", true));
   CHECK(check_ptr(workspace, "workspace", true));
-  const size_t need = aquakv_paged_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries);
+  const size_t need = aquakv_paged_attend_workspace_bytes(L, pages, batch, q_heads, table_pages, q_rows, max_queries, with_tree);
   if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
   const PoolRanges pool = pool_ranges(L, pages);
   const Params params = params_of(L);

@@ -274,7 +274,7 @@ struct PagedAttendArgs {
   const uint32_t* tree;                           // nullable, [q_rows, tree_words]: bit j of row r: it sees draft j of its sequence (paged_tree.hip)
   int tree_words;
 };
-size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a);
+size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a, bool tree);
 // Many queries (bf16): 8 waves x 32 rows per workgroup.
 hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_tree_rows(int dtype, int n_codewords, int cols, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream);

@@ -216,13 +216,9 @@ static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a, b
   return p;
 }
 
-size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a) {
-  size_t most = 0;                                         // (one size for calls with and without a tree)
-  for (const bool tree : {false, true}) {
-    const PagedPlan p = plan_of(dtype, n_codewords, a, tree);
-    if (p.merge) most = std::max(most, (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2));
-  }
-  return most;
+size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a, bool tree) {
+  const PagedPlan p = plan_of(dtype, n_codewords, a, tree);
+  return p.merge ? (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2) : 0;
 }
 
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& args, void* workspace, hipStream_t stream) {

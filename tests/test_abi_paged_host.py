@@ -183,3 +183,28 @@ def test_more_than_a_launch_holds(kw):
     c = Buffers(**({"kv_heads": kw["kv_heads"]} if "kv_heads" in kw else {}))
     c.n.update({k: v for k, v in kw.items() if k != "kv_heads"})
     assert c.attend() == B.AQUAKV_EUNSUPPORTED and c.size() == 0
+
+
+@pytest.mark.parametrize("batch,queries,pages,page,want", [
+    (32, 64, 64, 64, 256), (8, 512, 64, 64, 256), (32, 128, 256, 64, 256), (8, 256, 64, 64, 256), (128, 48, 63, 64, 256),      # blocks of 256 rows that fill the chip
+    (1, 512, 96, 64, (4 * 512 * QH * 130 * 4 + 8 + 255) // 256 * 256 + 256)])                                                  # 8 blocks of 8 heads in 4 pieces
+def test_chunks_need_their_own_workspace_and_no_more(batch, queries, pages, page, want):
+    """Not that of a tree of as many drafts: the call takes what its own size says, and refuses a byte less."""
+    c = Buffers()
+    c.n.update(n_pages=100000, page_tokens=page, batch=batch, table_pages=pages, q_rows=batch * queries, max_queries=queries)
+    sizes = (c.layer, c.pages(), batch, QH, pages, batch * queries, queries)
+    plain, tree = (B._lib.aquakv_paged_attend_workspace_bytes(*sizes, i) for i in (0, 1))
+    assert plain == want and c.size() == max(plain, tree)
+    c.n["ws"] = plain - 1
+    assert c.attend() == B.AQUAKV_EWORKSPACE
+    c.n["ws"], c.a["out"] = plain, c.a["q"]                   # (what is looked at behind the workspace: nothing is launched)
+    assert c.attend() == B.AQUAKV_EINVAL and "overlaps" in B.aquakv_last_error()
+
+
+def test_sizes_of_calls_that_are_refused_are_0():
+    for kw in (dict(batch=-1), dict(batch=70000), dict(q_heads=12), dict(table_pages=0)):
+        c = Buffers()
+        c.n.update(kw)
+        n = c.n
+        for tree in (0, 1):
+            assert B._lib.aquakv_paged_attend_workspace_bytes(c.layer, c.pages(), n["batch"], n["q_heads"], n["table_pages"], n["q_rows"], n["max_queries"], tree) == 0

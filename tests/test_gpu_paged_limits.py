@@ -142,3 +142,30 @@ def test_equal_weights_of_two_million_tokens(batch, queries, step):
     print(f"  off by {off:.3g}", flush=True)
     # (a query sees up to 130 tokens less of 2^21, 2^-14 of them)
     assert off <= 3 * 2.0 ** -8 + 2.0 ** -13
+
+
+@pytest.mark.parametrize("fmt,QH,counts,tree", [("grid256", 32, [33] * 32, False), ("grid256", 32, [33] * 32, True), ("grid64", 8, [1] * 5, False), ("grid64", 8, [1] * 5, True),
+                                                ("rtn4", 32, [64] * 3, False), ("rtn4", 32, [64] * 3, True)])
+def test_each_call_with_its_own_workspace(fmt, QH, counts, tree):
+    """What its size says and no byte of what lies behind."""
+    need_gpu()
+    from paper_2501_19392_amd import binding as B
+    from tests import tree_utils as T
+    print(f"case own workspace {fmt} QH={QH} {counts[0]} of {len(counts)} tree={tree}", flush=True)
+    n, batch = counts[0], len(counts)
+    lengths = [n + (61 * b) % 240 for b in range(batch)]
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, 8, lengths, 16, seed=11)
+    trees = [T.random_tree(n, gen) if tree else torch.ones(n, n, dtype=torch.bool).tril() for _ in counts]
+    q = (1.5 * torch.randn(n * batch, QH, 128, generator=gen)).bfloat16().cuda()
+    size = B.aquakv_paged_attend_workspace_bytes(lg, pages, batch, QH, table.shape[1], n * batch, n, tree)
+    if len(counts) == 32:
+        assert (size == 256) != tree                       # (sequences fill the chip: whole ones, and trees of few rows in pieces)
+    ws, out = torch.full((size + 4096,), 0xFF, dtype=torch.uint8, device="cuda"), torch.full_like(q, float("nan"))
+    if tree:
+        bits = torch.cat([T.words_of(t, -(-n // 32)) for t in trees]).cuda()
+        B.aquakv_paged_attend_tree(lg, pages, batch, QH, table.cuda(), lens.cuda(), q, n, None, bits, SCALE, out, ws[:size])
+    else:
+        B.aquakv_paged_attend(lg, pages, batch, QH, table.cuda(), lens.cuda(), q, n, None, SCALE, out, ws[:size])
+    torch.cuda.synchronize()
+    assert (ws[size:] == 0xFF).all()
+    P.check(out, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, "bf16"), fmt)
