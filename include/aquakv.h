@@ -569,7 +569,7 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   pages that to_table [batch, to_pages] names, which may not be ones that the call reads; entries in any order, some more than once.  What goes from or to a
  *   token outside its table or a page that is not in the pool is left out.  Rows that are written against this, or for two entries or sequences, hold
  *   anything afterwards, and so does what is read from such rows.  Keys keep the rotation that they have.
- *   workspace: aquakv_paged_keep_workspace_bytes() bytes for the same layer, pages and sizes (with_mass: 0, or 1 where mass is given).
+ *   workspace: aquakv_paged_keep_workspace_bytes() bytes for the same layer, pages and sizes (with_mass: 0, or 1 where mass is given); 256 with to_table.
  *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens
  * (tokens = 0), sequences or queries (batch, q_rows or max_queries = 0) nothing is done, and buffers but the pool's may be NULL.

@@ -668,6 +668,7 @@ def aquakv_paged_select(layer, pages, batch: int, page_table, seq_lens, mass, bu
 
 
 def aquakv_paged_keep_workspace_bytes(layer, pages, batch: int, max_kept: int, with_mass: bool) -> int:
+    """What moves in place need; to other pages (to_table) 256 bytes do."""
     return _lib.aquakv_paged_keep_workspace_bytes(_layer_ref(layer), _pages_ref(pages), batch, max_kept, int(with_mass))
 
 

@@ -1913,7 +1913,8 @@ int aquakv_paged_keep(const aquakv_layer* L, const aquakv_pages* pages, int32_t 
   if (misaligned_to(to_table, 4)) return fail(AQUAKV_EALIGN, "to_table is not 4-byte aligned");
   CHECK(check_ptr(mass, "mass", false));
   CHECK(check_ptr(workspace, "workspace", true));
-  const size_t need = aquakv_paged_keep_workspace_bytes(L, pages, batch, max_kept, mass != nullptr);
+  // (rows that go to other pages are not staged)
+  const size_t need = to_table != nullptr ? 256 : aquakv_paged_keep_workspace_bytes(L, pages, batch, max_kept, mass != nullptr);
   if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
   const PoolRanges pool = pool_ranges(L, pages);
   const size_t tokens = (size_t)pages->n_pages * pages->page_tokens, ints = (size_t)batch * sizeof(int32_t);

@@ -198,3 +198,19 @@ def test_chunks_need_no_results_of_pieces(batch, queries):
     c = Buffers()
     c.n.update(n_pages=100000, page_tokens=64, batch=batch, table_pages=256, q_rows=batch * queries, max_queries=queries)
     assert 0 < c.size("tree") < 1 << 20
+
+
+@pytest.mark.parametrize("batch,most", [(1, 32768), (3, 65536), (2, 7)])
+def test_rows_to_other_pages_need_no_room_for_them(batch, most):
+    """Only moves in place of few sequences go through the workspace."""
+    c = Buffers()
+    c.n.update(n_pages=100000, page_tokens=64, batch=batch, table_pages=2000, to_pages=1200, max_kept=most)
+    c.n["ws"] = 255
+    assert c.keep() == B.AQUAKV_EWORKSPACE
+    c.n["ws"], c.a["mass"] = 256, c.a["kept"]                 # (what is looked at behind the workspace: nothing is launched)
+    assert c.keep() == B.AQUAKV_EINVAL and "overlaps" in B.aquakv_last_error()
+    c.a["to"] = None
+    if most > 1024:
+        assert c.size("keep") > most * 1024 and c.keep() == B.AQUAKV_EWORKSPACE
+    else:
+        assert c.keep() == B.AQUAKV_EINVAL and "overlaps" in B.aquakv_last_error()

@@ -211,3 +211,25 @@ def test_rows_behind_4_gib(way):
     target = rows[:m] if to is None else (to[0].long()[:, None] * page + torch.arange(page)).view(-1)[:m]
     for k in POOL:
         assert torch.equal(getattr(pages, k)[target.cuda()].cpu(), src[k][kept[0].long()]), k
+
+
+def test_many_rows_to_other_pages_without_room_for_them():
+    """One sequence of more entries than go by columns, in a workspace of 256 bytes of which nothing is touched."""
+    from paper_2501_19392_amd import binding as B
+    most, page, H = 3000, 16, 3
+    to_pages = -(-most // page)
+    lo, lg, pages, table, lens, gen = T.cache("bf16", "grid64", H, [3500], page, room=3 + to_pages)
+    used = set(table.view(-1).tolist())
+    to = torch.tensor([p for p in range(pages.n_pages) if p not in used][:to_pages], dtype=torch.int32)[None]
+    kept = torch.randperm(3500, generator=gen)[:most].to(torch.int32)[None]
+    n_kept = torch.tensor([most], dtype=torch.int32)
+    mass = torch.rand(pages.n_pages, H, page, generator=gen)
+    assert B.aquakv_paged_keep_workspace_bytes(lg, pages, 1, most, True) > 256
+    pool = {k: getattr(pages, k).cpu() for k in POOL}
+    want, want_mass = kept_by_hand(pool, mass, page, pages.n_pages, table.tolist(), kept, n_kept, None, to.tolist())
+    ws, got = torch.full((4096,), 0xff, dtype=torch.uint8, device="cuda"), mass.cuda()
+    B.aquakv_paged_keep(lg, pages, 1, table.cuda(), kept.cuda(), n_kept.cuda(), None, to.cuda(), got, ws[:256])
+    torch.cuda.synchronize()
+    for k in POOL:
+        assert torch.equal(getattr(pages, k).cpu(), want[k]), k
+    assert torch.equal(got.cpu(), want_mass) and (ws == 0xff).all()
