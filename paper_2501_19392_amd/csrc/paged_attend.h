@@ -56,7 +56,8 @@ __device__ __forceinline__ PagedQueries paged_queries(const PagedAttendArgs& a, 
 
 // The tokens of all sequences are cut into pieces of equally many tiles, so that about a.slots of them cover the batch whatever its
 // lengths (each sequence has one at least): item i of the launch is piece `piece` of `pieces` of sequence b (-1: behind the last).
-struct Share { int b, piece, pieces, tiles, items; };
+// RESULTS: `results` is the number of pieces ahead of this sequence's that are not the only one of theirs.
+struct Share { int b, piece, pieces, tiles, items, results; };
 template <int TILE> __device__ __forceinline__ int tiles_of(const PagedAttendArgs& a, int b) {
   return b < a.batch ? max(tiles_of_tokens(length_of(a, a.seq_lens[b]), TILE), 1) : 0;
 }
@@ -70,8 +71,8 @@ __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143 /* row_bcast:31 */, 0xc, 0xf, false);
   return x;
 }
-template <int TILE = kTile> __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
-  Share s = {-1, 0, 1, 0, 0};
+template <int TILE = kTile, bool RESULTS = false> __device__ __forceinline__ Share share_of(const PagedAttendArgs& a, int lane, int item) {
+  Share s = {-1, 0, 1, 0, 0, 0};
   if (a.batch == 1) {
     const int n = max(tiles_of_tokens(length_of(a, const_ints(a.seq_lens)[0]), TILE), 1);
     s.tiles = max((n + a.slots - 1) / a.slots, short_piece(n, a.slots));
@@ -96,20 +97,24 @@ template <int TILE = kTile> __device__ __forceinline__ Share share_of(const Page
     }
   }
   s.tiles = max(s.tiles, short_piece(total, a.slots));
+  int results = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     if (a.batch > 64) tiles = tiles_of<TILE>(a, b0 + lane);
     const int mine = (int)((uint32_t)(tiles + s.tiles - 1) / (uint32_t)s.tiles);
     const int end = s.items + wave_scan(mine);             // items up to and with this sequence
     const uint64_t past = __builtin_amdgcn_ballot_w64(end > item);
+    const int held = RESULTS ? results + wave_scan(mine > 1 ? mine : 0) : 0;      // results up to and with this sequence
     if (past != 0 && s.b < 0) {
       const int l = __builtin_ctzll(past);
       s.b = b0 + l;
       s.pieces = __builtin_amdgcn_readlane(mine, l);
+      if constexpr (RESULTS) s.results = __builtin_amdgcn_readlane(held, l) - (s.pieces > 1 ? s.pieces : 0);
       s.piece = item - (__builtin_amdgcn_readlane(end, l) - s.pieces);
     }
     s.items = __builtin_amdgcn_readlane(end, 63);
+    if constexpr (RESULTS) results = __builtin_amdgcn_readlane(held, 63);
   }
-  s.b = uniform(s.b); s.piece = uniform(s.piece); s.pieces = uniform(s.pieces); s.tiles = uniform(s.tiles); s.items = uniform(s.items);
+  s.b = uniform(s.b); s.piece = uniform(s.piece); s.pieces = uniform(s.pieces); s.tiles = uniform(s.tiles); s.items = uniform(s.items); s.results = uniform(s.results);
   return s;
 }
 

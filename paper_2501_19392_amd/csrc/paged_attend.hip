@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) void paged_merge_rows_kernel(const PagedAttend
 // How a launch is laid out, from sizes alone (lengths and counts of queries are on the device): by max_queries, whatever the sequences have.  So single queries
 // beside a chunk are walked by one workgroup a kv head each, as a block of 256 rows is: 31 over 16 384 tokens and a chunk of 512, 32 heads, 2.1 ms, in a call of
 // their own 94 us, the chunk by itself 99.
-struct PagedPlan { unsigned blocks, row_tiles, rows_apart; int slots, row_blocks; int64_t items; int cols; bool merge, many, by_rows; };
+struct PagedPlan { unsigned blocks, row_tiles, rows_apart; int slots, row_blocks; int64_t items, results; int cols; bool merge, many, by_rows; };      // results: kept for the merge
 // Results of a sequence beyond which the merge has 1024 threads a row, of 256 (one query of 131 072 tokens 41.0 us, for 45.0; beyond 8: 32 x 4000 tokens
 // 37.4 for 34.4).
 constexpr int kManyPieces = 64;
@@ -151,13 +151,17 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
   const int64_t rows = std::max<int64_t>(max_queries, 1) * (q_heads / H), most = (table_pages * page_tokens + kTile - 1) / kTile;      // tiles of a sequence
   if (sizeof(T) == 2 && tree && tree_in_blocks(rows, is_rtn(NCW), batch * most * H)) {      // one workgroup a CU, pieces of equal size over all sequences
     const int row_blocks = (int)((rows + kTileRows - 1) / kTileRows), room = (int)std::max<int64_t>(256 / (H * row_blocks), 1);
-    // Whole sequences, with no results to keep and join, where they are several rounds of workgroups by themselves: 208 rows of 128 x 2000 tokens 312 us, in
-    // pieces 315, of 128 uneven ones 300, 305; 576 rows of 64 uneven ones of up to 4000 tokens 702, 714.
-    const int slots = batch >= 4 * room ? 1 : room;
+    // Whole sequences, with no results to keep and join, where they are several rounds of workgroups by themselves and none can be much longer than a round: 256 rows of
+    // 128 x 4000 tokens 847 us, in pieces 862, of 128 uneven ones 483, 497, one of 4000 among 127 of 500 187, 194; but one of 8000 321, 203, of 16 384 638, 224, of
+    // 131 072 4952, 498; of 8000 among 255 358, 365, of 16 384 642, 412.
+    const int64_t tokens = table_pages * page_tokens;
+    const bool whole = batch >= 4 * room && (tokens <= 4096 || (tokens <= 16384 && batch >= 8 * room));
+    const int slots = whole ? 1 : room;
     const int64_t tiles = std::max<int64_t>((table_pages * page_tokens + 63) / 64, 1);
-    const int64_t items = slots == 1 ? batch : std::min(batch * tiles, std::max<int64_t>(slots - batch, std::max(slots / 2, 1)) + batch);
+    const int64_t items = slots == 1 ? batch : std::min(batch * tiles, piece_room(slots, (int)batch) + batch);
     if (items * H < (1 << 22)) {                           // (threads of a launch: below 2^32)
       p.row_blocks = row_blocks; p.slots = slots; p.items = items;
+      p.results = std::min<int64_t>(items, piece_results(slots, (int)batch));
       p.merge = tiles > 1 && slots > 1;
       p.by_rows = items <= 16 * batch;
       p.many = items > kManyPieces * batch;
@@ -169,7 +173,7 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
     // ... of 4 tiles of 64 at least, of 2 where there is one block of rows and so little to join (180 rows over 700 tokens: 28.0 us, 22.2; 160 over 6000: 34.3, 31.5;
     // 1200 rows over 300: 23.3, 26.2)
     p.slots = (int)std::max<int64_t>(std::min(256 / std::max<int64_t>(batch * H * p.row_blocks, 1), most / (p.row_blocks == 1 ? 4 : 8)), 1);
-    p.items = batch * p.slots;
+    p.items = p.results = batch * p.slots;
     p.merge = p.slots > 1;
     p.by_rows = p.slots <= 16;
     p.many = p.slots > kManyPieces;
@@ -196,11 +200,11 @@ template <typename T, int NCW> PagedPlan paged_plan(int64_t batch, int64_t table
     const int64_t groups = (pieces + waves - 1) / waves;
     p.blocks = (unsigned)((groups + 7) / 8 * 8 * H);
     if (p.rows_apart) p.blocks = (unsigned)((groups * p.row_tiles + 7) / 8 * 8 * H);
-    p.items = groups + batch;
+    p.items = p.results = groups + batch;
     p.merge = groups > 1;
   } else {
     p.blocks = (unsigned)((pieces * H + waves - 1) / waves);
-    p.items = pieces;
+    p.items = p.results = pieces;
     p.merge = most > 1;
   }
   p.many = p.items > kManyPieces * batch;
@@ -218,7 +222,7 @@ static PagedPlan plan_of(int dtype, int n_codewords, const PagedAttendArgs& a, b
 
 size_t paged_attend_workspace_bytes(int dtype, int n_codewords, const PagedAttendArgs& a, bool tree) {
   const PagedPlan p = plan_of(dtype, n_codewords, a, tree);
-  return p.merge ? (size_t)p.items * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2) : 0;
+  return p.merge ? (size_t)p.results * a.max_queries * a.q_heads * (kGroup + 2) * sizeof(float) + (size_t)a.batch * sizeof(int2) : 0;
 }
 
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& args, void* workspace, hipStream_t stream) {
@@ -230,8 +234,8 @@ hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs
   a.row_tiles = (int)plan.row_tiles;
   a.rows_apart = (int)plan.rows_apart;
   a.part = static_cast<float*>(workspace);
-  a.stats = a.part + plan.items * a.max_queries * a.q_heads * kGroup;
-  a.heads = plan.merge ? reinterpret_cast<int2*>(a.stats + plan.items * a.max_queries * a.q_heads * 2) : nullptr;
+  a.stats = a.part + plan.results * a.max_queries * a.q_heads * kGroup;
+  a.heads = plan.merge ? reinterpret_cast<int2*>(a.stats + plan.results * a.max_queries * a.q_heads * 2) : nullptr;
   a.page_groups = a.pool.page_tokens / 8;
   a.page_magic = a.page_groups == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / a.page_groups);
   if (plan.row_blocks != 0) {

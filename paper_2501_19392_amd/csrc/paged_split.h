@@ -18,11 +18,16 @@ constexpr TokenRange piece_range(int piece, int each, int tile, int tokens) {
 }
 
 // tiles per piece with which ceil(tiles / piece) over all sequences is at most max(slots, slots / 2 + batch), whatever the lengths
-constexpr int piece_tiles(int total, int slots, int batch) {
+constexpr int piece_room(int slots, int batch) {
   const int half = slots / 2 > 1 ? slots / 2 : 1;
-  const uint32_t room = (uint32_t)(slots - batch > half ? slots - batch : half);
+  return slots - batch > half ? slots - batch : half;
+}
+constexpr int piece_tiles(int total, int slots, int batch) {
+  const uint32_t room = (uint32_t)piece_room(slots, batch);
   return (int)(((uint32_t)total + room - 1) / room);
 }
+// Pieces of sequences that are in more than one, at most: x tiles in pieces of n < x are ceil(x / n) < 2 x / n of them, and total / n <= room.
+constexpr int piece_results(int slots, int batch) { return 2 * piece_room(slots, batch); }
 // Short pieces make half as many: two waves of one tile take as long as one of two, whose results are half as many to write and to join (one query of
 // 10 000 tokens, 313 tiles: 20.0 us in pieces of one tile, 15.9 of two; of 6000 14.9, 14.6; 5 queries of 2000 tokens of 8 sequences: 20.5 in pieces of two, 18.6 of
 // three, 19.7 of four).  Longer ones want all waves there are (32 x 16 384 tokens: 95 us, on half of the waves 111).

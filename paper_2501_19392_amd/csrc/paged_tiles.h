@@ -202,10 +202,10 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
   TokenRange range = {};
   if constexpr (TREE) {                                    // blockIdx: (piece of all sequences and kv head, block of rows)
     const int item = blockIdx.x / a.H;
-    const Share share = share_of<kTokens>(a, lane, item);
+    const Share share = share_of<kTokens, true>(a, lane, item);
     if (share.b < 0) return;
     b = share.b; piece = share.piece; block = blockIdx.y;
-    first_result = item - piece; results = share.pieces;
+    first_result = share.results; results = share.pieces;      // (sequences in one piece keep none)
     range = {share.tiles, 0};
   } else {                                                 // (piece, block of rows: the last ones, which see most tokens, first; kv head), sequence
     piece = (blockIdx.x / a.H) % a.slots; block = a.row_blocks - 1 - blockIdx.x / a.H / a.slots; b = blockIdx.y;

@@ -214,3 +214,14 @@ def test_rows_to_other_pages_need_no_room_for_them(batch, most):
         assert c.size("keep") > most * 1024 and c.keep() == B.AQUAKV_EWORKSPACE
     else:
         assert c.keep() == B.AQUAKV_EINVAL and "overlaps" in B.aquakv_last_error()
+
+
+@pytest.mark.parametrize("batch,queries,room,small", [
+    (128, 64, 4096, True), (128, 64, 4160, False), (128, 64, 131072, False), (256, 64, 16384, True), (256, 64, 16448, False), (2000, 64, 131072, False), (64, 144, 2048, True),
+    (64, 144, 32768, False), (32, 2048, 131072, True)])      # (2048: a sequence's blocks of rows fill the chip)
+def test_sequences_are_whole_where_none_can_be_long(batch, queries, room, small):
+    """Trees in blocks of 256 rows: with room for long sequences there are results of pieces, of as many as fill the chip, however many sequences there are."""
+    c = Buffers()
+    c.n.update(n_pages=1000000, page_tokens=64, batch=batch, table_pages=room // 64, q_rows=batch * queries, max_queries=queries)
+    size = B._lib.aquakv_paged_attend_workspace_bytes(c.layer, c.pages(), batch, QH, room // 64, batch * queries, queries, 1)
+    assert size == 256 if small else 1 << 20 < size < 40 << 20

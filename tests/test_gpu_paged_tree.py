@@ -248,3 +248,30 @@ def test_query_without_numbers(fmt, QH, n):
     got = attend(lg, pages, table, lens, q, [n, n], trees)
     assert got.cpu()[bad].isnan().all()
     P.check(got.cpu()[~bad], want[~bad], bound[~bad], fmt)
+
+
+@pytest.mark.parametrize("fmt,batch,long", [("grid64", 70, {3: 5000, 66: 3001}), ("rtn4", 64, {63: 4000}), ("grid256", 130, {0: 2500, 64: 700, 129: 6000}), ("grid16", 66, {})])
+def test_long_sequences_among_many_in_blocks_of_rows(fmt, batch, long):
+    """With room for long sequences they are cut, and only those: beside sequences in one piece, without rows or tokens, in batches of more than a wave's lanes."""
+    from paper_2501_19392_amd import binding as B
+    H, QH, page, most = 8, 128, 16, 17
+    print(f"case long among many {fmt} {batch} {long}", flush=True)
+    gen = torch.Generator().manual_seed(78)
+    lengths, counts = torch.randint(17, 320, (batch,), generator=gen).tolist(), torch.randint(0, 18, (batch,), generator=gen).tolist()
+    lengths[1], lengths[2], counts[1] = 0, 1, 0
+    for b, n in long.items():
+        lengths[b], counts[b] = n, 17 - b % 5
+    counts[2] = min(counts[2], 1)
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, H, lengths, page, seed=12)
+    table = torch.cat([table, torch.full((batch, 1100 - table.shape[1]), -1, dtype=torch.int32)], 1).contiguous()
+    trees = [T.random_tree(n, gen) for n in counts]
+    q = queries(gen, sum(counts), QH, "bf16")
+    start = torch.tensor([sum(counts[:b]) for b in range(batch + 1)], dtype=torch.int32).cuda()
+    size = B.aquakv_paged_attend_workspace_bytes(lg, pages, batch, QH, 1100, q.shape[0], most, True)
+    assert size > 1 << 20
+    ws, out = torch.full((size + 4096,), 0xff, dtype=torch.uint8, device="cuda"), torch.full_like(q, float("nan"))
+    bits = torch.cat([T.words_of(t, 1) for t in trees]).cuda()
+    B.aquakv_paged_attend_tree(lg, pages, batch, QH, table.cuda(), lens.cuda(), q, most, start, bits, SCALE, out, ws[:size])
+    torch.cuda.synchronize()
+    assert (ws[size:] == 0xff).all()
+    P.check(out, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, "bf16"), fmt)

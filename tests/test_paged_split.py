@@ -74,3 +74,39 @@ def test_the_pieces_of_a_batch(ask, slots, lengths):
         for n in sorted(set(lengths)):
             pieces = -(-max(-(-n // 32), 1) // each)
             covered(ask([("r", i, each, 32, n) for i in range(pieces)]), n, 32, each)
+
+
+RESULTS = """
+#include <cstdio>
+#include "paged_split.h"
+using namespace aquakv::paged;
+int main() {
+  int a, b, c;
+  while (std::scanf("%d %d %d", &a, &b, &c) == 3) std::printf("%d %d\\n", piece_tiles(a, b, c), piece_results(b, c));
+}
+"""
+
+
+def test_the_results_of_sequences_in_several_pieces(tmp_path):
+    """Whatever the lengths, there is room for the pieces of all sequences that have more than one (also where pieces are longer than they have to be, or as
+    short as makes no more of them than `slots`)."""
+    import random
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    (tmp_path / "t.cpp").write_text(RESULTS)
+    subprocess.run(["g++", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", CSRC, "-o", str(tmp_path / "t"), str(tmp_path / "t.cpp")], check=True)
+    rng, calls = random.Random(4), []
+    for _ in range(4000):
+        slots, batch = rng.choice([1, 2, 3, 4, 5, 8, 16, 31, 32, 64, 170]), rng.choice([2, 3, 5, 16, 31, 64, 65, 128, 200])
+        top = rng.choice([2, 5, 40, 2000, 10 ** 6])
+        tiles = [rng.randint(1, top) if rng.random() < rng.choice([0.02, 0.5, 1.0]) else 1 for _ in range(batch)]
+        calls.append((slots, tiles))
+    text = "\n".join(f"{sum(t)} {s} {len(t)}" for s, t in calls)
+    out = subprocess.run([str(tmp_path / "t")], input=text, check=True, capture_output=True, text=True).stdout.split()
+    for (slots, tiles), each, room in zip(calls, map(int, out[::2]), map(int, out[1::2])):
+        def kept(n):
+            return sum(-(-t // n) for t in tiles if t > n)
+        assert kept(each) <= room and kept(each + 1) <= room and kept(4 * each) <= room
+        if 2 * len(tiles) <= slots:                                         # the fewest tiles that do
+            fewest = next(n for n in range(max(-(-sum(tiles) // slots), 1), each + 1) if sum(-(-t // n) for t in tiles) <= slots or n == each)
+            assert kept(fewest) <= room
