@@ -552,7 +552,7 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   as they were; where a sequence has more than max_queries rows, those that are not answered add nothing.  A page that two sequences name has
  *   anything in its mass afterwards.  After drafts were accepted (aquakv_paged_keep) the accepted ones are the last tokens, and their queries are taken here.
  *   Both dtypes: products of two fp16 numbers for each factor (22 bits), fp32 sums in a fixed order: the same bits each time.  Beyond the limits of
- *   aquakv_paged_attend: table_pages * page_tokens * kv_heads < 2^31.  workspace: aquakv_paged_weights_workspace_bytes() bytes, which hold the scores of all
+ *   aquakv_paged_attend: table_pages * page_tokens * kv_heads < 2^31 (more than 8 rows of a kv head: the first two as a multiple of 128).  workspace: aquakv_paged_weights_workspace_bytes() bytes, which hold the scores of all
  *   tokens there is room for where a kv head has at most 8 rows (queries x query heads), else 8 bytes for each row and 32 tokens and 544 for each row.  A query
  *   without numbers reaches the tokens that it sees, no others.
  *
@@ -569,7 +569,8 @@ int aquakv_attend_cache(const aquakv_cache_layer* layers, int32_t n_layers, cons
  *   pages that to_table [batch, to_pages] names, which may not be ones that the call reads; entries in any order, some more than once.  What goes from or to a
  *   token outside its table or a page that is not in the pool is left out.  Rows that are written against this, or for two entries or sequences, hold
  *   anything afterwards, and so does what is read from such rows.  Keys keep the rotation that they have.
- *   workspace: aquakv_paged_keep_workspace_bytes() bytes for the same layer, pages and sizes (with_mass: 0, or 1 where mass is given); 256 with to_table.
+ *   workspace: aquakv_paged_keep_workspace_bytes() bytes for the same layer, pages and sizes (with_mass: 0, or 1 where mass is given); 256 with to_table.  max_kept < 2^29 (to other pages, or in place
+ *   where that workspace is more than 256 bytes: 2^29 - 31).
  *
  * Nothing that these calls write may overlap anything else they are given: AQUAKV_EINVAL before anything is launched.  Without tokens
  * (tokens = 0), sequences or queries (batch, q_rows or max_queries = 0) nothing is done, and buffers but the pool's may be NULL.
@@ -618,7 +619,7 @@ int aquakv_paged_keep(const aquakv_layer* layer, const aquakv_pages* pages, int3
  *   the way back for tables of magnitude 1, and the gradient for any.  fp32 arithmetic, one rounding to dtype.
  *   Token t is at x + t * x_stride elements and goes to out + t * out_stride (rows contiguous, 16-byte aligned).  out = x with the same stride: in place;
  *   otherwise they may not overlap.  A token whose position is outside the tables is left out: its row of `out` stays as it was.  positions: int32 [tokens].
- *   tokens * (heads / 4, rounded up) < 2^27.
+ *   tokens * (heads / 4, rounded up) < 2^27 (fp32 pairs: 2^27 - 7).
  *
  * aquakv_rotary_tables -- rope_cos, rope_sin [rows, rotary_dim / 2] for positions first ... first + rows - 1 (below 2^31):
  *   magnitude * cos, sin(position * w_i),  w_i = base^(-2 i / rotary_dim) (k_i + (1 - k_i) / factor):

@@ -1818,8 +1818,10 @@ int aquakv_paged_weights(const aquakv_layer* L, const aquakv_pages* pages, int32
   if (q_start == nullptr && q_rows != (int64_t)batch * max_queries)
     return fail(AQUAKV_EINVAL, "q_rows=%lld: without q_start every one of %d sequences has %d", (long long)q_rows, batch, max_queries);
   if (!std::isfinite(keep)) return fail(AQUAKV_EINVAL, "keep=%g", (double)keep);
-  // (threads of a launch: below 2^32, two a token and kv head)
-  if ((int64_t)table_pages * pages->page_tokens * L->kv_heads >= ((int64_t)1 << 31))
+  // (threads of a launch: below 2^32, two a token and kv head; many rows: in whole workgroups of 128 tokens)
+  const bool many = (int64_t)max_queries * (q_heads / L->kv_heads) > aquakv::kWeightsFewRows;
+  const int64_t room = (int64_t)table_pages * pages->page_tokens;
+  if ((many ? (room + 127) / 128 * 128 : room) * L->kv_heads >= ((int64_t)1 << 31))
     return fail(AQUAKV_EUNSUPPORTED, "%d pages of %d tokens of %d heads", table_pages, pages->page_tokens, L->kv_heads);
   if (batch == 0 || q_rows == 0 || max_queries == 0) return AQUAKV_OK;
   const int64_t row = (int64_t)q_heads * 128;
@@ -1913,6 +1915,9 @@ int aquakv_paged_keep(const aquakv_layer* L, const aquakv_pages* pages, int32_t 
   if (misaligned_to(to_table, 4)) return fail(AQUAKV_EALIGN, "to_table is not 4-byte aligned");
   CHECK(check_ptr(mass, "mass", false));
   CHECK(check_ptr(workspace, "workspace", true));
+  // (workgroups of 256 threads for 32 entries, but where columns of rows move in place)
+  if (max_kept > (1 << 29) - 32 && (to_table != nullptr || aquakv_paged_keep_workspace_bytes(L, pages, batch, max_kept, 0) > 256))
+    return fail(AQUAKV_EUNSUPPORTED, "max_kept=%d", max_kept);
   // (rows that go to other pages are not staged)
   const size_t need = to_table != nullptr ? 256 : aquakv_paged_keep_workspace_bytes(L, pages, batch, max_kept, mass != nullptr);
   if (workspace_bytes < need) return fail(AQUAKV_EWORKSPACE, "workspace %zu B < required %zu B", workspace_bytes, need);
@@ -1941,8 +1946,9 @@ int aquakv_rotary(int32_t dtype, int64_t tokens, int32_t heads, const void* x, i
   if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return fail(AQUAKV_EINVAL, "rotary_dim=%d of heads of 128", rotary_dim);
   if (rotary_dim % 16) return fail(AQUAKV_EUNSUPPORTED, "rotary_dim=%d: multiples of 16 are built", rotary_dim);
   if (layout != AQUAKV_ROTARY_HALVES && layout != AQUAKV_ROTARY_PAIRS) return fail(AQUAKV_EINVAL, "layout=%d", layout);
-  // (threads of a launch: below 2^32, up to 32 for four heads of a token)
-  if (tokens >= (1LL << 27) || tokens * ((heads + 3LL) / 4) >= (1LL << 27)) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, heads);
+  // (threads of a launch, in whole workgroups: below 2^32, up to 31 for four heads of a token, and 32 for fp32 pairs)
+  const int64_t most = (1LL << 27) - (dtype == AQUAKV_FP32 && layout == AQUAKV_ROTARY_PAIRS ? 7 : 0);
+  if (tokens >= most || tokens * ((heads + 3LL) / 4) >= most) return fail(AQUAKV_EUNSUPPORTED, "tokens=%lld of %d heads", (long long)tokens, heads);
   if (tokens == 0) return AQUAKV_OK;
   const int64_t row = (int64_t)heads * 128;
   const size_t eb = elem_bytes(dtype), angles = (size_t)rope_rows * (rotary_dim / 2) * sizeof(float);

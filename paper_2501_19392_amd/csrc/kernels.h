@@ -280,6 +280,7 @@ hipError_t launch_paged_tiles(int n_codewords, const PagedAttendArgs& a, hipStre
 hipError_t launch_paged_tree_rows(int dtype, int n_codewords, int cols, dim3 blocks, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_tree_tiles(int n_codewords, const PagedAttendArgs& a, hipStream_t stream);
 hipError_t launch_paged_attend(int dtype, int n_codewords, const PagedAttendArgs& a, void* workspace, hipStream_t stream);
+constexpr int kWeightsFewRows = 8;                // of a kv head, up to which attention weights keep the scores
 // Attention weights added to mass [n_pages, H, page_tokens] (paged_weights.hip); of the arguments out, tree and values are not used.
 size_t paged_weights_workspace_bytes(int n_codewords, const PagedAttendArgs& a);
 hipError_t launch_paged_weights(int dtype, int n_codewords, const PagedAttendArgs& a, float keep, float* mass, void* workspace, hipStream_t stream);

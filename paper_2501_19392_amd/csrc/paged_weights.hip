@@ -10,7 +10,7 @@ namespace {
 
 using namespace paged;
 
-constexpr int kFewRows = 8;                                // of a kv head, whose scores are kept (else they are taken again)
+constexpr int kFewRows = kWeightsFewRows;                  // of a kv head, whose scores are kept (else they are taken again)
 constexpr int kMassWaves = 4, kStaged = 2, kBehind = 4 * kStaged, kMassTokens = kTile * kMassWaves;      // of a workgroup that takes many rows
 
 struct WeightsArgs {

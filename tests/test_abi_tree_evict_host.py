@@ -225,3 +225,26 @@ def test_sequences_are_whole_where_none_can_be_long(batch, queries, room, small)
     c.n.update(n_pages=1000000, page_tokens=64, batch=batch, table_pages=room // 64, q_rows=batch * queries, max_queries=queries)
     size = B._lib.aquakv_paged_attend_workspace_bytes(c.layer, c.pages(), batch, QH, room // 64, batch * queries, queries, 1)
     assert size == 256 if small else 1 << 20 < size < 40 << 20
+
+
+@pytest.mark.parametrize("call,kw,refused", [
+    ("weights", dict(kv=1024, q_heads=16384, table_pages=(1 << 18) - 1, page_tokens=8, max_queries=1), True),       # 2^14 workgroups of 128 tokens, 1024 heads, 256 threads each
+    ("weights", dict(kv=1024, q_heads=16384, table_pages=(1 << 18) - 17, page_tokens=8, max_queries=1), False),     # one workgroup less
+    ("weights", dict(kv=1024, q_heads=8192, table_pages=(1 << 18) - 1, page_tokens=8, max_queries=1), False),       # few rows: in other workgroups
+    ("keep", dict(max_kept=(1 << 29) - 31), True), ("keep", dict(max_kept=(1 << 29) - 32), False),                  # workgroups of 32 entries
+    ("keep", dict(max_kept=(1 << 29) - 1, to=None, batch=1), True), ("keep", dict(max_kept=(1 << 29) - 1, to=None, batch=64), False),      # in place, by columns
+    ("rotary", dict(tokens=(1 << 27) - 7, heads=1, dtype=B.AQUAKV_FP32, layout=1, x_stride=128, out_stride=128), True),      # 32 threads for a token
+    ("rotary", dict(tokens=(1 << 27) - 8, heads=1, dtype=B.AQUAKV_FP32, layout=1, x_stride=128, out_stride=128), False),
+    ("rotary", dict(tokens=(1 << 27) - 1, heads=1, layout=1, x_stride=128, out_stride=128), False)])
+def test_launches_in_whole_workgroups_stay_below_2_32_threads(call, kw, refused):
+    """(Calls that are not refused get as far as buffers that overlap.)"""
+    c = Buffers(**({"kv_heads": kw["kv"]} if "kv" in kw else {}))
+    c.a = {k: v << 8 for k, v in c.a.items()}                # (as far apart as the buffers are large)
+    c.n.update({k: v for k, v in kw.items() if k not in ("kv", "to")}, ws=1 << 62)
+    if "kv" in kw:
+        c.n.update(q_stride=kw["q_heads"] * 128, q_rows=2)
+    if "to" in kw:
+        c.a["to"] = None
+    c.a[{"weights": "mass", "keep": "mass", "rotary": "out"}[call]] = c.a[{"weights": "lens", "keep": "n_kept", "rotary": "cos"}[call]]
+    assert getattr(c, call)() == (B.AQUAKV_EUNSUPPORTED if refused else B.AQUAKV_EINVAL), B.aquakv_last_error()
+    assert refused or "overlaps" in B.aquakv_last_error()
