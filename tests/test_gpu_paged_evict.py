@@ -233,3 +233,38 @@ def test_many_rows_to_other_pages_without_room_for_them():
     for k in POOL:
         assert torch.equal(getattr(pages, k).cpu(), want[k]), k
     assert torch.equal(got.cpu(), want_mass) and (ws == 0xff).all()
+
+
+@pytest.mark.parametrize("kind", ["plain", "ties", "odd"])
+@pytest.mark.parametrize("H,lengths,page,budget,n_first,n_last", [
+    (8, [40000, 17001, 9000, 30001, 0, 1, 36864], 128, 12000, 100, 1000), (5, [20000, 19999, 16385, 12288], 64, 8193, 4096, 4097), (3, [70000, 50000], 256, 49999, 5, 0),
+    (2, [18000, 17000, 300], 40, 0, 0, 0)])
+def test_selecting_from_many_long_sequences(kind, H, lengths, page, budget, n_first, n_last):
+    """Slabs of several sequences, each with its own: some end inside a slab, one is below the budget, pages are missing, masses are no numbers."""
+    print(f"case select long {kind} H={H} {lengths} budget={budget}", flush=True)
+    lo, lg, pages, table, lens, gen = T.cache("bf16", "grid16", H, lengths, page)
+    mass = masses(kind, pages.n_pages, H, page, gen)
+    if kind == "odd":
+        for b in range(len(lengths)):
+            table[b, 1], table[b, 50 + b], table[b, 1 + b] = -1, pages.n_pages + b, -5
+    kept, n_kept = select(lg, pages, table, lens, mass, budget, n_first, n_last)
+    for b, n in enumerate(lengths):
+        want = wanted(mass.numpy(), table[b], n, pages.n_pages, page, budget, n_first, n_last)
+        assert n_kept[b] == len(want) == min(n, budget), b
+        assert (kept[b, :len(want)] == want).all(), b
+        assert (kept[b, len(want):] == -1).all(), b
+
+
+@pytest.mark.parametrize("room", [0, 20000])
+def test_selecting_from_more_sequences_than_a_wave_has_lanes(room):
+    """With page tables as wide as the longest one, and wider: by a workgroup each, and by slabs, most of which have nothing."""
+    H, page, batch, budget = 2, 16, 133, 150
+    gen = torch.Generator().manual_seed(21)
+    lengths = torch.randint(0, 400, (batch,), generator=gen).tolist()
+    lo, lg, pages, table, lens, gen = T.cache("bf16", "grid16", H, lengths, page)
+    table = torch.cat([table, torch.full((batch, max(room // page - table.shape[1], 0)), -1, dtype=torch.int32)], 1).contiguous()
+    mass = masses("ties", pages.n_pages, H, page, gen)
+    kept, n_kept = select(lg, pages, table, lens, mass, budget, 3, 20)
+    for b, n in enumerate(lengths):
+        want = wanted(mass.numpy(), table[b], n, pages.n_pages, page, budget, 3, 20)
+        assert n_kept[b] == len(want) and (kept[b, :len(want)] == want).all() and (kept[b, len(want):] == -1).all(), b

@@ -275,3 +275,18 @@ def test_long_sequences_among_many_in_blocks_of_rows(fmt, batch, long):
     torch.cuda.synchronize()
     assert (ws[size:] == 0xff).all()
     P.check(out, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, "bf16"), fmt)
+
+
+@pytest.mark.parametrize("dtype,fmt,QH", [("bf16", "grid256", 8), ("bf16", "rtn4", 16), ("bf16", "grid64", 2), ("fp32", "grid16", 4)])
+def test_more_sequences_than_a_wave_has_lanes(dtype, fmt, QH):
+    """Waves of few rows: pieces are shared out by other code from 65 sequences on."""
+    batch, H, page, most = 101, 2, 16, 6
+    gen = torch.Generator().manual_seed(79)
+    lengths, counts = torch.randint(6, 300, (batch,), generator=gen).tolist(), torch.randint(0, most + 1, (batch,), generator=gen).tolist()
+    lengths[3], lengths[70], lengths[80], counts[70] = 2500, 3100, 0, most
+    lo, lg, pages, table, lens, gen = T.cache(dtype, fmt, H, lengths, page, seed=13)
+    trees = [T.random_tree(n, gen) for n in counts]
+    q = queries(gen, sum(counts), QH, dtype)
+    got = attend(lg, pages, table, lens, q, counts, trees, max_queries=most)
+    torch.cuda.synchronize()
+    P.check(got, *T.reference(lo, pages, table, lens, q, counts, trees, SCALE, dtype), fmt)

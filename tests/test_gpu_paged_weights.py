@@ -225,3 +225,19 @@ def test_query_without_numbers(backbone, n, bad):
     off = (got.double() - want.flatten())[seen:length].abs()
     assert (off <= bound.flatten()[seen:length]).all()
     assert torch.equal(got[length:], mass.flatten()[length:])
+
+
+@pytest.mark.parametrize("fmt,QH,most,batch,room", [("grid256", 8, 1, 70, 0), ("rtn4", 8, 2, 131, 0), ("grid64", 8, 2, 65, 30000), ("grid256", 8, 11, 70, 0), ("rtn2", 16, 5, 129, 9000)])
+def test_more_sequences_than_a_wave_has_lanes(fmt, QH, most, batch, room):
+    """Pieces are shared out by other code from 65 sequences on; with page tables as wide as the longest one, and much wider."""
+    H, page = 2, 16
+    print(f"case weights of many {fmt} {batch} sequences of {most}, room {room}", flush=True)
+    gen = torch.Generator().manual_seed(31)
+    lengths, counts = torch.randint(0, 400, (batch,), generator=gen).tolist(), torch.randint(0, most + 1, (batch,), generator=gen).tolist()
+    lengths[5], lengths[64], counts[64] = 3000, 2111, most
+    lo, lg, pages, table, lens, gen = T.cache("bf16", fmt, H, lengths, page, seed=7)
+    table = torch.cat([table, torch.full((batch, max(room // page - table.shape[1], 0)), -1, dtype=torch.int32)], 1).contiguous()
+    q = (1.5 * torch.randn(sum(counts), QH, 128, generator=gen)).bfloat16().cuda()
+    mass = some_mass(pages, H, gen)
+    got = weights(lg, pages, table, lens, q, counts, 0.75, mass, max_queries=most)
+    check(got, mass, *wanted(lo, pages, table, lens, q, counts, most, 0.75, mass))
