@@ -556,7 +556,7 @@ template <int NCW, int TERMS> struct Codes {
     float ref, sum;                                        // weights are 2^(score - ref)
   };
   // ---- scores of product p: s[column][half][p] += keys * query
-  template <int COLS, typename Col> static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const Col (&col)[COLS],
+  template <int COLS> static __device__ __forceinline__ void scores(const Keys& w, int p, const unsigned char* lds, int lane, const Column (&col)[COLS],
                                                                     f32x4 (&s)[COLS][kRtn ? 2 : 1][2]) {
     const uint32_t x[4] = {w.k[p].x, w.k[p].y, w.k[p].z, w.k[p].w};
     if constexpr (kRtn) {

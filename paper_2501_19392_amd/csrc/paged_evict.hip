@@ -6,16 +6,20 @@
 namespace aquakv {
 namespace {
 
-// Token -> its page in the pool, -1: not there; its place in the page.
 struct PageDivider { uint32_t tokens, magic; };
+struct InPage { uint32_t page, in; };                      // token / tokens of a page, and the rest
+__device__ __forceinline__ InPage in_page(const PageDivider& d, uint32_t token) {
+  uint32_t page = (uint32_t)(((uint64_t)token * d.magic) >> 32);             // (one short at most)
+  if (token - page * d.tokens >= d.tokens) ++page;
+  return {page, token - page * d.tokens};
+}
+// Token -> its page in the pool, -1: not there; its place in the page.
 struct Place { int page; uint32_t in; };
 __device__ __forceinline__ Place place_of_token(const int32_t* table, int table_pages, const PageDivider& d, int n_pages, int64_t token) {
   if (token < 0 || token >= (int64_t)table_pages * d.tokens) return {-1, 0u};
-  const uint32_t t = (uint32_t)token;
-  uint32_t page = (uint32_t)(((uint64_t)t * d.magic) >> 32);                 // (one short at most)
-  if (t - page * d.tokens >= d.tokens) ++page;
-  const int at = table[page];
-  return {(uint32_t)at < (uint32_t)n_pages ? at : -1, t - page * d.tokens};
+  const InPage t = in_page(d, (uint32_t)token);
+  const int at = table[t.page];
+  return {(uint32_t)at < (uint32_t)n_pages ? at : -1, t.in};
 }
 PageDivider divider(int page_tokens) { return {(uint32_t)page_tokens, (uint32_t)((uint64_t(1) << 32) / (uint32_t)page_tokens)}; }
 
@@ -39,10 +43,9 @@ template <int N> __device__ __forceinline__ void token_keys(const PagedSelectArg
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const uint32_t token = (uint32_t)min((int64_t)t + (int64_t)k * step, (int64_t)to - 1);
-    uint32_t p = (uint32_t)(((uint64_t)token * d.magic) >> 32);              // (one short at most)
-    if (token - p * d.tokens >= d.tokens) ++p;
-    in[k] = token - p * d.tokens;
-    page[k] = table[p];
+    const InPage p = in_page(d, token);
+    in[k] = p.in;
+    page[k] = table[p.page];
     key[k] = (int)token < a.n_first || (int)token >= len - a.n_last ? kAlways : 1u;
   }
   const float* at[N];
@@ -330,9 +333,8 @@ __device__ __forceinline__ void store_unit(uint8_t* p, int unit, const u32x4& x)
   else *reinterpret_cast<uint16_t*>(p) = (uint16_t)x.x;
 }
 __device__ __forceinline__ Place place_of_row(const PageDivider& d, int row) {
-  uint32_t page = (uint32_t)(((uint64_t)(uint32_t)row * d.magic) >> 32);
-  if (row - page * d.tokens >= d.tokens) ++page;
-  return {(int)page, row - page * d.tokens};
+  const InPage r = in_page(d, (uint32_t)row);
+  return {(int)r.page, r.in};
 }
 // Places that entry i of sequence b goes from and to, page -1: nothing to move.
 struct Move { Place from, to; };
@@ -350,7 +352,7 @@ __device__ __forceinline__ Move move_of(const PagedKeepArgs& a, const PageDivide
 
 // In place: a workgroup takes a column of up to 128 bytes of one array's rows through the entries of a sequence, a round of them after the other.  As entries ascend, none
 // of the rows that a round writes is read later, so that two rounds more are on their way meanwhile; within a round all reads come back before anything is
-// written.  32 x 3800 of 4000 rows 72 us, 3.6 TB/s (a copy 5.2); what is left are the rounds' waits, for few sequences all there is.  blockIdx = (array and column,
+// written.  32 x 3800 of 4000 rows 69 us, 3.7 TB/s (a copy 5.2); what is left are the rounds' waits, for few sequences all there is.  blockIdx = (array and column,
 // sequence).
 constexpr int kMoveThreads = 1024, kMoveUnits = 2, kMoveLanes = 8, kMoveChunk = 4096;
 struct Columns { int first[6]; };                          // blockIdx.x from which an array's columns go
@@ -464,8 +466,8 @@ KeepLaunch keep_launch(const PagedKeepArgs& a) {
   l.d = divider(a.pool.page_tokens);
   return l;
 }
-// In place through the workspace, in two launches: few sequences of many entries, whose columns are too few workgroups (1 x 3800 entries: 17.4 us, by columns 26; 1 x 20 000:
-// 26.6, 147; 8 x 7900, 64 columns: 62, 65; 32 x 3800: 113, 81; 1 x 900: 16.0, 10.5).
+// In place through the workspace, in two launches: few sequences of many entries, whose columns are too few workgroups (1 x 3800 entries: 17.3 us, by columns 23.6; 1 x 20 000:
+// 28.4, 134; 8 x 7900, 64 columns: 61, 58; 32 x 3800: 104, 69; 1 x 900: 16.4, 9.5).
 bool through_workspace(int64_t batch, int64_t max_kept, int64_t code_row) { return max_kept > 1024 && batch * 2 * ((code_row + 127) / 128) < 64; }
 
 }  // namespace

@@ -17,11 +17,12 @@ constexpr TokenRange piece_range(int piece, int each, int tile, int tokens) {
   return {first * tile, tiles - first > each ? (first + each) * tile : tokens};
 }
 
-// tiles per piece with which ceil(tiles / piece) over all sequences is at most max(slots, slots / 2 + batch), whatever the lengths
+// whole pieces that all tiles together may make
 constexpr int piece_room(int slots, int batch) {
   const int half = slots / 2 > 1 ? slots / 2 : 1;
   return slots - batch > half ? slots - batch : half;
 }
+// tiles per piece with which ceil(tiles / piece) over all sequences is at most max(slots, slots / 2 + batch), whatever the lengths
 constexpr int piece_tiles(int total, int slots, int batch) {
   const uint32_t room = (uint32_t)piece_room(slots, batch);
   return (int)(((uint32_t)total + room - 1) / room);

@@ -320,9 +320,9 @@ __device__ __forceinline__ int64_t token_tiles(const WeightsArgs& x) { return (x
 
 // Many rows: a wave has 32 tokens of a kv head as operands, which take their conversion once, and goes through the row tiles, whose operands its workgroup brings to LDS,
 // kStaged of them while the ones before are multiplied.  First for the statistics of the rows over its tokens, then, when those are joined, for the weights.
-// 64 queries of 4 heads a kv head over 12 288 tokens: 25.4 and 23.9 us, of which 6 are the way in; matrix cores busy in 45 % of a wave's time, vector pipes in as much, the rest
-// waits for operands from LDS, which is as busy.  (Row tiles requested behind a bound or a branch: 28 and 25; operands straight from the caches: 31 and 30.)
-// The grid is there once (look-ups are few, and meet in banks as they will): LDS has room for four workgroups.  blockIdx = (128 tokens and kv head, sequence).
+// 64 queries of 4 heads a kv head over 12 288 tokens: 25.4 and 23.9 us, of which 6 are the way in; matrix cores busy in 42 % of the cycles, vector pipes in 50, LDS in 35, of which
+// 22 % are bank conflicts; a wave's products and exponentials follow each other.  (Row tiles requested behind a bound or a branch: 28 and 25; operands straight from the caches: 31 and 30.)
+// The grid is there once (look-ups are few, and meet in banks as they will): a CU has three workgroups, by LDS (42 to 44 KB each) as by registers.  blockIdx = (128 tokens and kv head, sequence).
 template <int NCW, bool MASS>
 __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu(3))) void weights_tokens_kernel(const PagedAttendArgs a, const WeightsArgs x) {
   typedef Codes<NCW, 2> C;
@@ -343,7 +343,8 @@ __global__ __launch_bounds__(64 * kMassWaves) __attribute__((amdgpu_waves_per_eu
   const int64_t head = ((int64_t)b * a.H + h) * x.tiles;
   struct Coming { u32x4 x[kEach]; };
   Coming even, odd;
-  // (Neither has a branch or a bound: loads wait for each other across the one, and the other is work.  There is room for kBehind row tiles behind the last one.)
+  // (Neither has a branch or a bound: loads wait for each other across the one, and the other is work, more than the 192 units of a stage's 1280 that are brought beside
+  // its row tiles'.  There is room for kBehind row tiles behind the last one.)
   const auto request = [&](Coming& coming, int tile) {
     const u32x4* const at = reinterpret_cast<const u32x4*>(x.packed + head + tile);
 #pragma unroll
